@@ -427,6 +427,57 @@ zc_status zc_dict_observe(zc_dict_t* dict, uint64_t input_bytes, uint64_t contai
 zc_status zc_dict_rebuild(zc_dict_t* dict, const zc_plan_t* plan, const uint64_t* h_hist);
 zc_status zc_dict_get_info(const zc_dict_t* dict, zc_dict_info* out);
 
+/* ---- operators on FP8 matrices with block scales ---------------------------------------------
+ * (No counterpart in the paper: what a program does with the tensors before it stores them and after it has
+ * decoded them.)  A matrix is FP8 elements, the bytes of ZC_FMT_FP8_E4M3 / ZC_FMT_FP8_E5M2, and scale bytes s, the
+ * bytes of ZC_FMT_SCALE_U8 in E8M0: an element stands for its FP8 value times 2^(s - 127), s = 255 for NaN.  128
+ * columns of one row (block_rows = 1) or of 128 rows (block_rows = 128) share a scale byte; the last blocks of a
+ * row or column may be partly filled.  Bytes behind the last column of a row are neither read for their value nor
+ * written.  The struct is read before a call returns; it is host memory, its pointers are device pointers. */
+typedef enum zc_real { ZC_REAL_F32 = 0, ZC_REAL_BF16 = 1, ZC_REAL_F16 = 2 } zc_real;
+
+typedef struct zc_fp8_matrix {
+    void* d_elems;              /* row r begins at d_elems + r * ld_elems; 16-byte aligned */
+    void* d_scales;             /* row block i begins at d_scales + i * ld_scales; ceil(rows / block_rows) of them */
+    uint64_t rows, cols;        /* below 2^31 */
+    uint64_t ld_elems;          /* bytes, a multiple of 16, at least cols */
+    uint64_t ld_scales;         /* bytes, at least ceil(cols / 128) */
+    uint32_t format;            /* ZC_FMT_FP8_E4M3 or ZC_FMT_FP8_E5M2 */
+    uint32_t block_rows;        /* 1 or 128 */
+} zc_fp8_matrix;
+
+/* Quantise a matrix X[rows][cols] of FP32, BF16 or FP16.
+ * Scale of a block: the least power of two 2^e, -127 <= e <= 127, with amax <= max * 2^e, amax over the block's
+ * finite elements, max = 448 (E4M3) or 57344 (E5M2); e = -127 for a block without a finite element other than 0.
+ * Element: X * 2^-e rounded to nearest even; NaN stays NaN; an infinity becomes NaN in E4M3, which has none, and
+ * stays in E5M2.
+ * d_in    row r begins at element r * ld_in; any alignment that the element type has
+ * q       receives X: q->rows x q->cols; null: not wanted
+ * qt      receives the transposed matrix, qt->rows = columns of X, qt->cols = rows of X, with blocks along ITS rows
+ *         (what a product over the rows of X takes); null: not wanted.  Same format and block_rows as q.
+ * The output buffers must not overlap each other or the input.  Asynchronous on cuda_stream.
+ * Errors: INVALID_ARG (null or misaligned pointers, pitches, q and qt that do not belong together), UNSUPPORTED
+ * (types, formats, block_rows), TOO_LARGE, CUDA. */
+zc_status zc_fp8_quantize(zc_real in_type, const void* d_in, uint64_t ld_in, const zc_fp8_matrix* q,
+                          const zc_fp8_matrix* qt, void* cuda_stream);
+
+/* Matrix product D = A B^T, or D += A B^T: D[m][n] = sum over k of A[m][k] * B[n][k], summed in FP32.
+ * a, b        M x K and N x K; formats and block_rows may differ
+ * d_out       M x N of out_type, row m begins at element m * ld_out
+ * accumulate  not 0: the product is added (in FP32, rounded once) to what d_out holds
+ * A linear layer is x W^T (a = activations, b = weights); the gradient of its input is dy (W^T)^T and that of its
+ * weights (dy^T)(x^T)^T, with the transposed matrices that zc_fp8_quantize makes.  K = 0 gives zeros.  The result
+ * does not depend on other calls and is the same every time.  Asynchronous on cuda_stream; needs no workspace.
+ * A wait inside the kernel that gives up leaves D undefined and is reported by zc_fp8_status.
+ * Errors: INVALID_ARG (null or misaligned pointers, pitches, different K), UNSUPPORTED (types, formats), TOO_LARGE,
+ * CUDA. */
+zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real out_type, void* d_out, uint64_t ld_out,
+                        uint32_t accumulate, void* cuda_stream);
+
+/* Waits for the stream, returns and clears what zc_fp8_matmul calls on the current device have left since the last
+ * query: ZC_OK or ZC_E_DEVICE_TIMEOUT.  Not inside a stream capture. */
+zc_status zc_fp8_status(void* cuda_stream);
+
 const char* zc_strerror(zc_status s);
 
 #ifdef __cplusplus

@@ -24,6 +24,8 @@ MODE_RAW, MODE_HUFF = 0, 1
 (OK, E_INVALID_ARG, E_UNSUPPORTED, E_BUFFER_TOO_SMALL, E_CORRUPT, E_CUDA, E_NOMEM, E_DEVICE_TIMEOUT, E_NO_CODE,
  E_TOO_LARGE) = range(10)
 NOALLOC_MAX_CHUNKS = 65536
+REAL_F32, REAL_BF16, REAL_F16 = 0, 1, 2
+_REAL = {torch.float32: REAL_F32, torch.bfloat16: REAL_BF16, torch.float16: REAL_F16}
 
 
 class ZcError(RuntimeError):
@@ -53,6 +55,11 @@ class Stats(C.Structure):
 class DictInfo(C.Structure):
     _fields_ = [("tolerance", C.c_double), ("baseline_ratio", C.c_double), ("last_ratio", C.c_double),
                 ("n_observed", C.c_uint64), ("n_rebuilds", C.c_uint64), ("has_baseline", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class Fp8MatrixDesc(C.Structure):
+    _fields_ = [("d_elems", C.c_void_p), ("d_scales", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64),
+                ("ld_elems", C.c_uint64), ("ld_scales", C.c_uint64), ("format", C.c_uint32), ("block_rows", C.c_uint32)]
 
 
 def _load():
@@ -150,6 +157,12 @@ def _load():
     L.zc_test_decoder_pieces.argtypes = [vp, C.c_uint32, C.c_uint64, C.POINTER(C.c_uint32)]
     L.zc_test_debug_counts.restype = C.c_int
     L.zc_test_debug_counts.argtypes = [C.POINTER(C.c_uint32)]
+    L.zc_fp8_quantize.restype = C.c_int
+    L.zc_fp8_quantize.argtypes = [C.c_int, vp, C.c_uint64, vp, vp, vp]
+    L.zc_fp8_matmul.restype = C.c_int
+    L.zc_fp8_matmul.argtypes = [vp, vp, C.c_int, vp, C.c_uint64, C.c_uint32, vp]
+    L.zc_fp8_status.restype = C.c_int
+    L.zc_fp8_status.argtypes = [vp]
     for name in ("zc_test_set_wait_limit", "zc_test_stall_encoder", "zc_test_stall_decoder"):
         getattr(L, name).restype = None
         getattr(L, name).argtypes = [C.c_uint32]
@@ -490,6 +503,86 @@ def batch_status(d_workspace: torch.Tensor, stream=None):
     failed = C.c_uint32(0xFFFFFFFF)
     st = _lib.zc_batch_status(d_workspace.data_ptr(), C.byref(failed), _stream_ptr(stream))
     return st, (None if failed.value == 0xFFFFFFFF else failed.value)
+
+
+# ---- operators on FP8 matrices with block scales ----
+
+def _real_matrix(t: torch.Tensor, what: str):
+    """(type code, address, row pitch in elements) of a 2-D tensor of real numbers with contiguous rows."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(t.shape)}, strides {t.stride()}")
+    real = _REAL.get(t.dtype)
+    if real is None:
+        raise TypeError(f"{what}: float32, bfloat16 or float16 is wanted, got {t.dtype}")
+    rows, cols = t.shape
+    return real, t.data_ptr(), (t.stride(0) if rows > 1 else max(t.stride(0), cols))
+
+
+def _on_current_device(*tensors):
+    """The library launches on the current device: tensors of another one are refused instead of read from there."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+class Fp8Matrix:
+    """zc_fp8_matrix: FP8 elements [rows, cols] and E8M0 scale bytes [ceil(rows / block_rows), ceil(cols / 128)], both
+    uint8 with contiguous rows; the elements' rows have a pitch that is a multiple of 16 bytes.  Marshalled once; keeps
+    its tensors alive."""
+
+    def __init__(self, elems: torch.Tensor, scales: torch.Tensor, fmt: int = FMT_FP8_E4M3, block_rows: int = 1):
+        for t, what in ((elems, "elems"), (scales, "scales")):
+            if t.dtype != torch.uint8 or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+                raise ValueError(f"{what}: a uint8 matrix with contiguous rows is wanted")
+        rows, cols = elems.shape
+        if block_rows in (1, 128) and tuple(scales.shape) != (-(-rows // block_rows), -(-cols // 128)):
+            raise ValueError(f"scales: shape {tuple(scales.shape)} does not fit {rows} x {cols} elements in blocks of {block_rows} x 128")
+        self.elems, self.scales, self.format, self.block_rows = elems, scales, fmt, block_rows
+        pitch = lambda t: t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])  # noqa: E731
+        self.desc = Fp8MatrixDesc(elems.data_ptr(), scales.data_ptr(), rows, cols, -(-pitch(elems) // 16) * 16 if rows <= 1 else pitch(elems),
+                                  pitch(scales), fmt, block_rows)
+        self._ref = C.addressof(self.desc)
+
+    @property
+    def shape(self):
+        return tuple(self.elems.shape)
+
+
+def fp8_empty(rows: int, cols: int, fmt: int = FMT_FP8_E4M3, block_rows: int = 1, device="cuda") -> Fp8Matrix:
+    """An Fp8Matrix of new buffers, contents undefined."""
+    pitch = -(-cols // 16) * 16
+    elems = torch.empty((rows, pitch), dtype=torch.uint8, device=device)[:, :cols]
+    return Fp8Matrix(elems, torch.empty((-(-rows // block_rows), -(-cols // 128)), dtype=torch.uint8, device=device), fmt, block_rows)
+
+
+def fp8_quantize(d_in: torch.Tensor, q: Optional[Fp8Matrix], qt: Optional[Fp8Matrix] = None, stream=None) -> Optional[Fp8Matrix]:
+    """zc_fp8_quantize: the matrix d_in into q and / or its transposed form into qt (asynchronous)."""
+    real, ptr, ld = _real_matrix(d_in, "d_in")
+    for m, shape in ((q, d_in.shape), (qt, d_in.shape[::-1])):
+        if m is not None:
+            if m.shape != tuple(shape):
+                raise ValueError(f"an output is {m.shape}, the matrix to quantise asks for {tuple(shape)}")
+            _on_current_device(m.elems, m.scales)
+    _on_current_device(d_in)
+    _check(_lib.zc_fp8_quantize(real, ptr, ld, q._ref if q is not None else None, qt._ref if qt is not None else None, _stream_ptr(stream)),
+           "zc_fp8_quantize")
+    return q
+
+
+def fp8_matmul(a: Fp8Matrix, b: Fp8Matrix, d_out: torch.Tensor, accumulate: bool = False, stream=None) -> torch.Tensor:
+    """zc_fp8_matmul: d_out = a b^T, or d_out += a b^T (asynchronous)."""
+    real, ptr, ld = _real_matrix(d_out, "d_out")
+    if tuple(d_out.shape) != (a.elems.shape[0], b.elems.shape[0]):
+        raise ValueError(f"d_out is {tuple(d_out.shape)}, the product is {(a.elems.shape[0], b.elems.shape[0])}")
+    _on_current_device(a.elems, a.scales, b.elems, b.scales, d_out)
+    _check(_lib.zc_fp8_matmul(a._ref, b._ref, real, ptr, ld, accumulate, _stream_ptr(stream)), "zc_fp8_matmul")
+    return d_out
+
+
+def fp8_status(stream=None) -> int:
+    """zc_fp8_status: device status of the fp8_matmul calls on the current device since the last query."""
+    return int(_lib.zc_fp8_status(_stream_ptr(stream)))
 
 
 def validate_container(p: Plan, h_container) -> int:

@@ -1,0 +1,353 @@
+// zc_fp8_matmul: D = A B^T of FP8 matrices with a scale byte per 128 columns, on the fifth-generation tensor cores.
+//
+// The instruction that takes FP8 operands with E8M0 scales multiplies 32 columns at a time and looks up one scale byte per
+// row of A and of B in tensor memory.  A scale byte that holds for 128 columns is simply looked up by four instructions in
+// a row, so the bytes go into the product as they are stored, four of them (512 columns) to a 32-bit word of tensor memory,
+// and no accumulator ever leaves tensor memory before the sum over k is complete.
+//
+// Roles of a thread block's warps: 0 copies tiles of 128 rows x 128 bytes into shared memory (tensor copies, 128-byte
+// swizzle; what lies outside of a matrix arrives as zeros), 1 issues the matrix instructions, 4-7 bring the accumulators
+// to memory, 8-11 bring the scale bytes into tensor memory.
+#include <cuda.h>
+
+#include "zc_fp8.cuh"
+
+namespace zc {
+
+constexpr int kMmThreads = 384;
+constexpr uint32_t kTile = 128;                  // rows of A, or of B, that a block copies per step
+constexpr uint32_t kStepBytes = 128;             // columns per step = bytes of the swizzle = columns of a scale byte
+constexpr uint32_t kTileBytes = kTile * kStepBytes;
+
+__device__ unsigned int g_fp8_timeout;           // a wait of a matrix product gave up
+
+struct MatmulParams {
+    const uint8_t *sa, *sb;                      // scale bytes
+    uint64_t ld_sa, ld_sb;
+    uint8_t* out;
+    uint64_t ld_out;                             // bytes
+    uint32_t m, n, steps;                        // rows of A, rows of B, steps of 128 columns
+    uint32_t square_a, square_b;                 // 128 rows share a scale byte
+    uint32_t idesc;                              // instruction descriptor without the scale selectors
+    uint32_t out_type, accumulate, out_wide;     // out_wide: every row of D begins on a 16-byte boundary
+    uint32_t tiles_m, tiles_n;
+    uint32_t spin_limit, skip_copy;
+};
+
+// Shared memory behind the operand stages.
+struct MatmulShared {
+    uint64_t full[8], empty[8];
+    uint64_t sf_full[2], sf_empty[2];
+    uint64_t acc_full[2], acc_empty[2];
+    uint32_t tmem, failed;
+};
+
+// Every wait is bounded: on giving up the block is marked, and the other roles' waits end with it.
+struct Waiter {
+    uint32_t limit;
+    volatile uint32_t* failed;
+    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const
+    {
+        for (uint32_t i = 0; i <= limit; ++i) {
+            if (bar_try(bar, parity)) return true;
+            if (*failed) return false;
+        }
+        *failed = 1;
+        atomicExch(&g_fp8_timeout, 1u);
+        return false;
+    }
+};
+
+// The scale bytes of steps first .. first + 3 of one row as a word; 127 (a factor of 1) where there is none.
+__device__ __forceinline__ uint32_t scale_word(const uint8_t* s, uint64_t ld, uint32_t square, uint32_t row, uint32_t rows, uint32_t first, uint32_t end)
+{
+    uint32_t w = 0x7F7F7F7Fu;
+    if (row < rows) {
+        const uint8_t* p = s + (uint64_t)(square ? row >> 7 : row) * ld + first;
+        if (first + 4 <= end && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return __ldg(reinterpret_cast<const uint32_t*>(p));
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (first + i < end) w = (w & ~(0xFFu << (8 * i))) | ((uint32_t)__ldg(p + i) << (8 * i));
+    }
+    return w;
+}
+
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+
+// COUNT consecutive values of a row of D, of which the first n exist.
+template <typename T, int COUNT>
+__device__ __forceinline__ void store_row(uint8_t* row, uint32_t col, uint32_t n, const float* v, uint32_t wide, uint32_t accumulate)
+{
+    T* p = reinterpret_cast<T*>(row) + col;
+    constexpr int PER = 16 / sizeof(T);
+    if (wide && n >= COUNT && COUNT % PER == 0) {
+#pragma unroll
+        for (int i = 0; i < COUNT; i += PER) {
+            union { uint4 q; T t[PER]; } x;
+            if (accumulate) x.q = *reinterpret_cast<const uint4*>(p + i);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) x.t[j] = from_float<T>(accumulate ? v[i + j] + to_float(x.t[j]) : v[i + j]);
+            *reinterpret_cast<uint4*>(p + i) = x.q;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i)
+        if ((uint32_t)i < n) p[i] = from_float<T>(accumulate ? v[i] + to_float(p[i]) : v[i]);
+}
+template <int COUNT>
+__device__ __forceinline__ void store_row(const MatmulParams& P, uint32_t row, uint32_t col, const float* v)
+{
+    if (row >= P.m || col >= P.n) return;
+    uint8_t* r = P.out + (uint64_t)row * P.ld_out;
+    const uint32_t n = P.n - col;
+    if (P.out_type == ZC_REAL_F32) store_row<float, COUNT>(r, col, n, v, P.out_wide, P.accumulate);
+    else if (P.out_type == ZC_REAL_BF16) store_row<__nv_bfloat16, COUNT>(r, col, n, v, P.out_wide, P.accumulate);
+    else store_row<__half, COUNT>(r, col, n, v, P.out_wide, P.accumulate);
+}
+
+// One tile of 128 x 128 per block; the `gridDim.z` blocks of a cluster share a tile, each takes a part of the steps, and the
+// parts are added up through the cluster's shared memory in the order of the ranks.
+constexpr uint32_t kSmallStages = 3;
+constexpr size_t kSmallSmem = 1024 + kSmallStages * 2 * kTileBytes + sizeof(MatmulShared);
+constexpr uint32_t kSmallCols = 256;             // tensor memory: 128 accumulator columns, then two sets of 4 + 4 scale columns
+constexpr uint32_t kSmallScales = 128;
+
+__global__ void __launch_bounds__(kMmThreads)
+matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MatmulParams P)
+{
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (base - smem_u32(raw)) + kSmallStages * 2 * kTileBytes);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t parts = gridDim.z, part = blockIdx.z;
+    const uint32_t m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
+    const uint32_t lo = (uint32_t)((uint64_t)P.steps * part / parts), hi = (uint32_t)((uint64_t)P.steps * (part + 1) / parts);
+    const Waiter wait{P.spin_limit, &S->failed};
+
+    if (warp == 0 && lane == 0) {
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+        for (uint32_t i = 0; i < kSmallStages; ++i) { bar_init(smem_u32(&S->full[i]), 1); bar_init(smem_u32(&S->empty[i]), 1); }
+        for (uint32_t i = 0; i < 2; ++i) { bar_init(smem_u32(&S->sf_full[i]), 4); bar_init(smem_u32(&S->sf_empty[i]), 1); }
+        bar_init(smem_u32(&S->acc_full[0]), 1);
+        S->failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc<1>(smem_u32(&S->tmem), kSmallCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = S->tmem;
+
+    uint32_t issued = 0;
+    if (warp == 0 && lane == 0) {
+        for (uint32_t i = lo; i < hi; ++i, ++issued) {
+            const uint32_t st = issued % kSmallStages;
+            if (issued >= kSmallStages && !wait(smem_u32(&S->empty[st]), (issued / kSmallStages - 1) & 1)) break;
+            const uint32_t bar = smem_u32(&S->full[st]);
+            bar_expect(bar, 2 * kTileBytes);
+            if (P.skip_copy) continue;
+            tensor_copy<1>(base + st * 2 * kTileBytes, &map_a, (int)(i * kStepBytes), (int)m0, bar);
+            tensor_copy<1>(base + st * 2 * kTileBytes + kTileBytes, &map_b, (int)(i * kStepBytes), (int)n0, bar);
+        }
+    } else if (warp == 1 && lane == 0) {
+        for (uint32_t i = 0; i < hi - lo; ++i) {
+            const uint32_t st = i % kSmallStages, set = (i >> 2) & 1;
+            if ((i & 3) == 0 && !wait(smem_u32(&S->sf_full[set]), (i >> 3) & 1)) break;
+            if (!wait(smem_u32(&S->full[st]), (i / kSmallStages) & 1)) break;
+            tc_fence_after();
+            const uint64_t da = operand_desc(base + st * 2 * kTileBytes), db = operand_desc(base + st * 2 * kTileBytes + kTileBytes);
+            const uint32_t idesc = P.idesc | ((i & 3) << 29) | ((i & 3) << 4);
+            const uint32_t sfa = tmem + kSmallScales + set * 8, sfb = sfa + 4;
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) mma_scaled<1>(tmem, da + 2 * j, db + 2 * j, idesc, sfa, sfb, i | j);
+            mma_commit<1>(smem_u32(&S->empty[st]));
+            if ((i & 3) == 3) mma_commit<1>(smem_u32(&S->sf_empty[set]));
+        }
+        mma_commit<1>(smem_u32(&S->acc_full[0]));
+    } else if (warp >= 8) {
+        const uint32_t quarter = (warp & 3) * (32u << 16);
+        for (uint32_t i = lo, k = 0; i < hi; i += 4, ++k) {
+            uint32_t a[4], b[4];
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                a[q] = scale_word(P.sa, P.ld_sa, P.square_a, m0 + 32 * q + lane, P.m, i, hi);
+                b[q] = scale_word(P.sb, P.ld_sb, P.square_b, n0 + 32 * q + lane, P.n, i, hi);
+            }
+            if (!__all_sync(0xFFFFFFFFu, k < 2 || wait(smem_u32(&S->sf_empty[k & 1]), ((k >> 1) - 1) & 1))) break;
+            tmem_st4(tmem + quarter + kSmallScales + (k & 1) * 8, a);
+            tmem_st4(tmem + quarter + kSmallScales + (k & 1) * 8 + 4, b);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive_cluster(smem_u32(&S->sf_full[k & 1]));
+        }
+    }
+    __syncwarp();
+    const uint32_t rows = P.m - m0 < kTile ? P.m - m0 : kTile;
+    if (warp >= 4 && warp < 8) {
+        const uint32_t quad = warp & 3, row = quad * 32 + lane;
+        if (__all_sync(0xFFFFFFFFu, wait(smem_u32(&S->acc_full[0]), 0) && !*wait.failed) && quad * 32 < rows) {
+            tc_fence_after();
+            for (uint32_t c = 0; c < 4; ++c) {
+                uint32_t v[32];
+                tmem_ld32(tmem + (quad * 32u << 16) + c * 32, v);
+                if (parts == 1) {
+                    store_row<32>(P, m0 + row, n0 + c * 32, reinterpret_cast<const float*>(v));
+                } else if (row < rows) {
+                    // the operand stages are free once the last instruction is done; 16-byte pieces turned by the row
+#pragma unroll
+                    for (uint32_t q = 0; q < 8; ++q) {
+                        const uint32_t at = base + row * 512 + (((c * 8 + q) ^ (row & 31)) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v[4 * q]), "r"(v[4 * q + 1]), "r"(v[4 * q + 2]), "r"(v[4 * q + 3]) : "memory");
+                    }
+                }
+            }
+            tc_fence_before();
+        }
+    }
+    __syncthreads();
+    if (parts > 1) {
+        cluster_sync();
+        // rank r adds up columns r * 128 / parts .. of all rows
+        const uint32_t pieces = 32 / parts, first = part * pieces;
+        for (uint32_t i = threadIdx.x; i < rows * pieces; i += kMmThreads) {
+            const uint32_t row = i / pieces, piece = first + i % pieces;
+            const uint32_t at = base + row * 512 + ((piece ^ (row & 31)) << 4);
+            float sum[4] = {0, 0, 0, 0};
+            for (uint32_t r = 0; r < parts; ++r) {
+                const float4 x = ld_cluster_f4(map_shared(at, r));
+                sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+            }
+            store_row<4>(P, m0 + row, n0 + piece * 4, sum);
+        }
+        cluster_sync();
+    }
+    // after a wait that gave up, copies may still be on their way into this block's shared memory
+    if (*wait.failed && warp == 0 && lane == 0 && !P.skip_copy)
+        for (uint32_t i = issued > kSmallStages ? issued - kSmallStages : 0; i < issued; ++i)
+            for (uint32_t t = 0; t <= P.spin_limit && !bar_try(smem_u32(&S->full[i % kSmallStages]), (i / kSmallStages) & 1); ++t) { }
+    __syncthreads();
+    if (warp == 1) tmem_free<1>(tmem, kSmallCols);
+}
+
+// D = 0 (K = 0): nothing to copy or multiply.
+__global__ void zero_kernel(const __grid_constant__ MatmulParams P, uint32_t width)
+{
+    for (uint64_t r = blockIdx.x; r < P.m; r += gridDim.x)
+        for (uint64_t i = threadIdx.x; i < (uint64_t)P.n * width; i += blockDim.x) P.out[r * P.ld_out + i] = 0;
+}
+
+// ---- host ----
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeFn encode_fn()
+{
+    static const EncodeFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) p = nullptr;
+        return (EncodeFn)p;
+    }();
+    return fn;
+}
+
+// A matrix as tiles of 128 rows x 128 bytes.
+static bool make_map(CUtensorMap* map, const zc_fp8_matrix* x)
+{
+    const cuuint64_t dims[2] = {x->cols, x->rows}, pitch[1] = {x->ld_elems};
+    const cuuint32_t box[2] = {kStepBytes, kTile}, step[2] = {1, 1};
+    return encode_fn() && encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, x->d_elems, dims, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static uint32_t instruction(const zc_fp8_matrix* a, const zc_fp8_matrix* b, uint32_t m, uint32_t n)
+{
+    const uint32_t fa = a->format == ZC_FMT_FP8_E5M2, fb = b->format == ZC_FMT_FP8_E5M2;
+    // A and B types, N / 8, E8M0 scales, M / 16; both operands have k as their fastest axis
+    return (fa << 7) | (fb << 10) | ((n >> 3) << 17) | (1u << 23) | ((m >> 4) << 24);
+}
+
+}  // namespace zc
+
+using namespace zc;
+
+extern "C" {
+
+zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real out_type, void* d_out, uint64_t ld_out,
+                        uint32_t accumulate, void* cuda_stream)
+{
+    if (const zc_status s = check_matrix(a)) return s;
+    if (const zc_status s = check_matrix(b)) return s;
+    const uint32_t width = real_bytes(out_type);
+    if (!width) return ZC_E_UNSUPPORTED;
+    if (a->cols != b->cols) return ZC_E_INVALID_ARG;
+    if (a->rows == 0 || b->rows == 0) return ZC_OK;
+    if (!d_out || reinterpret_cast<uintptr_t>(d_out) % width || ld_out < b->rows || ld_out >= (1ull << 39)) return ZC_E_INVALID_ARG;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    MatmulParams P{};
+    P.out = (uint8_t*)d_out;
+    P.ld_out = ld_out * width;
+    P.m = (uint32_t)a->rows;
+    P.n = (uint32_t)b->rows;
+    if (a->cols == 0) {
+        if (!accumulate) zero_kernel<<<(uint32_t)std::min<uint64_t>(P.m, 1024), 256, 0, st>>>(P, width);
+        return cudaGetLastError() == cudaSuccess ? ZC_OK : ZC_E_CUDA;
+    }
+    P.sa = (const uint8_t*)a->d_scales;
+    P.sb = (const uint8_t*)b->d_scales;
+    P.ld_sa = a->ld_scales;
+    P.ld_sb = b->ld_scales;
+    P.steps = (uint32_t)ceil_div(a->cols, kStepBytes);
+    P.square_a = a->block_rows == 128;
+    P.square_b = b->block_rows == 128;
+    P.out_type = out_type;
+    P.accumulate = accumulate != 0;
+    P.out_wide = reinterpret_cast<uintptr_t>(d_out) % 16 == 0 && P.ld_out % 16 == 0;
+    P.spin_limit = test_knobs().spin_limit;
+    P.skip_copy = test_knobs().skip_copy;
+    CUtensorMap map_a, map_b;
+    if (!make_map(&map_a, a) || !make_map(&map_b, b)) return ZC_E_CUDA;
+    P.tiles_m = (uint32_t)ceil_div(P.m, kTile);
+    P.tiles_n = (uint32_t)ceil_div(P.n, kTile);
+    P.idesc = instruction(a, b, 128, 128);
+    if (P.tiles_m > 65535) return ZC_E_TOO_LARGE;
+    const uint64_t tiles = (uint64_t)P.tiles_m * P.tiles_n;
+    uint32_t parts = 1;
+    while (parts < 8 && tiles * parts * 2 <= 2 * (uint64_t)sm_count() && P.steps >= 4 * parts) parts *= 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(P.tiles_n, P.tiles_m, parts);
+    cfg.blockDim = dim3(kMmThreads);
+    cfg.dynamicSmemBytes = kSmallSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {1, 1, parts};
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(matmul_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem) != cudaSuccess) return ZC_E_CUDA;
+    if (cudaLaunchKernelEx(&cfg, matmul_small_kernel, map_a, map_b, P) != cudaSuccess) return ZC_E_CUDA;
+    return ZC_OK;
+}
+
+zc_status zc_fp8_status(void* cuda_stream)
+{
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    unsigned int h = 0;
+    const unsigned int zero = 0;
+    if (cudaMemcpyFromSymbolAsync(&h, g_fp8_timeout, sizeof h, 0, cudaMemcpyDeviceToHost, st) != cudaSuccess) return ZC_E_CUDA;
+    if (cudaMemcpyToSymbolAsync(g_fp8_timeout, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st) != cudaSuccess) return ZC_E_CUDA;
+    if (cudaStreamSynchronize(st) != cudaSuccess) return ZC_E_CUDA;
+    return h ? ZC_E_DEVICE_TIMEOUT : ZC_OK;
+}
+
+}  // extern "C"
