@@ -478,6 +478,45 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
  * query: ZC_OK or ZC_E_DEVICE_TIMEOUT.  Not inside a stream capture. */
 zc_status zc_fp8_status(void* cuda_stream);
 
+/* A mixture-of-experts layer for a few tokens (1 to ZC_FP8_MOE_MAX_TOKENS).  For a token x:
+ *   logits = router x; the top_k largest (ties: the lowest index first; NaN counts as the lowest value); p = softmax
+ *   over those top_k; y = sum over them of p_e * down_e (silu(gate_e x) * (up_e x)), silu(v) = v / (1 + exp(-v)).
+ * The weights are FP8 with 128 x 128 blocks; every expert's matrix has scale bytes of its own, beginning with its first
+ * row.  Only the experts that a token chose are read.  Sums are FP32, those of the router FP64 over parts of 128
+ * columns; the hidden vector of an expert is kept with 16 bits of precision.  Rows are read in pieces of 16 bytes: of
+ * every row, the last one included, the whole pitch belongs to the buffer. */
+typedef struct zc_fp8_moe_layer {
+    const void* d_router;       /* [n_experts][hidden] of real_type, row pitch ld_router elements */
+    const void* d_gate_up;      /* [n_experts][2][inter] rows of hidden bytes, row pitch ld_gate_up bytes: gate, then up */
+    const void* d_gate_up_scales; /* [n_experts][2][ceil(inter / 128)][ceil(hidden / 128)], no padding */
+    const void* d_down;         /* [n_experts][hidden] rows of inter bytes, row pitch ld_down bytes */
+    const void* d_down_scales;  /* [n_experts][ceil(hidden / 128)][ceil(inter / 128)], no padding */
+    uint64_t ld_router;         /* elements, a multiple of 8 */
+    uint64_t ld_gate_up, ld_down; /* bytes, multiples of 16 */
+    uint32_t n_experts;         /* 1 .. ZC_FP8_MOE_MAX_EXPERTS */
+    uint32_t top_k;             /* 1 .. min(n_experts, ZC_FP8_MOE_MAX_TOP_K) */
+    uint32_t hidden, inter;     /* 1 .. 65536 */
+    uint32_t format;            /* of the weights: ZC_FMT_FP8_E4M3 or ZC_FMT_FP8_E5M2 */
+    uint32_t real_type;         /* of router, x and y: ZC_REAL_BF16 or ZC_REAL_F16 */
+} zc_fp8_moe_layer;
+#define ZC_FP8_MOE_MAX_TOKENS 64u
+#define ZC_FP8_MOE_MAX_EXPERTS 256u
+#define ZC_FP8_MOE_MAX_TOP_K 16u
+
+/* Bytes of device scratch zc_fp8_moe needs; 0 for arguments that it would refuse. */
+size_t zc_fp8_moe_workspace_bytes(const zc_fp8_moe_layer* layer, uint32_t n_tokens);
+/* d_x        [n_tokens][hidden], row pitch ld_x elements, a multiple of 8
+ * d_out      [n_tokens][hidden], row pitch ld_out elements; any alignment that the type has; must not overlap d_x
+ * d_ids      [n_tokens][top_k] uint32_t, receives the experts in order of their logits; may be null
+ * d_weights  [n_tokens][top_k] float, receives p; may be null
+ * d_workspace  workspace_bytes >= zc_fp8_moe_workspace_bytes() bytes, 256-byte aligned, contents need not be initialised
+ * Asynchronous on cuda_stream.  n_tokens = 0 returns ZC_OK and launches nothing.
+ * Errors: INVALID_ARG (null or misaligned pointers, pitches, sizes), UNSUPPORTED (types, formats), TOO_LARGE (tokens,
+ * experts, top_k, hidden or inter above their limits), BUFFER_TOO_SMALL (workspace), CUDA. */
+zc_status zc_fp8_moe(const zc_fp8_moe_layer* layer, uint32_t n_tokens, const void* d_x, uint64_t ld_x, void* d_out,
+                     uint64_t ld_out, uint32_t* d_ids, float* d_weights, void* d_workspace, size_t workspace_bytes,
+                     void* cuda_stream);
+
 const char* zc_strerror(zc_status s);
 
 #ifdef __cplusplus

@@ -10,6 +10,7 @@ importing this module fails loudly when it is not — there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional
 
@@ -60,6 +61,13 @@ class DictInfo(C.Structure):
 class Fp8MatrixDesc(C.Structure):
     _fields_ = [("d_elems", C.c_void_p), ("d_scales", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64),
                 ("ld_elems", C.c_uint64), ("ld_scales", C.c_uint64), ("format", C.c_uint32), ("block_rows", C.c_uint32)]
+
+
+class Fp8MoeLayerDesc(C.Structure):
+    _fields_ = [("d_router", C.c_void_p), ("d_gate_up", C.c_void_p), ("d_gate_up_scales", C.c_void_p), ("d_down", C.c_void_p),
+                ("d_down_scales", C.c_void_p), ("ld_router", C.c_uint64), ("ld_gate_up", C.c_uint64), ("ld_down", C.c_uint64),
+                ("n_experts", C.c_uint32), ("top_k", C.c_uint32), ("hidden", C.c_uint32), ("inter", C.c_uint32),
+                ("format", C.c_uint32), ("real_type", C.c_uint32)]
 
 
 def _load():
@@ -161,6 +169,10 @@ def _load():
     L.zc_fp8_quantize.argtypes = [C.c_int, vp, C.c_uint64, vp, vp, vp]
     L.zc_fp8_matmul.restype = C.c_int
     L.zc_fp8_matmul.argtypes = [vp, vp, C.c_int, vp, C.c_uint64, C.c_uint32, vp]
+    L.zc_fp8_moe_workspace_bytes.restype = C.c_size_t
+    L.zc_fp8_moe_workspace_bytes.argtypes = [vp, C.c_uint32]
+    L.zc_fp8_moe.restype = C.c_int
+    L.zc_fp8_moe.argtypes = [vp, C.c_uint32, vp, C.c_uint64, vp, C.c_uint64, vp, vp, vp, C.c_size_t, vp]
     L.zc_fp8_status.restype = C.c_int
     L.zc_fp8_status.argtypes = [vp]
     for name in ("zc_test_set_wait_limit", "zc_test_stall_encoder", "zc_test_stall_decoder"):
@@ -583,6 +595,61 @@ def fp8_matmul(a: Fp8Matrix, b: Fp8Matrix, d_out: torch.Tensor, accumulate: bool
 def fp8_status(stream=None) -> int:
     """zc_fp8_status: device status of the fp8_matmul calls on the current device since the last query."""
     return int(_lib.zc_fp8_status(_stream_ptr(stream)))
+
+
+class Fp8MoeLayer:
+    """zc_fp8_moe_layer: router [experts, hidden] in BF16 or FP16 (row pitch a multiple of 8), gate_up uint8
+    [experts, 2, inter, hidden] and down uint8 [experts, hidden, inter] (row pitches multiples of 16, no gaps between
+    matrices), scale bytes [experts, 2, ceil(inter / 128), ceil(hidden / 128)] and [experts, ceil(hidden / 128),
+    ceil(inter / 128)], contiguous.  Marshalled once; keeps its tensors alive."""
+
+    def __init__(self, router: torch.Tensor, gate_up: torch.Tensor, gate_up_scales: torch.Tensor, down: torch.Tensor,
+                 down_scales: torch.Tensor, top_k: int, fmt: int = FMT_FP8_E4M3):
+        experts, two, inter, hidden = gate_up.shape
+        blocks = lambda n: -(-n // 128)  # noqa: E731
+        if two != 2 or tuple(down.shape) != (experts, hidden, inter) or tuple(router.shape) != (experts, hidden):
+            raise ValueError(f"gate_up {tuple(gate_up.shape)}, down {tuple(down.shape)} and router {tuple(router.shape)} do not belong together")
+        if tuple(gate_up_scales.shape) != (experts, 2, blocks(inter), blocks(hidden)) or tuple(down_scales.shape) != (experts, blocks(hidden), blocks(inter)):
+            raise ValueError("the scale bytes do not fit the matrices in blocks of 128 x 128")
+        if any(t.dtype != torch.uint8 for t in (gate_up, gate_up_scales, down, down_scales)):
+            raise ValueError("weights and scale bytes are uint8")
+        if not gate_up_scales.is_contiguous() or not down_scales.is_contiguous():
+            raise ValueError("scale bytes are contiguous")
+        for t in (gate_up, down):
+            pitch = t.stride(-2)
+            want = tuple(pitch * math.prod(t.shape[i + 1: -1]) for i in range(t.dim() - 1)) + (1,)
+            if any(s != w for s, w, n in zip(t.stride(), want, t.shape) if n > 1):
+                raise ValueError(f"matrices follow one another with one row pitch: strides {t.stride()}")
+        real, ptr, ld = _real_matrix(router, "router")
+        self.experts, self.hidden, self.inter, self.top_k, self.dtype = experts, hidden, inter, top_k, router.dtype
+        self.tensors = (router, gate_up, gate_up_scales, down, down_scales)
+        self.desc = Fp8MoeLayerDesc(ptr, gate_up.data_ptr(), gate_up_scales.data_ptr(), down.data_ptr(), down_scales.data_ptr(), ld,
+                                    gate_up.stride(-2), down.stride(-2), experts, top_k, hidden, inter, fmt, real)
+        self._ref = C.addressof(self.desc)
+
+    def workspace_bytes(self, n_tokens: int) -> int:
+        return int(_lib.zc_fp8_moe_workspace_bytes(self._ref, n_tokens))
+
+
+def fp8_moe(layer: Fp8MoeLayer, d_x: torch.Tensor, d_out: torch.Tensor, d_workspace: torch.Tensor, d_ids: Optional[torch.Tensor] = None,
+            d_weights: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """zc_fp8_moe: d_out = the layer applied to the tokens d_x (asynchronous).  d_ids (int32) and d_weights (float32),
+    [tokens, top_k] and contiguous, receive the experts chosen and their weights."""
+    _, x_ptr, ld_x = _real_matrix(d_x, "d_x")
+    _, y_ptr, ld_y = _real_matrix(d_out, "d_out")
+    tokens = d_x.shape[0]
+    if d_x.dtype != layer.dtype or d_out.dtype != layer.dtype:
+        raise TypeError(f"the layer works in {layer.dtype}, d_x is {d_x.dtype}, d_out {d_out.dtype}")
+    if d_x.shape[1] != layer.hidden or d_out.shape != d_x.shape:
+        raise ValueError(f"d_x is {tuple(d_x.shape)}, d_out {tuple(d_out.shape)}, the layer's width {layer.hidden}")
+    for t, dtype in ((d_ids, torch.int32), (d_weights, torch.float32)):
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != (tokens, layer.top_k) or not t.is_contiguous()):
+            raise ValueError(f"d_ids and d_weights are contiguous int32 and float32 of shape {(tokens, layer.top_k)}")
+    _on_current_device(d_x, d_out, d_workspace, d_ids, d_weights, *layer.tensors)
+    _check(_lib.zc_fp8_moe(layer._ref, tokens, x_ptr, ld_x if tokens > 1 else -(-ld_x // 8) * 8, y_ptr, ld_y, d_ids.data_ptr() if d_ids is not None else None,
+                           d_weights.data_ptr() if d_weights is not None else None, d_workspace.data_ptr(),
+                           d_workspace.numel() * d_workspace.element_size(), _stream_ptr(stream)), "zc_fp8_moe")
+    return d_out
 
 
 def validate_container(p: Plan, h_container) -> int:

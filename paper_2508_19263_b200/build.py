@@ -15,11 +15,12 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libzc.so")
 OBJDIR = os.path.join(HERE, "build")
 SOURCES = ["zc_host.cpp", "zc_hist.cu", "zc_encode.cu", "zc_encode_fmt.cu", "zc_decode.cu",
-           "zc_fp8_quantize.cu", "zc_fp8_matmul.cu"]
+           "zc_fp8_quantize.cu", "zc_fp8_matmul.cu", "zc_fp8_moe.cu"]
 # (source, extra flags, object name): the encoder's and the decoder's kernels are compiled one element format per object
 # (ZC_ENC_FMT, ZC_DEC_PART), so that the longest compiles of the build run four ways in parallel
 UNITS = [("zc_host.cpp", [], "zc_host.cpp.o"), ("zc_hist.cu", [], "zc_hist.cu.o"), ("zc_encode.cu", [], "zc_encode.cu.o"),
-         ("zc_fp8_quantize.cu", [], "zc_fp8_quantize.cu.o"), ("zc_fp8_matmul.cu", [], "zc_fp8_matmul.cu.o")] + \
+         ("zc_fp8_quantize.cu", [], "zc_fp8_quantize.cu.o"), ("zc_fp8_matmul.cu", [], "zc_fp8_matmul.cu.o"),
+         ("zc_fp8_moe.cu", [], "zc_fp8_moe.cu.o")] + \
         [("zc_encode_fmt.cu", [f"-DZC_ENC_FMT={k}"], f"zc_encode.fmt{k}.o") for k in (1, 2, 3, 4)] + \
         [("zc_decode.cu", [f"-DZC_DEC_PART={k}"], f"zc_decode.part{k}.o") for k in (1, 2, 3, 4)]
 HEADERS = ["zc_internal.h", "zc_bits.cuh", "zc_device.cuh", "zc_encode.cuh", "zc_fp8.cuh"]
