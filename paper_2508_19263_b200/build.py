@@ -23,7 +23,7 @@ UNITS = [("zc_host.cpp", [], "zc_host.cpp.o"), ("zc_hist.cu", [], "zc_hist.cu.o"
          ("zc_fp8_moe.cu", [], "zc_fp8_moe.cu.o")] + \
         [("zc_encode_fmt.cu", [f"-DZC_ENC_FMT={k}"], f"zc_encode.fmt{k}.o") for k in (1, 2, 3, 4)] + \
         [("zc_decode.cu", [f"-DZC_DEC_PART={k}"], f"zc_decode.part{k}.o") for k in (1, 2, 3, 4)]
-HEADERS = ["zc_internal.h", "zc_bits.cuh", "zc_device.cuh", "zc_encode.cuh", "zc_fp8.cuh"]
+HEADERS = ["zc_internal.h", "zc_bits.cuh", "zc_device.cuh", "zc_encode.cuh", "zc_fp8.cuh", "zc_fp8_tensor.cuh"]
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 
 

@@ -34,11 +34,30 @@ inline zc_status check_matrix(const zc_fp8_matrix* m)
     return ZC_OK;
 }
 
+zc_status moe_read_timeout(cudaStream_t st);              // zc_fp8_status, for the kernels of zc_fp8_moe
+
 // 2^(s-127) of a scale byte; 255 is NaN.  Bit pattern s << 23 but for 2^-127, which is subnormal in FP32.
 __device__ __forceinline__ float scale_value(uint32_t s)
 {
     return __uint_as_float(s == 255u ? 0x7FC00000u : s ? s << 23 : 0x00400000u);
 }
+
+__device__ __forceinline__ float finite_abs(float v)
+{
+    const float a = fabsf(v);
+    return a < __int_as_float(0x7F800000) ? a : 0.0f;        // NaN compares false as well
+}
+
+// Scale byte of a block: e + 127.
+template <bool E5M2>
+__device__ __forceinline__ uint32_t scale_byte(float amax)
+{
+    const uint32_t b = __float_as_uint(amax);
+    const int e = (int)(b >> 23) - 127 - (E5M2 ? 15 : 8) + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return b == 0 || e < -127 ? 0u : (uint32_t)(e + 127);    // e <= 128 - 8: no clamp above
+}
+__device__ __forceinline__ float inverse_scale(uint32_t s) { return __uint_as_float((254u - s) << 23); }   // 2^-(s-127), s <= 247
+
 
 // ---- 32-byte global accesses (one sector per lane); 32-byte aligned ----
 __device__ __forceinline__ void ld_v8(const void* p, uint32_t v[8])
@@ -91,6 +110,12 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
 }
+// Ordered within the block only.  At the cluster's scope every arrival waits for the thread's earlier writes and every wait
+// drops the L1: 0.8 us a step of the mixture-of-experts kernels instead of 0.3.
+__device__ __forceinline__ void bar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t cluster_bar)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_bar) : "memory");
@@ -98,7 +123,7 @@ __device__ __forceinline__ void bar_arrive_cluster(uint32_t cluster_bar)
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
@@ -180,6 +205,24 @@ __device__ __forceinline__ void tmem_st4(uint32_t addr, const uint32_t v[4])
     asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" :: "r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// eight columns of a quarter's 32 lanes; not complete before tmem_ld_wait
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, float v[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(addr));
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// 512 bytes of scale words, [32][4] in shared memory, to four columns of every quarter of tensor memory: word (i, j) is that
+// of row 32 j + i
+__device__ __forceinline__ void tmem_copy_scales(uint32_t addr, uint32_t shared)
+{
+    // no swizzle, groups of eight 16-byte rows 128 bytes apart
+    const uint64_t desc = (uint64_t)((shared & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(addr), "l"(desc) : "memory");
+}
+// shared memory written by ordinary stores becomes visible to tensor copies and matrix instructions
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // Operand tile in shared memory: rows of 128 bytes in the 128-byte swizzle, groups of 8 rows 1024 bytes apart
 __device__ __forceinline__ uint64_t operand_desc(uint32_t addr)

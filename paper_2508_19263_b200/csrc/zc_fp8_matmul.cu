@@ -8,9 +8,7 @@
 // Roles of a thread block's warps: 0 copies tiles of 128 rows x 128 bytes into shared memory (tensor copies, 128-byte
 // swizzle; what lies outside of a matrix arrives as zeros), 1 issues the matrix instructions, 4-7 bring the accumulators
 // to memory, 8-11 bring the scale bytes into tensor memory.
-#include <cuda.h>
-
-#include "zc_fp8.cuh"
+#include "zc_fp8_tensor.cuh"
 
 namespace zc {
 
@@ -18,8 +16,6 @@ constexpr int kMmThreads = 384;
 constexpr uint32_t kTile = 128;                  // rows of A, or of B, that a block copies per step
 constexpr uint32_t kStepBytes = 128;             // columns per step = bytes of the swizzle = columns of a scale byte
 constexpr uint32_t kTileBytes = kTile * kStepBytes;
-
-__device__ unsigned int g_fp8_timeout;           // a wait of a matrix product gave up
 
 struct MatmulParams {
     const uint8_t *sa, *sb;                      // scale bytes
@@ -41,36 +37,6 @@ struct MatmulShared {
     uint64_t acc_full[2], acc_empty[2];
     uint32_t tmem, failed;
 };
-
-// Every wait is bounded: on giving up the block is marked, and the other roles' waits end with it.
-struct Waiter {
-    uint32_t limit;
-    volatile uint32_t* failed;
-    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const
-    {
-        for (uint32_t i = 0; i <= limit; ++i) {
-            if (bar_try(bar, parity)) return true;
-            if (*failed) return false;
-        }
-        *failed = 1;
-        atomicExch(&g_fp8_timeout, 1u);
-        return false;
-    }
-};
-
-// The scale bytes of steps first .. first + 3 of one row as a word; 127 (a factor of 1) where there is none.
-__device__ __forceinline__ uint32_t scale_word(const uint8_t* s, uint64_t ld, uint32_t square, uint32_t row, uint32_t rows, uint32_t first, uint32_t end)
-{
-    uint32_t w = 0x7F7F7F7Fu;
-    if (row < rows) {
-        const uint8_t* p = s + (uint64_t)(square ? row >> 7 : row) * ld + first;
-        if (first + 4 <= end && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return __ldg(reinterpret_cast<const uint32_t*>(p));
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i)
-            if (first + i < end) w = (w & ~(0xFFu << (8 * i))) | ((uint32_t)__ldg(p + i) << (8 * i));
-    }
-    return w;
-}
 
 template <typename T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
@@ -187,7 +153,7 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive_cluster(smem_u32(&S->sf_full[k & 1]));
+            if (lane == 0) bar_arrive(smem_u32(&S->sf_full[k & 1]));
         }
     }
     __syncwarp();
@@ -245,38 +211,6 @@ __global__ void zero_kernel(const __grid_constant__ MatmulParams P, uint32_t wid
         for (uint64_t i = threadIdx.x; i < (uint64_t)P.n * width; i += blockDim.x) P.out[r * P.ld_out + i] = 0;
 }
 
-// ---- host ----
-
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeFn encode_fn()
-{
-    static const EncodeFn fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) p = nullptr;
-        return (EncodeFn)p;
-    }();
-    return fn;
-}
-
-// A matrix as tiles of 128 rows x 128 bytes.
-static bool make_map(CUtensorMap* map, const zc_fp8_matrix* x)
-{
-    const cuuint64_t dims[2] = {x->cols, x->rows}, pitch[1] = {x->ld_elems};
-    const cuuint32_t box[2] = {kStepBytes, kTile}, step[2] = {1, 1};
-    return encode_fn() && encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, x->d_elems, dims, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-static uint32_t instruction(const zc_fp8_matrix* a, const zc_fp8_matrix* b, uint32_t m, uint32_t n)
-{
-    const uint32_t fa = a->format == ZC_FMT_FP8_E5M2, fb = b->format == ZC_FMT_FP8_E5M2;
-    // A and B types, N / 8, E8M0 scales, M / 16; both operands have k as their fastest axis
-    return (fa << 7) | (fb << 10) | ((n >> 3) << 17) | (1u << 23) | ((m >> 4) << 24);
-}
-
 }  // namespace zc
 
 using namespace zc;
@@ -316,10 +250,10 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
     P.spin_limit = test_knobs().spin_limit;
     P.skip_copy = test_knobs().skip_copy;
     CUtensorMap map_a, map_b;
-    if (!make_map(&map_a, a) || !make_map(&map_b, b)) return ZC_E_CUDA;
+    if (!make_map(&map_a, a->d_elems, a->rows, a->cols, a->ld_elems, kTile) || !make_map(&map_b, b->d_elems, b->rows, b->cols, b->ld_elems, kTile)) return ZC_E_CUDA;
     P.tiles_m = (uint32_t)ceil_div(P.m, kTile);
     P.tiles_n = (uint32_t)ceil_div(P.n, kTile);
-    P.idesc = instruction(a, b, 128, 128);
+    P.idesc = instruction_of(a->format, b->format, 128, 128);
     if (P.tiles_m > 65535) return ZC_E_TOO_LARGE;
     const uint64_t tiles = (uint64_t)P.tiles_m * P.tiles_n;
     uint32_t parts = 1;
@@ -341,13 +275,8 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
 
 zc_status zc_fp8_status(void* cuda_stream)
 {
-    cudaStream_t st = (cudaStream_t)cuda_stream;
-    unsigned int h = 0;
-    const unsigned int zero = 0;
-    if (cudaMemcpyFromSymbolAsync(&h, g_fp8_timeout, sizeof h, 0, cudaMemcpyDeviceToHost, st) != cudaSuccess) return ZC_E_CUDA;
-    if (cudaMemcpyToSymbolAsync(g_fp8_timeout, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st) != cudaSuccess) return ZC_E_CUDA;
-    if (cudaStreamSynchronize(st) != cudaSuccess) return ZC_E_CUDA;
-    return h ? ZC_E_DEVICE_TIMEOUT : ZC_OK;
+    const zc_status product = read_timeout((cudaStream_t)cuda_stream), layer = moe_read_timeout((cudaStream_t)cuda_stream);
+    return product != ZC_OK ? product : layer;
 }
 
 }  // extern "C"

@@ -1,45 +1,54 @@
 // zc_fp8_moe: a mixture-of-experts layer for a few tokens, in two kernels.
 //
-// With a few tokens the time goes into reading the chosen experts' weights once, so both kernels stream them straight into
-// registers: a warp's step is a tile of 16 rows x 64 bytes (two 16-byte loads a lane, four steps ahead), turned into BF16 (FP16
-// for FP16 activations), which hold FP8 values exactly, and multiplied with up to 32 tokens by warp-wide matrix
-// instructions.  The order of k inside an instruction is free as long as both operands agree on it: lane 4 g + t takes bytes
-// 16 t .. 16 t + 15 of rows g and g + 8, so no weight passes through shared memory.  Tiles of all chosen experts form one
-// sequence that is cut into equal ranges, one per block; within a block every warp takes its share of k of each tile, and the
-// warps' parts are added up in shared memory in the order of the warps.
+// With a few tokens the time goes into reading the chosen experts' weights once.  They are streamed by tensor copies into shared
+// memory and multiplied there as they are, FP8 with their scale bytes, on the fifth-generation tensor cores: no thread ever
+// touches a weight.  (Widening them in registers for warp-wide BF16 instructions took 350 instructions per KiB and ran at a
+// sixth of the memory's rate.)  The instruction wants FP8 on the other side as well, so an activation is written as a sum of
+// E4M3 pieces, v = 2^s (q0 + 2^-4 q1 + 2^-8 q2 + ...), with s from the largest magnitude of 128 columns: q_i is what the
+// pieces before it leave, rounded, and each piece takes at least four bits more.  Three pieces hold BF16 and FP16 exactly
+// (8 and 11 bits) down to 2^-17 of the largest of the 128, and nothing smaller is off by more than 2^-25 of it.  The
+// pieces are rows of the same operand, so they cost columns of the accumulator, and their sum is taken in FP32 at the end.
 //
-//   kernel 1  routes (every cluster for itself, so that no block waits for another cluster), then gate and up: a tile is 8 rows of
-//             gate and the same 8 of up, so that a thread ends with both and writes silu(gate) * up * p
-//   kernel 2  down: 16 rows a tile, one FP32 row of partial results per (token, expert); the block that completes a
-//             tile's last expert adds the experts up in the order of the token's list
-#include "zc_fp8.cuh"
+// Rows are handed out in groups of eight, the swizzle's height: tiles of all chosen experts form one sequence of groups that is cut
+// into equal ranges, one per block.
+//
+//   kernel 1  routes (every cluster for itself, so that no block waits for another cluster), then gate and up: a tile is up to 64
+//             rows of gate and the same of up in alternating groups, so that a warp ends with both
+//   kernel 2  down: up to 128 rows a tile, one FP32 row of partial results per (token, expert); the block that completes a
+//             group's last expert adds the experts up in the order of the token's list
+//
+// Warps of a block: 0 tensor copies, 1 matrix instructions, 2 the weights' scale bytes, 4-7 results, 8-13 the activations' pieces (14, 15: routing only).
+#include "zc_fp8_tensor.cuh"
 
 namespace zc {
 
-constexpr uint32_t kMoeWarps = 8, kMoeThreads = 32 * kMoeWarps;
+constexpr uint32_t kMoeWarps = 16, kMoeThreads = 32 * kMoeWarps;
 constexpr uint32_t kMoeCluster = 4;
-constexpr uint32_t kMoeSlots = 8;                // results of 16 rows x 8 tokens that a block adds up at a time
 constexpr uint32_t kMoePass = 32;                // tokens that share a reading of a tile
-constexpr uint32_t kMoeAhead = 4;                // steps that a warp's loads are ahead
 constexpr uint32_t kMaxTokens = ZC_FP8_MOE_MAX_TOKENS, kMaxExperts = ZC_FP8_MOE_MAX_EXPERTS;
 constexpr uint32_t kMaxRows = kMaxTokens * ZC_FP8_MOE_MAX_TOP_K;
+constexpr uint32_t kMoeStages = 6;
+constexpr uint32_t kMoeStageBytes = 16384 + 16384 + 1024 + 1024;   // weights, pieces, scale words of both (the rest keeps 1 KiB alignment)
+constexpr uint32_t kMoeTmemCols = 512;           // two accumulators of 128 columns, then 4 + 4 scale columns per stage
+constexpr uint32_t kMoeTmemScales = 256;
 
 struct MoeParams {
     const uint8_t *x, *router;                   // rows of BF16 or FP16
     uint64_t ld_x, ld_router;                    // elements
-    const uint8_t *gate_up, *gate_up_scales, *down, *down_scales;
-    uint64_t ld_gate_up, ld_down;
+    const uint8_t *gate_up_scales, *down_scales;
     uint32_t tokens, experts, top_k, hidden, inter;
     uint32_t hidden_pad, inter_pad;              // rounded up to 64 columns
+    uint32_t idesc;                              // matrix instruction without its N
     uint32_t *ids_out;
     float *weights_out;
     uint8_t *y;
     uint64_t ld_y;                               // elements
+    uint32_t spin_limit, skip_copy;
     // workspace
-    uint32_t *route;                             // [0]: chosen experts; then their numbers, their first rows
+    uint32_t *route;                             // [0]: chosen experts, [1]: passes; then the experts' numbers, their first rows and passes
     uint32_t *row_of;                            // [tokens][top_k]: row of a token's j-th expert
-    uint32_t *done;                              // [tiles of down]: experts whose part is written
-    uint16_t *h;                                 // [rows][2][inter_pad]: BF16, upper and lower part
+    uint32_t *done;                              // [groups of down]: passes of experts whose part is written
+    float *h;                                    // [rows][inter_pad]
     float *z;                                    // [rows][hidden_pad]
 };
 
@@ -50,34 +59,26 @@ struct Routing {
     uint16_t first[kMaxExperts + 1];             // first row of an expert's tokens
     uint16_t pass[kMaxExperts + 1];              // passes of the experts before
 };
-struct SlotInfo { uint16_t active, count; uint32_t tile, row; };
 struct MoeShared {
+    uint64_t full[kMoeStages], empty[kMoeStages], acc_full[2], acc_empty[2];
+    uint32_t tmem, failed;
     Routing R;
-    SlotInfo slot[2][kMoeSlots];
-    float row_p[kMaxRows];
     uint8_t row_token[kMaxRows];
-    float p[kMaxRows];                           // [tokens of this block][top_k] of the cluster's share, then of all tokens
+    float row_p[kMaxRows];
+    uint32_t last[16];
+};
+// while routing, where the stages will be
+struct MoeRouting {
+    double items[32 * 128], logits[64 * kMaxTokens];
+    float p[kMaxRows];                           // of this block's share of the tokens
     uint16_t id[kMaxRows];
     float p_all[kMaxRows];
     uint16_t id_all[kMaxRows];
     unsigned long long mask[kMaxExperts];        // tokens that chose the expert
-    uint32_t last[kMoeSlots];
 };
+constexpr size_t kMoeSmem = 1024 + kMoeStages * kMoeStageBytes + sizeof(MoeShared);
+static_assert(sizeof(MoeRouting) <= kMoeStages * kMoeStageBytes && kMoeSmem <= kMaxSmem, "shared memory");
 
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-// two FP8 bytes as a pair of FP16 or BF16 (both exact)
-template <bool E5M2, bool HALF>
-__device__ __forceinline__ uint32_t widen(uint32_t two)
-{
-    const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, E5M2 ? __NV_E5M2 : __NV_E4M3);
-    if (HALF) return (uint32_t)r.x | ((uint32_t)r.y << 16);
-    const float2 f = __half22float2(__half2(r));
-    return pack_bf16(f.x, f.y);
-}
 template <bool HALF>
 __device__ __forceinline__ void mma16(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1)
 {
@@ -100,183 +101,262 @@ __device__ __forceinline__ uint4 zero4() { return make_uint4(0, 0, 0, 0); }
 
 // ---- the weights' stream --------------------------------------------------------------------------------------------
 
-// Where a warp's loads, or its products, are: expert, tile of rows, pass over the expert's tokens, chunk of 64 columns.
-struct Cursor {
-    uint32_t active, tile, pass, chunk;
+// A tile: `groups` groups of eight rows (UP: of gate and of up each) of a chosen expert, for up to 32 of its tokens.
+struct Tile {
+    uint32_t active, expert, group, groups, row, count;      // row, count: its tokens' rows
 };
 
-// UP: tiles of 8 + 8 rows of gate and up, x as the other operand; else tiles of 16 rows of down, h as the other operand.
-template <bool UP, bool E5M2, bool HALF>
-struct Stream {
-    const MoeParams& P;
-    MoeShared& S;
-    float4* parts;                               // [2][kMoeSlots][kMoeWarps][32]
-    uint32_t tiles, cols, c_lo, c_hi, n_warps;
-    uint32_t g, t, lane, warp;
-
-    struct Step { uint4 a, b; uint32_t s; };
-
-    __device__ __forceinline__ uint32_t passes(uint32_t active) const { return S.R.pass[active + 1] - S.R.pass[active]; }
-
-    __device__ __forceinline__ void advance(Cursor& c) const
+// The tiles of units first .. end - 1, a unit being a group of an expert; all roles walk through them alike.
+template <bool UP>
+struct Tiles {
+    static constexpr uint32_t kMost = UP ? 8 : 16;
+    const Routing& R;
+    uint32_t per_expert, at, end, pass;
+    __device__ __forceinline__ Tiles(const Routing& r, uint32_t rows, uint32_t block, uint32_t blocks)
+        : R(r), per_expert((rows + 7) >> 3), pass(0)
     {
-        if (++c.chunk < c_hi) return;
-        c.chunk = c_lo;
-        if (++c.pass < passes(c.active)) return;
-        c.pass = 0;
-        if (++c.tile < tiles) return;
-        c.tile = 0;
-        ++c.active;
+        const uint64_t units = (uint64_t)per_expert * r.n_active;
+        at = (uint32_t)(units * block / blocks);
+        end = (uint32_t)(units * (block + 1) / blocks);
     }
-
-    __device__ __forceinline__ Step load(const Cursor& c) const
+    __device__ __forceinline__ bool next(Tile& t)
     {
-        Step r{zero4(), zero4(), 0};
-        const uint32_t e = S.R.expert[c.active], col = c.chunk * 64 + 16 * t, sc = c.chunk >> 1;
-        const uint32_t limit = UP ? P.inter : P.hidden;
-        const uint32_t row_a = UP ? c.tile * 8 + g : c.tile * 16 + g, row_b = UP ? row_a : row_a + 8;
-        const uint64_t ld = UP ? P.ld_gate_up : P.ld_down;
-        const uint8_t* w = UP ? P.gate_up + (uint64_t)e * 2 * P.inter * ld : P.down + (uint64_t)e * P.hidden * ld;
-        const uint32_t sld = (cols + 127) >> 7, srows = (limit + 127) >> 7;
-        const uint8_t* s = (UP ? P.gate_up_scales + (uint64_t)e * 2 * srows * sld : P.down_scales + (uint64_t)e * srows * sld) + sc;
-        if (col < cols) {
-            if (row_a < limit) r.a = ld_stream_v4(w + (uint64_t)row_a * ld + col);
-            if (row_b < limit) r.b = ld_stream_v4(w + (uint64_t)(UP ? P.inter + row_b : row_b) * ld + col);
-        }
-        const uint32_t srow = (UP ? c.tile * 8 : c.tile * 16) >> 7;
-        if (srow < srows) {
-            const uint32_t s0 = __ldg(s + (uint64_t)srow * sld), s1 = UP ? __ldg(s + (uint64_t)(srows + srow) * sld) : s0;
-            r.s = s0 | (s1 << 8);
-        }
-        return r;
+        if (at >= end) return false;
+        t.active = at / per_expert;
+        t.expert = R.expert[t.active];
+        t.group = at - t.active * per_expert;
+        const uint32_t left = min(end - at, per_expert - t.group);
+        t.groups = min(left, kMost);
+        // a remainder is shared by the last two tiles
+        if (left > kMost && left < 2 * kMost) t.groups = (left + 1) / 2;
+        t.row = R.first[t.active] + pass * kMoePass;
+        const uint32_t n = R.first[t.active + 1] - t.row;
+        t.count = min(n, kMoePass);
+        if (n > kMoePass) ++pass;
+        else { pass = 0; at += t.groups; }
+        return true;
     }
+};
 
-    __device__ __forceinline__ void multiply(const Cursor& c, Step w, float acc[4][4], uint32_t row, uint32_t count) const
-    {
-        const uint32_t col = c.chunk * 64 + 16 * t;
-        if (col + 16 > cols) {
-            const uint32_t n = col < cols ? cols - col : 0;
-            w.a = first_bytes(w.a, n);
-            w.b = first_bytes(w.b, n);
-        }
-        const uint32_t wa[4] = {w.a.x, w.a.y, w.a.z, w.a.w}, wb[4] = {w.b.x, w.b.y, w.b.z, w.b.w};
-        uint32_t a[4][4];
+// Four activations of a lane as PIECES E4M3 words, in the block scale of the warp's 128 columns.
+template <int PIECES>
+__device__ __forceinline__ void make_pieces(const float v[4], uint32_t words[PIECES], uint32_t& scale)
+{
+    float m = fmaxf(fmaxf(finite_abs(v[0]), finite_abs(v[1])), fmaxf(finite_abs(v[2]), finite_abs(v[3])));
+    m = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m)));
+    scale = scale_byte<false>(m);
+    const float inv = inverse_scale(scale);
+    float f[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            a[j][0] = widen<E5M2, HALF>(wa[j] & 0xFFFFu);
-            a[j][1] = widen<E5M2, HALF>(wb[j] & 0xFFFFu);
-            a[j][2] = widen<E5M2, HALF>(wa[j] >> 16);
-            a[j][3] = widen<E5M2, HALF>(wb[j] >> 16);
-        }
-        const float s0 = scale_value(w.s & 255u), s1 = UP ? scale_value(w.s >> 8) : s0;
+    for (int i = 0; i < 4; ++i) f[i] = fabsf(v[i]) < __int_as_float(0x7F800000) ? v[i] * inv : __int_as_float(0x7FC00000);   // E4M3 has no infinity
 #pragma unroll
-        for (uint32_t n = 0; n < 4; ++n) {
-            if (n * 8 >= count) break;
-            float v[4] = {0, 0, 0, 0};
-            const bool mine = n * 8 + g < count;
-            if (UP) {
-                const uint8_t* x = P.x + 2 * ((uint64_t)(mine ? S.row_token[row + n * 8 + g] : 0) * P.ld_x + col);
-                uint4 lo = mine && col < cols ? ld_cached_v4(x) : zero4();
-                uint4 hi = mine && col + 8 < cols ? ld_cached_v4(x + 16) : zero4();
-                if (col + 16 > cols) {
-                    const uint32_t have = col < cols ? 2 * (cols - col) : 0;
-                    lo = first_bytes(lo, have);
-                    hi = first_bytes(hi, have > 16 ? have - 16 : 0);
-                }
-                mma16<HALF>(v, a[0], lo.x, lo.y);
-                mma16<HALF>(v, a[1], lo.z, lo.w);
-                mma16<HALF>(v, a[2], hi.x, hi.y);
-                mma16<HALF>(v, a[3], hi.z, hi.w);
-            } else {
-                // written by the kernel before this one: through L2, not the read-only path that it might have been fetched by
-                const uint16_t* h = P.h + (uint64_t)(row + n * 8 + (mine ? g : 0)) * 2 * P.inter_pad + col;
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const uint4* q = reinterpret_cast<const uint4*>(h + part * P.inter_pad);
-                    const uint4 lo = mine ? q[0] : zero4(), hi = mine ? q[1] : zero4();
-                    mma16<false>(v, a[0], lo.x, lo.y);
-                    mma16<false>(v, a[1], lo.z, lo.w);
-                    mma16<false>(v, a[2], hi.x, hi.y);
-                    mma16<false>(v, a[3], hi.z, hi.w);
-                }
-            }
-            acc[n][0] = fmaf(v[0], s0, acc[n][0]);
-            acc[n][1] = fmaf(v[1], s0, acc[n][1]);
-            acc[n][2] = fmaf(v[2], s1, acc[n][2]);
-            acc[n][3] = fmaf(v[3], s1, acc[n][3]);
+    for (int k = 0; k < PIECES; ++k) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
+        // scales end at 2^-127: what would need a smaller one is left out
+        words[k] = scale >= 4u * k ? lo | (hi << 16) : 0u;
+        if (k + 1 < PIECES) {
+            const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)lo, __NV_E4M3)));
+            const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)hi, __NV_E4M3)));
+            f[0] = (f[0] - a.x) * 16.0f;
+            f[1] = (f[1] - a.y) * 16.0f;
+            f[2] = (f[2] - b.x) * 16.0f;
+            f[3] = (f[3] - b.y) * 16.0f;
         }
     }
+}
 
-    // All warps, for the block's range of the tiles; `finish(batch)` after each batch of up to kMoeSlots results.
-    template <typename Finish>
-    __device__ __forceinline__ void run(uint32_t first, uint32_t end, Finish finish)
-    {
-        if (first >= end) return;
-        const uint32_t chunks = (cols + 63) >> 6;
-        n_warps = chunks < kMoeWarps ? chunks : kMoeWarps;
-        const bool busy = warp < n_warps;
-        c_lo = busy ? chunks * warp / n_warps : 0;
-        c_hi = busy ? chunks * (warp + 1) / n_warps : 1;
-        // the tile numbered `first`: passes over an expert's tokens lie next to each other, so that the second finds the tile cached
-        Cursor at{0, 0, 0, c_lo};
-        while (first >= (uint32_t)S.R.pass[at.active + 1] * tiles) ++at.active;
-        const uint32_t rest = first - S.R.pass[at.active] * tiles;
-        at.tile = rest / passes(at.active);
-        at.pass = rest % passes(at.active);
-        Cursor ahead = at;
-        uint32_t to_load = busy ? (end - first) * (c_hi - c_lo) : 0;
-        Step ring[kMoeAhead];
-#pragma unroll
-        for (uint32_t i = 0; i < kMoeAhead; ++i) {
-            ring[i] = Step{zero4(), zero4(), 0};
-            if (to_load) { ring[i] = load(ahead); advance(ahead); --to_load; }
-        }
-        float acc[4][4] = {};
-        uint32_t batch = 0, used = 0, left = end - first;
-        while (left) {
-#pragma unroll
-            for (uint32_t i = 0; i < kMoeAhead; ++i) {
-                if (!left) break;
-                const uint32_t row = S.R.first[at.active] + at.pass * kMoePass;
-                const uint32_t n = S.R.first[at.active + 1] - row, count = n < kMoePass ? n : kMoePass, need = (count + 7) >> 3;
-                if (used + need > kMoeSlots) {               // uniform: every warp sees the same tiles
-                    finish(batch, used);
-                    ++batch;
-                    used = 0;
-                }
-                if (busy) {
-                    multiply(at, ring[i], acc, row, count);
-                    if (to_load) { ring[i] = load(ahead); advance(ahead); --to_load; }
-                }
-                if (!busy || at.chunk + 1 == c_hi) {
-#pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) {
-                        if (k >= need) break;
-                        if (busy) parts[(((batch & 1) * kMoeSlots + used + k) * kMoeWarps + warp) * 32 + lane] = make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
-                        if (warp == 0 && lane == 0)
-                            S.slot[batch & 1][used + k] = SlotInfo{(uint16_t)at.active, (uint16_t)(count - 8 * k < 8 ? count - 8 * k : 8), at.tile, row + 8 * k};
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) acc[k][q] = 0.0f;
+// What a block does after the routing: its share of gate and up (UP) or of down.  HALF: activations of gate and up are FP16.
+template <bool UP, bool HALF, int PIECES, typename Finish>
+__device__ __forceinline__ void stream_weights(const MoeParams& P, const CUtensorMap* map, MoeShared& S, uint32_t base, uint32_t blocks, Finish finish)
+{
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t cols = UP ? P.hidden : P.inter, rows = UP ? P.inter : P.hidden;
+    const uint32_t steps = (cols + 127) >> 7;
+    const Waiter wait{P.spin_limit, &S.failed};
+    Tiles<UP> tiles(S.R, rows, blockIdx.x, blocks);
+    Tile t;
+    uint32_t n = 0;                              // steps so far
+    const uint32_t tmem = S.tmem;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            bool ok = true;
+            while (ok && tiles.next(t)) {
+                const uint32_t row0 = t.expert * (UP ? 2 * P.inter : P.hidden) + t.group * 8;
+                for (uint32_t k = 0; k < steps; ++k, ++n) {
+                    const uint32_t st = n % kMoeStages;
+                    if (n >= kMoeStages && !(ok = wait(smem_u32(&S.empty[st]), (n / kMoeStages - 1) & 1))) break;
+                    const uint32_t bar = smem_u32(&S.full[st]), to = base + st * kMoeStageBytes;
+                    bar_expect(bar, t.groups * (UP ? 2048 : 1024));
+                    if (P.skip_copy) continue;
+                    for (uint32_t i = 0; i < t.groups; ++i) {
+                        tensor_copy<1>(to + i * (UP ? 2048 : 1024), map, (int)(k * 128), (int)(row0 + 8 * i), bar);
+                        if (UP) tensor_copy<1>(to + i * 2048 + 1024, map, (int)(k * 128), (int)(row0 + P.inter + 8 * i), bar);
                     }
-                    used += need;
-                    --left;
                 }
-                advance(at);
+            }
+            // after a wait that gave up, copies may still be on their way into this block's shared memory
+            if (!ok && !P.skip_copy)
+                for (uint32_t i = n > kMoeStages ? n - kMoeStages : 0; i < n; ++i)
+                    for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S.full[i % kMoeStages]), (i / kMoeStages) & 1); ++q) { }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            uint32_t tile = 0;
+            bool ok = true;
+            while (ok && tiles.next(t)) {
+                const uint32_t buf = tile & 1, d = tmem + buf * 128;
+                const uint32_t cols_d = (((t.count + 7) & ~7u) * PIECES + 15) & ~15u;      // what is behind the last piece is computed and not used
+                const uint32_t idesc = P.idesc | ((cols_d >> 3) << 17);
+                if (tile >= 2 && !(ok = wait(smem_u32(&S.acc_empty[buf]), ((tile >> 1) - 1) & 1))) break;
+                tc_fence_after();
+                for (uint32_t k = 0; k < steps; ++k, ++n) {
+                    const uint32_t st = n % kMoeStages;
+                    if (!(ok = wait(smem_u32(&S.full[st]), (n / kMoeStages) & 1))) break;
+                    tc_fence_after();
+                    const uint32_t at = base + st * kMoeStageBytes, sf = tmem + kMoeTmemScales + st * 8;
+                    tmem_copy_scales(sf, at + 32768);
+                    tmem_copy_scales(sf + 4, at + 32768 + 512);
+                    const uint64_t da = operand_desc(at), db = operand_desc(at + 16384);
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) mma_scaled<1>(d, da + 2 * j, db + 2 * j, idesc, sf, sf + 4, k | j);
+                    mma_commit<1>(smem_u32(&S.empty[st]));
+                }
+                mma_commit<1>(smem_u32(&S.acc_full[buf]));
+                ++tile;
             }
         }
-        finish(batch, used);
-    }
-
-    __device__ __forceinline__ float4 sum(uint32_t batch, uint32_t slot) const
-    {
-        float4 s = make_float4(0, 0, 0, 0);
-        for (uint32_t w = 0; w < n_warps; ++w) {
-            const float4 v = parts[(((batch & 1) * kMoeSlots + slot) * kMoeWarps + w) * 32 + lane];
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    } else if (warp == 2) {
+        // scale bytes of the weights, four steps at a time; row r of the tile's operand is row 32 j + lane
+        const uint32_t sld = steps, srows = (rows + 127) >> 7;
+        bool ok = true;
+        while (ok && tiles.next(t)) {
+            const uint8_t* s = (UP ? P.gate_up_scales + (uint64_t)t.expert * 2 * srows * sld : P.down_scales + (uint64_t)t.expert * srows * sld);
+            const uint8_t* mine[4];
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                const uint32_t g = 4 * j + (lane >> 3);                  // group of the operand
+                const uint32_t r = min((t.group + (UP ? g >> 1 : g)) * 8 + (lane & 7), rows - 1);
+                mine[j] = s + (uint64_t)((UP && (g & 1) ? srows : 0) + (r >> 7)) * sld;
+            }
+            uint32_t w[4];
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) w[j] = scale_word(mine[j], 0, 0, 0, 1, 0, steps);
+            for (uint32_t k = 0; k < steps && ok; k += 4) {
+                uint32_t next[4];
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) next[j] = k + 4 < steps ? scale_word(mine[j], 0, 0, 0, 1, k + 4, steps) : 0;
+                for (uint32_t q = 0; q < 4 && k + q < steps; ++q, ++n) {
+                    const uint32_t st = n % kMoeStages;
+                    if (!(ok = __all_sync(0xFFFFFFFFu, n < kMoeStages || wait(smem_u32(&S.empty[st]), (n / kMoeStages - 1) & 1)))) break;
+                    const uint32_t at = base + st * kMoeStageBytes + 32768 + lane * 16;
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"((w[0] >> (8 * q)) & 255u), "r"((w[1] >> (8 * q)) & 255u),
+                                 "r"((w[2] >> (8 * q)) & 255u), "r"((w[3] >> (8 * q)) & 255u) : "memory");
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_u32(&S.full[st]));
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) w[j] = next[j];
+            }
         }
-        return s;
+    } else if (warp >= 8) {
+        // a warp has a stage of its own: the time of all stages for the latency of its loads, and it sees every phase of its
+        // stage's barrier (a wait by parity that skipped one would take the phase before for it)
+        const uint32_t st = warp - 8, at = base + st * kMoeStageBytes;
+        bool ok = true;
+        while (ok && tiles.next(t)) {
+            const uint32_t padded = (t.count + 7) & ~7u;
+            for (uint32_t k = 0; k < steps; ++k, ++n) {
+                if (n % kMoeStages != st) continue;
+                const uint32_t col = k * 128 + lane * 4;
+                for (uint32_t c = 0; c < t.count; c += 8) {
+                    uint4 raw[8];
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) {
+                        raw[i] = zero4();
+                        if (c + i < t.count && col < cols) {
+                            if (UP) {
+                                const uint2 v = __ldg(reinterpret_cast<const uint2*>(P.x + 2 * ((uint64_t)S.row_token[t.row + c + i] * P.ld_x + col)));
+                                raw[i].x = v.x;
+                                raw[i].y = v.y;
+                            } else {
+                                raw[i] = *reinterpret_cast<const uint4*>(P.h + (uint64_t)(t.row + c + i) * P.inter_pad + col);
+                            }
+                        }
+                    }
+                    if (c == 0 && !(ok = __all_sync(0xFFFFFFFFu, n < kMoeStages || wait(smem_u32(&S.empty[st]), (n / kMoeStages - 1) & 1)))) break;
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) {
+                        if (c + i >= t.count) break;
+                        float v[4];
+                        if (UP) {
+                            const uint32_t w[2] = {raw[i].x, raw[i].y};
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const uint16_t u = (uint16_t)(w[q >> 1] >> (16 * (q & 1)));
+                                v[q] = HALF ? __half2float(__ushort_as_half(u)) : __bfloat162float(__ushort_as_bfloat16(u));
+                            }
+                        } else {
+                            v[0] = __uint_as_float(raw[i].x); v[1] = __uint_as_float(raw[i].y);
+                            v[2] = __uint_as_float(raw[i].z); v[3] = __uint_as_float(raw[i].w);
+                        }
+                        if (col + 4 > cols)
+#pragma unroll
+                            for (uint32_t q = 0; q < 4; ++q)
+                                if (col + q >= cols) v[q] = 0.0f;
+                        uint32_t words[PIECES], scale;
+                        make_pieces<PIECES>(v, words, scale);
+#pragma unroll
+                        for (uint32_t q = 0; q < PIECES; ++q) {
+                            const uint32_t r = q * padded + c + i;
+                            sts32(at + 16384 + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4, words[q]);
+                            if (lane == q) sts32(at + 32768 + 512 + (r & 31) * 16 + (r >> 5) * 4, scale >= 4u * q ? scale - 4u * q : 0u);
+                        }
+                    }
+                }
+                if (!ok) break;
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_u32(&S.full[st]));
+            }
+        }
+    } else if (warp >= 4) {
+        const uint32_t quad = warp & 3;
+        uint32_t tile = 0;
+        while (tiles.next(t)) {
+            const uint32_t buf = tile & 1, padded = (t.count + 7) & ~7u;
+            // the four warps go on, or stop, together: they meet at a barrier of their own
+            uint32_t ok = wait(smem_u32(&S.acc_full[buf]), (tile >> 1) & 1) && !*wait.failed;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %0, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "+r"(ok) :: "memory");
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t d = tmem + (quad * 32u << 16) + buf * 128;
+            for (uint32_t c = 0; c < t.count; c += 8) {
+                float part[PIECES][8];
+#pragma unroll
+                for (uint32_t q = 0; q < PIECES; ++q) tmem_ld8(d + q * padded + c, part[q]);
+                tmem_ld_wait();
+                // the smallest pieces first
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float sum = part[PIECES - 1][i];
+#pragma unroll
+                    for (int q = PIECES - 2; q >= 0; --q) sum += part[q][i];
+                    part[0][i] = sum;
+                }
+                finish.store(t, c, quad * 32 + lane, part[0]);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_u32(&S.acc_empty[buf]));
+            finish.tile_done(t);
+            ++tile;
+        }
     }
-};
+    __syncwarp();
+}
 
 // ---- routing ----------------------------------------------------------------------------------------------------------
 
@@ -355,10 +435,10 @@ __device__ __forceinline__ void router_logits(const MoeParams& P, uint32_t rank,
 }
 
 // The top_k experts and their weights for this block's share of the tokens (rank, rank + 4, ...), one warp a token.
-__device__ __forceinline__ void choose(const MoeParams& P, uint32_t rank, const double* logits, MoeShared& S)
+__device__ __forceinline__ void choose(const MoeParams& P, uint32_t rank, MoeRouting& S)
 {
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t base = smem_u32(logits);
+    const uint32_t base = smem_u32(S.logits);
     for (uint32_t i = warp; rank + i * kMoeCluster < P.tokens; i += kMoeWarps) {
         const uint32_t tok = rank + i * kMoeCluster;
         unsigned long long key[kMaxExperts / 32];
@@ -404,7 +484,7 @@ __device__ __forceinline__ void choose(const MoeParams& P, uint32_t rank, const 
 }
 
 // From the tokens' choices to the experts' lists: tokens of an expert in ascending order, experts in ascending order.
-__device__ __forceinline__ void make_lists(const MoeParams& P, MoeShared& S)
+__device__ __forceinline__ void make_lists(const MoeParams& P, MoeRouting& S, Routing& R)
 {
     const uint32_t tid = threadIdx.x, n = P.tokens * P.top_k;
     for (uint32_t e = tid; e < kMaxExperts; e += kMoeThreads) S.mask[e] = 0;
@@ -429,125 +509,176 @@ __device__ __forceinline__ void make_lists(const MoeParams& P, MoeShared& S)
         for (uint32_t k = 0; k < 8; ++k) {
             const uint32_t cnt = __popcll(S.mask[tid * 8 + k]);
             if (!cnt) continue;
-            S.R.expert[at] = (uint16_t)(tid * 8 + k);
-            S.R.first[at] = (uint16_t)row;
-            S.R.pass[at] = (uint16_t)pass;
+            R.expert[at] = (uint16_t)(tid * 8 + k);
+            R.first[at] = (uint16_t)row;
+            R.pass[at] = (uint16_t)pass;
             ++at;
             row += cnt;
             pass += (cnt + kMoePass - 1) / kMoePass;
         }
         if (tid == 31) {
-            S.R.n_active = b;
-            S.R.n_passes = c;
-            S.R.first[b] = (uint16_t)a;
-            S.R.pass[b] = (uint16_t)c;
+            R.n_active = b;
+            R.n_passes = c;
+            R.first[b] = (uint16_t)a;
+            R.pass[b] = (uint16_t)c;
         }
     }
     __syncthreads();
 }
 
 struct RowFinder {
-    const MoeShared& S;
+    const MoeRouting& S;
+    const Routing& R;
     // row of a token in the list of expert e: the first row of e is that of the number of (token, expert) pairs before it
     __device__ __forceinline__ uint32_t operator()(uint32_t e, uint32_t token) const
     {
-        uint32_t lo = 0, hi = S.R.n_active;
+        uint32_t lo = 0, hi = R.n_active;
         while (hi - lo > 1) {
             const uint32_t mid = (lo + hi) / 2;
-            if (S.R.expert[mid] <= e) lo = mid; else hi = mid;
+            if (R.expert[mid] <= e) lo = mid; else hi = mid;
         }
-        return S.R.first[lo] + __popcll(S.mask[e] & ((1ull << token) - 1));
+        return R.first[lo] + __popcll(S.mask[e] & ((1ull << token) - 1));
     }
 };
 
-constexpr size_t kMoePartBytes = 2ull * kMoeSlots * kMoeWarps * 32 * sizeof(float4);          // 64 KiB
-constexpr size_t kMoeSmem = kMoePartBytes + sizeof(MoeShared);
-static_assert(kMoePartBytes >= (32 * 128 + 64 * kMaxTokens) * sizeof(double), "the router's sums lie where the tiles' parts will be");
-
-template <bool E5M2, bool HALF>
-__global__ void __launch_bounds__(kMoeThreads, 2)
-moe_up_kernel(const __grid_constant__ MoeParams P)
+// Barriers and tensor memory; all threads.
+__device__ __forceinline__ void moe_setup(MoeShared& S)
 {
-    extern __shared__ __align__(16) uint8_t raw[];
-    float4* parts = reinterpret_cast<float4*>(raw);
-    MoeShared& S = *reinterpret_cast<MoeShared*>(raw + kMoePartBytes);
-    double* items = reinterpret_cast<double*>(raw);
-    double* logits = items + 32 * 128;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp == 0 && lane == 0) {
+        for (uint32_t i = 0; i < kMoeStages; ++i) { bar_init(smem_u32(&S.full[i]), 3); bar_init(smem_u32(&S.empty[i]), 1); }
+        for (uint32_t i = 0; i < 2; ++i) { bar_init(smem_u32(&S.acc_full[i]), 1); bar_init(smem_u32(&S.acc_empty[i]), 4); }
+        S.failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc<1>(smem_u32(&S.tmem), kMoeTmemCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+}
+
+// silu(gate) * up * p into the hidden vectors; groups of gate and up alternate, so a lane's partner is eight lanes away
+struct FinishUp {
+    const MoeParams& P;
+    const MoeShared& S;
+    __device__ __forceinline__ void store(const Tile& t, uint32_t c, uint32_t row, const float v[8]) const
+    {
+        const uint32_t ch = (t.group + (row >> 4)) * 8 + (row & 7);
+        const bool gate = (row & 8) == 0 && (row >> 4) < t.groups && ch < P.inter;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const float up = __shfl_xor_sync(0xFFFFFFFFu, v[i], 8);
+            if (gate && c + i < t.count)
+                P.h[(uint64_t)(t.row + c + i) * P.inter_pad + ch] = v[i] / (1.0f + expf(-v[i])) * up * S.row_p[t.row + c + i];
+        }
+    }
+    __device__ __forceinline__ void tile_done(const Tile&) const { }
+};
+
+template <bool HALF>
+struct FinishDown {
+    const MoeParams& P;
+    MoeShared& S;
+    uint32_t n_passes;
+    __device__ __forceinline__ void store(const Tile& t, uint32_t c, uint32_t row, const float v[8]) const
+    {
+        const uint32_t r = t.group * 8 + row;
+        if (row >= t.groups * 8 || r >= P.hidden) return;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (c + i < t.count) P.z[(uint64_t)(t.row + c + i) * P.hidden_pad + r] = v[i];
+    }
+    // the four warps: whoever completes a group's last pass adds the experts up
+    __device__ __forceinline__ void tile_done(const Tile& t) const
+    {
+        const uint32_t tid = threadIdx.x & 127;
+        __threadfence();
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (tid < t.groups) {
+            S.last[tid] = atomicAdd(&P.done[t.group + tid], 1u) + 1 == n_passes;
+            __threadfence();
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        for (uint32_t i = tid; i < t.groups * 8 * P.tokens; i += 128) {
+            const uint32_t g = (i >> 3) % t.groups, tok = (i >> 3) / t.groups, r = (t.group + g) * 8 + (i & 7);
+            if (!S.last[g] || r >= P.hidden) continue;
+            float y = 0;
+            for (uint32_t j = 0; j < P.top_k; ++j) y += __ldcg(P.z + (uint64_t)__ldcg(P.row_of + tok * P.top_k + j) * P.hidden_pad + r);
+            if (HALF) reinterpret_cast<__half*>(P.y)[(uint64_t)tok * P.ld_y + r] = __float2half_rn(y);
+            else reinterpret_cast<__nv_bfloat16*>(P.y)[(uint64_t)tok * P.ld_y + r] = __float2bfloat16_rn(y);
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+    }
+};
+
+// hidden vectors: twelve bits in three pieces err a sixteenth of what rounding y to BF16 does; FP16 takes sixteen in four
+template <bool HALF> constexpr int kHiddenPieces = HALF ? 4 : 3;
+
+template <bool HALF>
+__global__ void __launch_bounds__(kMoeThreads, 1)
+moe_up_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ MoeParams P)
+{
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    uint8_t* aligned = raw + (base - smem_u32(raw));
+    MoeShared& S = *reinterpret_cast<MoeShared*>(aligned + kMoeStages * kMoeStageBytes);
+    MoeRouting& T = *reinterpret_cast<MoeRouting*>(aligned);
     const uint32_t tid = threadIdx.x, rank = cluster_rank();
     const uint32_t n_rows = P.tokens * P.top_k;
 
     grid_launch_dependents();
-    router_logits<HALF>(P, rank, items, logits);
+    if (tid == 0) prefetch_map(&map);
+    moe_setup(S);
+    router_logits<HALF>(P, rank, T.items, T.logits);
     cluster_sync();
-    choose(P, rank, logits, S);
+    choose(P, rank, T);
     cluster_sync();
     for (uint32_t i = tid; i < n_rows; i += kMoeThreads) {
         const uint32_t tok = i / P.top_k, j = i % P.top_k, at = (tok / kMoeCluster) * P.top_k + j, from = tok % kMoeCluster;
         float p;
         uint16_t id;
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p) : "r"(map_shared(smem_u32(&S.p[at]), from)) : "memory");
-        asm volatile("ld.shared::cluster.u16 %0, [%1];" : "=h"(id) : "r"(map_shared(smem_u32(&S.id[at]), from)) : "memory");
-        S.p_all[i] = p;
-        S.id_all[i] = id;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p) : "r"(map_shared(smem_u32(&T.p[at]), from)) : "memory");
+        asm volatile("ld.shared::cluster.u16 %0, [%1];" : "=h"(id) : "r"(map_shared(smem_u32(&T.id[at]), from)) : "memory");
+        T.p_all[i] = p;
+        T.id_all[i] = id;
     }
-    cluster_sync();                              // nobody reads this block's shared memory any more
-    make_lists(P, S);
-    const RowFinder row_of{S};
+    make_lists(P, T, S.R);
+    const RowFinder row_of{T, S.R};
     for (uint32_t i = tid; i < n_rows; i += kMoeThreads) {
-        const uint32_t r = row_of(S.id_all[i], i / P.top_k);
-        S.row_p[r] = S.p_all[i];
+        const uint32_t r = row_of(T.id_all[i], i / P.top_k);
+        S.row_p[r] = T.p_all[i];
         S.row_token[r] = (uint8_t)(i / P.top_k);
         if (blockIdx.x == 0) {
             P.row_of[i] = r;
-            if (P.ids_out) P.ids_out[i] = S.id_all[i];
-            if (P.weights_out) P.weights_out[i] = S.p_all[i];
+            if (P.ids_out) P.ids_out[i] = T.id_all[i];
+            if (P.weights_out) P.weights_out[i] = T.p_all[i];
         }
     }
     if (blockIdx.x == 0) {
-        for (uint32_t i = tid; i < (P.hidden + 15) / 16; i += kMoeThreads) P.done[i] = 0;
+        for (uint32_t i = tid; i < (P.hidden + 7) / 8; i += kMoeThreads) P.done[i] = 0;
         for (uint32_t i = tid; i <= S.R.n_active; i += kMoeThreads) {
             if (i < S.R.n_active) P.route[2 + i] = S.R.expert[i];
             P.route[2 + kMaxExperts + i] = (uint32_t)S.R.first[i] | ((uint32_t)S.R.pass[i] << 16);
         }
         if (tid == 0) { P.route[0] = S.R.n_active; P.route[1] = S.R.n_passes; }
     }
+    fence_async_shared();                        // the routing's shared memory becomes the stages'
+    cluster_sync();                              // and no other block reads from it any more
+    stream_weights<true, HALF, 3>(P, &map, S, base, gridDim.x, FinishUp{P, S});
     __syncthreads();
-
-    const uint32_t tiles = P.inter_pad / 8;
-    Stream<true, E5M2, HALF> W{P, S, parts, tiles, P.hidden, 0, 0, 0, (tid & 31) >> 2, tid & 3, tid & 31, tid >> 5};
-    const uint64_t total = (uint64_t)tiles * S.R.n_passes;
-    W.run((uint32_t)(total * blockIdx.x / gridDim.x), (uint32_t)(total * (blockIdx.x + 1) / gridDim.x), [&](uint32_t batch, uint32_t used) {
-        __syncthreads();
-        const uint32_t slot = tid >> 5;
-        if (slot < used) {
-            const SlotInfo I = S.slot[batch & 1][slot];
-            const float4 v = W.sum(batch, slot);
-            const uint32_t ch = I.tile * 8 + W.g;
-#pragma unroll
-            for (uint32_t k = 0; k < 2; ++k) {
-                const uint32_t n = 2 * W.t + k;
-                if (n >= I.count) continue;
-                const float gate = k ? v.y : v.x, up = k ? v.w : v.z;
-                const float h = gate / (1.0f + expf(-gate)) * up * S.row_p[I.row + n];
-                // upper and lower half in BF16 each, 16 bits together: one of 8 bits would err as much as rounding y does
-                const __nv_bfloat16 hi = __float2bfloat16_rn(h);
-                const __nv_bfloat16 lo = __float2bfloat16_rn(isinf(__bfloat162float(hi)) ? 0.0f : h - __bfloat162float(hi));
-                uint16_t* to = P.h + (uint64_t)(I.row + n) * 2 * P.inter_pad + ch;
-                to[0] = *reinterpret_cast<const uint16_t*>(&hi);
-                to[P.inter_pad] = *reinterpret_cast<const uint16_t*>(&lo);
-            }
-        }
-    });
+    if (tid < 64 && tid >= 32) tmem_free<1>(S.tmem, kMoeTmemCols);
 }
 
-template <bool E5M2, bool HALF>
-__global__ void __launch_bounds__(kMoeThreads, 2)
-moe_down_kernel(const __grid_constant__ MoeParams P)
+template <bool HALF>
+__global__ void __launch_bounds__(kMoeThreads, 1)
+moe_down_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ MoeParams P)
 {
-    extern __shared__ __align__(16) uint8_t raw[];
-    float4* parts = reinterpret_cast<float4*>(raw);
-    MoeShared& S = *reinterpret_cast<MoeShared*>(raw + kMoePartBytes);
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    MoeShared& S = *reinterpret_cast<MoeShared*>(raw + (base - smem_u32(raw)) + kMoeStages * kMoeStageBytes);
     const uint32_t tid = threadIdx.x;
+    if (tid == 0) prefetch_map(&map);
+    moe_setup(S);
     grid_wait();
     const uint32_t n_active = P.route[0], n_passes = P.route[1];
     for (uint32_t i = tid; i <= n_active; i += kMoeThreads) {
@@ -556,43 +687,11 @@ moe_down_kernel(const __grid_constant__ MoeParams P)
         S.R.first[i] = (uint16_t)v;
         S.R.pass[i] = (uint16_t)(v >> 16);
     }
+    if (tid == 0) { S.R.n_active = n_active; S.R.n_passes = n_passes; }
     __syncthreads();
-    const uint32_t tiles = (P.hidden + 15) / 16;
-    Stream<false, E5M2, false> W{P, S, parts, tiles, P.inter, 0, 0, 0, (tid & 31) >> 2, tid & 3, tid & 31, tid >> 5};
-    const uint64_t total = (uint64_t)tiles * n_passes;
-    W.run((uint32_t)(total * blockIdx.x / gridDim.x), (uint32_t)(total * (blockIdx.x + 1) / gridDim.x), [&](uint32_t batch, uint32_t used) {
-        __syncthreads();
-        const uint32_t slot = tid >> 5;
-        if (slot < used) {
-            const SlotInfo I = S.slot[batch & 1][slot];
-            const float4 v = W.sum(batch, slot);
-            float* z = P.z + (uint64_t)(I.row + 2 * W.t) * P.hidden_pad + I.tile * 16 + W.g;
-            if (2 * W.t < I.count) { z[0] = v.x; z[8] = v.z; }
-            if (2 * W.t + 1 < I.count) { z[P.hidden_pad] = v.y; z[P.hidden_pad + 8] = v.w; }
-            __threadfence();
-        }
-        __syncthreads();
-        // one arrival per tile and pass: at its first slot
-        if (tid < used) {
-            const SlotInfo I = S.slot[batch & 1][tid];
-            const uint32_t r = I.row - S.R.first[I.active];
-            S.last[tid] = r % kMoePass == 0 ? atomicAdd(&P.done[I.tile], 1u) + 1 == n_passes : 0;
-            __threadfence();
-        }
-        __syncthreads();
-        for (uint32_t k = 0; k < used; ++k) {
-            if (!S.last[k]) continue;
-            const uint32_t row0 = S.slot[batch & 1][k].tile * 16;
-            for (uint32_t i = tid; i < P.tokens * 16; i += kMoeThreads) {
-                const uint32_t tok = i >> 4, r = row0 + (i & 15);
-                if (r >= P.hidden) continue;
-                float y = 0;
-                for (uint32_t j = 0; j < P.top_k; ++j) y += __ldcg(P.z + (uint64_t)P.row_of[tok * P.top_k + j] * P.hidden_pad + r);
-                if (HALF) reinterpret_cast<__half*>(P.y)[(uint64_t)tok * P.ld_y + r] = __float2half_rn(y);
-                else reinterpret_cast<__nv_bfloat16*>(P.y)[(uint64_t)tok * P.ld_y + r] = __float2bfloat16_rn(y);
-            }
-        }
-    });
+    stream_weights<false, HALF, kHiddenPieces<HALF>>(P, &map, S, base, gridDim.x, FinishDown<HALF>{P, S, n_passes});
+    __syncthreads();
+    if (tid < 64 && tid >= 32) tmem_free<1>(S.tmem, kMoeTmemCols);
 }
 
 // ---- host ----
@@ -606,7 +705,7 @@ static MoeLayout moe_layout(const zc_fp8_moe_layer* L, uint32_t tokens)
     auto take = [&](size_t bytes) { const size_t here = at; at += round_up(bytes, 256); return here; };
     o.route = take(4 * (2 + 2 * kMaxExperts + 2));
     o.row_of = take(4 * rows);
-    o.done = take(4 * (hidden_pad / 16));
+    o.done = take(4 * (hidden_pad / 8));
     o.h = take(4 * rows * inter_pad);
     o.z = take(4 * rows * hidden_pad);
     o.total = at;
@@ -626,12 +725,31 @@ static zc_status check_layer(const zc_fp8_moe_layer* L, uint32_t tokens)
     return ZC_OK;
 }
 
-template <bool E5M2, bool HALF>
-static cudaError_t launch_moe(const MoeParams& P, cudaStream_t st)
+// Blocks of `kernel` that are on the GPU at once, in whole clusters: one per SM where clusters of four fill it.
+static uint32_t resident_blocks(const void* kernel, uint32_t cluster)
 {
-    cudaError_t e = cudaFuncSetAttribute(moe_up_kernel<E5M2, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMoeSmem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(moe_down_kernel<E5M2, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMoeSmem);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((uint32_t)sm_count() / cluster * cluster);
+    cfg.blockDim = dim3(kMoeThreads);
+    cfg.dynamicSmemBytes = kMoeSmem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {cluster, 1, 1};
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) return 0;
+    return std::min((uint32_t)n * cluster, cfg.gridDim.x);
+}
+
+template <bool HALF>
+static cudaError_t launch_moe(const CUtensorMap& up, const CUtensorMap& down, const MoeParams& P, cudaStream_t st)
+{
+    cudaError_t e = cudaFuncSetAttribute(moe_up_kernel<HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMoeSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(moe_down_kernel<HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMoeSmem);
     if (e != cudaSuccess) return e;
+    static const uint32_t up_blocks = resident_blocks((const void*)moe_up_kernel<HALF>, kMoeCluster);
+    if (!up_blocks) return cudaErrorUnknown;
     cudaLaunchConfig_t cfg{};
     cfg.blockDim = dim3(kMoeThreads);
     cfg.dynamicSmemBytes = kMoeSmem;
@@ -641,14 +759,16 @@ static cudaError_t launch_moe(const MoeParams& P, cudaStream_t st)
     cfg.numAttrs = 1;
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim = {kMoeCluster, 1, 1};
-    cfg.gridDim = dim3(2 * (uint32_t)sm_count() / kMoeCluster * kMoeCluster);
-    e = cudaLaunchKernelEx(&cfg, moe_up_kernel<E5M2, HALF>, P);
+    cfg.gridDim = dim3(up_blocks);
+    e = cudaLaunchKernelEx(&cfg, moe_up_kernel<HALF>, up, P);
     if (e != cudaSuccess) return e;
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(2 * (uint32_t)sm_count());
-    return cudaLaunchKernelEx(&cfg, moe_down_kernel<E5M2, HALF>, P);
+    cfg.gridDim = dim3((uint32_t)sm_count());
+    return cudaLaunchKernelEx(&cfg, moe_down_kernel<HALF>, down, P);
 }
+
+zc_status moe_read_timeout(cudaStream_t st) { return read_timeout(st); }
 
 }  // namespace zc
 
@@ -678,12 +798,11 @@ zc_status zc_fp8_moe(const zc_fp8_moe_layer* layer, uint32_t n_tokens, const voi
     P.router = (const uint8_t*)layer->d_router;
     P.ld_x = ld_x;
     P.ld_router = layer->ld_router;
-    P.gate_up = (const uint8_t*)layer->d_gate_up;
     P.gate_up_scales = (const uint8_t*)layer->d_gate_up_scales;
-    P.down = (const uint8_t*)layer->d_down;
     P.down_scales = (const uint8_t*)layer->d_down_scales;
-    P.ld_gate_up = layer->ld_gate_up;
-    P.ld_down = layer->ld_down;
+    P.idesc = instruction_of(layer->format, ZC_FMT_FP8_E4M3, 128, 0);
+    P.spin_limit = test_knobs().spin_limit;
+    P.skip_copy = test_knobs().skip_copy;
     P.tokens = n_tokens;
     P.experts = layer->n_experts;
     P.top_k = layer->top_k;
@@ -698,12 +817,13 @@ zc_status zc_fp8_moe(const zc_fp8_moe_layer* layer, uint32_t n_tokens, const voi
     P.route = (uint32_t*)(ws + o.route);
     P.row_of = (uint32_t*)(ws + o.row_of);
     P.done = (uint32_t*)(ws + o.done);
-    P.h = (uint16_t*)(ws + o.h);
+    P.h = (float*)(ws + o.h);
     P.z = (float*)(ws + o.z);
-    const bool e5m2 = layer->format == ZC_FMT_FP8_E5M2, half = layer->real_type == ZC_REAL_F16;
+    CUtensorMap up, down;
+    if (!make_map(&up, layer->d_gate_up, (uint64_t)layer->n_experts * 2 * layer->inter, layer->hidden, layer->ld_gate_up, 8) ||
+        !make_map(&down, layer->d_down, (uint64_t)layer->n_experts * layer->hidden, layer->inter, layer->ld_down, 8)) return ZC_E_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const cudaError_t e = e5m2 ? (half ? launch_moe<true, true>(P, st) : launch_moe<true, false>(P, st))
-                               : (half ? launch_moe<false, true>(P, st) : launch_moe<false, false>(P, st));
+    const cudaError_t e = layer->real_type == ZC_REAL_F16 ? launch_moe<true>(up, down, P, st) : launch_moe<false>(up, down, P, st);
     return e == cudaSuccess ? ZC_OK : ZC_E_CUDA;
 }
 

@@ -52,22 +52,6 @@ __device__ __forceinline__ void load16(const uint8_t* p, uint32_t n, float v[16]
     for (uint32_t i = 0; i < 16; ++i) v[i] = i < n ? RealOf<T>::get(reinterpret_cast<const T*>(p)[i]) : 0.0f;
 }
 
-__device__ __forceinline__ float finite_abs(float v)
-{
-    const float a = fabsf(v);
-    return a < __int_as_float(0x7F800000) ? a : 0.0f;        // NaN compares false as well
-}
-
-// Scale byte of a block: e + 127.
-template <bool E5M2>
-__device__ __forceinline__ uint32_t scale_byte(float amax)
-{
-    const uint32_t b = __float_as_uint(amax);
-    const int e = (int)(b >> 23) - 127 - (E5M2 ? 15 : 8) + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-    return b == 0 || e < -127 ? 0u : (uint32_t)(e + 127);    // e <= 128 - 8: no clamp above
-}
-__device__ __forceinline__ float inverse_scale(uint32_t s) { return __uint_as_float((254u - s) << 23); }   // 2^-(s-127), s <= 247
-
 // Four elements times `inv` as FP8 bytes.  The conversion saturates infinities, so they are put right after it (rare).
 template <bool E5M2>
 __device__ __forceinline__ uint32_t to_fp8x4(const float v[4], float inv)

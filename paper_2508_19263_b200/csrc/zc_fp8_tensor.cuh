@@ -1,0 +1,85 @@
+// What the kernels that multiply on the fifth-generation tensor cores share: bounded waits, scale words, tensor maps.
+#pragma once
+#include <cuda.h>
+
+#include "zc_fp8.cuh"
+
+namespace zc {
+
+static __device__ unsigned int g_fp8_timeout;    // a wait of a kernel of this file's user gave up (one word per translation unit)
+
+// Every wait is bounded: on giving up the block is marked, and the other roles' waits end with it.
+struct Waiter {
+    uint32_t limit;
+    volatile uint32_t* failed;
+    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const
+    {
+        for (uint32_t i = 0; i <= limit; ++i) {
+            if (bar_try(bar, parity)) return true;
+            if (*failed) return false;
+        }
+        *failed = 1;
+        atomicExch(&g_fp8_timeout, 1u);
+        return false;
+    }
+};
+
+// The scale bytes of steps first .. first + 3 of one row as a word; 127 (a factor of 1) where there is none.
+__device__ __forceinline__ uint32_t scale_word(const uint8_t* s, uint64_t ld, uint32_t square, uint32_t row, uint32_t rows, uint32_t first, uint32_t end)
+{
+    uint32_t w = 0x7F7F7F7Fu;
+    if (row < rows) {
+        const uint8_t* p = s + (uint64_t)(square ? row >> 7 : row) * ld + first;
+        if (first + 4 <= end && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return __ldg(reinterpret_cast<const uint32_t*>(p));
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (first + i < end) w = (w & ~(0xFFu << (8 * i))) | ((uint32_t)__ldg(p + i) << (8 * i));
+    }
+    return w;
+}
+
+// ---- host ----
+
+// Waits for the stream, reads and clears the calling translation unit's word.
+static zc_status read_timeout(cudaStream_t st)
+{
+    unsigned int h = 0;
+    const unsigned int zero = 0;
+    if (cudaMemcpyFromSymbolAsync(&h, g_fp8_timeout, sizeof h, 0, cudaMemcpyDeviceToHost, st) != cudaSuccess) return ZC_E_CUDA;
+    if (cudaMemcpyToSymbolAsync(g_fp8_timeout, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st) != cudaSuccess) return ZC_E_CUDA;
+    if (cudaStreamSynchronize(st) != cudaSuccess) return ZC_E_CUDA;
+    return h ? ZC_E_DEVICE_TIMEOUT : ZC_OK;
+}
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeFn encode_fn()
+{
+    static const EncodeFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) p = nullptr;
+        return (EncodeFn)p;
+    }();
+    return fn;
+}
+
+// A matrix of bytes as tiles of `height` rows x 128 bytes in the 128-byte swizzle; what lies outside reads as zeros.
+static bool make_map(CUtensorMap* map, const void* elems, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t height)
+{
+    const cuuint64_t dims[2] = {cols, rows}, pitch[1] = {ld};
+    const cuuint32_t box[2] = {128, height}, step[2] = {1, 1};
+    return encode_fn() && encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(elems), dims, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Descriptor of the scaled FP8 instruction without its scale selectors.
+static uint32_t instruction_of(uint32_t format_a, uint32_t format_b, uint32_t m, uint32_t n)
+{
+    const uint32_t fa = format_a == ZC_FMT_FP8_E5M2, fb = format_b == ZC_FMT_FP8_E5M2;
+    // A and B types, N / 8, E8M0 scales, M / 16; both operands have k as their fastest axis
+    return (fa << 7) | (fb << 10) | ((n >> 3) << 17) | (1u << 23) | ((m >> 4) << 24);
+}
+
+}  // namespace zc

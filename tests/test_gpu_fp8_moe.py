@@ -16,6 +16,13 @@ def blocks(n):
     return -(-n // 128)
 
 
+def largest_of_128(v):
+    """The largest magnitude of every 128 columns, at each of them."""
+    wide = np.zeros((v.shape[0], blocks(v.shape[1]) * 128))
+    wide[:, : v.shape[1]] = np.abs(v)
+    return np.repeat(wide.reshape(v.shape[0], -1, 128).max(axis=2), 128, 1)[:, : v.shape[1]]
+
+
 class Layer:
     """A layer of random weights; bytes behind the rows' ends are NaN, so that a use of them shows."""
 
@@ -75,15 +82,20 @@ class Layer:
             gate, up = x[tok] @ m[0].T, x[tok] @ m[1].T
             # FP32 sums of exact products: at most a unit in the last place of a partial sum for each of the additions
             unit = 2.0 ** -23
-            d_gate, d_up = (hidden + 8) * unit * (np.abs(x[tok]) @ np.abs(m[0]).T), (hidden + 8) * unit * (np.abs(x[tok]) @ np.abs(m[1]).T)
+            # x in three pieces of E4M3, each rounding what the ones before leave: exact for 8 and 11 bits but where a piece is
+            # below the smallest normal value; its step there is 2^-9 2^-8 2^s, and the largest of 128 columns is above 224 2^s
+            d_x = 2.0 ** -25 * largest_of_128(x[tok])
+            d_gate, d_up = ((hidden + 8) * unit * (np.abs(x[tok]) @ np.abs(w).T) + d_x @ np.abs(w).T for w in m[:2])
             silu = gate / (1 + np.exp(-gate))
             w = p[tok, slot][:, None]
             h = w * silu * up
-            # |silu'| <= 1.1; a few roundings in FP32; the two BF16 parts keep 16 bits (2^-17 of the value and, near the end of
-            # BF16's range, nothing here); the router's parts of 128 columns are FP32 sums, so a logit is off by 128 units of its
-            # part and p by twice that relative
+            # |silu'| <= 1.1; a few roundings in FP32; three (FP16: four) pieces of E4M3 leave 2^-4 of the value each, or half of
+            # the last one's smallest step; the router's parts of 128 columns are FP32 sums, so a logit is off by 128 units of
+            # its part and p by twice that relative
+            pieces = 4 if self.layer.dtype == torch.float16 else 3
             d_logit = 128 * unit * (np.abs(x[tok]) @ np.abs(self.router[e].double().cpu().numpy())).max()
-            d_h = w * (1.1 * d_gate * np.abs(up) + np.abs(silu) * d_up + 1.1 * d_gate * d_up) + np.abs(h) * (16 * unit + 2.0 ** -17 + 2 * d_logit)
+            d_h = w * (1.1 * d_gate * np.abs(up) + np.abs(silu) * d_up + 1.1 * d_gate * d_up) + np.abs(h) * (16 * unit + 2 * d_logit)
+            d_h = d_h + 2.0 ** (-4 * pieces) * (np.abs(h) + d_h) + 2.0 ** (-13 - 4 * pieces) * largest_of_128(np.abs(h) + d_h)
             y[tok] += h @ m[2].T
             bound[tok] += d_h @ np.abs(m[2]).T + (inter + 16 + self.top_k) * unit * ((np.abs(h) + d_h) @ np.abs(m[2]).T)
         return y, ids, p, bound
@@ -174,6 +186,23 @@ def test_graph_streams_and_shared_weights():
             g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(y, L.run(x)[0]) for x, y in zip(xs, outs))
+
+
+def test_a_wait_that_runs_out_is_reported_and_later_calls_work():
+    L = Layer(8, 2, 512, 256, zc.FMT_FP8_E4M3, torch.bfloat16, 8)
+    x = L.tokens(20, 5)
+    want = L.run(x)
+    try:
+        zc.test_set_wait_limit(1000)
+        zc.test_stall_decoder(True)                                          # no copies are started
+        L.run(x)
+        assert zc.fp8_status() == zc.E_DEVICE_TIMEOUT
+    finally:
+        zc.test_set_wait_limit(0)
+        zc.test_stall_decoder(False)
+    assert zc.fp8_status() == zc.OK                                          # read once
+    assert all(torch.equal(a, b) for a, b in zip(L.run(x), want))
+    assert zc.fp8_status() == zc.OK
 
 
 def _through_the_codec(fmt, t):
