@@ -268,7 +268,8 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
     at[0].val.clusterDim = {1, 1, parts};
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaFuncSetAttribute(matmul_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem) != cudaSuccess) return ZC_E_CUDA;
+    static OncePerDevice once;
+    if (!once([] { return (uint32_t)(cudaFuncSetAttribute(matmul_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem) == cudaSuccess); })) return ZC_E_CUDA;
     if (cudaLaunchKernelEx(&cfg, matmul_small_kernel, map_a, map_b, P) != cudaSuccess) return ZC_E_CUDA;
     return ZC_OK;
 }

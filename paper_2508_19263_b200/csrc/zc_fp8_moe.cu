@@ -29,8 +29,11 @@ constexpr uint32_t kMaxTokens = ZC_FP8_MOE_MAX_TOKENS, kMaxExperts = ZC_FP8_MOE_
 constexpr uint32_t kMaxRows = kMaxTokens * ZC_FP8_MOE_MAX_TOP_K;
 constexpr uint32_t kMoeStages = 6;
 constexpr uint32_t kMoeStageBytes = 16384 + 16384 + 1024 + 1024;   // weights, pieces, scale words of both (the rest keeps 1 KiB alignment)
+constexpr uint32_t kMoeHeights = 5;              // tensor copies of 8, 16, 32, 64 and 128 rows
 constexpr uint32_t kMoeTmemCols = 512;           // two accumulators of 128 columns, then 4 + 4 scale columns per stage
 constexpr uint32_t kMoeTmemScales = 256;
+
+struct MoeMaps { CUtensorMap of[kMoeHeights]; };
 
 struct MoeParams {
     const uint8_t *x, *router;                   // rows of BF16 or FP16
@@ -63,13 +66,15 @@ struct MoeShared {
     uint64_t full[kMoeStages], empty[kMoeStages], acc_full[2], acc_empty[2];
     uint32_t tmem, failed;
     Routing R;
-    uint8_t row_token[kMaxRows];
+    alignas(16) float other[2][64][4];           // kernel 1: what the other half of the result warps needs
     float row_p[kMaxRows];
+    uint16_t row_of[kMaxRows];                   // kernel 2: rows of the tokens' experts
+    uint8_t row_token[kMaxRows];
     uint32_t last[16];
 };
 // while routing, where the stages will be
 struct MoeRouting {
-    double items[32 * 128], logits[64 * kMaxTokens];
+    double items[16 * 128], logits[kMaxExperts * kMaxTokens];
     float p[kMaxRows];                           // of this block's share of the tokens
     uint16_t id[kMaxRows];
     float p_all[kMaxRows];
@@ -101,34 +106,44 @@ __device__ __forceinline__ uint4 zero4() { return make_uint4(0, 0, 0, 0); }
 
 // ---- the weights' stream --------------------------------------------------------------------------------------------
 
-// A tile: `groups` groups of eight rows (UP: of gate and of up each) of a chosen expert, for up to 32 of its tokens.
+// A tile: `groups` groups of eight rows (UP: of gate, and behind 64 rows of up) of a chosen expert, for up to 32 of its tokens.
 struct Tile {
     uint32_t active, expert, group, groups, row, count;      // row, count: its tokens' rows
 };
 
-// The tiles of units first .. end - 1, a unit being a group of an expert; all roles walk through them alike.
+// The tiles of units first .. end - 1; all roles walk through them alike.  A unit is a group of an expert.  UP: expert by
+// expert.  Down: bands of 128 rows, in each of them expert by expert, so that a band is complete, and its experts can be added up, when a
+// few neighbouring blocks have done with it, and not all bands at once at the very end.
 template <bool UP>
 struct Tiles {
     static constexpr uint32_t kMost = UP ? 8 : 16;
     const Routing& R;
-    uint32_t per_expert, at, end, pass;
+    uint32_t groups, at, end, pass;
     __device__ __forceinline__ Tiles(const Routing& r, uint32_t rows, uint32_t block, uint32_t blocks)
-        : R(r), per_expert((rows + 7) >> 3), pass(0)
+        : R(r), groups((rows + 7) >> 3), pass(0)
     {
-        const uint64_t units = (uint64_t)per_expert * r.n_active;
+        const uint64_t units = (uint64_t)groups * r.n_active;
         at = (uint32_t)(units * block / blocks);
         end = (uint32_t)(units * (block + 1) / blocks);
     }
     __device__ __forceinline__ bool next(Tile& t)
     {
         if (at >= end) return false;
-        t.active = at / per_expert;
+        uint32_t left;
+        if (UP) {
+            t.active = at / groups;
+            t.group = at - t.active * groups;
+            left = min(end - at, groups - t.group);
+            // a remainder is shared by the last two tiles
+            t.groups = left > kMost && left < 2 * kMost ? (left + 1) / 2 : min(left, kMost);
+        } else {
+            const uint32_t band = at / (kMost * R.n_active), first = band * kMost, height = min(groups - first, kMost);
+            const uint32_t in = at - first * R.n_active;
+            t.active = in / height;
+            t.group = first + in - t.active * height;
+            t.groups = min(end - at, first + height - t.group);
+        }
         t.expert = R.expert[t.active];
-        t.group = at - t.active * per_expert;
-        const uint32_t left = min(end - at, per_expert - t.group);
-        t.groups = min(left, kMost);
-        // a remainder is shared by the last two tiles
-        if (left > kMost && left < 2 * kMost) t.groups = (left + 1) / 2;
         t.row = R.first[t.active] + pass * kMoePass;
         const uint32_t n = R.first[t.active + 1] - t.row;
         t.count = min(n, kMoePass);
@@ -168,7 +183,7 @@ __device__ __forceinline__ void make_pieces(const float v[4], uint32_t words[PIE
 
 // What a block does after the routing: its share of gate and up (UP) or of down.  HALF: activations of gate and up are FP16.
 template <bool UP, bool HALF, int PIECES, typename Finish>
-__device__ __forceinline__ void stream_weights(const MoeParams& P, const CUtensorMap* map, MoeShared& S, uint32_t base, uint32_t blocks, Finish finish)
+__device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps& maps, MoeShared& S, uint32_t base, uint32_t blocks, Finish finish)
 {
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t cols = UP ? P.hidden : P.inter, rows = UP ? P.inter : P.hidden;
@@ -190,9 +205,14 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const CUtenso
                     const uint32_t bar = smem_u32(&S.full[st]), to = base + st * kMoeStageBytes;
                     bar_expect(bar, t.groups * (UP ? 2048 : 1024));
                     if (P.skip_copy) continue;
-                    for (uint32_t i = 0; i < t.groups; ++i) {
-                        tensor_copy<1>(to + i * (UP ? 2048 : 1024), map, (int)(k * 128), (int)(row0 + 8 * i), bar);
-                        if (UP) tensor_copy<1>(to + i * 2048 + 1024, map, (int)(k * 128), (int)(row0 + P.inter + 8 * i), bar);
+                    // as few copies as there are bits in the number of groups: one of 8 rows takes the copy engine as long as one of 64
+                    uint32_t i = 0;
+#pragma unroll
+                    for (int b = UP ? 3 : 4; b >= 0; --b) {
+                        if (!(t.groups >> b & 1)) continue;
+                        tensor_copy<1>(to + i * 1024, &maps.of[b], (int)(k * 128), (int)(row0 + 8 * i), bar);
+                        if (UP) tensor_copy<1>(to + 8192 + i * 1024, &maps.of[b], (int)(k * 128), (int)(row0 + P.inter + 8 * i), bar);
+                        i += 1u << b;
                     }
                 }
             }
@@ -228,25 +248,28 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const CUtenso
             }
         }
     } else if (warp == 2) {
-        // scale bytes of the weights, four steps at a time; row r of the tile's operand is row 32 j + lane
+        // scale bytes of the weights, four steps at a time and four steps ahead; row r of the tile's operand is row 32 j + lane
         const uint32_t sld = steps, srows = (rows + 127) >> 7;
-        bool ok = true;
-        while (ok && tiles.next(t)) {
+        const uint8_t* mine[4];
+        auto find_rows = [&] {
             const uint8_t* s = (UP ? P.gate_up_scales + (uint64_t)t.expert * 2 * srows * sld : P.down_scales + (uint64_t)t.expert * srows * sld);
-            const uint8_t* mine[4];
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) {
-                const uint32_t g = 4 * j + (lane >> 3);                  // group of the operand
-                const uint32_t r = min((t.group + (UP ? g >> 1 : g)) * 8 + (lane & 7), rows - 1);
-                mine[j] = s + (uint64_t)((UP && (g & 1) ? srows : 0) + (r >> 7)) * sld;
+                const uint32_t r = min((t.group + (UP ? 4 * (j & 1) : 4 * j)) * 8 + lane, rows - 1);
+                mine[j] = s + (uint64_t)((UP && j >= 2 ? srows : 0) + (r >> 7)) * sld;
             }
-            uint32_t w[4];
+        };
+        auto fetch = [&](uint32_t k, uint32_t w[4]) {
 #pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) w[j] = scale_word(mine[j], 0, 0, 0, 1, 0, steps);
+            for (uint32_t j = 0; j < 4; ++j) w[j] = scale_word(mine[j], 0, 0, 0, 1, k, steps);
+        };
+        uint32_t w[4], ahead[4];
+        bool ok = true, more = tiles.next(t);
+        if (more) { find_rows(); fetch(0, w); }
+        while (ok && more) {
             for (uint32_t k = 0; k < steps && ok; k += 4) {
-                uint32_t next[4];
-#pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) next[j] = k + 4 < steps ? scale_word(mine[j], 0, 0, 0, 1, k + 4, steps) : 0;
+                if (k + 4 < steps) fetch(k + 4, ahead);
+                else if ((more = tiles.next(t))) { find_rows(); fetch(0, ahead); }
                 for (uint32_t q = 0; q < 4 && k + q < steps; ++q, ++n) {
                     const uint32_t st = n % kMoeStages;
                     if (!(ok = __all_sync(0xFFFFFFFFu, n < kMoeStages || wait(smem_u32(&S.empty[st]), (n / kMoeStages - 1) & 1)))) break;
@@ -258,7 +281,7 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const CUtenso
                     if (lane == 0) bar_arrive(smem_u32(&S.full[st]));
                 }
 #pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) w[j] = next[j];
+                for (uint32_t j = 0; j < 4; ++j) w[j] = ahead[j];
             }
         }
     } else if (warp >= 8) {
@@ -271,7 +294,7 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const CUtenso
             for (uint32_t k = 0; k < steps; ++k, ++n) {
                 if (n % kMoeStages != st) continue;
                 const uint32_t col = k * 128 + lane * 4;
-                for (uint32_t c = 0; c < t.count; c += 8) {
+                for (uint32_t c = 0; c < padded; c += 8) {
                     uint4 raw[8];
 #pragma unroll
                     for (uint32_t i = 0; i < 8; ++i) {
@@ -287,32 +310,34 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const CUtenso
                         }
                     }
                     if (c == 0 && !(ok = __all_sync(0xFFFFFFFFu, n < kMoeStages || wait(smem_u32(&S.empty[st]), (n / kMoeStages - 1) & 1)))) break;
+                    // four tokens at a time, whether they are there or not (their rows are): the chain of roundings is long
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) {
-                        if (c + i >= t.count) break;
-                        float v[4];
-                        if (UP) {
-                            const uint32_t w[2] = {raw[i].x, raw[i].y};
+                    for (uint32_t f = 0; f < 8; f += 4) {
+                        if (c + f >= t.count) break;
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                const uint16_t u = (uint16_t)(w[q >> 1] >> (16 * (q & 1)));
-                                v[q] = HALF ? __half2float(__ushort_as_half(u)) : __bfloat162float(__ushort_as_bfloat16(u));
+                        for (uint32_t i = f; i < f + 4; ++i) {
+                            float v[4];
+                            if (UP) {
+                                const uint32_t u[2] = {raw[i].x, raw[i].y};
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    const uint16_t s = (uint16_t)(u[q >> 1] >> (16 * (q & 1)));
+                                    v[q] = HALF ? __half2float(__ushort_as_half(s)) : __bfloat162float(__ushort_as_bfloat16(s));
+                                }
+                            } else {
+                                v[0] = __uint_as_float(raw[i].x); v[1] = __uint_as_float(raw[i].y);
+                                v[2] = __uint_as_float(raw[i].z); v[3] = __uint_as_float(raw[i].w);
                             }
-                        } else {
-                            v[0] = __uint_as_float(raw[i].x); v[1] = __uint_as_float(raw[i].y);
-                            v[2] = __uint_as_float(raw[i].z); v[3] = __uint_as_float(raw[i].w);
-                        }
-                        if (col + 4 > cols)
 #pragma unroll
-                            for (uint32_t q = 0; q < 4; ++q)
-                                if (col + q >= cols) v[q] = 0.0f;
-                        uint32_t words[PIECES], scale;
-                        make_pieces<PIECES>(v, words, scale);
+                            for (uint32_t q = 0; q < 4; ++q) v[q] = col + q < cols ? v[q] : 0.0f;
+                            uint32_t words[PIECES], scale;
+                            make_pieces<PIECES>(v, words, scale);
 #pragma unroll
-                        for (uint32_t q = 0; q < PIECES; ++q) {
-                            const uint32_t r = q * padded + c + i;
-                            sts32(at + 16384 + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4, words[q]);
-                            if (lane == q) sts32(at + 32768 + 512 + (r & 31) * 16 + (r >> 5) * 4, scale >= 4u * q ? scale - 4u * q : 0u);
+                            for (uint32_t q = 0; q < PIECES; ++q) {
+                                const uint32_t r = q * padded + c + i;
+                                sts32(at + 16384 + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4, words[q]);
+                                if (lane == q) sts32(at + 32768 + 512 + (r & 31) * 16 + (r >> 5) * 4, scale >= 4u * q ? scale - 4u * q : 0u);
+                            }
                         }
                     }
                 }
@@ -346,7 +371,7 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const CUtenso
                     for (int q = PIECES - 2; q >= 0; --q) sum += part[q][i];
                     part[0][i] = sum;
                 }
-                finish.store(t, c, quad * 32 + lane, part[0]);
+                finish.store(t, c, quad, lane, part[0]);
             }
             tc_fence_before();
             __syncwarp();
@@ -360,12 +385,16 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const CUtenso
 
 // ---- routing ----------------------------------------------------------------------------------------------------------
 
-// order of doubles as unsigned numbers; NaN below everything, both zeros alike
+// order of doubles as unsigned numbers, and back; NaN (1) below everything but what is not there (0), both zeros alike
 __device__ __forceinline__ unsigned long long order_key(double v)
 {
-    if (v != v) return 0;
+    if (v != v) return 1;
     const unsigned long long b = (unsigned long long)__double_as_longlong(v + 0.0);
     return (b >> 63) ? ~b : b | (1ull << 63);
+}
+__device__ __forceinline__ double value_of(unsigned long long key)
+{
+    return key == 1 ? __longlong_as_double(0x7FF8000000000000ll) : __longlong_as_double((long long)((key >> 63) ? key & ~(1ull << 63) : ~key));
 }
 __device__ __forceinline__ double ld_cluster_f64(uint32_t addr)
 {
@@ -374,27 +403,27 @@ __device__ __forceinline__ double ld_cluster_f64(uint32_t addr)
     return v;
 }
 
-// The logits of this block's experts (tiles of 16: rank, rank + 4, ...) for all tokens, logits[local expert][token].  Products
-// of parts of 128 columns are summed by the matrix instructions in FP32, the parts in FP64: what separates two experts' logits
-// decides which weights are used, and 2^-24 of the sum of a part is far below what the activations' own rounding moves.
+// This block's part of the logits, logits[expert][token]: of the columns' parts of 128 the cluster's blocks take a share each, so
+// that a cluster reads router and tokens once.  Products of a part are summed by the matrix instructions in FP32, the parts in FP64:
+// what separates two experts' logits decides which weights are used, and 2^-24 of the sum of a part is far below what the
+// activations' own rounding moves.
 template <bool HALF>
-__device__ __forceinline__ void router_logits(const MoeParams& P, uint32_t rank, double* items, double* logits)
+__device__ __forceinline__ void router_logits(const MoeParams& P, uint32_t rank, MoeRouting& S)
 {
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const uint32_t all_tiles = (P.experts + 15) >> 4, nt = (P.tokens + 7) >> 3;
-    const uint32_t mt = all_tiles > rank ? (all_tiles - rank + kMoeCluster - 1) / kMoeCluster : 0, tasks = mt * nt;
-    const uint32_t parts = (P.hidden + 127) >> 7;
+    const uint32_t mt = (P.experts + 15) >> 4, nt = (P.tokens + 7) >> 3, tasks = mt * nt;
+    const uint32_t all = (P.hidden + 127) >> 7, lo = all * rank / kMoeCluster, parts = all * (rank + 1) / kMoeCluster - lo;
     uint32_t split = 1;
     while (split * 2 * tasks <= kMoeWarps && split * 2 <= parts) split *= 2;
     for (uint32_t item = warp; item < tasks * split; item += kMoeWarps) {
         const uint32_t task = item / split, slice = item % split;
-        const uint32_t e0 = (rank + (task / nt) * kMoeCluster) * 16, tok = (task % nt) * 8 + g;
+        const uint32_t e0 = (task / nt) * 16, tok = (task % nt) * 8 + g;
         const bool ok_a = e0 + g < P.experts, ok_b = e0 + g + 8 < P.experts, ok_x = tok < P.tokens;
         const uint8_t* ra = P.router + 2 * (uint64_t)(ok_a ? e0 + g : 0) * P.ld_router;
         const uint8_t* rb = P.router + 2 * (uint64_t)(ok_b ? e0 + g + 8 : 0) * P.ld_router;
         const uint8_t* xr = P.x + 2 * (uint64_t)(ok_x ? tok : 0) * P.ld_x;
         double sum[4] = {0, 0, 0, 0};
-        for (uint32_t part = parts * slice / split; part < parts * (slice + 1) / split; ++part) {
+        for (uint32_t part = lo + parts * slice / split; part < lo + parts * (slice + 1) / split; ++part) {
             uint4 a[4], b[4], x[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -413,24 +442,28 @@ __device__ __forceinline__ void router_logits(const MoeParams& P, uint32_t rank,
             float v[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t lo[4] = {a[j].x, b[j].x, a[j].y, b[j].y}, hi[4] = {a[j].z, b[j].z, a[j].w, b[j].w};
-                mma16<HALF>(v, lo, x[j].x, x[j].y);
-                mma16<HALF>(v, hi, x[j].z, x[j].w);
+                const uint32_t first[4] = {a[j].x, b[j].x, a[j].y, b[j].y}, second[4] = {a[j].z, b[j].z, a[j].w, b[j].w};
+                mma16<HALF>(v, first, x[j].x, x[j].y);
+                mma16<HALF>(v, second, x[j].z, x[j].w);
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) sum[q] += (double)v[q];
         }
-        double* to = items + item * 128 + lane;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) to[q * 32] = sum[q];
+        for (uint32_t q = 0; q < 4; ++q) {
+            const uint32_t e = e0 + g + 8 * (q >> 1), k = (task % nt) * 8 + 2 * t + (q & 1);
+            if (split > 1) S.items[item * 128 + q * 32 + lane] = sum[q];
+            else if (e < P.experts && k < P.tokens) S.logits[e * kMaxTokens + k] = sum[q];
+        }
     }
+    if (split == 1) return;
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < tasks * 128; i += kMoeThreads) {
         const uint32_t task = i >> 7, q = (i >> 5) & 3, l = i & 31;
         double s = 0;
-        for (uint32_t k = 0; k < split; ++k) s += items[(task * split + k) * 128 + q * 32 + l];
+        for (uint32_t k = 0; k < split; ++k) s += S.items[(task * split + k) * 128 + q * 32 + l];
         const uint32_t e = (task / nt) * 16 + (l >> 2) + 8 * (q >> 1), tok = (task % nt) * 8 + 2 * (l & 3) + (q & 1);
-        if (tok < P.tokens) logits[e * kMaxTokens + tok] = s;
+        if (e < P.experts && tok < P.tokens) S.logits[e * kMaxTokens + tok] = s;
     }
 }
 
@@ -446,11 +479,11 @@ __device__ __forceinline__ void choose(const MoeParams& P, uint32_t rank, MoeRou
         for (uint32_t k = 0; k < kMaxExperts / 32; ++k) {
             const uint32_t e = k * 32 + lane;
             key[k] = 0;
-            // + 1: an expert that is there beats a place behind the last one even when its logit is NaN
             if (e < P.experts) {
-                const uint32_t tile = e >> 4, local = (tile / kMoeCluster) * 16 + (e & 15);
-                const unsigned long long o = order_key(ld_cluster_f64(map_shared(base + 8 * (local * kMaxTokens + tok), tile % kMoeCluster)));
-                key[k] = o ? o : 1;
+                double v = 0;
+#pragma unroll
+                for (uint32_t r = 0; r < kMoeCluster; ++r) v += ld_cluster_f64(map_shared(base + 8 * (e * kMaxTokens + tok), r));
+                key[k] = order_key(v);
             }
         }
         double largest = 0;
@@ -468,8 +501,7 @@ __device__ __forceinline__ void choose(const MoeParams& P, uint32_t rank, MoeRou
 #pragma unroll
             for (uint32_t k = 0; k < kMaxExperts / 32; ++k)
                 if (k * 32 + lane == e) key[k] = 0;
-            const uint32_t tile = e >> 4, local = (tile / kMoeCluster) * 16 + (e & 15);
-            const double v = ld_cluster_f64(map_shared(base + 8 * (local * kMaxTokens + tok), tile % kMoeCluster));
+            const double v = value_of(((unsigned long long)hi << 32) | lo);
             if (j == 0) largest = v;
             const float p = expf((float)(v - largest));      // the difference in FP64, the exponential in FP32
             total += p;
@@ -557,19 +589,27 @@ __device__ __forceinline__ void moe_setup(MoeShared& S)
     tc_fence_after();
 }
 
-// silu(gate) * up * p into the hidden vectors; groups of gate and up alternate, so a lane's partner is eight lanes away
+// silu(gate) * up * p into the hidden vectors.  Warps 0 and 1 have the gates, 2 and 3 the ups of the same channels: each half
+// gives the other what it needs of every second half of the tokens through shared memory.
 struct FinishUp {
     const MoeParams& P;
-    const MoeShared& S;
-    __device__ __forceinline__ void store(const Tile& t, uint32_t c, uint32_t row, const float v[8]) const
+    MoeShared& S;
+    __device__ __forceinline__ void store(const Tile& t, uint32_t c, uint32_t quad, uint32_t lane, const float v[8]) const
     {
-        const uint32_t ch = (t.group + (row >> 4)) * 8 + (row & 7);
-        const bool gate = (row & 8) == 0 && (row >> 4) < t.groups && ch < P.inter;
+        const uint32_t row = (quad & 1) * 32 + lane, ch = t.group * 8 + row, mine = quad >> 1;     // gates' warps take tokens 0-3, ups' 4-7
+        float* out = S.other[mine ^ 1][row];
+        *reinterpret_cast<float4*>(out) = mine ? make_float4(v[0], v[1], v[2], v[3]) : make_float4(v[4], v[5], v[6], v[7]);
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const float4 x = *reinterpret_cast<const float4*>(S.other[mine][row]);
+        const float o[4] = {x.x, x.y, x.z, x.w};
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (row < t.groups * 8 && ch < P.inter) {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) {
-            const float up = __shfl_xor_sync(0xFFFFFFFFu, v[i], 8);
-            if (gate && c + i < t.count)
-                P.h[(uint64_t)(t.row + c + i) * P.inter_pad + ch] = v[i] / (1.0f + expf(-v[i])) * up * S.row_p[t.row + c + i];
+            for (uint32_t i = 0; i < 4; ++i) {
+                const uint32_t n = c + 4 * mine + i;
+                const float gate = mine ? o[i] : v[i], up = mine ? v[4 + i] : o[i];
+                if (n < t.count) P.h[(uint64_t)(t.row + n) * P.inter_pad + ch] = gate / (1.0f + expf(-gate)) * up * S.row_p[t.row + n];
+            }
         }
     }
     __device__ __forceinline__ void tile_done(const Tile&) const { }
@@ -580,15 +620,15 @@ struct FinishDown {
     const MoeParams& P;
     MoeShared& S;
     uint32_t n_passes;
-    __device__ __forceinline__ void store(const Tile& t, uint32_t c, uint32_t row, const float v[8]) const
+    __device__ __forceinline__ void store(const Tile& t, uint32_t c, uint32_t quad, uint32_t lane, const float v[8]) const
     {
-        const uint32_t r = t.group * 8 + row;
+        const uint32_t row = quad * 32 + lane, r = t.group * 8 + row;
         if (row >= t.groups * 8 || r >= P.hidden) return;
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i)
             if (c + i < t.count) P.z[(uint64_t)(t.row + c + i) * P.hidden_pad + r] = v[i];
     }
-    // the four warps: whoever completes a group's last pass adds the experts up
+    // the four warps: whoever completes a group's last pass adds the experts up, four columns of a token a thread
     __device__ __forceinline__ void tile_done(const Tile& t) const
     {
         const uint32_t tid = threadIdx.x & 127;
@@ -599,13 +639,23 @@ struct FinishDown {
             __threadfence();
         }
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        for (uint32_t i = tid; i < t.groups * 8 * P.tokens; i += 128) {
-            const uint32_t g = (i >> 3) % t.groups, tok = (i >> 3) / t.groups, r = (t.group + g) * 8 + (i & 7);
-            if (!S.last[g] || r >= P.hidden) continue;
-            float y = 0;
-            for (uint32_t j = 0; j < P.top_k; ++j) y += __ldcg(P.z + (uint64_t)__ldcg(P.row_of + tok * P.top_k + j) * P.hidden_pad + r);
-            if (HALF) reinterpret_cast<__half*>(P.y)[(uint64_t)tok * P.ld_y + r] = __float2half_rn(y);
-            else reinterpret_cast<__nv_bfloat16*>(P.y)[(uint64_t)tok * P.ld_y + r] = __float2bfloat16_rn(y);
+        const uint32_t g = (tid & 31) >> 1, r = (t.group + g) * 8 + (tid & 1) * 4;
+        if (g < t.groups && S.last[g] && r < P.hidden) {
+            for (uint32_t tok = tid >> 5; tok < P.tokens; tok += 4) {
+                float y[4] = {0, 0, 0, 0};
+                const uint16_t* rows = S.row_of + tok * P.top_k;
+#pragma unroll 8
+                for (uint32_t j = 0; j < P.top_k; ++j) {
+                    const float4 z = __ldcg(reinterpret_cast<const float4*>(P.z + (uint64_t)rows[j] * P.hidden_pad + r));
+                    y[0] += z.x; y[1] += z.y; y[2] += z.z; y[3] += z.w;
+                }
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    if (r + i >= P.hidden) break;
+                    if (HALF) reinterpret_cast<__half*>(P.y)[(uint64_t)tok * P.ld_y + r + i] = __float2half_rn(y[i]);
+                    else reinterpret_cast<__nv_bfloat16*>(P.y)[(uint64_t)tok * P.ld_y + r + i] = __float2bfloat16_rn(y[i]);
+                }
+            }
         }
         asm volatile("bar.sync 1, 128;" ::: "memory");
     }
@@ -616,7 +666,7 @@ template <bool HALF> constexpr int kHiddenPieces = HALF ? 4 : 3;
 
 template <bool HALF>
 __global__ void __launch_bounds__(kMoeThreads, 1)
-moe_up_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ MoeParams P)
+moe_up_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ MoeParams P)
 {
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -627,9 +677,9 @@ moe_up_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ M
     const uint32_t n_rows = P.tokens * P.top_k;
 
     grid_launch_dependents();
-    if (tid == 0) prefetch_map(&map);
+    if (tid < kMoeHeights) prefetch_map(&maps.of[tid]);
     moe_setup(S);
-    router_logits<HALF>(P, rank, T.items, T.logits);
+    router_logits<HALF>(P, rank, T);
     cluster_sync();
     choose(P, rank, T);
     cluster_sync();
@@ -664,20 +714,20 @@ moe_up_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ M
     }
     fence_async_shared();                        // the routing's shared memory becomes the stages'
     cluster_sync();                              // and no other block reads from it any more
-    stream_weights<true, HALF, 3>(P, &map, S, base, gridDim.x, FinishUp{P, S});
+    stream_weights<true, HALF, 3>(P, maps, S, base, gridDim.x, FinishUp{P, S});
     __syncthreads();
     if (tid < 64 && tid >= 32) tmem_free<1>(S.tmem, kMoeTmemCols);
 }
 
 template <bool HALF>
 __global__ void __launch_bounds__(kMoeThreads, 1)
-moe_down_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ MoeParams P)
+moe_down_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ MoeParams P)
 {
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     MoeShared& S = *reinterpret_cast<MoeShared*>(raw + (base - smem_u32(raw)) + kMoeStages * kMoeStageBytes);
     const uint32_t tid = threadIdx.x;
-    if (tid == 0) prefetch_map(&map);
+    if (tid < kMoeHeights) prefetch_map(&maps.of[tid]);
     moe_setup(S);
     grid_wait();
     const uint32_t n_active = P.route[0], n_passes = P.route[1];
@@ -687,9 +737,10 @@ moe_down_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__
         S.R.first[i] = (uint16_t)v;
         S.R.pass[i] = (uint16_t)(v >> 16);
     }
+    for (uint32_t i = tid; i < P.tokens * P.top_k; i += kMoeThreads) S.row_of[i] = (uint16_t)P.row_of[i];
     if (tid == 0) { S.R.n_active = n_active; S.R.n_passes = n_passes; }
     __syncthreads();
-    stream_weights<false, HALF, kHiddenPieces<HALF>>(P, &map, S, base, gridDim.x, FinishDown<HALF>{P, S, n_passes});
+    stream_weights<false, HALF, kHiddenPieces<HALF>>(P, maps, S, base, gridDim.x, FinishDown<HALF>{P, S, n_passes});
     __syncthreads();
     if (tid < 64 && tid >= 32) tmem_free<1>(S.tmem, kMoeTmemCols);
 }
@@ -743,12 +794,15 @@ static uint32_t resident_blocks(const void* kernel, uint32_t cluster)
 }
 
 template <bool HALF>
-static cudaError_t launch_moe(const CUtensorMap& up, const CUtensorMap& down, const MoeParams& P, cudaStream_t st)
+static cudaError_t launch_moe(const MoeMaps& up, const MoeMaps& down, const MoeParams& P, cudaStream_t st)
 {
-    cudaError_t e = cudaFuncSetAttribute(moe_up_kernel<HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMoeSmem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(moe_down_kernel<HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMoeSmem);
-    if (e != cudaSuccess) return e;
-    static const uint32_t up_blocks = resident_blocks((const void*)moe_up_kernel<HALF>, kMoeCluster);
+    cudaError_t e = cudaSuccess;
+    static OncePerDevice once;
+    const uint32_t up_blocks = once([&]() -> uint32_t {
+        if (cudaFuncSetAttribute(moe_up_kernel<HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMoeSmem) != cudaSuccess) return 0;
+        if (cudaFuncSetAttribute(moe_down_kernel<HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMoeSmem) != cudaSuccess) return 0;
+        return resident_blocks((const void*)moe_up_kernel<HALF>, kMoeCluster);
+    });
     if (!up_blocks) return cudaErrorUnknown;
     cudaLaunchConfig_t cfg{};
     cfg.blockDim = dim3(kMoeThreads);
@@ -819,9 +873,10 @@ zc_status zc_fp8_moe(const zc_fp8_moe_layer* layer, uint32_t n_tokens, const voi
     P.done = (uint32_t*)(ws + o.done);
     P.h = (float*)(ws + o.h);
     P.z = (float*)(ws + o.z);
-    CUtensorMap up, down;
-    if (!make_map(&up, layer->d_gate_up, (uint64_t)layer->n_experts * 2 * layer->inter, layer->hidden, layer->ld_gate_up, 8) ||
-        !make_map(&down, layer->d_down, (uint64_t)layer->n_experts * layer->hidden, layer->inter, layer->ld_down, 8)) return ZC_E_CUDA;
+    MoeMaps up, down;
+    for (uint32_t b = 0; b < kMoeHeights; ++b)
+        if (!make_map(&up.of[b], layer->d_gate_up, (uint64_t)layer->n_experts * 2 * layer->inter, layer->hidden, layer->ld_gate_up, 8u << b) ||
+            !make_map(&down.of[b], layer->d_down, (uint64_t)layer->n_experts * layer->hidden, layer->inter, layer->ld_down, 8u << b)) return ZC_E_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const cudaError_t e = layer->real_type == ZC_REAL_F16 ? launch_moe<true>(up, down, P, st) : launch_moe<false>(up, down, P, st);
     return e == cudaSuccess ? ZC_OK : ZC_E_CUDA;

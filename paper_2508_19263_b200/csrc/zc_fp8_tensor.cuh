@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <atomic>
+
 #include "zc_fp8.cuh"
 
 namespace zc {
@@ -50,6 +52,20 @@ static zc_status read_timeout(cudaStream_t st)
     if (cudaStreamSynchronize(st) != cudaSuccess) return ZC_E_CUDA;
     return h ? ZC_E_DEVICE_TIMEOUT : ZC_OK;
 }
+
+// A number that is worked out on a device's first use (0: it failed, and is tried again), kept per device.
+struct OncePerDevice {
+    std::atomic<uint32_t> value[64] = {};
+    template <typename F>
+    uint32_t operator()(F work)
+    {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return work();
+        uint32_t v = value[dev].load(std::memory_order_relaxed);
+        if (!v) { v = work(); value[dev].store(v, std::memory_order_relaxed); }
+        return v;
+    }
+};
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
