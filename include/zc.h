@@ -482,9 +482,9 @@ zc_status zc_fp8_status(void* cuda_stream);
  *   logits = router x; the top_k largest (ties: the lowest index first; NaN counts as the lowest value); p = softmax
  *   over those top_k; y = sum over them of p_e * down_e (silu(gate_e x) * (up_e x)), silu(v) = v / (1 + exp(-v)).
  * The weights are FP8 with 128 x 128 blocks; every expert's matrix has scale bytes of its own, beginning with its first
- * row.  Only the experts that a token chose are read.  Sums are FP32, those of the router FP64 over parts of 128
+ * row.  Only the experts that a token chose are read.  Sums are FP32, those of the router FP64 over parts of 64
  * columns.  x is used to 2^-25 of the largest magnitude of its 128 columns, and exactly where it is above 2^-17 of it; the
- * hidden vector of an expert is kept with 12 bits (BF16 layers) or 16 bits (FP16 layers) of precision; an infinity in either
+ * hidden vector of an expert is kept with 11 bits (BF16 layers) or 15 bits (FP16 layers) of precision; an infinity in either
  * gives NaN.  Rows are read in pieces of 16 bytes: of every row, the last one included, the whole pitch belongs to the
  * buffer.  A wait inside a kernel that gives up leaves the outputs undefined and is reported by zc_fp8_status. */
 typedef struct zc_fp8_moe_layer {

@@ -59,6 +59,10 @@ __device__ __forceinline__ uint32_t scale_byte(float amax)
 __device__ __forceinline__ float inverse_scale(uint32_t s) { return __uint_as_float((254u - s) << 23); }   // 2^-(s-127), s <= 247
 
 
+__device__ __forceinline__ void sts128(uint32_t addr, const uint32_t v[4])
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
 // ---- 32-byte global accesses (one sector per lane); 32-byte aligned ----
 __device__ __forceinline__ void ld_v8(const void* p, uint32_t v[8])
 {
@@ -69,6 +73,13 @@ __device__ __forceinline__ uint4 ld_stream_v4(const void* p)
 {
     uint4 v;
     asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+__device__ __forceinline__ uint4 lds128(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
 
@@ -85,6 +96,7 @@ __device__ __forceinline__ uint32_t cluster_rank()
 }
 __device__ __forceinline__ void cluster_sync()
 {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // the same place in the shared memory of the cluster's block `rank`
@@ -124,6 +136,15 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+
+// the same wait for what another block of the cluster wrote before it arrived
+__device__ __forceinline__ bool bar_try_cluster(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
@@ -200,12 +221,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t v[32])
                  : "r"(addr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void tmem_st4(uint32_t addr, const uint32_t v[4])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" :: "r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
 // eight columns of a quarter's 32 lanes; not complete before tmem_ld_wait
 __device__ __forceinline__ void tmem_ld8(uint32_t addr, float v[8])
 {
@@ -213,13 +228,15 @@ __device__ __forceinline__ void tmem_ld8(uint32_t addr, float v[8])
                  : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(addr));
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-// 512 bytes of scale words, [32][4] in shared memory, to four columns of every quarter of tensor memory: word (i, j) is that
-// of row 32 j + i
+// 512 bytes of scale words, [32][4] in shared memory, to four columns of every quarter of tensor memory (in every block of the
+// group, from its own shared memory): word (i, j) is that of row 32 j + i
+template <int GROUP>
 __device__ __forceinline__ void tmem_copy_scales(uint32_t addr, uint32_t shared)
 {
     // no swizzle, groups of eight 16-byte rows 128 bytes apart
     const uint64_t desc = (uint64_t)((shared & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(addr), "l"(desc) : "memory");
+    if (GROUP == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(addr), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" :: "r"(addr), "l"(desc) : "memory");
 }
 // shared memory written by ordinary stores becomes visible to tensor copies and matrix instructions
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }

@@ -7,7 +7,7 @@
 //
 // Roles of a thread block's warps: 0 copies tiles of 128 rows x 128 bytes into shared memory (tensor copies, 128-byte
 // swizzle; what lies outside of a matrix arrives as zeros), 1 issues the matrix instructions, 4-7 bring the accumulators
-// to memory, 8-11 bring the scale bytes into tensor memory.
+// to memory, 8-11 bring the scale bytes into shared memory.
 #include "zc_fp8_tensor.cuh"
 
 namespace zc {
@@ -30,13 +30,21 @@ struct MatmulParams {
     uint32_t spin_limit, skip_copy;
 };
 
-// Shared memory behind the operand stages.
+// The scale words of four steps are a warp's own work, in turn with three others: each has the time of sixteen steps for the
+// latency of its loads, a buffer in shared memory, and sees every phase of the buffer's barrier.  (All four warps loading all
+// words straight into their quarters of tensor memory, a word ahead, took 498 us of a product that takes 349 without.)  Tensor
+// memory has two sets of words.
+constexpr uint32_t kScaleBufs = 4;
+constexpr uint32_t kScaleBufBytes = 512 + 1024;  // 128 rows of A, up to 256 of B
+
+// Shared memory behind the operand stages and the scale words.
 struct MatmulShared {
     uint64_t full[8], empty[8];
-    uint64_t sf_full[2], sf_empty[2];
-    uint64_t acc_full[2], acc_empty[2];
+    uint64_t sf_full[kScaleBufs], sf_empty[kScaleBufs];
+    uint64_t acc_full[2], acc_empty[1];
     uint32_t tmem, failed;
 };
+
 
 template <typename T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
@@ -81,7 +89,7 @@ __device__ __forceinline__ void store_row(const MatmulParams& P, uint32_t row, u
 // One tile of 128 x 128 per block; the `gridDim.z` blocks of a cluster share a tile, each takes a part of the steps, and the
 // parts are added up through the cluster's shared memory in the order of the ranks.
 constexpr uint32_t kSmallStages = 3;
-constexpr size_t kSmallSmem = 1024 + kSmallStages * 2 * kTileBytes + sizeof(MatmulShared);
+constexpr size_t kSmallSmem = 1024 + kSmallStages * 2 * kTileBytes + kScaleBufs * kScaleBufBytes + sizeof(MatmulShared);
 constexpr uint32_t kSmallCols = 256;             // tensor memory: 128 accumulator columns, then two sets of 4 + 4 scale columns
 constexpr uint32_t kSmallScales = 128;
 
@@ -90,7 +98,8 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 {
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (base - smem_u32(raw)) + kSmallStages * 2 * kTileBytes);
+    const uint32_t words_at = base + kSmallStages * 2 * kTileBytes;
+    MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (words_at - smem_u32(raw)) + kScaleBufs * kScaleBufBytes);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t parts = gridDim.z, part = blockIdx.z;
     const uint32_t m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
@@ -101,7 +110,7 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         prefetch_map(&map_a);
         prefetch_map(&map_b);
         for (uint32_t i = 0; i < kSmallStages; ++i) { bar_init(smem_u32(&S->full[i]), 1); bar_init(smem_u32(&S->empty[i]), 1); }
-        for (uint32_t i = 0; i < 2; ++i) { bar_init(smem_u32(&S->sf_full[i]), 4); bar_init(smem_u32(&S->sf_empty[i]), 1); }
+        for (uint32_t i = 0; i < kScaleBufs; ++i) { bar_init(smem_u32(&S->sf_full[i]), 1); bar_init(smem_u32(&S->sf_empty[i]), 1); }
         bar_init(smem_u32(&S->acc_full[0]), 1);
         S->failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -125,35 +134,41 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         }
     } else if (warp == 1 && lane == 0) {
         for (uint32_t i = 0; i < hi - lo; ++i) {
-            const uint32_t st = i % kSmallStages, set = (i >> 2) & 1;
-            if ((i & 3) == 0 && !wait(smem_u32(&S->sf_full[set]), (i >> 3) & 1)) break;
+            const uint32_t st = i % kSmallStages, word = i >> 2, buf = word % kScaleBufs;
+            const uint32_t sfa = tmem + kSmallScales + (word & 1) * 8, sfb = sfa + 4;
             if (!wait(smem_u32(&S->full[st]), (i / kSmallStages) & 1)) break;
+            if ((i & 3) == 0) {
+                if (!wait(smem_u32(&S->sf_full[buf]), (word / kScaleBufs) & 1)) break;
+                // the set's words of eight steps ago are not looked up any more
+                if (word >= 2 && !wait(smem_u32(&S->sf_empty[(word - 2) % kScaleBufs]), ((word - 2) / kScaleBufs) & 1)) break;
+                tc_fence_after();
+                tmem_copy_scales<1>(sfa, words_at + buf * kScaleBufBytes);
+                tmem_copy_scales<1>(sfb, words_at + buf * kScaleBufBytes + 512);
+            }
             tc_fence_after();
             const uint64_t da = operand_desc(base + st * 2 * kTileBytes), db = operand_desc(base + st * 2 * kTileBytes + kTileBytes);
             const uint32_t idesc = P.idesc | ((i & 3) << 29) | ((i & 3) << 4);
-            const uint32_t sfa = tmem + kSmallScales + set * 8, sfb = sfa + 4;
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) mma_scaled<1>(tmem, da + 2 * j, db + 2 * j, idesc, sfa, sfb, i | j);
             mma_commit<1>(smem_u32(&S->empty[st]));
-            if ((i & 3) == 3) mma_commit<1>(smem_u32(&S->sf_empty[set]));
+            if ((i & 3) == 3) mma_commit<1>(smem_u32(&S->sf_empty[buf]));
         }
         mma_commit<1>(smem_u32(&S->acc_full[0]));
     } else if (warp >= 8) {
-        const uint32_t quarter = (warp & 3) * (32u << 16);
-        for (uint32_t i = lo, k = 0; i < hi; i += 4, ++k) {
+        const uint32_t buf = warp - 8, at = words_at + buf * kScaleBufBytes + lane * 16;
+        for (uint32_t i = lo + 4 * buf, k = 0; i < hi; i += 4 * kScaleBufs, ++k) {
             uint32_t a[4], b[4];
 #pragma unroll
             for (uint32_t q = 0; q < 4; ++q) {
                 a[q] = scale_word(P.sa, P.ld_sa, P.square_a, m0 + 32 * q + lane, P.m, i, hi);
                 b[q] = scale_word(P.sb, P.ld_sb, P.square_b, n0 + 32 * q + lane, P.n, i, hi);
             }
-            if (!__all_sync(0xFFFFFFFFu, k < 2 || wait(smem_u32(&S->sf_empty[k & 1]), ((k >> 1) - 1) & 1))) break;
-            tmem_st4(tmem + quarter + kSmallScales + (k & 1) * 8, a);
-            tmem_st4(tmem + quarter + kSmallScales + (k & 1) * 8 + 4, b);
-            tmem_st_wait();
-            tc_fence_before();
+            if (!__all_sync(0xFFFFFFFFu, k == 0 || wait(smem_u32(&S->sf_empty[buf]), (k - 1) & 1))) break;
+            sts128(at, a);
+            sts128(at + 512, b);
+            fence_async_shared();
             __syncwarp();
-            if (lane == 0) bar_arrive(smem_u32(&S->sf_full[k & 1]));
+            if (lane == 0) bar_arrive(smem_u32(&S->sf_full[buf]));
         }
     }
     __syncwarp();
@@ -204,11 +219,186 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     if (warp == 1) tmem_free<1>(tmem, kSmallCols);
 }
 
+// Tiles of 256 x 256 per pair of blocks: each block holds 128 rows of A and 128 of B, the matrix instruction of the pair reads
+// both blocks' shared memory, and each block ends with 128 x 256 accumulators.  Two accumulators of 256 columns and the scale
+// words do not fit into 512 columns of tensor memory side by side, so the two overlap by 32 columns: the result warps empty these
+// first, and the next tile's instructions begin when they have, while the other 224 columns are still on their way out.
+constexpr uint32_t kLargeStages = 6;
+constexpr size_t kLargeSmem = 1024 + kLargeStages * 2 * kTileBytes + kScaleBufs * kScaleBufBytes + sizeof(MatmulShared);
+constexpr uint32_t kLargeCols = 512, kLargeSecond = 224, kLargeScales = 480;     // two sets of 4 + 8 scale columns
+constexpr uint32_t kSwath = 8;                   // rows of tiles that are walked through together, column by column
+
+__device__ __forceinline__ void large_tile(const MatmulParams& P, uint32_t i, uint32_t& m, uint32_t& n)
+{
+    const uint32_t per = kSwath * P.tiles_n, swath = i / per, first = swath * kSwath;
+    const uint32_t height = min(P.tiles_m - first, kSwath), in = i - swath * per;
+    n = in / height;
+    m = first + in - n * height;
+}
+
+__global__ void __launch_bounds__(kMmThreads, 1)
+matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MatmulParams P)
+{
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t words_at = base + kLargeStages * 2 * kTileBytes;
+    MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (words_at - smem_u32(raw)) + kScaleBufs * kScaleBufBytes);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = P.tiles_m * P.tiles_n;
+    const Waiter wait{P.spin_limit, &S->failed};
+
+    if (warp == 0 && lane == 0) {
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+        for (uint32_t i = 0; i < kLargeStages; ++i) { bar_init(smem_u32(&S->full[i]), 1); bar_init(smem_u32(&S->empty[i]), 1); }
+        for (uint32_t i = 0; i < kScaleBufs; ++i) { bar_init(smem_u32(&S->sf_full[i]), 2); bar_init(smem_u32(&S->sf_empty[i]), 1); }
+        for (uint32_t i = 0; i < 2; ++i) bar_init(smem_u32(&S->acc_full[i]), 1);
+        bar_init(smem_u32(&S->acc_empty[0]), 8);
+        S->failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc<2>(smem_u32(&S->tmem), kLargeCols);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();                              // the pair's barriers are there before either block uses them
+    tc_fence_after();
+    const uint32_t tmem = S->tmem;
+
+    if (warp == 0 && lane == 0) {
+        // both blocks copy their halves; the bytes count on the first block's barrier
+        uint32_t st = 0, round = 0;
+        bool ok = true;
+        for (uint32_t i = pair; i < tiles && ok; i += pairs) {
+            uint32_t tm, tn;
+            large_tile(P, i, tm, tn);
+            const int row_a = (int)(tm * 256 + rank * 128), row_b = (int)(tn * 256 + rank * 128);
+            for (uint32_t k = 0; k < P.steps; ++k) {
+                if (!(ok = round == 0 || wait(smem_u32(&S->empty[st]), (round - 1) & 1))) break;
+                if (rank == 0) bar_expect(smem_u32(&S->full[st]), 4 * kTileBytes);
+                const uint32_t bar = map_shared(smem_u32(&S->full[st]), 0), to = base + st * 2 * kTileBytes;
+                if (!P.skip_copy) {
+                    tensor_copy<2>(to, &map_a, (int)(k * kStepBytes), row_a, bar);
+                    tensor_copy<2>(to + kTileBytes, &map_b, (int)(k * kStepBytes), row_b, bar);
+                }
+                if (++st == kLargeStages) { st = 0; ++round; }
+            }
+        }
+        // after a wait that gave up, copies may still be on their way into the pair's shared memory
+        if (!ok && !P.skip_copy && rank == 0)
+            for (uint32_t i = 0; i < kLargeStages; ++i) {
+                const uint32_t r = i < st ? round : round - 1;
+                if (round == 0 && i >= st) continue;
+                for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S->full[i]), r & 1); ++q) { }
+            }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        uint32_t st = 0, round = 0, word = 0, tile = 0;
+        bool ok = true;
+        for (uint32_t i = pair; i < tiles && ok; i += pairs, ++tile) {
+            const uint32_t d = tmem + (tile & 1 ? kLargeSecond : 0);
+            // the columns that this tile's accumulator shares with the one before it are empty, and with them all of the one before that
+            if (tile && !(ok = wait.across(smem_u32(&S->acc_empty[0]), (tile - 1) & 1))) break;
+            for (uint32_t k = 0; k < P.steps; ++k) {
+                const uint32_t buf = word % kScaleBufs, sfa = tmem + kLargeScales + (word & 1) * 12, sfb = sfa + 4;
+                if (!(ok = wait(smem_u32(&S->full[st]), round & 1))) break;
+                if ((k & 3) == 0) {
+                    if (!(ok = wait.across(smem_u32(&S->sf_full[buf]), (word / kScaleBufs) & 1))) break;
+                    // the set's words of two before are not looked up any more
+                    if (word >= 2 && !(ok = wait(smem_u32(&S->sf_empty[(word - 2) % kScaleBufs]), ((word - 2) / kScaleBufs) & 1))) break;
+                    tc_fence_after();
+                    const uint32_t from = words_at + buf * kScaleBufBytes;
+                    tmem_copy_scales<2>(sfa, from);
+                    tmem_copy_scales<2>(sfb, from + 512);
+                    tmem_copy_scales<2>(sfb + 4, from + 1024);
+                }
+                tc_fence_after();
+                const uint64_t da = operand_desc(base + st * 2 * kTileBytes), db = operand_desc(base + st * 2 * kTileBytes + kTileBytes);
+                const uint32_t idesc = P.idesc | ((k & 3) << 29) | ((k & 3) << 4);
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) mma_scaled<2>(d, da + 2 * j, db + 2 * j, idesc, sfa, sfb, k | j);
+                mma_commit<2>(smem_u32(&S->empty[st]));
+                if ((k & 3) == 3 || k + 1 == P.steps) { mma_commit<2>(smem_u32(&S->sf_empty[buf])); ++word; }
+                if (++st == kLargeStages) { st = 0; ++round; }
+            }
+            mma_commit<2>(smem_u32(&S->acc_full[tile & 1]));
+        }
+    } else if (warp >= 8) {
+        // this block's 128 rows of A and the pair's 256 of B
+        const uint32_t buf = warp - 8, at = words_at + buf * kScaleBufBytes + lane * 16, per = (P.steps + 3) >> 2;
+        uint32_t round = 0;
+        for (uint32_t w = buf, i = pair; i < tiles; w += kScaleBufs, ++round) {
+            while (w >= per && i < tiles) { w -= per; i += pairs; }
+            if (i >= tiles) break;
+            uint32_t tm, tn, a[4], b[8];
+            large_tile(P, i, tm, tn);
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) a[q] = scale_word(P.sa, P.ld_sa, P.square_a, tm * 256 + rank * 128 + 32 * q + lane, P.m, 4 * w, P.steps);
+#pragma unroll
+            for (uint32_t q = 0; q < 8; ++q) b[q] = scale_word(P.sb, P.ld_sb, P.square_b, tn * 256 + 32 * q + lane, P.n, 4 * w, P.steps);
+            if (!__all_sync(0xFFFFFFFFu, round == 0 || wait(smem_u32(&S->sf_empty[buf]), (round - 1) & 1))) break;
+            sts128(at, a);
+            sts128(at + 512, b);
+            sts128(at + 1024, b + 4);
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) bar_arrive_cluster(map_shared(smem_u32(&S->sf_full[buf]), 0));
+        }
+    } else if (warp >= 4) {
+        const uint32_t quad = warp & 3;
+        uint32_t tile = 0;
+        for (uint32_t i = pair; i < tiles; i += pairs, ++tile) {
+            uint32_t tm, tn;
+            large_tile(P, i, tm, tn);
+            if (!__all_sync(0xFFFFFFFFu, wait(smem_u32(&S->acc_full[tile & 1]), (tile >> 1) & 1) && !*wait.failed)) break;
+            tc_fence_after();
+            const uint32_t row = tm * 256 + rank * 128 + quad * 32 + lane;
+            const uint32_t d = tmem + (quad * 32u << 16) + (tile & 1 ? kLargeSecond : 0);
+#pragma unroll 1
+            for (uint32_t q = 0; q < 8; ++q) {
+                const uint32_t c = tile & 1 ? q : (q + 7) & 7;           // the shared columns first
+                uint32_t v[32];
+                tmem_ld32(d + c * 32, v);
+                if (q == 0) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive_cluster(map_shared(smem_u32(&S->acc_empty[0]), 0));
+                }
+                store_row<32>(P, row, tn * 256 + c * 32, reinterpret_cast<const float*>(v));
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();                              // nothing of either block arrives at, or is copied into, the other any more
+    tc_fence_after();
+    if (warp == 1) tmem_free<2>(tmem, kLargeCols);
+}
+
 // D = 0 (K = 0): nothing to copy or multiply.
 __global__ void zero_kernel(const __grid_constant__ MatmulParams P, uint32_t width)
 {
     for (uint64_t r = blockIdx.x; r < P.m; r += gridDim.x)
         for (uint64_t i = threadIdx.x; i < (uint64_t)P.n * width; i += blockDim.x) P.out[r * P.ld_out + i] = 0;
+}
+
+#ifndef ZC_LARGE_FROM
+#define ZC_LARGE_FROM 37
+#endif
+// Blocks of the large kernel that are on the GPU at once, in whole pairs.
+static uint32_t large_blocks()
+{
+    if (cudaFuncSetAttribute(matmul_large_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLargeSmem) != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((uint32_t)sm_count() / 2 * 2);
+    cfg.blockDim = dim3(kMmThreads);
+    cfg.dynamicSmemBytes = kLargeSmem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {2, 1, 1};
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, (const void*)matmul_large_kernel, &cfg) != cudaSuccess || n <= 0) return 0;
+    return std::min((uint32_t)n * 2, cfg.gridDim.x);
 }
 
 }  // namespace zc
@@ -253,9 +443,31 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
     if (!make_map(&map_a, a->d_elems, a->rows, a->cols, a->ld_elems, kTile) || !make_map(&map_b, b->d_elems, b->rows, b->cols, b->ld_elems, kTile)) return ZC_E_CUDA;
     P.tiles_m = (uint32_t)ceil_div(P.m, kTile);
     P.tiles_n = (uint32_t)ceil_div(P.n, kTile);
-    P.idesc = instruction_of(a->format, b->format, 128, 128);
     if (P.tiles_m > 65535) return ZC_E_TOO_LARGE;
     const uint64_t tiles = (uint64_t)P.tiles_m * P.tiles_n;
+    const uint64_t large = ceil_div(P.m, 256) * ceil_div(P.n, 256);
+    if (large >= ZC_LARGE_FROM) {
+        static OncePerDevice once;
+        const uint32_t blocks = once([] { return large_blocks(); });
+        if (!blocks) return ZC_E_CUDA;
+        P.tiles_m = (uint32_t)ceil_div(P.m, 256);
+        P.tiles_n = (uint32_t)ceil_div(P.n, 256);
+        if (large >= (1ull << 31)) return ZC_E_TOO_LARGE;
+        P.idesc = instruction_of(a->format, b->format, 256, 256);
+        const uint32_t grid = (uint32_t)std::min<uint64_t>(blocks, 2 * large);
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(grid);
+        cfg.blockDim = dim3(kMmThreads);
+        cfg.dynamicSmemBytes = kLargeSmem;
+        cfg.stream = st;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim = {2, 1, 1};
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, matmul_large_kernel, map_a, map_b, P) == cudaSuccess ? ZC_OK : ZC_E_CUDA;
+    }
+    P.idesc = instruction_of(a->format, b->format, 128, 128);
     uint32_t parts = 1;
     while (parts < 8 && tiles * parts * 2 <= 2 * (uint64_t)sm_count() && P.steps >= 4 * parts) parts *= 2;
     cudaLaunchConfig_t cfg{};

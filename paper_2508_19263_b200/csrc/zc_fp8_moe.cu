@@ -17,23 +17,32 @@
 //   kernel 2  down: up to 128 rows a tile, one FP32 row of partial results per (token, expert); the block that completes a
 //             group's last expert adds the experts up in the order of the token's list
 //
-// Warps of a block: 0 tensor copies, 1 matrix instructions, 2 the weights' scale bytes, 4-7 results, 8-13 the activations' pieces (14, 15: routing only).
+// Warps of a block: 0 tensor copies, 1 matrix instructions, 2 the weights' scale bytes, 4-7 results, 8-23 the activations' pieces.
 #include "zc_fp8_tensor.cuh"
 
 namespace zc {
 
-constexpr uint32_t kMoeWarps = 16, kMoeThreads = 32 * kMoeWarps;
+constexpr uint32_t kMoeWarps = 24, kMoeThreads = 32 * kMoeWarps;
 constexpr uint32_t kMoeCluster = 4;
-constexpr uint32_t kMoePass = 32;                // tokens that share a reading of a tile
 constexpr uint32_t kMaxTokens = ZC_FP8_MOE_MAX_TOKENS, kMaxExperts = ZC_FP8_MOE_MAX_EXPERTS;
 constexpr uint32_t kMaxRows = kMaxTokens * ZC_FP8_MOE_MAX_TOP_K;
-constexpr uint32_t kMoeStages = 6;
-constexpr uint32_t kMoeStageBytes = 16384 + 16384 + 1024 + 1024;   // weights, pieces, scale words of both (the rest keeps 1 KiB alignment)
+constexpr uint32_t kBuilders = 16;               // warps that make pieces
+constexpr uint32_t kMoeMaxStages = 9;
+constexpr uint32_t kMoeStageSpace = 208896;      // shared memory for stages: weights, pieces, 1 KiB of scale words each
 constexpr uint32_t kMoeHeights = 5;              // tensor copies of 8, 16, 32, 64 and 128 rows
 constexpr uint32_t kMoeTmemCols = 512;           // two accumulators of 128 columns, then 4 + 4 scale columns per stage
 constexpr uint32_t kMoeTmemScales = 256;
 
 struct MoeMaps { CUtensorMap of[kMoeHeights]; };
+
+// rows of pieces of `count` tokens: each piece's rounded up to 8, all to 16 (what is behind the last piece is multiplied and not used)
+__host__ __device__ constexpr uint32_t piece_rows(uint32_t count, uint32_t pieces) { return (((count + 7) & ~7u) * pieces + 15) & ~15u; }
+__host__ __device__ constexpr uint32_t stage_size(uint32_t pass, uint32_t pieces) { return 16384 + piece_rows(pass, pieces) * 128 + 1024; }
+__host__ __device__ constexpr uint32_t stage_count(uint32_t pass, uint32_t pieces)
+{
+    return kMoeStageSpace / stage_size(pass, pieces) < kMoeMaxStages ? kMoeStageSpace / stage_size(pass, pieces) : kMoeMaxStages;
+}
+static_assert(piece_rows(32, 4) <= 128 && stage_count(32, 4) == 6 && stage_count(8, 3) == 9, "stages");
 
 struct MoeParams {
     const uint8_t *x, *router;                   // rows of BF16 or FP16
@@ -42,6 +51,7 @@ struct MoeParams {
     uint32_t tokens, experts, top_k, hidden, inter;
     uint32_t hidden_pad, inter_pad;              // rounded up to 64 columns
     uint32_t idesc;                              // matrix instruction without its N
+    uint32_t pass;                               // tokens that share a reading of a tile
     uint32_t *ids_out;
     float *weights_out;
     uint8_t *y;
@@ -57,13 +67,13 @@ struct MoeParams {
 
 // What a block knows of the routing.
 struct Routing {
-    uint32_t n_active, n_passes;                 // chosen experts; of up to 32 tokens each
+    uint32_t n_active, n_passes;                 // chosen experts; of up to P.pass tokens each
     uint16_t expert[kMaxExperts];
     uint16_t first[kMaxExperts + 1];             // first row of an expert's tokens
     uint16_t pass[kMaxExperts + 1];              // passes of the experts before
 };
 struct MoeShared {
-    uint64_t full[kMoeStages], empty[kMoeStages], acc_full[2], acc_empty[2];
+    uint64_t full[kMoeMaxStages], empty[kMoeMaxStages], acc_full[2], acc_empty[2];
     uint32_t tmem, failed;
     Routing R;
     alignas(16) float other[2][64][4];           // kernel 1: what the other half of the result warps needs
@@ -74,15 +84,17 @@ struct MoeShared {
 };
 // while routing, where the stages will be
 struct MoeRouting {
-    double items[16 * 128], logits[kMaxExperts * kMaxTokens];
     float p[kMaxRows];                           // of this block's share of the tokens
     uint16_t id[kMaxRows];
     float p_all[kMaxRows];
     uint16_t id_all[kMaxRows];
     unsigned long long mask[kMaxExperts];        // tokens that chose the expert
+    // [token, rounded up to 8][expert, to 16]; behind them the warps' sums of logits that several share (there are few then), and
+    // columns of router and tokens
+    double logits[1];
 };
-constexpr size_t kMoeSmem = 1024 + kMoeStages * kMoeStageBytes + sizeof(MoeShared);
-static_assert(sizeof(MoeRouting) <= kMoeStages * kMoeStageBytes && kMoeSmem <= kMaxSmem, "shared memory");
+constexpr size_t kMoeSmem = 1024 + kMoeStageSpace + sizeof(MoeShared);
+static_assert(sizeof(MoeRouting) + 8 * kMaxExperts * kMaxTokens + (kMaxExperts + kMaxTokens) * 192 + 16 <= kMoeStageSpace && kMoeSmem <= kMaxSmem, "shared memory");
 
 template <bool HALF>
 __device__ __forceinline__ void mma16(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1)
@@ -106,103 +118,164 @@ __device__ __forceinline__ uint4 zero4() { return make_uint4(0, 0, 0, 0); }
 
 // ---- the weights' stream --------------------------------------------------------------------------------------------
 
-// A tile: `groups` groups of eight rows (UP: of gate, and behind 64 rows of up) of a chosen expert, for up to 32 of its tokens.
+// A tile: `groups` groups of eight rows (UP: of gate, and behind 64 rows of up) of a chosen expert, for up to P.pass of its tokens.
 struct Tile {
-    uint32_t active, expert, group, groups, row, count;      // row, count: its tokens' rows
+    uint32_t expert, group, groups, row, count;  // row, count: its tokens' rows
 };
 
-// The tiles of units first .. end - 1; all roles walk through them alike.  A unit is a group of an expert.  UP: expert by
-// expert.  Down: bands of 128 rows, in each of them expert by expert, so that a band is complete, and its experts can be added up, when a
-// few neighbouring blocks have done with it, and not all bands at once at the very end.
+// How the rows of an expert are cut: `per` tiles of `height` groups.
+struct Cut { uint32_t height, per; };
+
+// A step of 128 columns takes the block about as long as `kFixed` groups' bytes do even when the tile is small, so blocks want few
+// and equal tiles: of all numbers of tiles a block the one whose tiles, as high as they then have to be, take the slowest block least.
+template <bool UP>
+__device__ __forceinline__ Cut cut_rows(uint32_t rows, uint32_t n_passes, uint32_t blocks)
+{
+    constexpr uint32_t kMost = UP ? 8 : 16, kFixed = UP ? 4 : 8;
+    const uint32_t groups = (rows + 7) >> 3, lane = threadIdx.x & 31;
+    const uint32_t least = (n_passes * ((groups + kMost - 1) / kMost) + blocks - 1) / blocks, rounds = least + lane;
+    const uint32_t per = min(rounds * blocks / n_passes, groups);
+    const uint32_t height = (groups + per - 1) / per;        // per > 0: `least` tiles a block are enough
+    const uint32_t cost = rounds * (kFixed + height);
+    const uint32_t best = __reduce_min_sync(0xFFFFFFFFu, cost);
+    const uint32_t who = __reduce_min_sync(0xFFFFFFFFu, cost == best ? lane : 32u);
+    Cut c;
+    c.height = __shfl_sync(0xFFFFFFFFu, height, who);
+    c.per = (groups + c.height - 1) / c.height;
+    return c;
+}
+
+// A block's tiles; all roles walk through them alike.  UP: expert by expert.  Down: band of rows by band of rows, in each of them
+// expert by expert, so that a band is complete, and its experts can be added up, when a few neighbouring blocks have done with it,
+// and not all bands at once at the very end.  The passes over an expert's tokens lie next to each other: the second finds the tile in
+// the L2.
 template <bool UP>
 struct Tiles {
-    static constexpr uint32_t kMost = UP ? 8 : 16;
     const Routing& R;
-    uint32_t groups, at, end, pass;
-    __device__ __forceinline__ Tiles(const Routing& r, uint32_t rows, uint32_t block, uint32_t blocks)
-        : R(r), groups((rows + 7) >> 3), pass(0)
+    const Cut cut;
+    const uint32_t groups, most;
+    uint32_t left, active, band, pass;
+    __device__ __forceinline__ Tiles(const Routing& r, const Cut& c, uint32_t rows, uint32_t most_, uint32_t block, uint32_t blocks)
+        : R(r), cut(c), groups((rows + 7) >> 3), most(most_), active(0)
     {
-        const uint64_t units = (uint64_t)groups * r.n_active;
-        at = (uint32_t)(units * block / blocks);
-        end = (uint32_t)(units * (block + 1) / blocks);
+        const uint32_t all = c.per * r.n_passes;             // at most 2^13 * 2^10; times the blocks still 32 bits
+        const uint32_t first = all * block / blocks;
+        left = all * (block + 1) / blocks - first;
+        const uint32_t v = UP ? first / c.per : first % r.n_passes;
+        if (UP) {
+            while (active + 1 < r.n_active && (uint32_t)r.pass[active + 1] * c.per <= first) ++active;
+            const uint32_t in = first - r.pass[active] * c.per, n = passes();
+            band = in / n;
+            pass = in - band * n;
+        } else {
+            band = first / r.n_passes;
+            while (active + 1 < r.n_active && r.pass[active + 1] <= v) ++active;
+            pass = v - r.pass[active];
+        }
     }
+    __device__ __forceinline__ uint32_t passes() const { return R.pass[active + 1] - R.pass[active]; }
     __device__ __forceinline__ bool next(Tile& t)
     {
-        if (at >= end) return false;
-        uint32_t left;
+        if (!left) return false;
+        --left;
+        t.expert = R.expert[active];
+        t.group = band * cut.height;
+        t.groups = min(cut.height, groups - t.group);
+        t.row = R.first[active] + pass * most;
+        t.count = min(R.first[active + 1] - t.row, most);
+        if (++pass < passes()) return true;
+        pass = 0;
         if (UP) {
-            t.active = at / groups;
-            t.group = at - t.active * groups;
-            left = min(end - at, groups - t.group);
-            // a remainder is shared by the last two tiles
-            t.groups = left > kMost && left < 2 * kMost ? (left + 1) / 2 : min(left, kMost);
-        } else {
-            const uint32_t band = at / (kMost * R.n_active), first = band * kMost, height = min(groups - first, kMost);
-            const uint32_t in = at - first * R.n_active;
-            t.active = in / height;
-            t.group = first + in - t.active * height;
-            t.groups = min(end - at, first + height - t.group);
+            if (++band == cut.per) { band = 0; ++active; }
+        } else if (++active == R.n_active) {
+            active = 0;
+            ++band;
         }
-        t.expert = R.expert[t.active];
-        t.row = R.first[t.active] + pass * kMoePass;
-        const uint32_t n = R.first[t.active + 1] - t.row;
-        t.count = min(n, kMoePass);
-        if (n > kMoePass) ++pass;
-        else { pass = 0; at += t.groups; }
         return true;
     }
 };
 
-// Four activations of a lane as PIECES E4M3 words, in the block scale of the warp's 128 columns.
-template <int PIECES>
-__device__ __forceinline__ void make_pieces(const float v[4], uint32_t words[PIECES], uint32_t& scale)
+__device__ __forceinline__ uint32_t to_pieces(__half2 v)
 {
-    float m = fmaxf(fmaxf(finite_abs(v[0]), finite_abs(v[1])), fmaxf(finite_abs(v[2]), finite_abs(v[3])));
-    m = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m)));
-    scale = scale_byte<false>(m);
+    return __nv_cvt_halfraw2_to_fp8x2(__half2_raw(v), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ __half2 of_pieces(uint32_t q)
+{
+    return __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)q, __NV_E4M3));
+}
+
+// Four activations of a lane as PIECES E4M3 words, in the block scale of the warp's 128 columns.  FP16 holds what is left behind a
+// piece: exactly for BF16 and FP16 activations (EXACT), to 2^-16 of the value for FP32 ones, whose first piece is split off in FP32.
+template <int PIECES, bool EXACT>
+__device__ __forceinline__ void make_pieces(float v[4], uint32_t words[PIECES], uint32_t& scale)
+{
+    const uint32_t m01 = max(__float_as_uint(v[0]) & 0x7FFFFFFFu, __float_as_uint(v[1]) & 0x7FFFFFFFu);
+    const uint32_t m23 = max(__float_as_uint(v[2]) & 0x7FFFFFFFu, __float_as_uint(v[3]) & 0x7FFFFFFFu);
+    uint32_t largest = __reduce_max_sync(0xFFFFFFFFu, max(m01, m23));
+    if (largest >= 0x7F800000u) {                // rare: infinities and NaN all become NaN, E4M3 has nothing else
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m = fmaxf(m, finite_abs(v[i]));
+            v[i] = fabsf(v[i]) < __int_as_float(0x7F800000) ? v[i] : __int_as_float(0x7FC00000);
+        }
+        largest = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m));
+    }
+    scale = scale_byte<false>(__uint_as_float(largest));
     const float inv = inverse_scale(scale);
     float f[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = fabsf(v[i]) < __int_as_float(0x7F800000) ? v[i] * inv : __int_as_float(0x7FC00000);   // E4M3 has no infinity
-#pragma unroll
-    for (int k = 0; k < PIECES; ++k) {
+    for (int i = 0; i < 4; ++i) f[i] = v[i] * inv;
+    const __half2 sixteen = __float2half2_rn(16.0f), minus = __float2half2_rn(-16.0f);
+    __half2 a, b;
+    if (EXACT) {
+        a = __floats2half2_rn(f[0], f[1]);
+        b = __floats2half2_rn(f[2], f[3]);
+    } else {
         const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
         const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
+        words[0] = lo | (hi << 16);
+        const float2 x = __half22float2(of_pieces(lo)), y = __half22float2(of_pieces(hi));
+        a = __floats2half2_rn((f[0] - x.x) * 16.0f, (f[1] - x.y) * 16.0f);
+        b = __floats2half2_rn((f[2] - y.x) * 16.0f, (f[3] - y.y) * 16.0f);
+    }
+#pragma unroll
+    for (int k = EXACT ? 0 : 1; k < PIECES; ++k) {
+        const uint32_t lo = to_pieces(a), hi = to_pieces(b);
         // scales end at 2^-127: what would need a smaller one is left out
         words[k] = scale >= 4u * k ? lo | (hi << 16) : 0u;
         if (k + 1 < PIECES) {
-            const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)lo, __NV_E4M3)));
-            const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)hi, __NV_E4M3)));
-            f[0] = (f[0] - a.x) * 16.0f;
-            f[1] = (f[1] - a.y) * 16.0f;
-            f[2] = (f[2] - b.x) * 16.0f;
-            f[3] = (f[3] - b.y) * 16.0f;
+            a = __hfma2(of_pieces(lo), minus, __hmul2(a, sixteen));
+            b = __hfma2(of_pieces(hi), minus, __hmul2(b, sixteen));
         }
     }
 }
 
 // What a block does after the routing: its share of gate and up (UP) or of down.  HALF: activations of gate and up are FP16.
 template <bool UP, bool HALF, int PIECES, typename Finish>
-__device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps& maps, MoeShared& S, uint32_t base, uint32_t blocks, Finish finish)
+__device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps& maps, MoeShared& S, const Cut& cut, uint32_t base, uint32_t blocks, Finish finish)
 {
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t cols = UP ? P.hidden : P.inter, rows = UP ? P.inter : P.hidden;
     const uint32_t steps = (cols + 127) >> 7;
     const Waiter wait{P.spin_limit, &S.failed};
-    Tiles<UP> tiles(S.R, rows, blockIdx.x, blocks);
+    const uint32_t stages = stage_count(P.pass, PIECES), stage_bytes = stage_size(P.pass, PIECES), scales_at = stage_bytes - 1024;
+    Tiles<UP> tiles(S.R, cut, rows, P.pass, blockIdx.x, blocks);
     Tile t;
-    uint32_t n = 0;                              // steps so far
     const uint32_t tmem = S.tmem;
+    // the stage of the present step and the parity of its round; `first`: no stage has been used yet
+    uint32_t st = 0, round = 0;
+    auto forward = [&] { if (++st == stages) { st = 0; ++round; } };
+    auto free_stage = [&] { return round == 0 || wait(smem_u32(&S.empty[st]), (round - 1) & 1); };
 
     if (warp == 0) {
         if (lane == 0) {
             bool ok = true;
             while (ok && tiles.next(t)) {
                 const uint32_t row0 = t.expert * (UP ? 2 * P.inter : P.hidden) + t.group * 8;
-                for (uint32_t k = 0; k < steps; ++k, ++n) {
-                    const uint32_t st = n % kMoeStages;
-                    if (n >= kMoeStages && !(ok = wait(smem_u32(&S.empty[st]), (n / kMoeStages - 1) & 1))) break;
-                    const uint32_t bar = smem_u32(&S.full[st]), to = base + st * kMoeStageBytes;
+                for (uint32_t k = 0; k < steps; ++k, forward()) {
+                    if (!(ok = free_stage())) break;
+                    const uint32_t bar = smem_u32(&S.full[st]), to = base + st * stage_bytes;
                     bar_expect(bar, t.groups * (UP ? 2048 : 1024));
                     if (P.skip_copy) continue;
                     // as few copies as there are bits in the number of groups: one of 8 rows takes the copy engine as long as one of 64
@@ -216,10 +289,14 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
                     }
                 }
             }
-            // after a wait that gave up, copies may still be on their way into this block's shared memory
+            // after a wait that gave up, copies may still be on their way into this block's shared memory: of this round up to
+            // the present stage, of the one before from there on
             if (!ok && !P.skip_copy)
-                for (uint32_t i = n > kMoeStages ? n - kMoeStages : 0; i < n; ++i)
-                    for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S.full[i % kMoeStages]), (i / kMoeStages) & 1); ++q) { }
+                for (uint32_t i = 0; i < stages; ++i) {
+                    const uint32_t r = i < st ? round : round - 1;
+                    if (round == 0 && i >= st) continue;
+                    for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S.full[i]), r & 1); ++q) { }
+                }
         }
     } else if (warp == 1) {
         if (lane == 0) {
@@ -227,17 +304,15 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
             bool ok = true;
             while (ok && tiles.next(t)) {
                 const uint32_t buf = tile & 1, d = tmem + buf * 128;
-                const uint32_t cols_d = (((t.count + 7) & ~7u) * PIECES + 15) & ~15u;      // what is behind the last piece is computed and not used
-                const uint32_t idesc = P.idesc | ((cols_d >> 3) << 17);
+                const uint32_t idesc = P.idesc | ((piece_rows(t.count, PIECES) >> 3) << 17);
                 if (tile >= 2 && !(ok = wait(smem_u32(&S.acc_empty[buf]), ((tile >> 1) - 1) & 1))) break;
                 tc_fence_after();
-                for (uint32_t k = 0; k < steps; ++k, ++n) {
-                    const uint32_t st = n % kMoeStages;
-                    if (!(ok = wait(smem_u32(&S.full[st]), (n / kMoeStages) & 1))) break;
+                for (uint32_t k = 0; k < steps; ++k, forward()) {
+                    if (!(ok = wait(smem_u32(&S.full[st]), round & 1))) break;
                     tc_fence_after();
-                    const uint32_t at = base + st * kMoeStageBytes, sf = tmem + kMoeTmemScales + st * 8;
-                    tmem_copy_scales(sf, at + 32768);
-                    tmem_copy_scales(sf + 4, at + 32768 + 512);
+                    const uint32_t at = base + st * stage_bytes, sf = tmem + kMoeTmemScales + st * 8;
+                    tmem_copy_scales<1>(sf, at + scales_at);
+                    tmem_copy_scales<1>(sf + 4, at + scales_at + 512);
                     const uint64_t da = operand_desc(at), db = operand_desc(at + 16384);
 #pragma unroll
                     for (uint32_t j = 0; j < 4; ++j) mma_scaled<1>(d, da + 2 * j, db + 2 * j, idesc, sf, sf + 4, k | j);
@@ -270,10 +345,9 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
             for (uint32_t k = 0; k < steps && ok; k += 4) {
                 if (k + 4 < steps) fetch(k + 4, ahead);
                 else if ((more = tiles.next(t))) { find_rows(); fetch(0, ahead); }
-                for (uint32_t q = 0; q < 4 && k + q < steps; ++q, ++n) {
-                    const uint32_t st = n % kMoeStages;
-                    if (!(ok = __all_sync(0xFFFFFFFFu, n < kMoeStages || wait(smem_u32(&S.empty[st]), (n / kMoeStages - 1) & 1)))) break;
-                    const uint32_t at = base + st * kMoeStageBytes + 32768 + lane * 16;
+                for (uint32_t q = 0; q < 4 && k + q < steps; ++q, forward()) {
+                    if (!(ok = __all_sync(0xFFFFFFFFu, free_stage()))) break;
+                    const uint32_t at = base + st * stage_bytes + scales_at + lane * 16;
                     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"((w[0] >> (8 * q)) & 255u), "r"((w[1] >> (8 * q)) & 255u),
                                  "r"((w[2] >> (8 * q)) & 255u), "r"((w[3] >> (8 * q)) & 255u) : "memory");
                     fence_async_shared();
@@ -285,21 +359,23 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
             }
         }
     } else if (warp >= 8) {
-        // a warp has a stage of its own: the time of all stages for the latency of its loads, and it sees every phase of its
-        // stage's barrier (a wait by parity that skipped one would take the phase before for it)
-        const uint32_t st = warp - 8, at = base + st * kMoeStageBytes;
-        bool ok = true;
-        while (ok && tiles.next(t)) {
-            const uint32_t padded = (t.count + 7) & ~7u;
-            for (uint32_t k = 0; k < steps; ++k, ++n) {
-                if (n % kMoeStages != st) continue;
-                const uint32_t col = k * 128 + lane * 4;
-                for (uint32_t c = 0; c < padded; c += 8) {
-                    uint4 raw[8];
+        // a warp has a stage of its own (two have one where there are at most eight): the time of all stages for the latency
+        // of its loads, and it sees every phase of its stage's barrier (a wait by parity that skipped one would take the phase
+        // before for it)
+        const uint32_t sharing = kBuilders / stages, own = (warp - 8) % stages, part = (warp - 8) / stages;
+        if (part < sharing) {
+            const uint32_t at = base + own * stage_bytes;
+            bool ok = true;
+            while (ok && tiles.next(t)) {
+                const uint32_t padded = (t.count + 7) & ~7u;
+                for (uint32_t k = 0; k < steps; ++k, forward()) {
+                    if (st != own) continue;
+                    const uint32_t col = k * 128 + lane * 4;
+                    auto fetch = [&](uint32_t c, uint4 raw[4]) {
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) {
-                        raw[i] = zero4();
-                        if (c + i < t.count && col < cols) {
+                        for (uint32_t i = 0; i < 4; ++i) {
+                            raw[i] = zero4();
+                            if (c + i >= t.count || col >= cols) continue;
                             if (UP) {
                                 const uint2 v = __ldg(reinterpret_cast<const uint2*>(P.x + 2 * ((uint64_t)S.row_token[t.row + c + i] * P.ld_x + col)));
                                 raw[i].x = v.x;
@@ -308,14 +384,15 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
                                 raw[i] = *reinterpret_cast<const uint4*>(P.h + (uint64_t)(t.row + c + i) * P.inter_pad + col);
                             }
                         }
-                    }
-                    if (c == 0 && !(ok = __all_sync(0xFFFFFFFFu, n < kMoeStages || wait(smem_u32(&S.empty[st]), (n / kMoeStages - 1) & 1)))) break;
+                    };
                     // four tokens at a time, whether they are there or not (their rows are): the chain of roundings is long
+                    uint4 raw[4], ahead[4];
+                    fetch(4 * part, raw);
+                    if (!(ok = __all_sync(0xFFFFFFFFu, free_stage()))) break;
+                    for (uint32_t c = 4 * part; c < t.count; c += 4 * sharing) {
+                        if (c + 4 * sharing < t.count) fetch(c + 4 * sharing, ahead);
 #pragma unroll
-                    for (uint32_t f = 0; f < 8; f += 4) {
-                        if (c + f >= t.count) break;
-#pragma unroll
-                        for (uint32_t i = f; i < f + 4; ++i) {
+                        for (uint32_t i = 0; i < 4; ++i) {
                             float v[4];
                             if (UP) {
                                 const uint32_t u[2] = {raw[i].x, raw[i].y};
@@ -328,23 +405,26 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
                                 v[0] = __uint_as_float(raw[i].x); v[1] = __uint_as_float(raw[i].y);
                                 v[2] = __uint_as_float(raw[i].z); v[3] = __uint_as_float(raw[i].w);
                             }
+                            if (k + 1 == steps) {
 #pragma unroll
-                            for (uint32_t q = 0; q < 4; ++q) v[q] = col + q < cols ? v[q] : 0.0f;
+                                for (uint32_t q = 0; q < 4; ++q) v[q] = col + q < cols ? v[q] : 0.0f;
+                            }
                             uint32_t words[PIECES], scale;
-                            make_pieces<PIECES>(v, words, scale);
+                            make_pieces<PIECES, UP>(v, words, scale);
 #pragma unroll
                             for (uint32_t q = 0; q < PIECES; ++q) {
                                 const uint32_t r = q * padded + c + i;
                                 sts32(at + 16384 + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4, words[q]);
-                                if (lane == q) sts32(at + 32768 + 512 + (r & 31) * 16 + (r >> 5) * 4, scale >= 4u * q ? scale - 4u * q : 0u);
+                                if (lane == q) sts32(at + scales_at + 512 + (r & 31) * 16 + (r >> 5) * 4, scale >= 4u * q ? scale - 4u * q : 0u);
                             }
                         }
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i) raw[i] = ahead[i];
                     }
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_u32(&S.full[st]));
                 }
-                if (!ok) break;
-                fence_async_shared();
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_u32(&S.full[st]));
             }
         }
     } else if (warp >= 4) {
@@ -403,67 +483,86 @@ __device__ __forceinline__ double ld_cluster_f64(uint32_t addr)
     return v;
 }
 
-// This block's part of the logits, logits[expert][token]: of the columns' parts of 128 the cluster's blocks take a share each, so
-// that a cluster reads router and tokens once.  Products of a part are summed by the matrix instructions in FP32, the parts in FP64:
-// what separates two experts' logits decides which weights are used, and 2^-24 of the sum of a part is far below what the
-// activations' own rounding moves.
+// This block's part of the logits, logits[token][expert]: the cluster's blocks take a share of the columns each, so that a cluster
+// reads router and tokens once; they pass through shared memory, from where every warp takes what its 16 experts x 8 tokens need.
+// Products of 64 columns are summed by the matrix instructions in FP32, these in FP64: what separates two experts' logits decides
+// which weights are used, and 2^-24 of such a sum is far below what the activations' own rounding moves.
 template <bool HALF>
 __device__ __forceinline__ void router_logits(const MoeParams& P, uint32_t rank, MoeRouting& S)
 {
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const uint32_t mt = (P.experts + 15) >> 4, nt = (P.tokens + 7) >> 3, tasks = mt * nt;
-    const uint32_t all = (P.hidden + 127) >> 7, lo = all * rank / kMoeCluster, parts = all * (rank + 1) / kMoeCluster - lo;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const uint32_t mt = (P.experts + 15) >> 4, nt = (P.tokens + 7) >> 3, tasks = mt * nt, padded = nt * 8;
+    const uint32_t rows_e = mt * 16, rows = rows_e + padded;
+    const uint32_t all = (P.hidden + 63) >> 6, lo = all * rank / kMoeCluster, hi = all * (rank + 1) / kMoeCluster;
     uint32_t split = 1;
-    while (split * 2 * tasks <= kMoeWarps && split * 2 <= parts) split *= 2;
-    for (uint32_t item = warp; item < tasks * split; item += kMoeWarps) {
-        const uint32_t task = item / split, slice = item % split;
-        const uint32_t e0 = (task / nt) * 16, tok = (task % nt) * 8 + g;
-        const bool ok_a = e0 + g < P.experts, ok_b = e0 + g + 8 < P.experts, ok_x = tok < P.tokens;
-        const uint8_t* ra = P.router + 2 * (uint64_t)(ok_a ? e0 + g : 0) * P.ld_router;
-        const uint8_t* rb = P.router + 2 * (uint64_t)(ok_b ? e0 + g + 8 : 0) * P.ld_router;
-        const uint8_t* xr = P.x + 2 * (uint64_t)(ok_x ? tok : 0) * P.ld_x;
-        double sum[4] = {0, 0, 0, 0};
-        for (uint32_t part = lo + parts * slice / split; part < lo + parts * (slice + 1) / split; ++part) {
-            uint4 a[4], b[4], x[4];
+    while (split * 2 * tasks <= kMoeWarps && split * 2 <= hi - lo) split *= 2;
+    double* items = S.logits + rows_e * padded;
+    const uint32_t staged = (smem_u32(items + (split > 1 ? kMoeWarps * 128 : 0)) + 15u) & ~15u;
+    const uint32_t room = kMoeStageSpace - (staged - smem_u32(&S));
+    // columns in pieces of 64 that fit at a time; rows of an odd multiple of 64 bytes keep the 16-byte reads of a warp apart
+    const uint32_t fit = min((room / rows - 64) / 128, max(hi - lo, 1u)), pitch = fit * 128 + 64;
+    double sum[4] = {0, 0, 0, 0};
+    if (split == 1)
+        for (uint32_t i = tid; i < rows_e * padded; i += kMoeThreads) S.logits[i] = 0;
+    for (uint32_t from = lo; from < hi; from += fit) {
+        const uint32_t now = min(fit, hi - from);
+        __syncthreads();
+        // six loads of a thread at a time: their latency is what this costs
+        for (uint32_t i0 = tid; i0 < rows * now * 8; i0 += 6 * kMoeThreads) {
+            uint4 v[6];
+            uint32_t to[6];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t col = part * 128 + j * 32 + 8 * t;
-                const bool in = col < P.hidden;
-                a[j] = in && ok_a ? ld_cached_v4(ra + 2 * col) : zero4();
-                b[j] = in && ok_b ? ld_cached_v4(rb + 2 * col) : zero4();
-                x[j] = in && ok_x ? ld_cached_v4(xr + 2 * col) : zero4();
-                if (in && col + 8 > P.hidden) {
-                    const uint32_t have = 2 * (P.hidden - col);
-                    a[j] = first_bytes(a[j], have);
-                    b[j] = first_bytes(b[j], have);
-                    x[j] = first_bytes(x[j], have);
+            for (uint32_t q = 0; q < 6; ++q) {
+                const uint32_t i = i0 + q * kMoeThreads;
+                const uint32_t row = i / (now * 8), piece = i - row * (now * 8), col = from * 64 + piece * 8;
+                const bool expert = row < rows_e;
+                const uint32_t r = expert ? row : row - rows_e;
+                to[q] = row < rows ? staged + row * pitch + piece * 16 : 0;
+                v[q] = zero4();
+                if (row < rows && col < P.hidden && r < (expert ? P.experts : P.tokens)) {
+                    v[q] = ld_cached_v4(expert ? P.router + 2 * ((uint64_t)r * P.ld_router + col) : P.x + 2 * ((uint64_t)r * P.ld_x + col));
+                    if (col + 8 > P.hidden) v[q] = first_bytes(v[q], 2 * (P.hidden - col));
                 }
             }
-            float v[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t first[4] = {a[j].x, b[j].x, a[j].y, b[j].y}, second[4] = {a[j].z, b[j].z, a[j].w, b[j].w};
-                mma16<HALF>(v, first, x[j].x, x[j].y);
-                mma16<HALF>(v, second, x[j].z, x[j].w);
+            for (uint32_t q = 0; q < 6; ++q)
+                if (to[q]) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(to[q]), "r"(v[q].x), "r"(v[q].y), "r"(v[q].z), "r"(v[q].w) : "memory");
+        }
+        __syncthreads();
+        for (uint32_t item = warp; item < tasks * split; item += kMoeWarps) {
+            const uint32_t task = item / split, slice = item - task * split, e0 = (task / nt) * 16, k0 = (task % nt) * 8;
+            const uint32_t ra = staged + (e0 + g) * pitch + 16 * t, rb = ra + 8 * pitch, rx = staged + (rows_e + k0 + g) * pitch + 16 * t;
+            double s[4] = {0, 0, 0, 0};
+            for (uint32_t u = now * slice / split; u < now * (slice + 1) / split; ++u) {
+                float v[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (uint32_t j = 0; j < 2; ++j) {
+                    const uint4 a = lds128(ra + u * 128 + j * 64), b = lds128(rb + u * 128 + j * 64), x = lds128(rx + u * 128 + j * 64);
+                    const uint32_t first[4] = {a.x, b.x, a.y, b.y}, second[4] = {a.z, b.z, a.w, b.w};
+                    mma16<HALF>(v, first, x.x, x.y);
+                    mma16<HALF>(v, second, x.z, x.w);
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) s[q] += (double)v[q];
             }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) sum[q] += (double)v[q];
-        }
-#pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-            const uint32_t e = e0 + g + 8 * (q >> 1), k = (task % nt) * 8 + 2 * t + (q & 1);
-            if (split > 1) S.items[item * 128 + q * 32 + lane] = sum[q];
-            else if (e < P.experts && k < P.tokens) S.logits[e * kMaxTokens + k] = sum[q];
+            for (uint32_t q = 0; q < 4; ++q) {
+                if (split > 1) sum[q] += s[q];               // a warp has one item at most
+                else S.logits[(k0 + 2 * t + (q & 1)) * rows_e + e0 + g + 8 * (q >> 1)] += s[q];
+            }
         }
     }
     if (split == 1) return;
+    if (warp < tasks * split) {
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) items[warp * 128 + q * 32 + lane] = sum[q];
+    }
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < tasks * 128; i += kMoeThreads) {
+    for (uint32_t i = tid; i < tasks * 128; i += kMoeThreads) {
         const uint32_t task = i >> 7, q = (i >> 5) & 3, l = i & 31;
         double s = 0;
-        for (uint32_t k = 0; k < split; ++k) s += S.items[(task * split + k) * 128 + q * 32 + l];
-        const uint32_t e = (task / nt) * 16 + (l >> 2) + 8 * (q >> 1), tok = (task % nt) * 8 + 2 * (l & 3) + (q & 1);
-        if (e < P.experts && tok < P.tokens) S.logits[e * kMaxTokens + tok] = s;
+        for (uint32_t k = 0; k < split; ++k) s += items[(task * split + k) * 128 + q * 32 + l];
+        S.logits[((task % nt) * 8 + 2 * (l & 3) + (q & 1)) * rows_e + (task / nt) * 16 + (l >> 2) + 8 * (q >> 1)] = s;
     }
 }
 
@@ -471,7 +570,7 @@ __device__ __forceinline__ void router_logits(const MoeParams& P, uint32_t rank,
 __device__ __forceinline__ void choose(const MoeParams& P, uint32_t rank, MoeRouting& S)
 {
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t base = smem_u32(S.logits);
+    const uint32_t base = smem_u32(S.logits), rows_e = (P.experts + 15) & ~15u;
     for (uint32_t i = warp; rank + i * kMoeCluster < P.tokens; i += kMoeWarps) {
         const uint32_t tok = rank + i * kMoeCluster;
         unsigned long long key[kMaxExperts / 32];
@@ -482,7 +581,7 @@ __device__ __forceinline__ void choose(const MoeParams& P, uint32_t rank, MoeRou
             if (e < P.experts) {
                 double v = 0;
 #pragma unroll
-                for (uint32_t r = 0; r < kMoeCluster; ++r) v += ld_cluster_f64(map_shared(base + 8 * (e * kMaxTokens + tok), r));
+                for (uint32_t r = 0; r < kMoeCluster; ++r) v += ld_cluster_f64(map_shared(base + 8 * (tok * rows_e + e), r));
                 key[k] = order_key(v);
             }
         }
@@ -530,7 +629,7 @@ __device__ __forceinline__ void make_lists(const MoeParams& P, MoeRouting& S, Ro
             const uint32_t c = __popcll(S.mask[tid * 8 + k]);
             tokens += c;
             active += c != 0;
-            passes += (c + kMoePass - 1) / kMoePass;
+            passes += (c + P.pass - 1) / P.pass;
         }
         uint32_t a = tokens, b = active, c = passes;
         for (uint32_t d = 1; d < 32; d <<= 1) {
@@ -546,7 +645,7 @@ __device__ __forceinline__ void make_lists(const MoeParams& P, MoeRouting& S, Ro
             R.pass[at] = (uint16_t)pass;
             ++at;
             row += cnt;
-            pass += (cnt + kMoePass - 1) / kMoePass;
+            pass += (cnt + P.pass - 1) / P.pass;
         }
         if (tid == 31) {
             R.n_active = b;
@@ -574,11 +673,11 @@ struct RowFinder {
 };
 
 // Barriers and tensor memory; all threads.
-__device__ __forceinline__ void moe_setup(MoeShared& S)
+__device__ __forceinline__ void moe_setup(MoeShared& S, uint32_t sharing)
 {
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (warp == 0 && lane == 0) {
-        for (uint32_t i = 0; i < kMoeStages; ++i) { bar_init(smem_u32(&S.full[i]), 3); bar_init(smem_u32(&S.empty[i]), 1); }
+        for (uint32_t i = 0; i < kMoeMaxStages; ++i) { bar_init(smem_u32(&S.full[i]), 2 + sharing); bar_init(smem_u32(&S.empty[i]), 1); }
         for (uint32_t i = 0; i < 2; ++i) { bar_init(smem_u32(&S.acc_full[i]), 1); bar_init(smem_u32(&S.acc_empty[i]), 4); }
         S.failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -671,14 +770,14 @@ moe_up_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ MoeP
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     uint8_t* aligned = raw + (base - smem_u32(raw));
-    MoeShared& S = *reinterpret_cast<MoeShared*>(aligned + kMoeStages * kMoeStageBytes);
+    MoeShared& S = *reinterpret_cast<MoeShared*>(aligned + kMoeStageSpace);
     MoeRouting& T = *reinterpret_cast<MoeRouting*>(aligned);
     const uint32_t tid = threadIdx.x, rank = cluster_rank();
     const uint32_t n_rows = P.tokens * P.top_k;
 
     grid_launch_dependents();
     if (tid < kMoeHeights) prefetch_map(&maps.of[tid]);
-    moe_setup(S);
+    moe_setup(S, kBuilders / stage_count(P.pass, 3));
     router_logits<HALF>(P, rank, T);
     cluster_sync();
     choose(P, rank, T);
@@ -714,7 +813,7 @@ moe_up_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ MoeP
     }
     fence_async_shared();                        // the routing's shared memory becomes the stages'
     cluster_sync();                              // and no other block reads from it any more
-    stream_weights<true, HALF, 3>(P, maps, S, base, gridDim.x, FinishUp{P, S});
+    stream_weights<true, HALF, 3>(P, maps, S, cut_rows<true>(P.inter, S.R.n_passes, gridDim.x), base, gridDim.x, FinishUp{P, S});
     __syncthreads();
     if (tid < 64 && tid >= 32) tmem_free<1>(S.tmem, kMoeTmemCols);
 }
@@ -725,22 +824,23 @@ moe_down_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ Mo
 {
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    MoeShared& S = *reinterpret_cast<MoeShared*>(raw + (base - smem_u32(raw)) + kMoeStages * kMoeStageBytes);
+    MoeShared& S = *reinterpret_cast<MoeShared*>(raw + (base - smem_u32(raw)) + kMoeStageSpace);
     const uint32_t tid = threadIdx.x;
     if (tid < kMoeHeights) prefetch_map(&maps.of[tid]);
-    moe_setup(S);
+    moe_setup(S, kBuilders / stage_count(P.pass, kHiddenPieces<HALF>));
     grid_wait();
+    // all of the lists at once, whatever is behind the last chosen expert: one latency
     const uint32_t n_active = P.route[0], n_passes = P.route[1];
-    for (uint32_t i = tid; i <= n_active; i += kMoeThreads) {
-        if (i < n_active) S.R.expert[i] = (uint16_t)P.route[2 + i];
-        const uint32_t v = P.route[2 + kMaxExperts + i];
-        S.R.first[i] = (uint16_t)v;
-        S.R.pass[i] = (uint16_t)(v >> 16);
+    if (tid <= kMaxExperts) {
+        const uint32_t v = P.route[2 + kMaxExperts + tid];
+        if (tid < kMaxExperts) S.R.expert[tid] = (uint16_t)P.route[2 + tid];
+        S.R.first[tid] = (uint16_t)v;
+        S.R.pass[tid] = (uint16_t)(v >> 16);
     }
     for (uint32_t i = tid; i < P.tokens * P.top_k; i += kMoeThreads) S.row_of[i] = (uint16_t)P.row_of[i];
     if (tid == 0) { S.R.n_active = n_active; S.R.n_passes = n_passes; }
     __syncthreads();
-    stream_weights<false, HALF, kHiddenPieces<HALF>>(P, maps, S, base, gridDim.x, FinishDown<HALF>{P, S, n_passes});
+    stream_weights<false, HALF, kHiddenPieces<HALF>>(P, maps, S, cut_rows<false>(P.hidden, n_passes, gridDim.x), base, gridDim.x, FinishDown<HALF>{P, S, n_passes});
     __syncthreads();
     if (tid < 64 && tid >= 32) tmem_free<1>(S.tmem, kMoeTmemCols);
 }
@@ -855,6 +955,9 @@ zc_status zc_fp8_moe(const zc_fp8_moe_layer* layer, uint32_t n_tokens, const voi
     P.gate_up_scales = (const uint8_t*)layer->d_gate_up_scales;
     P.down_scales = (const uint8_t*)layer->d_down_scales;
     P.idesc = instruction_of(layer->format, ZC_FMT_FP8_E4M3, 128, 0);
+    // Tokens per reading of a tile: the stages that hold their pieces get larger and fewer with them (9 of 8 tokens, 8 of 16, 6 or 7 of 32), an expert
+    // that more tokens chose is read again, from the L2.  Above 9 tokens an expert on average many have more than 16.
+    P.pass = n_tokens <= 8 ? 8 : n_tokens <= 16 || n_tokens * layer->top_k <= 9 * layer->n_experts ? 16 : 32;
     P.spin_limit = test_knobs().spin_limit;
     P.skip_copy = test_knobs().skip_copy;
     P.tokens = n_tokens;

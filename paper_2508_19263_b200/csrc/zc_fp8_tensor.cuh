@@ -14,16 +14,18 @@ static __device__ unsigned int g_fp8_timeout;    // a wait of a kernel of this f
 struct Waiter {
     uint32_t limit;
     volatile uint32_t* failed;
+    template <bool CLUSTER = false>
     __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const
     {
         for (uint32_t i = 0; i <= limit; ++i) {
-            if (bar_try(bar, parity)) return true;
+            if (CLUSTER ? bar_try_cluster(bar, parity) : bar_try(bar, parity)) return true;
             if (*failed) return false;
         }
         *failed = 1;
         atomicExch(&g_fp8_timeout, 1u);
         return false;
     }
+    __device__ __forceinline__ bool across(uint32_t bar, uint32_t parity) const { return operator()<true>(bar, parity); }
 };
 
 // The scale bytes of steps first .. first + 3 of one row as a word; 127 (a factor of 1) where there is none.

@@ -90,12 +90,12 @@ class Layer:
             w = p[tok, slot][:, None]
             h = w * silu * up
             # |silu'| <= 1.1; a few roundings in FP32; three (FP16: four) pieces of E4M3 leave 2^-4 of the value each, or half of
-            # the last one's smallest step; the router's parts of 128 columns are FP32 sums, so a logit is off by 128 units of
+            # the last one's smallest step, and what the first leaves is held in FP16, 2^-12 of 2^-4; the router's parts of 128 columns are FP32 sums, so a logit is off by 128 units of
             # its part and p by twice that relative
             pieces = 4 if self.layer.dtype == torch.float16 else 3
             d_logit = 128 * unit * (np.abs(x[tok]) @ np.abs(self.router[e].double().cpu().numpy())).max()
             d_h = w * (1.1 * d_gate * np.abs(up) + np.abs(silu) * d_up + 1.1 * d_gate * d_up) + np.abs(h) * (16 * unit + 2 * d_logit)
-            d_h = d_h + 2.0 ** (-4 * pieces) * (np.abs(h) + d_h) + 2.0 ** (-13 - 4 * pieces) * largest_of_128(np.abs(h) + d_h)
+            d_h = d_h + (2.0 ** (-4 * pieces) + 2.0 ** -16) * (np.abs(h) + d_h) + 2.0 ** (-13 - 4 * pieces) * largest_of_128(np.abs(h) + d_h)
             y[tok] += h @ m[2].T
             bound[tok] += d_h @ np.abs(m[2]).T + (inter + 16 + self.top_k) * unit * ((np.abs(h) + d_h) @ np.abs(m[2]).T)
         return y, ids, p, bound
