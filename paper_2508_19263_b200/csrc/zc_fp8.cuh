@@ -87,6 +87,18 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr)
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// ---- warps ----
+// One lane of a converged warp.  Copies, matrix instructions and commits take their operands from uniform registers: in a loop
+// that the whole warp goes through, with the one lane chosen at each of them, the operands are there; in a loop that only lane 0
+// goes through each of them is moved there first (0.56 us a step of the large matrix product instead of 0.37).
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is != 0;
+}
+__device__ __forceinline__ uint32_t warp_index() { return __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0); }
+
 // ---- clusters ----
 __device__ __forceinline__ uint32_t cluster_rank()
 {

@@ -100,7 +100,7 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t words_at = base + kSmallStages * 2 * kTileBytes;
     MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (words_at - smem_u32(raw)) + kScaleBufs * kScaleBufBytes);
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t warp = warp_index(), lane = threadIdx.x & 31;
     const uint32_t parts = gridDim.z, part = blockIdx.z;
     const uint32_t m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
     const uint32_t lo = (uint32_t)((uint64_t)P.steps * part / parts), hi = (uint32_t)((uint64_t)P.steps * (part + 1) / parts);
@@ -122,38 +122,46 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     const uint32_t tmem = S->tmem;
 
     uint32_t issued = 0;
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         for (uint32_t i = lo; i < hi; ++i, ++issued) {
             const uint32_t st = issued % kSmallStages;
-            if (issued >= kSmallStages && !wait(smem_u32(&S->empty[st]), (issued / kSmallStages - 1) & 1)) break;
+            if (issued >= kSmallStages && !wait.warp(smem_u32(&S->empty[st]), (issued / kSmallStages - 1) & 1)) break;
             const uint32_t bar = smem_u32(&S->full[st]);
-            bar_expect(bar, 2 * kTileBytes);
-            if (P.skip_copy) continue;
-            tensor_copy<1>(base + st * 2 * kTileBytes, &map_a, (int)(i * kStepBytes), (int)m0, bar);
-            tensor_copy<1>(base + st * 2 * kTileBytes + kTileBytes, &map_b, (int)(i * kStepBytes), (int)n0, bar);
+            if (elect_one()) {
+                bar_expect(bar, 2 * kTileBytes);
+                if (!P.skip_copy) {
+                    tensor_copy<1>(base + st * 2 * kTileBytes, &map_a, (int)(i * kStepBytes), (int)m0, bar);
+                    tensor_copy<1>(base + st * 2 * kTileBytes + kTileBytes, &map_b, (int)(i * kStepBytes), (int)n0, bar);
+                }
+            }
         }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         for (uint32_t i = 0; i < hi - lo; ++i) {
             const uint32_t st = i % kSmallStages, word = i >> 2, buf = word % kScaleBufs;
             const uint32_t sfa = tmem + kSmallScales + (word & 1) * 8, sfb = sfa + 4;
-            if (!wait(smem_u32(&S->full[st]), (i / kSmallStages) & 1)) break;
-            if ((i & 3) == 0) {
-                if (!wait(smem_u32(&S->sf_full[buf]), (word / kScaleBufs) & 1)) break;
+            const bool fresh = (i & 3) == 0;
+            if (!wait.warp(smem_u32(&S->full[st]), (i / kSmallStages) & 1)) break;
+            if (fresh) {
+                if (!wait.warp(smem_u32(&S->sf_full[buf]), (word / kScaleBufs) & 1)) break;
                 // the set's words of eight steps ago are not looked up any more
-                if (word >= 2 && !wait(smem_u32(&S->sf_empty[(word - 2) % kScaleBufs]), ((word - 2) / kScaleBufs) & 1)) break;
-                tc_fence_after();
-                tmem_copy_scales<1>(sfa, words_at + buf * kScaleBufBytes);
-                tmem_copy_scales<1>(sfb, words_at + buf * kScaleBufBytes + 512);
+                if (word >= 2 && !wait.warp(smem_u32(&S->sf_empty[(word - 2) % kScaleBufs]), ((word - 2) / kScaleBufs) & 1)) break;
             }
             tc_fence_after();
             const uint64_t da = operand_desc(base + st * 2 * kTileBytes), db = operand_desc(base + st * 2 * kTileBytes + kTileBytes);
             const uint32_t idesc = P.idesc | ((i & 3) << 29) | ((i & 3) << 4);
+            if (elect_one()) {
+                if (fresh) {
+                    tmem_copy_scales<1>(sfa, words_at + buf * kScaleBufBytes);
+                    tmem_copy_scales<1>(sfb, words_at + buf * kScaleBufBytes + 512);
+                }
 #pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) mma_scaled<1>(tmem, da + 2 * j, db + 2 * j, idesc, sfa, sfb, i | j);
-            mma_commit<1>(smem_u32(&S->empty[st]));
-            if ((i & 3) == 3) mma_commit<1>(smem_u32(&S->sf_empty[buf]));
+                for (uint32_t j = 0; j < 4; ++j) mma_scaled<1>(tmem, da + 2 * j, db + 2 * j, idesc, sfa, sfb, i | j);
+                mma_commit<1>(smem_u32(&S->empty[st]));
+                if ((i & 3) == 3) mma_commit<1>(smem_u32(&S->sf_empty[buf]));
+            }
+            __syncwarp();
         }
-        mma_commit<1>(smem_u32(&S->acc_full[0]));
+        if (elect_one()) mma_commit<1>(smem_u32(&S->acc_full[0]));
     } else if (warp >= 8) {
         const uint32_t buf = warp - 8, at = words_at + buf * kScaleBufBytes + lane * 16;
         for (uint32_t i = lo + 4 * buf, k = 0; i < hi; i += 4 * kScaleBufs, ++k) {
@@ -243,7 +251,7 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t words_at = base + kLargeStages * 2 * kTileBytes;
     MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (words_at - smem_u32(raw)) + kScaleBufs * kScaleBufBytes);
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t warp = warp_index(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = P.tiles_m * P.tiles_n;
     const Waiter wait{P.spin_limit, &S->failed};
 
@@ -264,7 +272,7 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = S->tmem;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         // both blocks copy their halves; the bytes count on the first block's barrier
         uint32_t st = 0, round = 0;
         bool ok = true;
@@ -273,53 +281,61 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             large_tile(P, i, tm, tn);
             const int row_a = (int)(tm * 256 + rank * 128), row_b = (int)(tn * 256 + rank * 128);
             for (uint32_t k = 0; k < P.steps; ++k) {
-                if (!(ok = round == 0 || wait(smem_u32(&S->empty[st]), (round - 1) & 1))) break;
-                if (rank == 0) bar_expect(smem_u32(&S->full[st]), 4 * kTileBytes);
+                if (!(ok = round == 0 || wait.warp(smem_u32(&S->empty[st]), (round - 1) & 1))) break;
                 const uint32_t bar = map_shared(smem_u32(&S->full[st]), 0), to = base + st * 2 * kTileBytes;
-                if (!P.skip_copy) {
-                    tensor_copy<2>(to, &map_a, (int)(k * kStepBytes), row_a, bar);
-                    tensor_copy<2>(to + kTileBytes, &map_b, (int)(k * kStepBytes), row_b, bar);
+                if (elect_one()) {
+                    if (rank == 0) bar_expect(smem_u32(&S->full[st]), 4 * kTileBytes);
+                    if (!P.skip_copy) {
+                        tensor_copy<2>(to, &map_a, (int)(k * kStepBytes), row_a, bar);
+                        tensor_copy<2>(to + kTileBytes, &map_b, (int)(k * kStepBytes), row_b, bar);
+                    }
                 }
                 if (++st == kLargeStages) { st = 0; ++round; }
             }
         }
         // after a wait that gave up, copies may still be on their way into the pair's shared memory
-        if (!ok && !P.skip_copy && rank == 0)
+        if (!ok && !P.skip_copy && rank == 0 && lane == 0)
             for (uint32_t i = 0; i < kLargeStages; ++i) {
                 const uint32_t r = i < st ? round : round - 1;
                 if (round == 0 && i >= st) continue;
                 for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S->full[i]), r & 1); ++q) { }
             }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
         uint32_t st = 0, round = 0, word = 0, tile = 0;
         bool ok = true;
         for (uint32_t i = pair; i < tiles && ok; i += pairs, ++tile) {
             const uint32_t d = tmem + (tile & 1 ? kLargeSecond : 0);
             // the columns that this tile's accumulator shares with the one before it are empty, and with them all of the one before that
-            if (tile && !(ok = wait.across(smem_u32(&S->acc_empty[0]), (tile - 1) & 1))) break;
+            if (tile && !(ok = wait.warp_across(smem_u32(&S->acc_empty[0]), (tile - 1) & 1))) break;
             for (uint32_t k = 0; k < P.steps; ++k) {
                 const uint32_t buf = word % kScaleBufs, sfa = tmem + kLargeScales + (word & 1) * 12, sfb = sfa + 4;
-                if (!(ok = wait(smem_u32(&S->full[st]), round & 1))) break;
-                if ((k & 3) == 0) {
-                    if (!(ok = wait.across(smem_u32(&S->sf_full[buf]), (word / kScaleBufs) & 1))) break;
+                const bool fresh = (k & 3) == 0, last = (k & 3) == 3 || k + 1 == P.steps;
+                if (!(ok = wait.warp(smem_u32(&S->full[st]), round & 1))) break;
+                if (fresh) {
+                    if (!(ok = wait.warp_across(smem_u32(&S->sf_full[buf]), (word / kScaleBufs) & 1))) break;
                     // the set's words of two before are not looked up any more
-                    if (word >= 2 && !(ok = wait(smem_u32(&S->sf_empty[(word - 2) % kScaleBufs]), ((word - 2) / kScaleBufs) & 1))) break;
-                    tc_fence_after();
-                    const uint32_t from = words_at + buf * kScaleBufBytes;
-                    tmem_copy_scales<2>(sfa, from);
-                    tmem_copy_scales<2>(sfb, from + 512);
-                    tmem_copy_scales<2>(sfb + 4, from + 1024);
+                    if (word >= 2 && !(ok = wait.warp(smem_u32(&S->sf_empty[(word - 2) % kScaleBufs]), ((word - 2) / kScaleBufs) & 1))) break;
                 }
                 tc_fence_after();
                 const uint64_t da = operand_desc(base + st * 2 * kTileBytes), db = operand_desc(base + st * 2 * kTileBytes + kTileBytes);
-                const uint32_t idesc = P.idesc | ((k & 3) << 29) | ((k & 3) << 4);
+                const uint32_t idesc = P.idesc | ((k & 3) << 29) | ((k & 3) << 4), from = words_at + buf * kScaleBufBytes;
+                if (elect_one()) {
+                    if (fresh) {
+                        tmem_copy_scales<2>(sfa, from);
+                        tmem_copy_scales<2>(sfb, from + 512);
+                        tmem_copy_scales<2>(sfb + 4, from + 1024);
+                    }
 #pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) mma_scaled<2>(d, da + 2 * j, db + 2 * j, idesc, sfa, sfb, k | j);
-                mma_commit<2>(smem_u32(&S->empty[st]));
-                if ((k & 3) == 3 || k + 1 == P.steps) { mma_commit<2>(smem_u32(&S->sf_empty[buf])); ++word; }
+                    for (uint32_t j = 0; j < 4; ++j) mma_scaled<2>(d, da + 2 * j, db + 2 * j, idesc, sfa, sfb, k | j);
+                    mma_commit<2>(smem_u32(&S->empty[st]));
+                    if (last) mma_commit<2>(smem_u32(&S->sf_empty[buf]));
+                }
+                __syncwarp();
+                word += last;
                 if (++st == kLargeStages) { st = 0; ++round; }
             }
-            mma_commit<2>(smem_u32(&S->acc_full[tile & 1]));
+            if (elect_one()) mma_commit<2>(smem_u32(&S->acc_full[tile & 1]));
+            __syncwarp();
         }
     } else if (warp >= 8) {
         // this block's 128 rows of A and the pair's 256 of B
@@ -366,6 +382,7 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             }
         }
     }
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     cluster_sync();                              // nothing of either block arrives at, or is copied into, the other any more

@@ -255,7 +255,7 @@ __device__ __forceinline__ void make_pieces(float v[4], uint32_t words[PIECES], 
 template <bool UP, bool HALF, int PIECES, typename Finish>
 __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps& maps, MoeShared& S, const Cut& cut, uint32_t base, uint32_t blocks, Finish finish)
 {
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t warp = warp_index(), lane = threadIdx.x & 31;
     const uint32_t cols = UP ? P.hidden : P.inter, rows = UP ? P.inter : P.hidden;
     const uint32_t steps = (cols + 127) >> 7;
     const Waiter wait{P.spin_limit, &S.failed};
@@ -269,58 +269,59 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
     auto free_stage = [&] { return round == 0 || wait(smem_u32(&S.empty[st]), (round - 1) & 1); };
 
     if (warp == 0) {
-        if (lane == 0) {
-            bool ok = true;
-            while (ok && tiles.next(t)) {
-                const uint32_t row0 = t.expert * (UP ? 2 * P.inter : P.hidden) + t.group * 8;
-                for (uint32_t k = 0; k < steps; ++k, forward()) {
-                    if (!(ok = free_stage())) break;
-                    const uint32_t bar = smem_u32(&S.full[st]), to = base + st * stage_bytes;
+        bool ok = true;
+        while (ok && tiles.next(t)) {
+            const uint32_t row0 = t.expert * (UP ? 2 * P.inter : P.hidden) + t.group * 8;
+            for (uint32_t k = 0; k < steps; ++k, forward()) {
+                if (!(ok = round == 0 || wait.warp(smem_u32(&S.empty[st]), (round - 1) & 1))) break;
+                const uint32_t bar = smem_u32(&S.full[st]), to = base + st * stage_bytes;
+                if (elect_one()) {
                     bar_expect(bar, t.groups * (UP ? 2048 : 1024));
-                    if (P.skip_copy) continue;
                     // as few copies as there are bits in the number of groups: one of 8 rows takes the copy engine as long as one of 64
                     uint32_t i = 0;
 #pragma unroll
                     for (int b = UP ? 3 : 4; b >= 0; --b) {
-                        if (!(t.groups >> b & 1)) continue;
+                        if (!(t.groups >> b & 1) || P.skip_copy) continue;
                         tensor_copy<1>(to + i * 1024, &maps.of[b], (int)(k * 128), (int)(row0 + 8 * i), bar);
                         if (UP) tensor_copy<1>(to + 8192 + i * 1024, &maps.of[b], (int)(k * 128), (int)(row0 + P.inter + 8 * i), bar);
                         i += 1u << b;
                     }
                 }
+                __syncwarp();
             }
-            // after a wait that gave up, copies may still be on their way into this block's shared memory: of this round up to
-            // the present stage, of the one before from there on
-            if (!ok && !P.skip_copy)
-                for (uint32_t i = 0; i < stages; ++i) {
-                    const uint32_t r = i < st ? round : round - 1;
-                    if (round == 0 && i >= st) continue;
-                    for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S.full[i]), r & 1); ++q) { }
-                }
         }
+        // after a wait that gave up, copies may still be on their way into this block's shared memory: of this round up to
+        // the present stage, of the one before from there on
+        if (!ok && !P.skip_copy && lane == 0)
+            for (uint32_t i = 0; i < stages; ++i) {
+                const uint32_t r = i < st ? round : round - 1;
+                if (round == 0 && i >= st) continue;
+                for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S.full[i]), r & 1); ++q) { }
+            }
     } else if (warp == 1) {
-        if (lane == 0) {
-            uint32_t tile = 0;
-            bool ok = true;
-            while (ok && tiles.next(t)) {
-                const uint32_t buf = tile & 1, d = tmem + buf * 128;
-                const uint32_t idesc = P.idesc | ((piece_rows(t.count, PIECES) >> 3) << 17);
-                if (tile >= 2 && !(ok = wait(smem_u32(&S.acc_empty[buf]), ((tile >> 1) - 1) & 1))) break;
+        uint32_t tile = 0;
+        bool ok = true;
+        while (ok && tiles.next(t)) {
+            const uint32_t buf = tile & 1, d = tmem + buf * 128;
+            const uint32_t idesc = P.idesc | ((piece_rows(t.count, PIECES) >> 3) << 17);
+            if (tile >= 2 && !(ok = wait.warp(smem_u32(&S.acc_empty[buf]), ((tile >> 1) - 1) & 1))) break;
+            for (uint32_t k = 0; k < steps; ++k, forward()) {
+                if (!(ok = wait.warp(smem_u32(&S.full[st]), round & 1))) break;
                 tc_fence_after();
-                for (uint32_t k = 0; k < steps; ++k, forward()) {
-                    if (!(ok = wait(smem_u32(&S.full[st]), round & 1))) break;
-                    tc_fence_after();
-                    const uint32_t at = base + st * stage_bytes, sf = tmem + kMoeTmemScales + st * 8;
+                const uint32_t at = base + st * stage_bytes, sf = tmem + kMoeTmemScales + st * 8;
+                const uint64_t da = operand_desc(at), db = operand_desc(at + 16384);
+                if (elect_one()) {
                     tmem_copy_scales<1>(sf, at + scales_at);
                     tmem_copy_scales<1>(sf + 4, at + scales_at + 512);
-                    const uint64_t da = operand_desc(at), db = operand_desc(at + 16384);
 #pragma unroll
                     for (uint32_t j = 0; j < 4; ++j) mma_scaled<1>(d, da + 2 * j, db + 2 * j, idesc, sf, sf + 4, k | j);
                     mma_commit<1>(smem_u32(&S.empty[st]));
                 }
-                mma_commit<1>(smem_u32(&S.acc_full[buf]));
-                ++tile;
+                __syncwarp();
             }
+            if (elect_one()) mma_commit<1>(smem_u32(&S.acc_full[buf]));
+            __syncwarp();
+            ++tile;
         }
     } else if (warp == 2) {
         // scale bytes of the weights, four steps at a time and four steps ahead; row r of the tile's operand is row 32 j + lane

@@ -25,7 +25,9 @@ struct Waiter {
         atomicExch(&g_fp8_timeout, 1u);
         return false;
     }
-    __device__ __forceinline__ bool across(uint32_t bar, uint32_t parity) const { return operator()<true>(bar, parity); }
+    // the same for all lanes of a converged warp at once
+    __device__ __forceinline__ bool warp(uint32_t bar, uint32_t parity) const { return __all_sync(0xFFFFFFFFu, operator()(bar, parity)); }
+    __device__ __forceinline__ bool warp_across(uint32_t bar, uint32_t parity) const { return __all_sync(0xFFFFFFFFu, operator()<true>(bar, parity)); }
 };
 
 // The scale bytes of steps first .. first + 3 of one row as a word; 127 (a factor of 1) where there is none.
