@@ -172,6 +172,15 @@ __device__ __forceinline__ void tensor_copy(uint32_t dst, const void* map, int x
         asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
                      :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+// the way back; one thread's copies are committed as a group
+__device__ __forceinline__ void tensor_store(const void* map, int x, int y, uint32_t src)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];\n\tcp.async.bulk.commit_group;"
+                 :: "l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+}
+// at most N of the thread's groups have not been read out of shared memory yet
+template <int N>
+__device__ __forceinline__ void tensor_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" :: "n"(N) : "memory"); }
 __device__ __forceinline__ void prefetch_map(const void* map)
 {
     asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");

@@ -27,6 +27,7 @@ struct MatmulParams {
     uint32_t idesc;                              // instruction descriptor without the scale selectors
     uint32_t out_type, accumulate, out_wide;     // out_wide: every row of D begins on a 16-byte boundary
     uint32_t tiles_m, tiles_n;
+    uint32_t by_copy;                            // the large kernel's results leave by tensor copies
     uint32_t spin_limit, skip_copy;
 };
 
@@ -232,9 +233,31 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 // words do not fit into 512 columns of tensor memory side by side, so the two overlap by 32 columns: the result warps empty these
 // first, and the next tile's instructions begin when they have, while the other 224 columns are still on their way out.
 constexpr uint32_t kLargeStages = 6;
-constexpr size_t kLargeSmem = 1024 + kLargeStages * 2 * kTileBytes + kScaleBufs * kScaleBufBytes + sizeof(MatmulShared);
+constexpr uint32_t kResultBytes = 32 * 64;       // what a warp sends off at a time: 32 rows x 64 bytes
+constexpr size_t kLargeSmem = 1024 + kLargeStages * 2 * kTileBytes + 8 * kResultBytes + kScaleBufs * kScaleBufBytes + sizeof(MatmulShared);
 constexpr uint32_t kLargeCols = 512, kLargeSecond = 224, kLargeScales = 480;     // two sets of 4 + 8 scale columns
 constexpr uint32_t kSwath = 8;                   // rows of tiles that are walked through together, column by column
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack_pair(const uint32_t v[2])
+{
+    union { T t[2]; uint32_t w; } x;
+    x.t[0] = from_float<T>(__uint_as_float(v[0]));
+    x.t[1] = from_float<T>(__uint_as_float(v[1]));
+    return x.w;
+}
+// A warp's 32 rows of 64 bytes, a row per lane, into one of its two buffers and off; the copy before the last one has been
+// read by then.
+__device__ __forceinline__ void send(const CUtensorMap& map, uint32_t buffer, uint32_t lane, int x, int y, const uint32_t w[16])
+{
+    if (lane == 0) tensor_store_wait_read<1>();
+    __syncwarp();
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) sts128(buffer + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4), w + 4 * j);
+    fence_async_shared();
+    __syncwarp();
+    if (lane == 0) tensor_store(&map, x, y, buffer);
+}
 
 __device__ __forceinline__ void large_tile(const MatmulParams& P, uint32_t i, uint32_t& m, uint32_t& n)
 {
@@ -245,11 +268,12 @@ __device__ __forceinline__ void large_tile(const MatmulParams& P, uint32_t i, ui
 }
 
 __global__ void __launch_bounds__(kMmThreads, 1)
-matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MatmulParams P)
+matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_d,
+                    const __grid_constant__ MatmulParams P)
 {
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    const uint32_t words_at = base + kLargeStages * 2 * kTileBytes;
+    const uint32_t results_at = base + kLargeStages * 2 * kTileBytes, words_at = results_at + 8 * kResultBytes;
     MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (words_at - smem_u32(raw)) + kScaleBufs * kScaleBufBytes);
     const uint32_t warp = warp_index(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = P.tiles_m * P.tiles_n;
@@ -360,14 +384,14 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         }
     } else if (warp >= 4) {
         const uint32_t quad = warp & 3;
-        uint32_t tile = 0;
+        uint32_t tile = 0, sent = 0;
         for (uint32_t i = pair; i < tiles; i += pairs, ++tile) {
             uint32_t tm, tn;
             large_tile(P, i, tm, tn);
             if (!__all_sync(0xFFFFFFFFu, wait(smem_u32(&S->acc_full[tile & 1]), (tile >> 1) & 1) && !*wait.failed)) break;
             tc_fence_after();
             const uint32_t row = tm * 256 + rank * 128 + quad * 32 + lane;
-            const uint32_t d = tmem + (quad * 32u << 16) + (tile & 1 ? kLargeSecond : 0);
+            const uint32_t d = tmem + (quad * 32u << 16) + (tile & 1 ? kLargeSecond : 0), results = results_at + quad * 2 * kResultBytes;
 #pragma unroll 1
             for (uint32_t q = 0; q < 8; ++q) {
                 const uint32_t c = tile & 1 ? q : (q + 7) & 7;           // the shared columns first
@@ -378,9 +402,25 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                     __syncwarp();
                     if (lane == 0) bar_arrive_cluster(map_shared(smem_u32(&S->acc_empty[0]), 0));
                 }
-                store_row<32>(P, row, tn * 256 + c * 32, reinterpret_cast<const float*>(v));
+                if (P.by_copy) {
+                    // rows of 64 bytes through shared memory: stores of 16 bytes to 32 rows at a time cost a tenth of the whole product
+                    const uint32_t row0 = tm * 256 + rank * 128 + quad * 32, col0 = tn * 256 + c * 32;
+                    if (row0 >= P.m || col0 >= P.n) continue;
+                    if (P.out_type == ZC_REAL_F32) {
+                        send(map_d, results + (sent++ & 1) * kResultBytes, lane, (int)col0, (int)row0, v);
+                        if (col0 + 16 < P.n) send(map_d, results + (sent++ & 1) * kResultBytes, lane, (int)col0 + 16, (int)row0, v + 16);
+                    } else {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) w[j] = P.out_type == ZC_REAL_BF16 ? pack_pair<__nv_bfloat16>(v + 2 * j) : pack_pair<__half>(v + 2 * j);
+                        send(map_d, results + (sent++ & 1) * kResultBytes, lane, (int)col0, (int)row0, w);
+                    }
+                } else {
+                    store_row<32>(P, row, tn * 256 + c * 32, reinterpret_cast<const float*>(v));
+                }
             }
         }
+        if (lane == 0) tensor_store_wait_read<0>();
     }
     __syncwarp();
     tc_fence_before();
@@ -471,6 +511,11 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
         P.tiles_n = (uint32_t)ceil_div(P.n, 256);
         if (large >= (1ull << 31)) return ZC_E_TOO_LARGE;
         P.idesc = instruction_of(a->format, b->format, 256, 256);
+        // a copy that runs over the last column is cut off at the next 16 bytes, not at the column: what lies behind it in the
+        // row would be overwritten
+        P.by_copy = P.out_wide && !P.accumulate && (uint64_t)P.n * width % 16 == 0;
+        CUtensorMap map_d = map_a;
+        if (P.by_copy && !make_result_map(&map_d, d_out, out_type, P.m, P.n, P.ld_out)) return ZC_E_CUDA;
         const uint32_t grid = (uint32_t)std::min<uint64_t>(blocks, 2 * large);
         cudaLaunchConfig_t cfg{};
         cfg.gridDim = dim3(grid);
@@ -482,7 +527,7 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
         at[0].val.clusterDim = {2, 1, 1};
         cfg.attrs = at;
         cfg.numAttrs = 1;
-        return cudaLaunchKernelEx(&cfg, matmul_large_kernel, map_a, map_b, P) == cudaSuccess ? ZC_OK : ZC_E_CUDA;
+        return cudaLaunchKernelEx(&cfg, matmul_large_kernel, map_a, map_b, map_d, P) == cudaSuccess ? ZC_OK : ZC_E_CUDA;
     }
     P.idesc = instruction_of(a->format, b->format, 128, 128);
     uint32_t parts = 1;

@@ -94,6 +94,16 @@ static bool make_map(CUtensorMap* map, const void* elems, uint64_t rows, uint64_
                                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// A matrix of results as pieces of 32 rows x 64 bytes in the 64-byte swizzle.
+static bool make_result_map(CUtensorMap* map, void* out, uint32_t type, uint64_t rows, uint64_t cols, uint64_t ld_bytes)
+{
+    const cuuint64_t dims[2] = {cols, rows}, pitch[1] = {ld_bytes};
+    const cuuint32_t box[2] = {64 / real_bytes(type), 32}, step[2] = {1, 1};
+    const CUtensorMapDataType t = type == ZC_REAL_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type == ZC_REAL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return encode_fn() && encode_fn()(map, t, 2, out, dims, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+                                      CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Descriptor of the scaled FP8 instruction without its scale selectors.
 static uint32_t instruction_of(uint32_t format_a, uint32_t format_b, uint32_t m, uint32_t n)
 {
