@@ -521,21 +521,32 @@ def batch_status(d_workspace: torch.Tensor, stream=None):
 
 def _real_matrix(t: torch.Tensor, what: str):
     """(type code, address, row pitch in elements) of a 2-D tensor of real numbers with contiguous rows."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(t.shape)}, strides {t.stride()}")
     real = _REAL.get(t.dtype)
     if real is None:
         raise TypeError(f"{what}: float32, bfloat16 or float16 is wanted, got {t.dtype}")
-    rows, cols = t.shape
-    return real, t.data_ptr(), (t.stride(0) if rows > 1 else max(t.stride(0), cols))
+    stride, shape = t.stride(), t.shape
+    if len(stride) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(shape)}, strides {stride}")
+    return real, t.data_ptr(), (stride[0] if shape[0] > 1 else max(stride[0], shape[1]))
 
 
-def _on_current_device(*tensors):
-    """The library launches on the current device: tensors of another one are refused instead of read from there."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _same_device(*indices) -> int:
+    """The library launches on the current device: tensors of another one (or of the host, -1) are refused instead of read from
+    there.  Returns the device's index."""
+    if -1 in indices:
+        raise ValueError("a tensor is in host memory")
+    dev = _current_device()
+    for i in indices:
+        if i != dev:
+            raise ValueError(f"a tensor is on cuda:{i}, the current device is cuda:{dev}")
+    return dev
+
+
+def _stream_of(stream, dev: int, _raw=getattr(torch._C, "_cuda_getCurrentRawStream", None)) -> int:
+    return _raw(dev) if stream is None and _raw is not None else _stream_ptr(stream)
 
 
 class Fp8Matrix:
@@ -555,10 +566,10 @@ class Fp8Matrix:
         self.desc = Fp8MatrixDesc(elems.data_ptr(), scales.data_ptr(), rows, cols, -(-pitch(elems) // 16) * 16 if rows <= 1 else pitch(elems),
                                   pitch(scales), fmt, block_rows)
         self._ref = C.addressof(self.desc)
-
-    @property
-    def shape(self):
-        return tuple(self.elems.shape)
+        self.shape = (rows, cols)
+        if elems.get_device() != scales.get_device():
+            raise ValueError(f"elems are on {elems.device}, scales on {scales.device}")
+        self._dev = elems.get_device()           # -1: host memory
 
 
 def fp8_empty(rows: int, cols: int, fmt: int = FMT_FP8_E4M3, block_rows: int = 1, device="cuda") -> Fp8Matrix:
@@ -571,24 +582,28 @@ def fp8_empty(rows: int, cols: int, fmt: int = FMT_FP8_E4M3, block_rows: int = 1
 def fp8_quantize(d_in: torch.Tensor, q: Optional[Fp8Matrix], qt: Optional[Fp8Matrix] = None, stream=None) -> Optional[Fp8Matrix]:
     """zc_fp8_quantize: the matrix d_in into q and / or its transposed form into qt (asynchronous)."""
     real, ptr, ld = _real_matrix(d_in, "d_in")
-    for m, shape in ((q, d_in.shape), (qt, d_in.shape[::-1])):
-        if m is not None:
-            if m.shape != tuple(shape):
-                raise ValueError(f"an output is {m.shape}, the matrix to quantise asks for {tuple(shape)}")
-            _on_current_device(m.elems, m.scales)
-    _on_current_device(d_in)
-    _check(_lib.zc_fp8_quantize(real, ptr, ld, q._ref if q is not None else None, qt._ref if qt is not None else None, _stream_ptr(stream)),
-           "zc_fp8_quantize")
+    rows, cols = d_in.shape
+    dev = d_in.get_device()
+    if q is not None and q.shape != (rows, cols):
+        raise ValueError(f"q is {q.shape}, the matrix to quantise asks for {(rows, cols)}")
+    if qt is not None and qt.shape != (cols, rows):
+        raise ValueError(f"qt is {qt.shape}, the matrix to quantise asks for {(cols, rows)}")
+    dev = _same_device(dev, q._dev if q is not None else dev, qt._dev if qt is not None else dev)
+    status = _lib.zc_fp8_quantize(real, ptr, ld, q._ref if q is not None else None, qt._ref if qt is not None else None, _stream_of(stream, dev))
+    if status != OK:
+        raise ZcError(status, "zc_fp8_quantize")
     return q
 
 
 def fp8_matmul(a: Fp8Matrix, b: Fp8Matrix, d_out: torch.Tensor, accumulate: bool = False, stream=None) -> torch.Tensor:
     """zc_fp8_matmul: d_out = a b^T, or d_out += a b^T (asynchronous)."""
     real, ptr, ld = _real_matrix(d_out, "d_out")
-    if tuple(d_out.shape) != (a.elems.shape[0], b.elems.shape[0]):
-        raise ValueError(f"d_out is {tuple(d_out.shape)}, the product is {(a.elems.shape[0], b.elems.shape[0])}")
-    _on_current_device(a.elems, a.scales, b.elems, b.scales, d_out)
-    _check(_lib.zc_fp8_matmul(a._ref, b._ref, real, ptr, ld, accumulate, _stream_ptr(stream)), "zc_fp8_matmul")
+    if d_out.shape != (a.shape[0], b.shape[0]):
+        raise ValueError(f"d_out is {tuple(d_out.shape)}, the product is {(a.shape[0], b.shape[0])}")
+    dev = _same_device(a._dev, b._dev, d_out.get_device())
+    status = _lib.zc_fp8_matmul(a._ref, b._ref, real, ptr, ld, accumulate, _stream_of(stream, dev))
+    if status != OK:
+        raise ZcError(status, "zc_fp8_matmul")
     return d_out
 
 
@@ -626,6 +641,9 @@ class Fp8MoeLayer:
         self.desc = Fp8MoeLayerDesc(ptr, gate_up.data_ptr(), gate_up_scales.data_ptr(), down.data_ptr(), down_scales.data_ptr(), ld,
                                     gate_up.stride(-2), down.stride(-2), experts, top_k, hidden, inter, fmt, real)
         self._ref = C.addressof(self.desc)
+        self._dev = router.get_device()
+        if any(t.get_device() != self._dev for t in self.tensors):
+            raise ValueError("the layer's tensors are on several devices")
 
     def workspace_bytes(self, n_tokens: int) -> int:
         return int(_lib.zc_fp8_moe_workspace_bytes(self._ref, n_tokens))
@@ -645,10 +663,13 @@ def fp8_moe(layer: Fp8MoeLayer, d_x: torch.Tensor, d_out: torch.Tensor, d_worksp
     for t, dtype in ((d_ids, torch.int32), (d_weights, torch.float32)):
         if t is not None and (t.dtype != dtype or tuple(t.shape) != (tokens, layer.top_k) or not t.is_contiguous()):
             raise ValueError(f"d_ids and d_weights are contiguous int32 and float32 of shape {(tokens, layer.top_k)}")
-    _on_current_device(d_x, d_out, d_workspace, d_ids, d_weights, *layer.tensors)
-    _check(_lib.zc_fp8_moe(layer._ref, tokens, x_ptr, ld_x if tokens > 1 else -(-ld_x // 8) * 8, y_ptr, ld_y, d_ids.data_ptr() if d_ids is not None else None,
-                           d_weights.data_ptr() if d_weights is not None else None, d_workspace.data_ptr(),
-                           d_workspace.numel() * d_workspace.element_size(), _stream_ptr(stream)), "zc_fp8_moe")
+    devices = [t.get_device() for t in (d_x, d_out, d_workspace, d_ids, d_weights) if t is not None]
+    dev = _same_device(layer._dev, *devices)
+    status = _lib.zc_fp8_moe(layer._ref, tokens, x_ptr, ld_x if tokens > 1 else -(-ld_x // 8) * 8, y_ptr, ld_y, d_ids.data_ptr() if d_ids is not None else None,
+                             d_weights.data_ptr() if d_weights is not None else None, d_workspace.data_ptr(),
+                             d_workspace.numel() * d_workspace.element_size(), _stream_of(stream, dev))
+    if status != OK:
+        raise ZcError(status, "zc_fp8_moe")
     return d_out
 
 
