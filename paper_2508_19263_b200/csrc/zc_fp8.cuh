@@ -84,6 +84,15 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr)
 }
 
 // ---- programmatic dependent launch ----
+// A kernel may be on the GPU, and set up its barriers and tensor memory, while the one before it in the stream ends; it
+// touches nothing that other kernels read or write before grid_wait(), which waits for all of them.
+inline cudaLaunchAttribute launch_early()
+{
+    cudaLaunchAttribute a{};
+    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a.val.programmaticStreamSerializationAllowed = 1;
+    return a;
+}
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -106,10 +115,20 @@ __device__ __forceinline__ uint32_t cluster_rank()
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void cluster_sync()
+__device__ __forceinline__ void cluster_arrive()
 {
     __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    cluster_arrive();
+    cluster_wait();
 }
 // the same place in the shared memory of the cluster's block `rank`
 __device__ __forceinline__ uint32_t map_shared(uint32_t addr, uint32_t rank)

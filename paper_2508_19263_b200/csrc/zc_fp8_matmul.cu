@@ -27,6 +27,10 @@ struct MatmulParams {
     uint32_t idesc;                              // instruction descriptor without the scale selectors
     uint32_t out_type, accumulate, out_wide;     // out_wide: every row of D begins on a 16-byte boundary
     uint32_t tiles_m, tiles_n;
+    // Rows of A and of B that a copy of the small kernel brings: no more than there are.  Rows beyond the matrix would arrive as zeros, in
+    // the copy engine's time; left out, their accumulators hold whatever comes of what lay in shared memory, and nobody reads them.
+    uint32_t rows_a, rows_b;
+    uint32_t stages;                             // of the small kernel
     uint32_t by_copy;                            // the large kernel's results leave by tensor copies
     uint32_t spin_limit, skip_copy;
 };
@@ -55,42 +59,42 @@ __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 
-// COUNT consecutive values of a row of D, of which the first n exist.
-template <typename T, int COUNT>
-__device__ __forceinline__ void store_row(uint8_t* row, uint32_t col, uint32_t n, const float* v, uint32_t wide, uint32_t accumulate)
+// A value, or 16 bytes of consecutive values, of D; they exist, and 16 bytes are aligned.
+template <typename T>
+__device__ __forceinline__ void put_one(uint8_t* row, uint32_t col, float v, uint32_t accumulate)
 {
     T* p = reinterpret_cast<T*>(row) + col;
-    constexpr int PER = 16 / sizeof(T);
-    if (wide && n >= COUNT && COUNT % PER == 0) {
-#pragma unroll
-        for (int i = 0; i < COUNT; i += PER) {
-            union { uint4 q; T t[PER]; } x;
-            if (accumulate) x.q = *reinterpret_cast<const uint4*>(p + i);
-#pragma unroll
-            for (int j = 0; j < PER; ++j) x.t[j] = from_float<T>(accumulate ? v[i + j] + to_float(x.t[j]) : v[i + j]);
-            *reinterpret_cast<uint4*>(p + i) = x.q;
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i)
-        if ((uint32_t)i < n) p[i] = from_float<T>(accumulate ? v[i] + to_float(p[i]) : v[i]);
+    *p = from_float<T>(accumulate ? v + to_float(*p) : v);
 }
-template <int COUNT>
-__device__ __forceinline__ void store_row(const MatmulParams& P, uint32_t row, uint32_t col, const float* v)
+template <typename T>
+__device__ __forceinline__ void put_wide(uint8_t* row, uint32_t col, const float* v, uint32_t accumulate)
 {
-    if (row >= P.m || col >= P.n) return;
+    constexpr int PER = 16 / sizeof(T);
+    T* p = reinterpret_cast<T*>(row) + col;
+    union { uint4 q; T t[PER]; } x;
+    if (accumulate) x.q = *reinterpret_cast<const uint4*>(p);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) x.t[j] = from_float<T>(accumulate ? v[j] + to_float(x.t[j]) : v[j]);
+    *reinterpret_cast<uint4*>(p) = x.q;
+}
+__device__ __forceinline__ void put_one(const MatmulParams& P, uint32_t row, uint32_t col, float v)
+{
     uint8_t* r = P.out + (uint64_t)row * P.ld_out;
-    const uint32_t n = P.n - col;
-    if (P.out_type == ZC_REAL_F32) store_row<float, COUNT>(r, col, n, v, P.out_wide, P.accumulate);
-    else if (P.out_type == ZC_REAL_BF16) store_row<__nv_bfloat16, COUNT>(r, col, n, v, P.out_wide, P.accumulate);
-    else store_row<__half, COUNT>(r, col, n, v, P.out_wide, P.accumulate);
+    if (P.out_type == ZC_REAL_F32) put_one<float>(r, col, v, P.accumulate);
+    else if (P.out_type == ZC_REAL_BF16) put_one<__nv_bfloat16>(r, col, v, P.accumulate);
+    else put_one<__half>(r, col, v, P.accumulate);
+}
+__device__ __forceinline__ void put_wide(const MatmulParams& P, uint32_t row, uint32_t col, const float* v)
+{
+    uint8_t* r = P.out + (uint64_t)row * P.ld_out;
+    if (P.out_type == ZC_REAL_F32) put_wide<float>(r, col, v, P.accumulate);
+    else if (P.out_type == ZC_REAL_BF16) put_wide<__nv_bfloat16>(r, col, v, P.accumulate);
+    else put_wide<__half>(r, col, v, P.accumulate);
 }
 
 // One tile of 128 x 128 per block; the `gridDim.z` blocks of a cluster share a tile, each takes a part of the steps, and the
 // parts are added up through the cluster's shared memory in the order of the ranks.
-constexpr uint32_t kSmallStages = 3;
-constexpr size_t kSmallSmem = 1024 + kSmallStages * 2 * kTileBytes + kScaleBufs * kScaleBufBytes + sizeof(MatmulShared);
+constexpr size_t small_smem(uint32_t stages) { return 1024 + stages * 2 * kTileBytes + kScaleBufs * kScaleBufBytes + sizeof(MatmulShared); }
 constexpr uint32_t kSmallCols = 256;             // tensor memory: 128 accumulator columns, then two sets of 4 + 4 scale columns
 constexpr uint32_t kSmallScales = 128;
 
@@ -98,8 +102,9 @@ __global__ void __launch_bounds__(kMmThreads)
 matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MatmulParams P)
 {
     extern __shared__ uint8_t raw[];
+    const uint32_t stages = P.stages;
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    const uint32_t words_at = base + kSmallStages * 2 * kTileBytes;
+    const uint32_t words_at = base + stages * 2 * kTileBytes;
     MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (words_at - smem_u32(raw)) + kScaleBufs * kScaleBufBytes);
     const uint32_t warp = warp_index(), lane = threadIdx.x & 31;
     const uint32_t parts = gridDim.z, part = blockIdx.z;
@@ -110,7 +115,7 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     if (warp == 0 && lane == 0) {
         prefetch_map(&map_a);
         prefetch_map(&map_b);
-        for (uint32_t i = 0; i < kSmallStages; ++i) { bar_init(smem_u32(&S->full[i]), 1); bar_init(smem_u32(&S->empty[i]), 1); }
+        for (uint32_t i = 0; i < stages; ++i) { bar_init(smem_u32(&S->full[i]), 1); bar_init(smem_u32(&S->empty[i]), 1); }
         for (uint32_t i = 0; i < kScaleBufs; ++i) { bar_init(smem_u32(&S->sf_full[i]), 1); bar_init(smem_u32(&S->sf_empty[i]), 1); }
         bar_init(smem_u32(&S->acc_full[0]), 1);
         S->failed = 0;
@@ -121,27 +126,29 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = S->tmem;
+    grid_launch_dependents();
+    grid_wait();                                 // what the kernels before this one wrote is there
 
-    uint32_t issued = 0;
+    uint32_t st = 0, round = 0;
     if (warp == 0) {
-        for (uint32_t i = lo; i < hi; ++i, ++issued) {
-            const uint32_t st = issued % kSmallStages;
-            if (issued >= kSmallStages && !wait.warp(smem_u32(&S->empty[st]), (issued / kSmallStages - 1) & 1)) break;
+        for (uint32_t i = lo; i < hi; ++i) {
+            if (round && !wait.warp(smem_u32(&S->empty[st]), (round - 1) & 1)) break;
             const uint32_t bar = smem_u32(&S->full[st]);
             if (elect_one()) {
-                bar_expect(bar, 2 * kTileBytes);
+                bar_expect(bar, (P.rows_a + P.rows_b) * kStepBytes);
                 if (!P.skip_copy) {
                     tensor_copy<1>(base + st * 2 * kTileBytes, &map_a, (int)(i * kStepBytes), (int)m0, bar);
                     tensor_copy<1>(base + st * 2 * kTileBytes + kTileBytes, &map_b, (int)(i * kStepBytes), (int)n0, bar);
                 }
             }
+            if (++st == stages) { st = 0; ++round; }
         }
     } else if (warp == 1) {
         for (uint32_t i = 0; i < hi - lo; ++i) {
-            const uint32_t st = i % kSmallStages, word = i >> 2, buf = word % kScaleBufs;
+            const uint32_t word = i >> 2, buf = word % kScaleBufs;
             const uint32_t sfa = tmem + kSmallScales + (word & 1) * 8, sfb = sfa + 4;
             const bool fresh = (i & 3) == 0;
-            if (!wait.warp(smem_u32(&S->full[st]), (i / kSmallStages) & 1)) break;
+            if (!wait.warp(smem_u32(&S->full[st]), round & 1)) break;
             if (fresh) {
                 if (!wait.warp(smem_u32(&S->sf_full[buf]), (word / kScaleBufs) & 1)) break;
                 // the set's words of eight steps ago are not looked up any more
@@ -161,6 +168,7 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 if ((i & 3) == 3) mma_commit<1>(smem_u32(&S->sf_empty[buf]));
             }
             __syncwarp();
+            if (++st == stages) { st = 0; ++round; }
         }
         if (elect_one()) mma_commit<1>(smem_u32(&S->acc_full[0]));
     } else if (warp >= 8) {
@@ -189,42 +197,65 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             for (uint32_t c = 0; c < 4; ++c) {
                 uint32_t v[32];
                 tmem_ld32(tmem + (quad * 32u << 16) + c * 32, v);
-                if (parts == 1) {
-                    store_row<32>(P, m0 + row, n0 + c * 32, reinterpret_cast<const float*>(v));
-                } else if (row < rows) {
-                    // the operand stages are free once the last instruction is done; 16-byte pieces turned by the row
+                // the operand stages are free once the last instruction is done; 16-byte pieces turned by the row
+                if (row < rows) {
 #pragma unroll
-                    for (uint32_t q = 0; q < 8; ++q) {
-                        const uint32_t at = base + row * 512 + (((c * 8 + q) ^ (row & 31)) << 4);
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v[4 * q]), "r"(v[4 * q + 1]), "r"(v[4 * q + 2]), "r"(v[4 * q + 3]) : "memory");
-                    }
+                    for (uint32_t q = 0; q < 8; ++q) sts128(base + row * 512 + (((c * 8 + q) ^ (row & 31)) << 4), v + 4 * q);
                 }
             }
             tc_fence_before();
         }
     }
     __syncthreads();
+    // Rank r adds up columns 128 r / parts .. of all rows, in the order of the ranks, in its own shared memory, where no other rank
+    // reads these columns.
+    const uint32_t width = 128 / parts, c0 = part * width, cols = P.n - n0;
     if (parts > 1) {
         cluster_sync();
-        // rank r adds up columns r * 128 / parts .. of all rows
-        const uint32_t pieces = 32 / parts, first = part * pieces;
+        const uint32_t pieces = width / 4;
         for (uint32_t i = threadIdx.x; i < rows * pieces; i += kMmThreads) {
-            const uint32_t row = i / pieces, piece = first + i % pieces;
+            const uint32_t row = i / pieces, piece = c0 / 4 + i - row * pieces;
             const uint32_t at = base + row * 512 + ((piece ^ (row & 31)) << 4);
-            float sum[4] = {0, 0, 0, 0};
-            for (uint32_t r = 0; r < parts; ++r) {
-                const float4 x = ld_cluster_f4(map_shared(at, r));
-                sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
-            }
-            store_row<4>(P, m0 + row, n0 + piece * 4, sum);
+            float4 x[8];
+#pragma unroll
+            for (uint32_t r = 0; r < 8; ++r)
+                if (r < parts) x[r] = ld_cluster_f4(map_shared(at, r));
+#pragma unroll
+            for (uint32_t r = 1; r < 8; ++r)
+                if (r < parts) { x[0].x += x[r].x; x[0].y += x[r].y; x[0].z += x[r].z; x[0].w += x[r].w; }
+            const uint32_t s[4] = {__float_as_uint(x[0].x), __float_as_uint(x[0].y), __float_as_uint(x[0].z), __float_as_uint(x[0].w)};
+            sts128(at, s);
         }
-        cluster_sync();
+        __syncthreads();
+        cluster_arrive();                        // this block has read all that it needs of the others
+    }
+    const uint32_t per = P.out_type == ZC_REAL_F32 ? 4 : 8;
+    if (P.out_wide && (cols >= 128 || cols % per == 0)) {
+        const uint32_t units = width / per;
+        for (uint32_t i = threadIdx.x; i < rows * units; i += kMmThreads) {
+            const uint32_t row = i / units, col = c0 + (i - row * units) * per, piece = col >> 2;
+            if (col >= cols) continue;
+            uint4 v[2];
+            v[0] = lds128(base + row * 512 + ((piece ^ (row & 31)) << 4));
+            if (per == 8) v[1] = lds128(base + row * 512 + (((piece + 1) ^ (row & 31)) << 4));
+            put_wide(P, m0 + row, n0 + col, reinterpret_cast<const float*>(v));
+        }
+    } else {
+        // no alignment to count on: a column a thread, so that a warp's stores lie next to each other
+        for (uint32_t i = threadIdx.x; i < rows * width; i += kMmThreads) {
+            const uint32_t row = i / width, col = c0 + (i - row * width);
+            if (col < cols) put_one(P, m0 + row, n0 + col, __uint_as_float(lds32(base + row * 512 + (((col >> 2) ^ (row & 31)) << 4) + (col & 3) * 4)));
+        }
     }
     // after a wait that gave up, copies may still be on their way into this block's shared memory
     if (*wait.failed && warp == 0 && lane == 0 && !P.skip_copy)
-        for (uint32_t i = issued > kSmallStages ? issued - kSmallStages : 0; i < issued; ++i)
-            for (uint32_t t = 0; t <= P.spin_limit && !bar_try(smem_u32(&S->full[i % kSmallStages]), (i / kSmallStages) & 1); ++t) { }
+        for (uint32_t i = 0; i < stages; ++i) {
+            const uint32_t r = i < st ? round : round - 1;
+            if (round == 0 && i >= st) continue;
+            for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S->full[i]), r & 1); ++q) { }
+        }
     __syncthreads();
+    if (parts > 1) cluster_wait();               // no other block reads from this one any more
     if (warp == 1) tmem_free<1>(tmem, kSmallCols);
 }
 
@@ -295,6 +326,8 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     cluster_sync();                              // the pair's barriers are there before either block uses them
     tc_fence_after();
     const uint32_t tmem = S->tmem;
+    grid_launch_dependents();
+    grid_wait();                                 // what the kernels before this one wrote is there
 
     if (warp == 0) {
         // both blocks copy their halves; the bytes count on the first block's barrier
@@ -390,7 +423,6 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             large_tile(P, i, tm, tn);
             if (!__all_sync(0xFFFFFFFFu, wait(smem_u32(&S->acc_full[tile & 1]), (tile >> 1) & 1) && !*wait.failed)) break;
             tc_fence_after();
-            const uint32_t row = tm * 256 + rank * 128 + quad * 32 + lane;
             const uint32_t d = tmem + (quad * 32u << 16) + (tile & 1 ? kLargeSecond : 0), results = results_at + quad * 2 * kResultBytes;
 #pragma unroll 1
             for (uint32_t q = 0; q < 8; ++q) {
@@ -416,7 +448,20 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                         send(map_d, results + (sent++ & 1) * kResultBytes, lane, (int)col0, (int)row0, w);
                     }
                 } else {
-                    store_row<32>(P, row, tn * 256 + c * 32, reinterpret_cast<const float*>(v));
+                    // no alignment to count on, or D to be added to: 16 columns in FP32 at a time through shared memory, so that
+                    // half a warp's stores lie next to each other
+                    const uint32_t row0 = tm * 256 + rank * 128 + quad * 32, col0 = tn * 256 + c * 32;
+                    if (row0 >= P.m || col0 >= P.n) continue;
+#pragma unroll
+                    for (uint32_t half = 0; half < 2; ++half) {
+                        __syncwarp();
+#pragma unroll
+                        for (uint32_t j = 0; j < 4; ++j) sts128(results + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4), v + half * 16 + 4 * j);
+                        __syncwarp();
+                        const uint32_t e = lane & 15, col = col0 + half * 16 + e;
+                        for (uint32_t r = lane >> 4; r < 32 && row0 + r < P.m; r += 2)
+                            if (col < P.n) put_one(P, row0 + r, col, __uint_as_float(lds32(results + r * 64 + (((e >> 2) ^ ((r >> 1) & 3)) << 4) + (e & 3) * 4)));
+                    }
                 }
             }
         }
@@ -496,14 +541,19 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
     P.out_wide = reinterpret_cast<uintptr_t>(d_out) % 16 == 0 && P.ld_out % 16 == 0;
     P.spin_limit = test_knobs().spin_limit;
     P.skip_copy = test_knobs().skip_copy;
-    CUtensorMap map_a, map_b;
-    if (!make_map(&map_a, a->d_elems, a->rows, a->cols, a->ld_elems, kTile) || !make_map(&map_b, b->d_elems, b->rows, b->cols, b->ld_elems, kTile)) return ZC_E_CUDA;
     P.tiles_m = (uint32_t)ceil_div(P.m, kTile);
     P.tiles_n = (uint32_t)ceil_div(P.n, kTile);
     if (P.tiles_m > 65535) return ZC_E_TOO_LARGE;
     const uint64_t tiles = (uint64_t)P.tiles_m * P.tiles_n;
     const uint64_t large = ceil_div(P.m, 256) * ceil_div(P.n, 256);
-    if (large >= ZC_LARGE_FROM) {
+    // Pairs of blocks from 37 tiles of 256 x 256 on, half of the GPU's pairs; below, four times as many tiles of 128 x 128 fill it
+    // better, and so they do for up to 128 tokens, where half of a pair's tile would be empty.
+    const bool pairs = P.m > 128 && P.n > 128 && large >= ZC_LARGE_FROM;
+    P.rows_a = pairs || P.m >= kTile ? kTile : (uint32_t)round_up(P.m, 8);
+    P.rows_b = pairs || P.n >= kTile ? kTile : (uint32_t)round_up(P.n, 8);
+    CUtensorMap map_a, map_b;
+    if (!make_map(&map_a, a->d_elems, a->rows, a->cols, a->ld_elems, P.rows_a) || !make_map(&map_b, b->d_elems, b->rows, b->cols, b->ld_elems, P.rows_b)) return ZC_E_CUDA;
+    if (pairs) {
         static OncePerDevice once;
         const uint32_t blocks = once([] { return large_blocks(); });
         if (!blocks) return ZC_E_CUDA;
@@ -522,28 +572,35 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
         cfg.blockDim = dim3(kMmThreads);
         cfg.dynamicSmemBytes = kLargeSmem;
         cfg.stream = st;
-        cudaLaunchAttribute at[1];
+        cudaLaunchAttribute at[2];
         at[0].id = cudaLaunchAttributeClusterDimension;
         at[0].val.clusterDim = {2, 1, 1};
+        at[1] = launch_early();
         cfg.attrs = at;
-        cfg.numAttrs = 1;
+        cfg.numAttrs = 2;
         return cudaLaunchKernelEx(&cfg, matmul_large_kernel, map_a, map_b, map_d, P) == cudaSuccess ? ZC_OK : ZC_E_CUDA;
     }
     P.idesc = instruction_of(a->format, b->format, 128, 128);
+    // Parts of k as long as there is an SM for each: 1 x 4096 x 4096 takes 13.2 us in 32 blocks, 8.3 in 128; 128 x 4096 x 4096 14.7 and
+    // 10.9.  Adding the parts up costs more the more rows there are, so these have 8 steps each at least, few rows 4
+    // (1024 x 1024 x 1024: 7.2 us in one part, 8.6 in two).
     uint32_t parts = 1;
-    while (parts < 8 && tiles * parts * 2 <= 2 * (uint64_t)sm_count() && P.steps >= 4 * parts) parts *= 2;
+    while (parts < 8 && tiles * parts * 2 <= (uint64_t)sm_count() && P.steps >= (P.m > 32 ? 16 : 8) * parts) parts *= 2;
+    // one block per SM has all of the shared memory, two have half of it each (64 x 14336 x 4096: 15.2 us, 18.3 with half)
+    P.stages = tiles * parts <= (uint64_t)sm_count() ? 6 : 3;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(P.tiles_n, P.tiles_m, parts);
     cfg.blockDim = dim3(kMmThreads);
-    cfg.dynamicSmemBytes = kSmallSmem;
+    cfg.dynamicSmemBytes = small_smem(P.stages);
     cfg.stream = st;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim = {1, 1, parts};
+    at[1] = launch_early();
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     static OncePerDevice once;
-    if (!once([] { return (uint32_t)(cudaFuncSetAttribute(matmul_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem) == cudaSuccess); })) return ZC_E_CUDA;
+    if (!once([] { return (uint32_t)(cudaFuncSetAttribute(matmul_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)small_smem(6)) == cudaSuccess); })) return ZC_E_CUDA;
     if (cudaLaunchKernelEx(&cfg, matmul_small_kernel, map_a, map_b, P) != cudaSuccess) return ZC_E_CUDA;
     return ZC_OK;
 }

@@ -776,9 +776,10 @@ moe_up_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ MoeP
     const uint32_t tid = threadIdx.x, rank = cluster_rank();
     const uint32_t n_rows = P.tokens * P.top_k;
 
-    grid_launch_dependents();
     if (tid < kMoeHeights) prefetch_map(&maps.of[tid]);
     moe_setup(S, kBuilders / stage_count(P.pass, 3));
+    grid_launch_dependents();
+    grid_wait();
     router_logits<HALF>(P, rank, T);
     cluster_sync();
     choose(P, rank, T);
@@ -829,6 +830,7 @@ moe_down_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ Mo
     const uint32_t tid = threadIdx.x;
     if (tid < kMoeHeights) prefetch_map(&maps.of[tid]);
     moe_setup(S, kBuilders / stage_count(P.pass, kHiddenPieces<HALF>));
+    grid_launch_dependents();
     grid_wait();
     // all of the lists at once, whatever is behind the last chosen expert: one latency
     const uint32_t n_active = P.route[0], n_passes = P.route[1];
@@ -909,16 +911,16 @@ static cudaError_t launch_moe(const MoeMaps& up, const MoeMaps& down, const MoeP
     cfg.blockDim = dim3(kMoeThreads);
     cfg.dynamicSmemBytes = kMoeSmem;
     cfg.stream = st;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
+    at[0] = launch_early();
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim = {kMoeCluster, 1, 1};
     cfg.attrs = at;
-    cfg.numAttrs = 1;
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim = {kMoeCluster, 1, 1};
+    cfg.numAttrs = 2;
     cfg.gridDim = dim3(up_blocks);
     e = cudaLaunchKernelEx(&cfg, moe_up_kernel<HALF>, up, P);
     if (e != cudaSuccess) return e;
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
     cfg.gridDim = dim3((uint32_t)sm_count());
     return cudaLaunchKernelEx(&cfg, moe_down_kernel<HALF>, down, P);
 }

@@ -84,6 +84,8 @@ template <typename T, bool E5M2, bool WIDE>
 __global__ void __launch_bounds__(kQuantThreads)
 quantize_rows_kernel(const __grid_constant__ QuantParams P)
 {
+    grid_launch_dependents();
+    grid_wait();
     const uint32_t sub = threadIdx.x & 7;
     const uint32_t n_blocks = P.rows * P.col_blocks;
     const uint32_t block = (blockIdx.x * kQuantThreads + threadIdx.x) >> 3;
@@ -116,6 +118,8 @@ quantize_tile_kernel(const __grid_constant__ QuantParams P)
     __shared__ __align__(16) uint32_t s_bytes[TRANS ? 128 * 32 : 1];     // [column][row / 4], turned by 4 words per 16 columns
     __shared__ float s_max[8][SQUARE ? 1 : 128];
     __shared__ uint32_t s_scale[SQUARE || !TRANS ? 1 : 128];
+    grid_launch_dependents();
+    grid_wait();
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rb = blockIdx.x / P.col_blocks, cb = blockIdx.x - rb * P.col_blocks;
     const uint32_t sub = tid & 7, rg = tid >> 3;
@@ -211,11 +215,17 @@ quantize_tile_kernel(const __grid_constant__ QuantParams P)
 template <typename T, bool E5M2, bool WIDE>
 static cudaError_t launch_quantize(const QuantParams& P, bool square, uint32_t n_blocks, uint32_t n_tiles, cudaStream_t st)
 {
-    if (square && P.qt) quantize_tile_kernel<T, E5M2, WIDE, true, true><<<n_tiles, kQuantThreads, 0, st>>>(P);
-    else if (square) quantize_tile_kernel<T, E5M2, WIDE, true, false><<<n_tiles, kQuantThreads, 0, st>>>(P);
-    else if (P.qt) quantize_tile_kernel<T, E5M2, WIDE, false, true><<<n_tiles, kQuantThreads, 0, st>>>(P);
-    else quantize_rows_kernel<T, E5M2, WIDE><<<(n_blocks + kQuantThreads / 8 - 1) / (kQuantThreads / 8), kQuantThreads, 0, st>>>(P);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at[1] = {launch_early()};
+    cfg.blockDim = dim3(kQuantThreads);
+    cfg.gridDim = dim3(square || P.qt ? n_tiles : (n_blocks + kQuantThreads / 8 - 1) / (kQuantThreads / 8));
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (square && P.qt) return cudaLaunchKernelEx(&cfg, quantize_tile_kernel<T, E5M2, WIDE, true, true>, P);
+    if (square) return cudaLaunchKernelEx(&cfg, quantize_tile_kernel<T, E5M2, WIDE, true, false>, P);
+    if (P.qt) return cudaLaunchKernelEx(&cfg, quantize_tile_kernel<T, E5M2, WIDE, false, true>, P);
+    return cudaLaunchKernelEx(&cfg, quantize_rows_kernel<T, E5M2, WIDE>, P);
 }
 
 }  // namespace zc
