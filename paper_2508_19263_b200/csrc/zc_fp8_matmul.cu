@@ -242,8 +242,10 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         }
     } else {
         // no alignment to count on: a column a thread, so that a warp's stores lie next to each other
+        const uint32_t shift = 31 - __clz(width);            // a power of two
+#pragma unroll 4
         for (uint32_t i = threadIdx.x; i < rows * width; i += kMmThreads) {
-            const uint32_t row = i / width, col = c0 + (i - row * width);
+            const uint32_t row = i >> shift, col = c0 + (i & (width - 1));
             if (col < cols) put_one(P, m0 + row, n0 + col, __uint_as_float(lds32(base + row * 512 + (((col >> 2) ^ (row & 31)) << 4) + (col & 3) * 4)));
         }
     }
