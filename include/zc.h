@@ -468,6 +468,8 @@ zc_status zc_fp8_quantize(zc_real in_type, const void* d_in, uint64_t ld_in, con
  * A linear layer is x W^T (a = activations, b = weights); the gradient of its input is dy (W^T)^T and that of its
  * weights (dy^T)(x^T)^T, with the transposed matrices that zc_fp8_quantize makes.  K = 0 gives zeros.  The result
  * does not depend on other calls and is the same every time.  Asynchronous on cuda_stream; needs no workspace.
+ * The sums are those of the tensor cores' FP32 accumulators: to nearest for some 4096 columns; beyond, sums of one sign
+ * fall short by a few units in the last place (relative 6e-7 at 14336 columns, 5e-6 at 65536).
  * A wait inside the kernel that gives up leaves D undefined and is reported by zc_fp8_status.
  * Errors: INVALID_ARG (null or misaligned pointers, pitches, different K), UNSUPPORTED (types, formats), TOO_LARGE,
  * CUDA. */

@@ -484,9 +484,10 @@ __global__ void zero_kernel(const __grid_constant__ MatmulParams P, uint32_t wid
         for (uint64_t i = threadIdx.x; i < (uint64_t)P.n * width; i += blockDim.x) P.out[r * P.ld_out + i] = 0;
 }
 
-#ifndef ZC_LARGE_FROM
-#define ZC_LARGE_FROM 37
-#endif
+// From this many tiles of 256 x 256 on, half of the GPU's pairs of blocks, a product goes to pairs; below, four times as many
+// tiles of 128 x 128 fill it better: 512 x 4096 x 4096 (32 tiles) takes 17.8 us in pairs, 16.0 in small tiles, 300 x 14336 x 4096
+// (112 tiles) 29.4 and 33.6, 1024 x 4096 x 1024 (64 tiles, 8 steps) 10.8 and 10.3.
+constexpr uint64_t kPairsFrom = 37;
 // Blocks of the large kernel that are on the GPU at once, in whole pairs.
 static uint32_t large_blocks()
 {
@@ -548,9 +549,8 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
     if (P.tiles_m > 65535) return ZC_E_TOO_LARGE;
     const uint64_t tiles = (uint64_t)P.tiles_m * P.tiles_n;
     const uint64_t large = ceil_div(P.m, 256) * ceil_div(P.n, 256);
-    // Pairs of blocks from 37 tiles of 256 x 256 on, half of the GPU's pairs; below, four times as many tiles of 128 x 128 fill it
-    // better, and so they do for up to 128 tokens, where half of a pair's tile would be empty.
-    const bool pairs = P.m > 128 && P.n > 128 && large >= ZC_LARGE_FROM;
+    // for up to 128 tokens half of a pair's tile would be empty (16 x 14336 x 4096: 20.3 us in pairs, 14.8 in small tiles)
+    const bool pairs = P.m > 128 && P.n > 128 && large >= kPairsFrom;
     P.rows_a = pairs || P.m >= kTile ? kTile : (uint32_t)round_up(P.m, 8);
     P.rows_b = pairs || P.n >= kTile ? kTile : (uint32_t)round_up(P.n, 8);
     CUtensorMap map_a, map_b;
@@ -565,7 +565,7 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
         P.idesc = instruction_of(a->format, b->format, 256, 256);
         // a copy that runs over the last column is cut off at the next 16 bytes, not at the column: what lies behind it in the
         // row would be overwritten
-        P.by_copy = P.out_wide && !P.accumulate && (uint64_t)P.n * width % 16 == 0;
+        P.by_copy = P.out_wide && !P.accumulate && (uint64_t)P.n * width % 16 == 0 && P.ld_out < (1ull << 40);
         CUtensorMap map_d = map_a;
         if (P.by_copy && !make_result_map(&map_d, d_out, out_type, P.m, P.n, P.ld_out)) return ZC_E_CUDA;
         const uint32_t grid = (uint32_t)std::min<uint64_t>(blocks, 2 * large);

@@ -15,7 +15,7 @@
 //   kernel 1  routes (every cluster for itself, so that no block waits for another cluster), then gate and up: a tile is up to 64
 //             rows of gate and the same of up in alternating groups, so that a warp ends with both
 //   kernel 2  down: up to 128 rows a tile, one FP32 row of partial results per (token, expert); the block that completes a
-//             group's last expert adds the experts up in the order of the token's list
+//             group's last expert adds the experts up in the order of the token's list, when it has done all its tiles
 //
 // Warps of a block: 0 tensor copies, 1 matrix instructions, 2 the weights' scale bytes, 4-7 results, 8-23 the activations' pieces.
 #include "zc_fp8_tensor.cuh"
@@ -30,6 +30,9 @@ constexpr uint32_t kBuilders = 16;               // warps that make pieces
 constexpr uint32_t kMoeMaxStages = 9;
 constexpr uint32_t kMoeStageSpace = 208896;      // shared memory for stages: weights, pieces, 1 KiB of scale words each
 constexpr uint32_t kMoeHeights = 5;              // tensor copies of 8, 16, 32, 64 and 128 rows
+// Tiles that complete a band at most: a block has up to 4 tiles per pass of an expert (8192 groups of rows in tiles of 16 on more than
+// 128 blocks) and 31 more, so it touches fewer bands than this; launch_moe refuses a GPU with so few SMs that it would not.
+constexpr uint32_t kMoeTodo = 64;
 constexpr uint32_t kMoeTmemCols = 512;           // two accumulators of 128 columns, then 4 + 4 scale columns per stage
 constexpr uint32_t kMoeTmemScales = 256;
 
@@ -80,7 +83,8 @@ struct MoeShared {
     float row_p[kMaxRows];
     uint16_t row_of[kMaxRows];                   // kernel 2: rows of the tokens' experts
     uint8_t row_token[kMaxRows];
-    uint32_t last[16];
+    uint2 todo[kMoeTodo];                        // kernel 2: first group, and which of its tile's groups, to add up
+    uint32_t n_todo;
 };
 // while routing, where the stages will be
 struct MoeRouting {
@@ -88,7 +92,8 @@ struct MoeRouting {
     uint16_t id[kMaxRows];
     float p_all[kMaxRows];
     uint16_t id_all[kMaxRows];
-    unsigned long long mask[kMaxExperts];        // tokens that chose the expert
+    alignas(8) uint32_t mask[2 * kMaxExperts];   // tokens that chose the expert
+    uint16_t first_of[kMaxExperts];              // a chosen expert's first row
     // [token, rounded up to 8][expert, to 16]; behind them the warps' sums of logits that several share (there are few then), and
     // columns of router and tokens
     double logits[1];
@@ -102,20 +107,6 @@ __device__ __forceinline__ void mma16(float c[4], const uint32_t a[4], uint32_t 
     if (HALF) mma_f16(c, a[0], a[1], a[2], a[3], b0, b1);
     else mma_bf16(c, a[0], a[1], a[2], a[3], b0, b1);
 }
-// the first n bytes of a 16-byte piece, the rest as zeros
-__device__ __forceinline__ uint4 first_bytes(uint4 v, uint32_t n)
-{
-    uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-        const uint32_t have = n > 4 * i ? n - 4 * i : 0;
-        if (have < 4) w[i] &= (1u << (8 * have)) - 1u;
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ uint4 ld_cached_v4(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
-__device__ __forceinline__ uint4 zero4() { return make_uint4(0, 0, 0, 0); }
-
 // ---- the weights' stream --------------------------------------------------------------------------------------------
 
 // A tile: `groups` groups of eight rows (UP: of gate, and behind 64 rows of up) of a chosen expert, for up to P.pass of its tokens.
@@ -161,15 +152,17 @@ struct Tiles {
         const uint32_t all = c.per * r.n_passes;             // at most 2^13 * 2^10; times the blocks still 32 bits
         const uint32_t first = all * block / blocks;
         left = all * (block + 1) / blocks - first;
-        const uint32_t v = UP ? first / c.per : first % r.n_passes;
+        const uint32_t v = UP ? 0 : first % r.n_passes;
+        // the last chosen expert whose passes begin at or before the first tile, found by the warp together
+        uint32_t before = 0;
+        for (uint32_t a = 1 + (threadIdx.x & 31); a < r.n_active; a += 32) before += (UP ? r.pass[a] * c.per <= first : r.pass[a] <= v);
+        active = __reduce_add_sync(0xFFFFFFFFu, before);
         if (UP) {
-            while (active + 1 < r.n_active && (uint32_t)r.pass[active + 1] * c.per <= first) ++active;
             const uint32_t in = first - r.pass[active] * c.per, n = passes();
             band = in / n;
             pass = in - band * n;
         } else {
             band = first / r.n_passes;
-            while (active + 1 < r.n_active && r.pass[active + 1] <= v) ++active;
             pass = v - r.pass[active];
         }
     }
@@ -375,7 +368,7 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
                     auto fetch = [&](uint32_t c, uint4 raw[4]) {
 #pragma unroll
                         for (uint32_t i = 0; i < 4; ++i) {
-                            raw[i] = zero4();
+                            raw[i] = make_uint4(0, 0, 0, 0);
                             if (c + i >= t.count || col >= cols) continue;
                             if (UP) {
                                 const uint2 v = __ldg(reinterpret_cast<const uint2*>(P.x + 2 * ((uint64_t)S.row_token[t.row + c + i] * P.ld_x + col)));
@@ -508,27 +501,18 @@ __device__ __forceinline__ void router_logits(const MoeParams& P, uint32_t rank,
     for (uint32_t from = lo; from < hi; from += fit) {
         const uint32_t now = min(fit, hi - from);
         __syncthreads();
-        // six loads of a thread at a time: their latency is what this costs
-        for (uint32_t i0 = tid; i0 < rows * now * 8; i0 += 6 * kMoeThreads) {
-            uint4 v[6];
-            uint32_t to[6];
-#pragma unroll
-            for (uint32_t q = 0; q < 6; ++q) {
-                const uint32_t i = i0 + q * kMoeThreads;
-                const uint32_t row = i / (now * 8), piece = i - row * (now * 8), col = from * 64 + piece * 8;
-                const bool expert = row < rows_e;
-                const uint32_t r = expert ? row : row - rows_e;
-                to[q] = row < rows ? staged + row * pitch + piece * 16 : 0;
-                v[q] = zero4();
-                if (row < rows && col < P.hidden && r < (expert ? P.experts : P.tokens)) {
-                    v[q] = ld_cached_v4(expert ? P.router + 2 * ((uint64_t)r * P.ld_router + col) : P.x + 2 * ((uint64_t)r * P.ld_x + col));
-                    if (col + 8 > P.hidden) v[q] = first_bytes(v[q], 2 * (P.hidden - col));
-                }
+        for (uint32_t row = warp; row < rows; row += kMoeWarps) {
+            const bool expert = row < rows_e;
+            const uint32_t r = expert ? row : row - rows_e;
+            const bool there = r < (expert ? P.experts : P.tokens);
+            const uint8_t* src = !there ? P.x : expert ? P.router + 2 * (uint64_t)r * P.ld_router : P.x + 2 * (uint64_t)r * P.ld_x;
+            for (uint32_t piece = lane; piece < now * 8; piece += 32) {
+                const uint32_t col = from * 64 + piece * 8;
+                const bool in = there && col < P.hidden;
+                async_copy16(staged + row * pitch + piece * 16, in ? src + 2 * col : P.x, in ? min(16u, 2 * (P.hidden - col)) : 0u);
             }
-#pragma unroll
-            for (uint32_t q = 0; q < 6; ++q)
-                if (to[q]) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(to[q]), "r"(v[q].x), "r"(v[q].y), "r"(v[q].z), "r"(v[q].w) : "memory");
         }
+        async_copy_wait();
         __syncthreads();
         for (uint32_t item = warp; item < tasks * split; item += kMoeWarps) {
             const uint32_t task = item / split, slice = item - task * split, e0 = (task / nt) * 16, k0 = (task % nt) * 8;
@@ -575,6 +559,7 @@ __device__ __forceinline__ void choose(const MoeParams& P, uint32_t rank, MoeRou
     for (uint32_t i = warp; rank + i * kMoeCluster < P.tokens; i += kMoeWarps) {
         const uint32_t tok = rank + i * kMoeCluster;
         unsigned long long key[kMaxExperts / 32];
+        const uint32_t words = (P.experts + 31) >> 5;
 #pragma unroll
         for (uint32_t k = 0; k < kMaxExperts / 32; ++k) {
             const uint32_t e = k * 32 + lane;
@@ -586,32 +571,37 @@ __device__ __forceinline__ void choose(const MoeParams& P, uint32_t rank, MoeRou
                 key[k] = order_key(v);
             }
         }
+        // lane j keeps the j-th choice
         double largest = 0;
-        float total = 0;
+        float total = 0, mine = 0;
+        uint32_t my_id = 0;
         for (uint32_t j = 0; j < P.top_k; ++j) {
-            unsigned long long best = 0;
+            unsigned long long best = key[0];
             uint32_t where = 0;
 #pragma unroll
-            for (uint32_t k = 0; k < kMaxExperts / 32; ++k)
+            for (uint32_t k = 1; k < kMaxExperts / 32; ++k) {
+                if (k >= words) break;
                 if (key[k] > best) { best = key[k]; where = k; }
+            }
             const uint32_t hi = __reduce_max_sync(0xFFFFFFFFu, (uint32_t)(best >> 32));
             const uint32_t lo = __reduce_max_sync(0xFFFFFFFFu, (uint32_t)(best >> 32) == hi ? (uint32_t)best : 0u);
             const bool tie = (uint32_t)(best >> 32) == hi && (uint32_t)best == lo;
             const uint32_t e = __reduce_min_sync(0xFFFFFFFFu, tie ? where * 32 + lane : 0xFFFFFFFFu);
 #pragma unroll
-            for (uint32_t k = 0; k < kMaxExperts / 32; ++k)
+            for (uint32_t k = 0; k < kMaxExperts / 32; ++k) {
+                if (k >= words) break;
                 if (k * 32 + lane == e) key[k] = 0;
+            }
             const double v = value_of(((unsigned long long)hi << 32) | lo);
             if (j == 0) largest = v;
             const float p = expf((float)(v - largest));      // the difference in FP64, the exponential in FP32
             total += p;
-            if (lane == 0) {
-                S.id[i * P.top_k + j] = (uint16_t)e;
-                S.p[i * P.top_k + j] = p;
-            }
+            if (lane == j) { mine = p; my_id = e; }
         }
-        if (lane == 0)
-            for (uint32_t j = 0; j < P.top_k; ++j) S.p[i * P.top_k + j] /= total;
+        if (lane < P.top_k) {
+            S.id[i * P.top_k + lane] = (uint16_t)my_id;
+            S.p[i * P.top_k + lane] = mine / total;
+        }
     }
 }
 
@@ -619,18 +609,23 @@ __device__ __forceinline__ void choose(const MoeParams& P, uint32_t rank, MoeRou
 __device__ __forceinline__ void make_lists(const MoeParams& P, MoeRouting& S, Routing& R)
 {
     const uint32_t tid = threadIdx.x, n = P.tokens * P.top_k;
-    for (uint32_t e = tid; e < kMaxExperts; e += kMoeThreads) S.mask[e] = 0;
+    for (uint32_t e = tid; e < 2 * kMaxExperts; e += kMoeThreads) S.mask[e] = 0;
     __syncthreads();
-    for (uint32_t i = tid; i < n; i += kMoeThreads) atomicOr(&S.mask[S.id_all[i]], 1ull << (i / P.top_k));
+    for (uint32_t i = tid; i < n; i += kMoeThreads) {
+        const uint32_t tok = i / P.top_k;
+        atomicOr(&S.mask[2 * S.id_all[i] + (tok >> 5)], 1u << (tok & 31));
+    }
     __syncthreads();
     if (tid < 32) {
         // each lane eight experts: counts of tokens, of chosen experts, of passes; sums over the lanes before
-        uint32_t tokens = 0, active = 0, passes = 0;
+        uint32_t count[8], tokens = 0, active = 0, passes = 0;
+#pragma unroll
         for (uint32_t k = 0; k < 8; ++k) {
-            const uint32_t c = __popcll(S.mask[tid * 8 + k]);
-            tokens += c;
-            active += c != 0;
-            passes += (c + P.pass - 1) / P.pass;
+            const uint2 m = *reinterpret_cast<const uint2*>(&S.mask[2 * (tid * 8 + k)]);
+            count[k] = __popc(m.x) + __popc(m.y);
+            tokens += count[k];
+            active += count[k] != 0;
+            passes += (count[k] + P.pass - 1) / P.pass;
         }
         uint32_t a = tokens, b = active, c = passes;
         for (uint32_t d = 1; d < 32; d <<= 1) {
@@ -638,15 +633,16 @@ __device__ __forceinline__ void make_lists(const MoeParams& P, MoeRouting& S, Ro
             if (tid >= d) { a += x; b += y; c += z; }
         }
         uint32_t row = a - tokens, at = b - active, pass = c - passes;
+#pragma unroll
         for (uint32_t k = 0; k < 8; ++k) {
-            const uint32_t cnt = __popcll(S.mask[tid * 8 + k]);
-            if (!cnt) continue;
+            if (!count[k]) continue;
             R.expert[at] = (uint16_t)(tid * 8 + k);
             R.first[at] = (uint16_t)row;
             R.pass[at] = (uint16_t)pass;
+            S.first_of[tid * 8 + k] = (uint16_t)row;
             ++at;
-            row += cnt;
-            pass += (cnt + P.pass - 1) / P.pass;
+            row += count[k];
+            pass += (count[k] + P.pass - 1) / P.pass;
         }
         if (tid == 31) {
             R.n_active = b;
@@ -658,20 +654,12 @@ __device__ __forceinline__ void make_lists(const MoeParams& P, MoeRouting& S, Ro
     __syncthreads();
 }
 
-struct RowFinder {
-    const MoeRouting& S;
-    const Routing& R;
-    // row of a token in the list of expert e: the first row of e is that of the number of (token, expert) pairs before it
-    __device__ __forceinline__ uint32_t operator()(uint32_t e, uint32_t token) const
-    {
-        uint32_t lo = 0, hi = R.n_active;
-        while (hi - lo > 1) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (R.expert[mid] <= e) lo = mid; else hi = mid;
-        }
-        return R.first[lo] + __popcll(S.mask[e] & ((1ull << token) - 1));
-    }
-};
+// Row of a token in the list of an expert that it chose.
+__device__ __forceinline__ uint32_t row_of(const MoeRouting& S, uint32_t e, uint32_t token)
+{
+    const uint32_t lo = S.mask[2 * e], hi = S.mask[2 * e + 1], below = (1u << (token & 31)) - 1u;
+    return S.first_of[e] + (token < 32 ? __popc(lo & below) : __popc(lo) + __popc(hi & below));
+}
 
 // Barriers and tensor memory; all threads.
 __device__ __forceinline__ void moe_setup(MoeShared& S, uint32_t sharing)
@@ -681,6 +669,7 @@ __device__ __forceinline__ void moe_setup(MoeShared& S, uint32_t sharing)
         for (uint32_t i = 0; i < kMoeMaxStages; ++i) { bar_init(smem_u32(&S.full[i]), 2 + sharing); bar_init(smem_u32(&S.empty[i]), 1); }
         for (uint32_t i = 0; i < 2; ++i) { bar_init(smem_u32(&S.acc_full[i]), 1); bar_init(smem_u32(&S.acc_empty[i]), 4); }
         S.failed = 0;
+        S.n_todo = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc<1>(smem_u32(&S.tmem), kMoeTmemCols);
@@ -728,36 +717,46 @@ struct FinishDown {
         for (uint32_t i = 0; i < 8; ++i)
             if (c + i < t.count) P.z[(uint64_t)(t.row + c + i) * P.hidden_pad + r] = v[i];
     }
-    // the four warps: whoever completes a group's last pass adds the experts up, four columns of a token a thread
+    // The four warps: whoever completes a group's last pass adds its experts up, at the end, with all of the block's threads (they wait
+    // for little but loads then: 128 threads took 16 us after the last product of 64 tokens).
     __device__ __forceinline__ void tile_done(const Tile& t) const
     {
         const uint32_t tid = threadIdx.x & 127;
         __threadfence();
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (tid < t.groups) {
-            S.last[tid] = atomicAdd(&P.done[t.group + tid], 1u) + 1 == n_passes;
+        if (tid < 32) {
+            const bool last = tid < t.groups && atomicAdd(&P.done[t.group + tid], 1u) + 1 == n_passes;
+            const uint32_t which = __ballot_sync(0xFFFFFFFFu, last);
             __threadfence();
-        }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        const uint32_t g = (tid & 31) >> 1, r = (t.group + g) * 8 + (tid & 1) * 4;
-        if (g < t.groups && S.last[g] && r < P.hidden) {
-            for (uint32_t tok = tid >> 5; tok < P.tokens; tok += 4) {
-                float y[4] = {0, 0, 0, 0};
-                const uint16_t* rows = S.row_of + tok * P.top_k;
-#pragma unroll 8
-                for (uint32_t j = 0; j < P.top_k; ++j) {
-                    const float4 z = __ldcg(reinterpret_cast<const float4*>(P.z + (uint64_t)rows[j] * P.hidden_pad + r));
-                    y[0] += z.x; y[1] += z.y; y[2] += z.z; y[3] += z.w;
-                }
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    if (r + i >= P.hidden) break;
-                    if (HALF) reinterpret_cast<__half*>(P.y)[(uint64_t)tok * P.ld_y + r + i] = __float2half_rn(y[i]);
-                    else reinterpret_cast<__nv_bfloat16*>(P.y)[(uint64_t)tok * P.ld_y + r + i] = __float2bfloat16_rn(y[i]);
-                }
+            if (tid == 0 && which) {
+                S.todo[S.n_todo] = make_uint2(t.group, which);
+                ++S.n_todo;
             }
         }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+    }
+    // Thread tid of n: four columns of a token at a time.
+    __device__ __forceinline__ void add_up(uint32_t tid, uint32_t n) const
+    {
+        const uint32_t todo = S.n_todo, per = 32 * P.tokens;
+        for (uint32_t i = tid; i < todo * per; i += n) {
+            const uint32_t k = i / per, in = i - k * per, tok = in >> 5, g = (in & 31) >> 1;
+            const uint2 what = S.todo[k];
+            const uint32_t r = (what.x + g) * 8 + (in & 1) * 4;
+            if (!(what.y >> g & 1) || r >= P.hidden) continue;
+            float y[4] = {0, 0, 0, 0};
+            const uint16_t* rows = S.row_of + tok * P.top_k;
+#pragma unroll 8
+            for (uint32_t j = 0; j < P.top_k; ++j) {
+                const float4 z = __ldcg(reinterpret_cast<const float4*>(P.z + (uint64_t)rows[j] * P.hidden_pad + r));
+                y[0] += z.x; y[1] += z.y; y[2] += z.z; y[3] += z.w;
+            }
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                if (r + q >= P.hidden) break;
+                if (HALF) reinterpret_cast<__half*>(P.y)[(uint64_t)tok * P.ld_y + r + q] = __float2half_rn(y[q]);
+                else reinterpret_cast<__nv_bfloat16*>(P.y)[(uint64_t)tok * P.ld_y + r + q] = __float2bfloat16_rn(y[q]);
+            }
+        }
     }
 };
 
@@ -794,9 +793,8 @@ moe_up_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ MoeP
         T.id_all[i] = id;
     }
     make_lists(P, T, S.R);
-    const RowFinder row_of{T, S.R};
     for (uint32_t i = tid; i < n_rows; i += kMoeThreads) {
-        const uint32_t r = row_of(T.id_all[i], i / P.top_k);
+        const uint32_t r = row_of(T, T.id_all[i], i / P.top_k);
         S.row_p[r] = T.p_all[i];
         S.row_token[r] = (uint8_t)(i / P.top_k);
         if (blockIdx.x == 0) {
@@ -843,7 +841,10 @@ moe_down_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ Mo
     for (uint32_t i = tid; i < P.tokens * P.top_k; i += kMoeThreads) S.row_of[i] = (uint16_t)P.row_of[i];
     if (tid == 0) { S.R.n_active = n_active; S.R.n_passes = n_passes; }
     __syncthreads();
-    stream_weights<false, HALF, kHiddenPieces<HALF>>(P, maps, S, cut_rows<false>(P.hidden, n_passes, gridDim.x), base, gridDim.x, FinishDown<HALF>{P, S, n_passes});
+    const FinishDown<HALF> finish{P, S, n_passes};
+    stream_weights<false, HALF, kHiddenPieces<HALF>>(P, maps, S, cut_rows<false>(P.hidden, n_passes, gridDim.x), base, gridDim.x, finish);
+    __syncthreads();
+    finish.add_up(tid, kMoeThreads);
     __syncthreads();
     if (tid < 64 && tid >= 32) tmem_free<1>(S.tmem, kMoeTmemCols);
 }
@@ -906,7 +907,7 @@ static cudaError_t launch_moe(const MoeMaps& up, const MoeMaps& down, const MoeP
         if (cudaFuncSetAttribute(moe_down_kernel<HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMoeSmem) != cudaSuccess) return 0;
         return resident_blocks((const void*)moe_up_kernel<HALF>, kMoeCluster);
     });
-    if (!up_blocks) return cudaErrorUnknown;
+    if (!up_blocks || sm_count() < 32) return cudaErrorUnknown;
     cudaLaunchConfig_t cfg{};
     cfg.blockDim = dim3(kMoeThreads);
     cfg.dynamicSmemBytes = kMoeSmem;
