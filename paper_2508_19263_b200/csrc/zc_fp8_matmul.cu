@@ -59,13 +59,7 @@ __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 
-// A value, or 16 bytes of consecutive values, of D; they exist, and 16 bytes are aligned.
-template <typename T>
-__device__ __forceinline__ void put_one(uint8_t* row, uint32_t col, float v, uint32_t accumulate)
-{
-    T* p = reinterpret_cast<T*>(row) + col;
-    *p = from_float<T>(accumulate ? v + to_float(*p) : v);
-}
+// 16 bytes of consecutive values of D; they exist and are aligned.
 template <typename T>
 __device__ __forceinline__ void put_wide(uint8_t* row, uint32_t col, const float* v, uint32_t accumulate)
 {
@@ -77,19 +71,38 @@ __device__ __forceinline__ void put_wide(uint8_t* row, uint32_t col, const float
     for (int j = 0; j < PER; ++j) x.t[j] = from_float<T>(accumulate ? v[j] + to_float(x.t[j]) : v[j]);
     *reinterpret_cast<uint4*>(p) = x.q;
 }
-__device__ __forceinline__ void put_one(const MatmulParams& P, uint32_t row, uint32_t col, float v)
-{
-    uint8_t* r = P.out + (uint64_t)row * P.ld_out;
-    if (P.out_type == ZC_REAL_F32) put_one<float>(r, col, v, P.accumulate);
-    else if (P.out_type == ZC_REAL_BF16) put_one<__nv_bfloat16>(r, col, v, P.accumulate);
-    else put_one<__half>(r, col, v, P.accumulate);
-}
 __device__ __forceinline__ void put_wide(const MatmulParams& P, uint32_t row, uint32_t col, const float* v)
 {
     uint8_t* r = P.out + (uint64_t)row * P.ld_out;
     if (P.out_type == ZC_REAL_F32) put_wide<float>(r, col, v, P.accumulate);
     else if (P.out_type == ZC_REAL_BF16) put_wide<__nv_bfloat16>(r, col, v, P.accumulate);
     else put_wide<__half>(r, col, v, P.accumulate);
+}
+
+// The small kernel's sums from shared memory without an alignment to count on: a column a thread, so that a warp's stores lie next to
+// each other, eight at a time.  `width` is a power of two.
+template <typename T>
+__device__ __forceinline__ void put_columns(const MatmulParams& P, uint32_t base, uint32_t rows, uint32_t width, uint32_t c0, uint32_t m0, uint32_t n0)
+{
+    const uint32_t shift = 31 - __clz(width);
+    for (uint32_t first = threadIdx.x; first < rows * width; first += 8 * kMmThreads) {
+        float x[8];
+        T* p[8];
+#pragma unroll
+        for (uint32_t q = 0; q < 8; ++q) {
+            const uint32_t i = first + q * kMmThreads, row = i >> shift, col = c0 + (i & (width - 1));
+            p[q] = nullptr;
+            if (row >= rows || n0 + col >= P.n) continue;
+            p[q] = reinterpret_cast<T*>(P.out + (uint64_t)(m0 + row) * P.ld_out) + n0 + col;
+            x[q] = __uint_as_float(lds32(base + row * 512 + (((col >> 2) ^ (row & 31)) << 4) + (col & 3) * 4));
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < 8; ++q)
+            if (p[q] && P.accumulate) x[q] += to_float(*p[q]);
+#pragma unroll
+        for (uint32_t q = 0; q < 8; ++q)
+            if (p[q]) *p[q] = from_float<T>(x[q]);
+    }
 }
 
 // One tile of 128 x 128 per block; the `gridDim.z` blocks of a cluster share a tile, each takes a part of the steps, and the
@@ -241,13 +254,9 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             put_wide(P, m0 + row, n0 + col, reinterpret_cast<const float*>(v));
         }
     } else {
-        // no alignment to count on: a column a thread, so that a warp's stores lie next to each other
-        const uint32_t shift = 31 - __clz(width);            // a power of two
-#pragma unroll 4
-        for (uint32_t i = threadIdx.x; i < rows * width; i += kMmThreads) {
-            const uint32_t row = i >> shift, col = c0 + (i & (width - 1));
-            if (col < cols) put_one(P, m0 + row, n0 + col, __uint_as_float(lds32(base + row * 512 + (((col >> 2) ^ (row & 31)) << 4) + (col & 3) * 4)));
-        }
+        if (P.out_type == ZC_REAL_F32) put_columns<float>(P, base, rows, width, c0, m0, n0);
+        else if (P.out_type == ZC_REAL_BF16) put_columns<__nv_bfloat16>(P, base, rows, width, c0, m0, n0);
+        else put_columns<__half>(P, base, rows, width, c0, m0, n0);
     }
     // after a wait that gave up, copies may still be on their way into this block's shared memory
     if (*wait.failed && warp == 0 && lane == 0 && !P.skip_copy)
@@ -290,6 +299,34 @@ __device__ __forceinline__ void send(const CUtensorMap& map, uint32_t buffer, ui
     fence_async_shared();
     __syncwarp();
     if (lane == 0) tensor_store(&map, x, y, buffer);
+}
+
+// The same without an alignment to count on, or with D to be added to: 16 columns in FP32 at a time through shared memory, so that half a
+// warp's stores lie next to each other, and sixteen reads, then sixteen stores, on their way at once.
+template <typename T>
+__device__ __forceinline__ void put_rows(const MatmulParams& P, uint32_t buffer, uint32_t lane, uint32_t row0, uint32_t col0, const uint32_t v[32])
+{
+    const uint32_t e = lane & 15, odd = lane >> 4;
+#pragma unroll
+    for (uint32_t half = 0; half < 2; ++half) {
+        const uint32_t col = col0 + half * 16 + e, n = col < P.n ? min(P.m - row0, 32u) : 0;
+        __syncwarp();
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) sts128(buffer + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4), v + half * 16 + 4 * j);
+        __syncwarp();
+        float x[16];
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i) x[i] = __uint_as_float(lds32(buffer + (2 * i + odd) * 64 + (((e >> 2) ^ (i & 3)) << 4) + (e & 3) * 4));
+        uint8_t* p = P.out + (uint64_t)(row0 + odd) * P.ld_out;
+        if (P.accumulate) {
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i)
+                if (2 * i + odd < n) x[i] += to_float(reinterpret_cast<const T*>(p + 2 * i * P.ld_out)[col]);
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i)
+            if (2 * i + odd < n) reinterpret_cast<T*>(p + 2 * i * P.ld_out)[col] = from_float<T>(x[i]);
+    }
 }
 
 __device__ __forceinline__ void large_tile(const MatmulParams& P, uint32_t i, uint32_t& m, uint32_t& n)
@@ -450,20 +487,11 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                         send(map_d, results + (sent++ & 1) * kResultBytes, lane, (int)col0, (int)row0, w);
                     }
                 } else {
-                    // no alignment to count on, or D to be added to: 16 columns in FP32 at a time through shared memory, so that
-                    // half a warp's stores lie next to each other
                     const uint32_t row0 = tm * 256 + rank * 128 + quad * 32, col0 = tn * 256 + c * 32;
                     if (row0 >= P.m || col0 >= P.n) continue;
-#pragma unroll
-                    for (uint32_t half = 0; half < 2; ++half) {
-                        __syncwarp();
-#pragma unroll
-                        for (uint32_t j = 0; j < 4; ++j) sts128(results + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4), v + half * 16 + 4 * j);
-                        __syncwarp();
-                        const uint32_t e = lane & 15, col = col0 + half * 16 + e;
-                        for (uint32_t r = lane >> 4; r < 32 && row0 + r < P.m; r += 2)
-                            if (col < P.n) put_one(P, row0 + r, col, __uint_as_float(lds32(results + r * 64 + (((e >> 2) ^ ((r >> 1) & 3)) << 4) + (e & 3) * 4)));
-                    }
+                    if (P.out_type == ZC_REAL_F32) put_rows<float>(P, results, lane, row0, col0, v);
+                    else if (P.out_type == ZC_REAL_BF16) put_rows<__nv_bfloat16>(P, results, lane, row0, col0, v);
+                    else put_rows<__half>(P, results, lane, row0, col0, v);
                 }
             }
         }
