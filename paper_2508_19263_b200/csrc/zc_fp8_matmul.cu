@@ -276,7 +276,8 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 // first, and the next tile's instructions begin when they have, while the other 224 columns are still on their way out.
 constexpr uint32_t kLargeStages = 6;
 constexpr uint32_t kResultBytes = 32 * 64;       // what a warp sends off at a time: 32 rows x 64 bytes
-constexpr size_t kLargeSmem = 1024 + kLargeStages * 2 * kTileBytes + 8 * kResultBytes + kScaleBufs * kScaleBufBytes + sizeof(MatmulShared);
+constexpr uint32_t kResultBufs = 3;              // per warp
+constexpr size_t kLargeSmem = 1024 + kLargeStages * 2 * kTileBytes + 4 * kResultBufs * kResultBytes + kScaleBufs * kScaleBufBytes + sizeof(MatmulShared);
 constexpr uint32_t kLargeCols = 512, kLargeSecond = 224, kLargeScales = 480;     // two sets of 4 + 8 scale columns
 constexpr uint32_t kSwath = 8;                   // rows of tiles that are walked through together, column by column
 
@@ -288,17 +289,18 @@ __device__ __forceinline__ uint32_t pack_pair(const uint32_t v[2])
     x.t[1] = from_float<T>(__uint_as_float(v[1]));
     return x.w;
 }
-// A warp's 32 rows of 64 bytes, a row per lane, into one of its two buffers and off; the copy before the last one has been
-// read by then.
+// A warp's 32 rows of 64 bytes, a row per lane, into the next of its buffers and off; what was sent from there last has been read
+// by then.
 __device__ __forceinline__ void send(const CUtensorMap& map, uint32_t buffer, uint32_t lane, int x, int y, const uint32_t w[16])
 {
-    if (lane == 0) tensor_store_wait_read<1>();
+    const bool one = elect_one();                // the same lane every time: groups are a thread's own
+    if (one) tensor_store_wait_read<kResultBufs - 1>();
     __syncwarp();
 #pragma unroll
     for (uint32_t j = 0; j < 4; ++j) sts128(buffer + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4), w + 4 * j);
     fence_async_shared();
     __syncwarp();
-    if (lane == 0) tensor_store(&map, x, y, buffer);
+    if (one) tensor_store(&map, x, y, buffer);
 }
 
 // The same without an alignment to count on, or with D to be added to: 16 columns in FP32 at a time through shared memory, so that half a
@@ -343,7 +345,7 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 {
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    const uint32_t results_at = base + kLargeStages * 2 * kTileBytes, words_at = results_at + 8 * kResultBytes;
+    const uint32_t results_at = base + kLargeStages * 2 * kTileBytes, words_at = results_at + 4 * kResultBufs * kResultBytes;
     MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (words_at - smem_u32(raw)) + kScaleBufs * kScaleBufBytes);
     const uint32_t warp = warp_index(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = P.tiles_m * P.tiles_n;
@@ -462,7 +464,7 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             large_tile(P, i, tm, tn);
             if (!__all_sync(0xFFFFFFFFu, wait(smem_u32(&S->acc_full[tile & 1]), (tile >> 1) & 1) && !*wait.failed)) break;
             tc_fence_after();
-            const uint32_t d = tmem + (quad * 32u << 16) + (tile & 1 ? kLargeSecond : 0), results = results_at + quad * 2 * kResultBytes;
+            const uint32_t d = tmem + (quad * 32u << 16) + (tile & 1 ? kLargeSecond : 0), results = results_at + quad * kResultBufs * kResultBytes;
 #pragma unroll 1
             for (uint32_t q = 0; q < 8; ++q) {
                 const uint32_t c = tile & 1 ? q : (q + 7) & 7;           // the shared columns first
@@ -478,13 +480,13 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                     const uint32_t row0 = tm * 256 + rank * 128 + quad * 32, col0 = tn * 256 + c * 32;
                     if (row0 >= P.m || col0 >= P.n) continue;
                     if (P.out_type == ZC_REAL_F32) {
-                        send(map_d, results + (sent++ & 1) * kResultBytes, lane, (int)col0, (int)row0, v);
-                        if (col0 + 16 < P.n) send(map_d, results + (sent++ & 1) * kResultBytes, lane, (int)col0 + 16, (int)row0, v + 16);
+                        send(map_d, results + (sent++ % kResultBufs) * kResultBytes, lane, (int)col0, (int)row0, v);
+                        if (col0 + 16 < P.n) send(map_d, results + (sent++ % kResultBufs) * kResultBytes, lane, (int)col0 + 16, (int)row0, v + 16);
                     } else {
                         uint32_t w[16];
 #pragma unroll
                         for (int j = 0; j < 16; ++j) w[j] = P.out_type == ZC_REAL_BF16 ? pack_pair<__nv_bfloat16>(v + 2 * j) : pack_pair<__half>(v + 2 * j);
-                        send(map_d, results + (sent++ & 1) * kResultBytes, lane, (int)col0, (int)row0, w);
+                        send(map_d, results + (sent++ % kResultBufs) * kResultBytes, lane, (int)col0, (int)row0, w);
                     }
                 } else {
                     const uint32_t row0 = tm * 256 + rank * 128 + quad * 32, col0 = tn * 256 + c * 32;
@@ -495,7 +497,8 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 }
             }
         }
-        if (lane == 0) tensor_store_wait_read<0>();
+        __syncwarp();
+        if (elect_one()) tensor_store_wait_read<0>();
     }
     __syncwarp();
     tc_fence_before();
