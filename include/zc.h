@@ -476,8 +476,8 @@ zc_status zc_fp8_quantize(zc_real in_type, const void* d_in, uint64_t ld_in, con
 zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real out_type, void* d_out, uint64_t ld_out,
                         uint32_t accumulate, void* cuda_stream);
 
-/* Waits for the stream, returns and clears what zc_fp8_matmul and zc_fp8_moe calls on the current device have left since the last
- * query: ZC_OK or ZC_E_DEVICE_TIMEOUT.  Not inside a stream capture. */
+/* Waits for the stream, returns and clears what zc_fp8_matmul and zc_fp8_moe calls on the current device have left since
+ * the last query: ZC_OK or ZC_E_DEVICE_TIMEOUT.  Not inside a stream capture. */
 zc_status zc_fp8_status(void* cuda_stream);
 
 /* A mixture-of-experts layer for a few tokens (1 to ZC_FP8_MOE_MAX_TOKENS).  For a token x:
@@ -487,8 +487,7 @@ zc_status zc_fp8_status(void* cuda_stream);
  * row.  Only the experts that a token chose are read.  Sums are FP32, those of the router FP64 over parts of 64
  * columns.  x is used to 2^-25 of the largest magnitude of its 128 columns, and exactly where it is above 2^-17 of it; the
  * hidden vector of an expert is kept with 11 bits (BF16 layers) or 15 bits (FP16 layers) of precision; an infinity in either
- * gives NaN.  Rows are read in pieces of 16 bytes: of every row, the last one included, the whole pitch belongs to the
- * buffer.  A wait inside a kernel that gives up leaves the outputs undefined and is reported by zc_fp8_status. */
+ * gives NaN.  A wait inside a kernel that gives up leaves the outputs undefined and is reported by zc_fp8_status. */
 typedef struct zc_fp8_moe_layer {
     const void* d_router;       /* [n_experts][hidden] of real_type, row pitch ld_router elements */
     const void* d_gate_up;      /* [n_experts][2][inter] rows of hidden bytes, row pitch ld_gate_up bytes: gate, then up */

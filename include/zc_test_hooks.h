@@ -26,7 +26,8 @@ zc_status zc_test_merge16(zc_format fmt, const uint8_t* h_e8, const uint8_t* h_s
  *   zc_test_set_wait_limit  polls after which a device-side wait gives up
  *   zc_test_stall_encoder   zc_compress hands out its batches from this number on, so batch 0 is
  *                           never packed and every look-back waits for a word nobody posts
- *   zc_test_stall_decoder   the decoder does not start the copies of the pieces it waits for */
+ *   zc_test_stall_decoder   the decoder does not start the copies of the pieces it waits for, nor do
+ *                           zc_fp8_matmul and zc_fp8_moe those of their operands */
 /* Launch shapes (host arithmetic only, no GPU): worker warps per block the encoder would use for a plan with n_coded
  * Huffman-coded streams (0..2), with or without a base tensor, in a launch of total_chunks chunks, and warps per block of
  * the decoder with one or both streams coded.  0 = the kernels cannot take this plan: more workers than the kernel is

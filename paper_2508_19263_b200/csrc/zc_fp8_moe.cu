@@ -371,9 +371,16 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
                             raw[i] = make_uint4(0, 0, 0, 0);
                             if (c + i >= t.count || col >= cols) continue;
                             if (UP) {
-                                const uint2 v = __ldg(reinterpret_cast<const uint2*>(P.x + 2 * ((uint64_t)S.row_token[t.row + c + i] * P.ld_x + col)));
-                                raw[i].x = v.x;
-                                raw[i].y = v.y;
+                                const uint8_t* x = P.x + 2 * ((uint64_t)S.row_token[t.row + c + i] * P.ld_x + col);
+                                if (col + 4 <= cols) {
+                                    const uint2 v = __ldg(reinterpret_cast<const uint2*>(x));
+                                    raw[i].x = v.x;
+                                    raw[i].y = v.y;
+                                } else {                     // a row may end where its buffer does
+                                    const uint16_t* e = reinterpret_cast<const uint16_t*>(x);
+                                    raw[i].x = e[0] | (col + 1 < cols ? (uint32_t)e[1] << 16 : 0u);
+                                    raw[i].y = col + 2 < cols ? e[2] : 0u;
+                                }
                             } else {
                                 raw[i] = *reinterpret_cast<const uint4*>(P.h + (uint64_t)(t.row + c + i) * P.inter_pad + col);
                             }

@@ -230,6 +230,56 @@ def test_streams_and_graphs():
         assert torch.equal(out.view(torch.uint8), eager.view(torch.uint8))
 
 
+def test_kernels_that_start_early_wait_for_those_before():
+    # every kernel here may be on the GPU before the one in front of it is done: inputs that change from pass to pass, without a wait
+    b = operand(384, 512, 2, 128, 22)
+    xs = [torch.randn((129, 512), generator=torch.Generator(device=DEV).manual_seed(i), device=DEV).bfloat16() for i in range(40)]
+    wants = []
+    for x in xs:
+        q, d = zc.fp8_empty(129, 512), torch.empty((129, 384), device=DEV)
+        zc.fp8_matmul(zc.fp8_quantize(x, q), b, d)
+        torch.cuda.synchronize()
+        wants.append(d)
+    x, q, d = torch.empty_like(xs[0]), zc.fp8_empty(129, 512), torch.empty((129, 384), device=DEV)
+    outs = [torch.empty_like(d) for _ in xs]
+    for src, out in zip(xs, outs):
+        x.copy_(src)
+        zc.fp8_quantize(x, q)
+        zc.fp8_matmul(q, b, d)
+        out.copy_(d)
+    assert all(torch.equal(a, w) for a, w in zip(outs, wants))
+
+
+def test_offsets_beyond_32_bits():
+    rows, cols = 66000, 33000                                                # 2.2e9 elements: FP8 offsets pass 2^31, BF16 ones 2^32
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(31)
+    tail = torch.randn((300, cols), generator=g, device=DEV).bfloat16()
+    x[-300:] = tail
+    q = zc.fp8_quantize(x, zc.fp8_empty(rows, cols))
+    del x
+    elems, scales, _ = ref.quantize(tail.double().cpu().numpy(), zc.FMT_FP8_E4M3, 1)
+    assert np.array_equal(q.elems[-300:].cpu().numpy(), elems) and np.array_equal(q.scales[-300:].cpu().numpy(), scales)
+    assert not bool(q.elems[:1000].any())
+    b = operand(40, cols, 2, 1, 32)
+    b.elems &= 0xBF
+    d = torch.empty((rows, 40), device=DEV)
+    zc.fp8_matmul(q, b, d)
+    last = zc.Fp8Matrix(q.elems[-300:], q.scales[-300:], zc.FMT_FP8_E4M3, 1)
+    want, magnitude = exact(last, b)
+    assert near(d[-300:], want, magnitude, cols) and not bool(d[:-300].any())
+    del q, last, d
+    # a result of 4.5 GB: the last rows and the first
+    a, b = operand(70000, 128, 2, 1, 33), operand(16000, 128, 2, 1, 34)
+    for m in (a, b):
+        m.elems &= 0xBF
+    d = torch.empty((70000, 16000), device=DEV)
+    zc.fp8_matmul(a, b, d)
+    for part in (slice(0, 50), slice(69950, 70000)):
+        want, magnitude = exact(zc.Fp8Matrix(a.elems[part], a.scales[part], a.format, 1), b)
+        assert near(d[part], want, magnitude, 128)
+
+
 def test_a_wait_that_runs_out_is_reported_and_later_calls_work():
     a, b = operand(256, 2048, 2, 1, 13), operand(512, 2048, 2, 128, 14)
     d = torch.empty((256, 512), device=DEV)

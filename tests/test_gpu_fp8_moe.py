@@ -129,9 +129,11 @@ def test_moe(tokens, experts, top_k, hidden, inter, fmt, real):
     assert all(torch.equal(a, b) for a, b in zip(got, again))                # the same every time
 
 
-def test_ties_go_to_the_lowest_index_and_all_tokens_may_choose_one_expert():
-    # all logits equal: experts 0 .. top_k - 1 for every token; the lists are as long as they get
-    L = Layer(70, 4, 256, 128, zc.FMT_FP8_E4M3, torch.bfloat16, 5, router=torch.zeros((70, 256), device=DEV))
+@pytest.mark.parametrize("real", list(REAL))
+@pytest.mark.parametrize("experts", [70, 8])
+def test_ties_go_to_the_lowest_index_and_all_tokens_may_choose_one_expert(real, experts):
+    # all logits equal: experts 0 .. top_k - 1 for every token; the lists are as long as they get, in passes of 16 and of 32 tokens
+    L = Layer(experts, 4, 256, 128, zc.FMT_FP8_E4M3, REAL[real], 5, router=torch.zeros((experts, 256), device=DEV))
     x = L.tokens(64, 1)
     y, ids, weights = L.run(x)
     assert ids.cpu().tolist() == [[0, 1, 2, 3]] * 64 and bool((weights == 0.25).all())
@@ -154,6 +156,15 @@ def test_a_token_of_nan_and_infinities_stays_by_itself():
     assert np.array_equal(ids[keep].cpu().numpy(), want_ids)
     assert torch.equal(ids[keep], clean[1][keep])
     assert (np.abs(y[keep].double().cpu().numpy() - want) <= bound + 2.0 ** -8 * (np.abs(want) + bound) + 2.0 ** -134).all()
+
+
+def test_a_token_whose_buffer_ends_with_it():
+    # one token of an odd width, no pitch behind it; what follows in the allocation is NaN
+    L = Layer(4, 2, 513, 64, zc.FMT_FP8_E4M3, torch.bfloat16, 10)
+    buf = torch.full((1024,), float("nan"), dtype=torch.bfloat16, device=DEV)
+    x = buf[:513].view(1, 513)
+    x.copy_(L.tokens(1, 6))
+    check(L, x, L.run(x))
 
 
 def test_graph_streams_and_shared_weights():
