@@ -36,12 +36,6 @@ inline zc_status check_matrix(const zc_fp8_matrix* m)
 
 zc_status moe_read_timeout(cudaStream_t st);              // zc_fp8_status, for the kernels of zc_fp8_moe
 
-// 2^(s-127) of a scale byte; 255 is NaN.  Bit pattern s << 23 but for 2^-127, which is subnormal in FP32.
-__device__ __forceinline__ float scale_value(uint32_t s)
-{
-    return __uint_as_float(s == 255u ? 0x7FC00000u : s ? s << 23 : 0x00400000u);
-}
-
 __device__ __forceinline__ float finite_abs(float v)
 {
     const float a = fabsf(v);
@@ -91,7 +85,9 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr)
 
 // ---- programmatic dependent launch ----
 // A kernel may be on the GPU, and set up its barriers and tensor memory, while the one before it in the stream ends; it
-// touches nothing that other kernels read or write before grid_wait(), which waits for all of them.
+// touches nothing that other kernels read or write before grid_wait(), which waits for all of them.  It lets the next one in
+// only after that, so that no more than two of a stream's kernels are there at a time and what the next one reads is not still
+// being read, and cached, by the one before this.
 inline cudaLaunchAttribute launch_early()
 {
     cudaLaunchAttribute a{};

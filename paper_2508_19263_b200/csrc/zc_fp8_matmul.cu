@@ -139,8 +139,8 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = S->tmem;
-    grid_launch_dependents();
     grid_wait();                                 // what the kernels before this one wrote is there
+    grid_launch_dependents();
 
     uint32_t st = 0, round = 0;
     if (warp == 0) {
@@ -367,8 +367,8 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     cluster_sync();                              // the pair's barriers are there before either block uses them
     tc_fence_after();
     const uint32_t tmem = S->tmem;
-    grid_launch_dependents();
     grid_wait();                                 // what the kernels before this one wrote is there
+    grid_launch_dependents();
 
     if (warp == 0) {
         // both blocks copy their halves; the bytes count on the first block's barrier

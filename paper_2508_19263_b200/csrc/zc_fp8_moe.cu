@@ -9,11 +9,11 @@
 // (8 and 11 bits) down to 2^-17 of the largest of the 128, and nothing smaller is off by more than 2^-25 of it.  The
 // pieces are rows of the same operand, so they cost columns of the accumulator, and their sum is taken in FP32 at the end.
 //
-// Rows are handed out in groups of eight, the swizzle's height: tiles of all chosen experts form one sequence of groups that is cut
-// into equal ranges, one per block.
+// Rows are handed out in groups of eight, the swizzle's height, in tiles whose height is chosen so that the blocks get equal numbers
+// of them (cut_rows); the tiles of all chosen experts form one sequence, of which each block takes a stretch.
 //
 //   kernel 1  routes (every cluster for itself, so that no block waits for another cluster), then gate and up: a tile is up to 64
-//             rows of gate and the same of up in alternating groups, so that a warp ends with both
+//             rows of gate and the same rows of up; the result warps of the two give each other half of the tokens
 //   kernel 2  down: up to 128 rows a tile, one FP32 row of partial results per (token, expert); the block that completes a
 //             group's last expert adds the experts up in the order of the token's list, when it has done all its tiles
 //
@@ -784,8 +784,8 @@ moe_up_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ MoeP
 
     if (tid < kMoeHeights) prefetch_map(&maps.of[tid]);
     moe_setup(S, kBuilders / stage_count(P.pass, 3));
-    grid_launch_dependents();
     grid_wait();
+    grid_launch_dependents();
     router_logits<HALF>(P, rank, T);
     cluster_sync();
     choose(P, rank, T);
@@ -835,8 +835,8 @@ moe_down_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ Mo
     const uint32_t tid = threadIdx.x;
     if (tid < kMoeHeights) prefetch_map(&maps.of[tid]);
     moe_setup(S, kBuilders / stage_count(P.pass, kHiddenPieces<HALF>));
-    grid_launch_dependents();
     grid_wait();
+    grid_launch_dependents();
     // all of the lists at once, whatever is behind the last chosen expert: one latency
     const uint32_t n_active = P.route[0], n_passes = P.route[1];
     if (tid <= kMaxExperts) {

@@ -150,7 +150,6 @@ template <typename T, bool E5M2, bool WIDE>
 __global__ void __launch_bounds__(kQuantThreads)
 quantize_rows_kernel(const __grid_constant__ QuantParams P)
 {
-    grid_launch_dependents();
     const uint32_t sub = threadIdx.x & 7;
     const uint32_t n_blocks = P.rows * P.col_blocks;
     const uint32_t block = (blockIdx.x * kQuantThreads + threadIdx.x) >> 3;
@@ -159,6 +158,7 @@ quantize_rows_kernel(const __grid_constant__ QuantParams P)
     const uint32_t col = cb * 128 + sub * 16;
     const uint32_t n = block < n_blocks && col < P.cols ? P.cols - col : 0;
     grid_wait();
+    grid_launch_dependents();
     const Raw<T> r = load16<T, WIDE>(P, P.in + (uint64_t)row * P.ld_in + (uint64_t)col * sizeof(T), n);
     bool odd;
     uint32_t m = largest(r, odd);
@@ -187,8 +187,8 @@ quantize_tile_kernel(const __grid_constant__ QuantParams P)
     __shared__ __align__(16) uint32_t s_bytes[TRANS ? 128 * 32 : 1];     // [column][row / 4], turned by 4 words per 16 columns
     __shared__ uint32_t s_max[8][SQUARE ? 1 : 8 * W];
     __shared__ uint32_t s_scale[SQUARE || !TRANS ? 1 : 128];
-    grid_launch_dependents();
     grid_wait();
+    grid_launch_dependents();
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rb = blockIdx.x / P.col_blocks, cb = blockIdx.x - rb * P.col_blocks;
     const uint32_t sub = tid & 7, rg = tid >> 3;
