@@ -486,8 +486,8 @@ zc_status zc_fp8_status(void* cuda_stream);
  * The weights are FP8 with 128 x 128 blocks; every expert's matrix has scale bytes of its own, beginning with its first
  * row.  Only the experts that a token chose are read.  Sums are FP32, those of the router FP64 over parts of 64
  * columns.  x is used to 2^-25 of the largest magnitude of its 128 columns, and exactly where it is above 2^-17 of it; the
- * hidden vector of an expert is kept with 11 bits (BF16 layers) or 15 bits (FP16 layers) of precision; an infinity in either
- * gives NaN.  A wait inside a kernel that gives up leaves the outputs undefined and is reported by zc_fp8_status. */
+ * hidden vector of an expert goes into the second product with 18 bits of precision, and to 2^-29 of the largest magnitude of
+ * its 128 columns; an infinity in either gives NaN.  A wait inside a kernel that gives up leaves the outputs undefined and is reported by zc_fp8_status. */
 typedef struct zc_fp8_moe_layer {
     const void* d_router;       /* [n_experts][hidden] of real_type, row pitch ld_router elements */
     const void* d_gate_up;      /* [n_experts][2][inter] rows of hidden bytes, row pitch ld_gate_up bytes: gate, then up */

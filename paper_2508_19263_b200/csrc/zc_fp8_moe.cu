@@ -5,9 +5,10 @@
 // touches a weight.  (Widening them in registers for warp-wide BF16 instructions took 350 instructions per KiB and ran at a
 // sixth of the memory's rate.)  The instruction wants FP8 on the other side as well, so an activation is written as a sum of
 // E4M3 pieces, v = 2^s (q0 + 2^-4 q1 + 2^-8 q2 + ...), with s from the largest magnitude of 128 columns: q_i is what the
-// pieces before it leave, rounded, and each piece takes at least four bits more.  Three pieces hold BF16 and FP16 exactly
-// (8 and 11 bits) down to 2^-17 of the largest of the 128, and nothing smaller is off by more than 2^-25 of it.  The
-// pieces are rows of the same operand, so they cost columns of the accumulator, and their sum is taken in FP32 at the end.
+// pieces before it leave, rounded.  The first leaves 2^-4 of the value, every other one, with four bits and a sign for what is at
+// most half a step, 2^-5 of that.  Three pieces hold BF16 and FP16 exactly (8 and 11 bits) down to 2^-17 of the largest of
+// the 128, and nothing smaller is off by more than 2^-25 of it.  The pieces are rows of the same operand, so they cost columns of
+// the accumulator, and their sum is taken in FP32 at the end.
 //
 // Rows are handed out in groups of eight, the swizzle's height, in tiles whose height is chosen so that the blocks get equal numbers
 // of them (cut_rows); the tiles of all chosen experts form one sequence, of which each block takes a stretch.
@@ -198,7 +199,8 @@ __device__ __forceinline__ __half2 of_pieces(uint32_t q)
 }
 
 // Four activations of a lane as PIECES E4M3 words, in the block scale of the warp's 128 columns.  FP16 holds what is left behind a
-// piece: exactly for BF16 and FP16 activations (EXACT), to 2^-16 of the value for FP32 ones, whose first piece is split off in FP32.
+// piece: exactly for BF16 and FP16 activations (EXACT); of FP32 ones it holds what is left behind the second, at most 2^-9 of the value,
+// to 2^-12 of that.  What is left behind the pieces before is exact in FP32.
 template <int PIECES, bool EXACT>
 __device__ __forceinline__ void make_pieces(float v[4], uint32_t words[PIECES], uint32_t& scale)
 {
@@ -225,15 +227,20 @@ __device__ __forceinline__ void make_pieces(float v[4], uint32_t words[PIECES], 
         a = __floats2half2_rn(f[0], f[1]);
         b = __floats2half2_rn(f[2], f[3]);
     } else {
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
-        words[0] = lo | (hi << 16);
-        const float2 x = __half22float2(of_pieces(lo)), y = __half22float2(of_pieces(hi));
-        a = __floats2half2_rn((f[0] - x.x) * 16.0f, (f[1] - x.y) * 16.0f);
-        b = __floats2half2_rn((f[2] - y.x) * 16.0f, (f[3] - y.y) * 16.0f);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
+            const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
+            words[k] = scale >= 4u * k ? lo | (hi << 16) : 0u;
+            const float2 x = __half22float2(of_pieces(lo)), y = __half22float2(of_pieces(hi));
+            f[0] = (f[0] - x.x) * 16.0f; f[1] = (f[1] - x.y) * 16.0f;
+            f[2] = (f[2] - y.x) * 16.0f; f[3] = (f[3] - y.y) * 16.0f;
+        }
+        a = __floats2half2_rn(f[0], f[1]);
+        b = __floats2half2_rn(f[2], f[3]);
     }
 #pragma unroll
-    for (int k = EXACT ? 0 : 1; k < PIECES; ++k) {
+    for (int k = EXACT ? 0 : 2; k < PIECES; ++k) {
         const uint32_t lo = to_pieces(a), hi = to_pieces(b);
         // scales end at 2^-127: what would need a smaller one is left out
         words[k] = scale >= 4u * k ? lo | (hi << 16) : 0u;
@@ -767,8 +774,10 @@ struct FinishDown {
     }
 };
 
-// hidden vectors: twelve bits in three pieces err a sixteenth of what rounding y to BF16 does; FP16 takes sixteen in four
-template <bool HALF> constexpr int kHiddenPieces = HALF ? 4 : 3;
+// Hidden vectors, FP32 in memory, go into the product as four pieces: 2^-19 of the value and 2^-21 for what FP16 holds of it, a
+// thousandth of half a step of y in BF16, a hundredth in FP16.  (Three pieces of BF16 layers left 2^-14: y of 64 tokens and 64 experts was
+// 2.5e-4 from that of an FP32 form, 7.3e-5 with four, both in 119 us: the builders have the time.)
+constexpr int kHiddenPieces = 4;
 
 template <bool HALF>
 __global__ void __launch_bounds__(kMoeThreads, 1)
@@ -834,7 +843,7 @@ moe_down_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ Mo
     MoeShared& S = *reinterpret_cast<MoeShared*>(raw + (base - smem_u32(raw)) + kMoeStageSpace);
     const uint32_t tid = threadIdx.x;
     if (tid < kMoeHeights) prefetch_map(&maps.of[tid]);
-    moe_setup(S, kBuilders / stage_count(P.pass, kHiddenPieces<HALF>));
+    moe_setup(S, kBuilders / stage_count(P.pass, kHiddenPieces));
     grid_wait();
     grid_launch_dependents();
     // all of the lists at once, whatever is behind the last chosen expert: one latency
@@ -849,7 +858,7 @@ moe_down_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ Mo
     if (tid == 0) { S.R.n_active = n_active; S.R.n_passes = n_passes; }
     __syncthreads();
     const FinishDown<HALF> finish{P, S, n_passes};
-    stream_weights<false, HALF, kHiddenPieces<HALF>>(P, maps, S, cut_rows<false>(P.hidden, n_passes, gridDim.x), base, gridDim.x, finish);
+    stream_weights<false, HALF, kHiddenPieces>(P, maps, S, cut_rows<false>(P.hidden, n_passes, gridDim.x), base, gridDim.x, finish);
     __syncthreads();
     finish.add_up(tid, kMoeThreads);
     __syncthreads();
