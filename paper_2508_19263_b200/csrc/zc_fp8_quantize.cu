@@ -152,7 +152,7 @@ quantize_rows_kernel(const __grid_constant__ QuantParams P)
 {
     const uint32_t sub = threadIdx.x & 7;
     const uint32_t n_blocks = P.rows * P.col_blocks;
-    const uint32_t block = (blockIdx.x * kQuantThreads + threadIdx.x) >> 3;
+    const uint32_t block = blockIdx.x * (kQuantThreads / 8) + (threadIdx.x >> 3);    // the threads' numbers would pass 32 bits
     // lanes behind the last block keep to the shuffles with nothing to load
     const uint32_t row = block / P.col_blocks, cb = block - row * P.col_blocks;
     const uint32_t col = cb * 128 + sub * 16;
