@@ -27,7 +27,11 @@ zc_status zc_test_merge16(zc_format fmt, const uint8_t* h_e8, const uint8_t* h_s
  *   zc_test_stall_encoder   zc_compress hands out its batches from this number on, so batch 0 is
  *                           never packed and every look-back waits for a word nobody posts
  *   zc_test_stall_decoder   the decoder does not start the copies of the pieces it waits for, nor do
- *                           zc_fp8_matmul and zc_fp8_moe those of their operands */
+ *                           zc_fp8_matmul and zc_fp8_moe those of their operands
+ *   zc_test_stall_math      zc_fp8_matmul and zc_fp8_moe copy their operands but start no matrix
+ *                           instruction, so that they give up with copies under way
+ *   zc_test_fp8_marks       what the last zc_fp8_status found: 1 a wait gave up, 2 a block that gave up waited until what
+ *                           it had under way was done, 4 it waited for that in vain */
 /* Launch shapes (host arithmetic only, no GPU): worker warps per block the encoder would use for a plan with n_coded
  * Huffman-coded streams (0..2), with or without a base tensor, in a launch of total_chunks chunks, and warps per block of
  * the decoder with one or both streams coded.  0 = the kernels cannot take this plan: more workers than the kernel is
@@ -42,6 +46,8 @@ uint32_t zc_test_decoder_pieces(const zc_plan_t* plan, uint32_t any_base, uint64
 void zc_test_set_wait_limit(uint32_t polls);
 void zc_test_stall_encoder(uint32_t first_ticket);
 void zc_test_stall_decoder(uint32_t on);
+void zc_test_stall_math(uint32_t on);
+uint32_t zc_test_fp8_marks(void);
 /* Development build of the library (compiled with -DZC_DEBUG_CHECKS=1): every shared-memory and global-memory
  * access the kernels make through their load/store helpers is checked against the block's shared window and the
  * buffers of the launch; a violation is counted and the access skipped (no trap, no fault).  This call waits for the

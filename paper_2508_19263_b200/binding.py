@@ -165,6 +165,8 @@ def _load():
     L.zc_test_decoder_pieces.argtypes = [vp, C.c_uint32, C.c_uint64, C.POINTER(C.c_uint32)]
     L.zc_test_debug_counts.restype = C.c_int
     L.zc_test_debug_counts.argtypes = [C.POINTER(C.c_uint32)]
+    L.zc_test_fp8_marks.restype = C.c_uint32
+    L.zc_test_fp8_marks.argtypes = []
     L.zc_fp8_quantize.restype = C.c_int
     L.zc_fp8_quantize.argtypes = [C.c_int, vp, C.c_uint64, vp, vp, vp]
     L.zc_fp8_matmul.restype = C.c_int
@@ -175,7 +177,7 @@ def _load():
     L.zc_fp8_moe.argtypes = [vp, C.c_uint32, vp, C.c_uint64, vp, C.c_uint64, vp, vp, vp, C.c_size_t, vp]
     L.zc_fp8_status.restype = C.c_int
     L.zc_fp8_status.argtypes = [vp]
-    for name in ("zc_test_set_wait_limit", "zc_test_stall_encoder", "zc_test_stall_decoder"):
+    for name in ("zc_test_set_wait_limit", "zc_test_stall_encoder", "zc_test_stall_decoder", "zc_test_stall_math"):
         getattr(L, name).restype = None
         getattr(L, name).argtypes = [C.c_uint32]
     return L
@@ -721,6 +723,16 @@ def test_stall_encoder(first_ticket: int) -> None:
 def test_stall_decoder(on: bool) -> None:
     """zc_test_stall_decoder."""
     _lib.zc_test_stall_decoder(1 if on else 0)
+
+
+def test_stall_math(on: bool) -> None:
+    """zc_test_stall_math."""
+    _lib.zc_test_stall_math(1 if on else 0)
+
+
+def test_fp8_marks() -> int:
+    """zc_test_fp8_marks."""
+    return int(_lib.zc_test_fp8_marks())
 
 
 def test_debug_counts():

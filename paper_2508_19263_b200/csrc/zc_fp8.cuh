@@ -34,7 +34,7 @@ inline zc_status check_matrix(const zc_fp8_matrix* m)
     return ZC_OK;
 }
 
-zc_status moe_read_timeout(cudaStream_t st);              // zc_fp8_status, for the kernels of zc_fp8_moe
+zc_status moe_read_marks(cudaStream_t st, uint32_t* marks);   // zc_fp8_status, for the kernels of zc_fp8_moe
 
 __device__ __forceinline__ float finite_abs(float v)
 {
@@ -139,6 +139,12 @@ __device__ __forceinline__ uint32_t map_shared(uint32_t addr, uint32_t rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr)
 {
     float4 v;
@@ -154,6 +160,11 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+// bytes that nobody will copy count as copied
+__device__ __forceinline__ void bar_forgo(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
 }
 // Ordered within the block only.  At the cluster's scope every arrival waits for the thread's earlier writes and every wait
 // drops the L1: 0.8 us a step of the mixture-of-experts kernels instead of 0.4.

@@ -32,7 +32,7 @@ struct MatmulParams {
     uint32_t rows_a, rows_b;
     uint32_t stages;                             // of the small kernel
     uint32_t by_copy;                            // the large kernel's results leave by tensor copies
-    uint32_t spin_limit, skip_copy;
+    uint32_t spin_limit, skip_copy, skip_math;
 };
 
 // The scale words of four steps are a warp's own work, in turn with three others: each has the time of sixteen steps for the
@@ -46,8 +46,9 @@ constexpr uint32_t kScaleBufBytes = 512 + 1024;  // 128 rows of A, up to 256 of 
 struct MatmulShared {
     uint64_t full[8], empty[8];
     uint64_t sf_full[kScaleBufs], sf_empty[kScaleBufs];
-    uint64_t acc_full[2], acc_empty[1];
-    uint32_t tmem, failed;
+    uint64_t acc_full[2], acc_empty[1], settled;
+    uint32_t tmem, failed, unsettled;            // unsettled: copies or matrix instructions that this block did not see the end of
+    uint32_t copied;                             // steps whose copies the block has started
 };
 
 
@@ -131,7 +132,7 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         for (uint32_t i = 0; i < stages; ++i) { bar_init(smem_u32(&S->full[i]), 1); bar_init(smem_u32(&S->empty[i]), 1); }
         for (uint32_t i = 0; i < kScaleBufs; ++i) { bar_init(smem_u32(&S->sf_full[i]), 1); bar_init(smem_u32(&S->sf_empty[i]), 1); }
         bar_init(smem_u32(&S->acc_full[0]), 1);
-        S->failed = 0;
+        S->failed = S->unsettled = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc<1>(smem_u32(&S->tmem), kSmallCols);
@@ -156,7 +157,7 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             }
             if (++st == stages) { st = 0; ++round; }
         }
-    } else if (warp == 1) {
+    } else if (warp == 1 && !P.skip_math) {
         for (uint32_t i = 0; i < hi - lo; ++i) {
             const uint32_t word = i >> 2, buf = word % kScaleBufs;
             const uint32_t sfa = tmem + kSmallScales + (word & 1) * 8, sfb = sfa + 4;
@@ -258,13 +259,12 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         else if (P.out_type == ZC_REAL_BF16) put_columns<__nv_bfloat16>(P, base, rows, width, c0, m0, n0);
         else put_columns<__half>(P, base, rows, width, c0, m0, n0);
     }
-    // after a wait that gave up, copies may still be on their way into this block's shared memory
-    if (*wait.failed && warp == 0 && lane == 0 && !P.skip_copy)
-        for (uint32_t i = 0; i < stages; ++i) {
-            const uint32_t r = i < st ? round : round - 1;
-            if (round == 0 && i >= st) continue;
-            for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S->full[i]), r & 1); ++q) { }
-        }
+    if (*wait.failed) {                          // whichever role gave up: see what copies and instructions are still under way
+        if (warp == 0 && !P.skip_copy && !settled_stage(smem_u32(S->full), lane, stages, st, round, P.spin_limit)) S->unsettled = 1;
+        if (warp == 1 && lane == 0 && !P.skip_math && !settled(smem_u32(&S->acc_full[0]), 0, P.spin_limit)) S->unsettled = 1;
+        __syncthreads();
+        if (threadIdx.x == 0) report(S->unsettled);
+    }
     __syncthreads();
     if (parts > 1) cluster_wait();               // no other block reads from this one any more
     if (warp == 1) tmem_free<1>(tmem, kSmallCols);
@@ -349,7 +349,7 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (words_at - smem_u32(raw)) + kScaleBufs * kScaleBufBytes);
     const uint32_t warp = warp_index(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = P.tiles_m * P.tiles_n;
-    const Waiter wait{P.spin_limit, &S->failed};
+    const Waiter wait{P.spin_limit, &S->failed, map_shared(smem_u32(&S->failed), rank ^ 1)};
 
     if (warp == 0 && lane == 0) {
         prefetch_map(&map_a);
@@ -358,7 +358,8 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         for (uint32_t i = 0; i < kScaleBufs; ++i) { bar_init(smem_u32(&S->sf_full[i]), 2); bar_init(smem_u32(&S->sf_empty[i]), 1); }
         for (uint32_t i = 0; i < 2; ++i) bar_init(smem_u32(&S->acc_full[i]), 1);
         bar_init(smem_u32(&S->acc_empty[0]), 8);
-        S->failed = 0;
+        bar_init(smem_u32(&S->settled), 1);
+        S->failed = S->unsettled = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc<2>(smem_u32(&S->tmem), kLargeCols);
@@ -391,14 +392,8 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 if (++st == kLargeStages) { st = 0; ++round; }
             }
         }
-        // after a wait that gave up, copies may still be on their way into the pair's shared memory
-        if (!ok && !P.skip_copy && rank == 0 && lane == 0)
-            for (uint32_t i = 0; i < kLargeStages; ++i) {
-                const uint32_t r = i < st ? round : round - 1;
-                if (round == 0 && i >= st) continue;
-                for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S->full[i]), r & 1); ++q) { }
-            }
-    } else if (warp == 1 && rank == 0) {
+        if (lane == 0) S->copied = round * kLargeStages + st;
+    } else if (warp == 1 && rank == 0 && !P.skip_math) {
         uint32_t st = 0, round = 0, word = 0, tile = 0;
         bool ok = true;
         for (uint32_t i = pair; i < tiles && ok; i += pairs, ++tile) {
@@ -505,6 +500,28 @@ matmul_large_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     __syncthreads();
     cluster_sync();                              // nothing of either block arrives at, or is copied into, the other any more
     tc_fence_after();
+    if (*wait.failed) {                          // both blocks know of it: but for what they left under way
+        if (rank == 0 && warp == 0 && lane == 0 && !P.skip_copy) {
+            // the bytes of both count here; where one of them is a few steps ahead, only its own come
+            const uint32_t mine = S->copied, other = ld_cluster_u32(map_shared(smem_u32(&S->copied), 1)), n = max(mine, other);
+            for (uint32_t i = n > kLargeStages ? n - kLargeStages : 0; i < n; ++i) {
+                const uint32_t bar = smem_u32(&S->full[i % kLargeStages]);
+                if (i >= mine) bar_expect(bar, 2 * kTileBytes);
+                else if (i >= other) bar_forgo(bar, 2 * kTileBytes);
+                if (!settled(bar, (i / kLargeStages) & 1, P.spin_limit)) S->unsettled = 1;
+            }
+        }
+        __syncwarp();
+        if (warp == 1) {
+            if (rank == 0 && elect_one()) mma_commit<2>(smem_u32(&S->settled));
+            if (lane == 0 && !settled(smem_u32(&S->settled), 0, P.spin_limit)) S->unsettled = 1;
+        }
+        __syncwarp();
+        __syncthreads();
+        if (threadIdx.x == 0) report(S->unsettled);
+        __syncwarp();
+        cluster_sync();
+    }
     if (warp == 1) tmem_free<2>(tmem, kLargeCols);
 }
 
@@ -575,6 +592,7 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
     P.out_wide = reinterpret_cast<uintptr_t>(d_out) % 16 == 0 && P.ld_out % 16 == 0;
     P.spin_limit = test_knobs().spin_limit;
     P.skip_copy = test_knobs().skip_copy;
+    P.skip_math = test_knobs().skip_math;
     P.tiles_m = (uint32_t)ceil_div(P.m, kTile);
     P.tiles_n = (uint32_t)ceil_div(P.n, kTile);
     if (P.tiles_m > 65535) return ZC_E_TOO_LARGE;
@@ -640,8 +658,11 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
 
 zc_status zc_fp8_status(void* cuda_stream)
 {
-    const zc_status product = read_timeout((cudaStream_t)cuda_stream), layer = moe_read_timeout((cudaStream_t)cuda_stream);
-    return product != ZC_OK ? product : layer;
+    uint32_t marks = 0;
+    const zc_status product = read_marks((cudaStream_t)cuda_stream, &marks), layer = moe_read_marks((cudaStream_t)cuda_stream, &marks);
+    test_knobs().fp8_marks = marks;
+    if (product != ZC_OK || layer != ZC_OK) return ZC_E_CUDA;
+    return marks ? ZC_E_DEVICE_TIMEOUT : ZC_OK;
 }
 
 }  // extern "C"

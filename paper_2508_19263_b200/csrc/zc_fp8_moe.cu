@@ -60,7 +60,7 @@ struct MoeParams {
     float *weights_out;
     uint8_t *y;
     uint64_t ld_y;                               // elements
-    uint32_t spin_limit, skip_copy;
+    uint32_t spin_limit, skip_copy, skip_math;
     // workspace
     uint32_t *route;                             // [0]: chosen experts, [1]: passes; then the experts' numbers, their first rows and passes
     uint32_t *row_of;                            // [tokens][top_k]: row of a token's j-th expert
@@ -77,8 +77,10 @@ struct Routing {
     uint16_t pass[kMaxExperts + 1];              // passes of the experts before
 };
 struct MoeShared {
-    uint64_t full[kMoeMaxStages], empty[kMoeMaxStages], acc_full[2], acc_empty[2];
-    uint32_t tmem, failed;
+    // copied: a stage's weights are there; full: its pieces and scale words are.  Apart, so that a block that gives up can wait for its
+    // copies whichever role gave up (0.7 us of the 29 that one token takes).
+    uint64_t copied[kMoeMaxStages], full[kMoeMaxStages], empty[kMoeMaxStages], acc_full[2], acc_empty[2];
+    uint32_t tmem, failed, unsettled;            // unsettled: copies or matrix instructions that this block did not see the end of
     Routing R;
     alignas(16) float other[2][64][4];           // kernel 1: what the other half of the result warps needs
     float row_p[kMaxRows];
@@ -252,6 +254,7 @@ __device__ __forceinline__ void make_pieces(float v[4], uint32_t words[PIECES], 
 }
 
 // What a block does after the routing: its share of gate and up (UP) or of down.  HALF: activations of gate and up are FP16.
+// All threads; they leave it together.
 template <bool UP, bool HALF, int PIECES, typename Finish>
 __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps& maps, MoeShared& S, const Cut& cut, uint32_t base, uint32_t blocks, Finish finish)
 {
@@ -274,7 +277,7 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
             const uint32_t row0 = t.expert * (UP ? 2 * P.inter : P.hidden) + t.group * 8;
             for (uint32_t k = 0; k < steps; ++k, forward()) {
                 if (!(ok = round == 0 || wait.warp(smem_u32(&S.empty[st]), (round - 1) & 1))) break;
-                const uint32_t bar = smem_u32(&S.full[st]), to = base + st * stage_bytes;
+                const uint32_t bar = smem_u32(&S.copied[st]), to = base + st * stage_bytes;
                 if (elect_one()) {
                     bar_expect(bar, t.groups * (UP ? 2048 : 1024));
                     // as few copies as there are bits in the number of groups: one of 8 rows takes the copy engine as long as one of 64
@@ -290,15 +293,9 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
                 __syncwarp();
             }
         }
-        // after a wait that gave up, copies may still be on their way into this block's shared memory: of this round up to
-        // the present stage, of the one before from there on
-        if (!ok && !P.skip_copy && lane == 0)
-            for (uint32_t i = 0; i < stages; ++i) {
-                const uint32_t r = i < st ? round : round - 1;
-                if (round == 0 && i >= st) continue;
-                for (uint32_t q = 0; q <= P.spin_limit && !bar_try(smem_u32(&S.full[i]), r & 1); ++q) { }
-            }
-    } else if (warp == 1) {
+        // nothing is copied into this block's shared memory any more, whether the block gave up or not
+        if (!P.skip_copy && !settled_stage(smem_u32(S.copied), lane, stages, st, round, P.spin_limit)) S.failed = S.unsettled = 1;
+    } else if (warp == 1 && !P.skip_math) {
         uint32_t tile = 0;
         bool ok = true;
         while (ok && tiles.next(t)) {
@@ -306,7 +303,7 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
             const uint32_t idesc = P.idesc | ((piece_rows(t.count, PIECES) >> 3) << 17);
             if (tile >= 2 && !(ok = wait.warp(smem_u32(&S.acc_empty[buf]), ((tile >> 1) - 1) & 1))) break;
             for (uint32_t k = 0; k < steps; ++k, forward()) {
-                if (!(ok = wait.warp(smem_u32(&S.full[st]), round & 1))) break;
+                if (!(ok = wait.warp_both(smem_u32(&S.full[st]), smem_u32(&S.copied[st]), round & 1))) break;
                 tc_fence_after();
                 const uint32_t at = base + st * stage_bytes, sf = tmem + kMoeTmemScales + st * 8;
                 const uint64_t da = operand_desc(at), db = operand_desc(at + 16384);
@@ -323,6 +320,8 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
             __syncwarp();
             ++tile;
         }
+        // nor do matrix instructions read from there
+        if (tile && lane == 0 && !settled(smem_u32(&S.acc_full[(tile - 1) & 1]), ((tile - 1) >> 1) & 1, P.spin_limit)) S.failed = S.unsettled = 1;
     } else if (warp == 2) {
         // scale bytes of the weights, four steps at a time and four steps ahead; row r of the tile's operand is row 32 j + lane
         const uint32_t sld = steps, srows = (rows + 127) >> 7;
@@ -469,6 +468,8 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
         }
     }
     __syncwarp();
+    __syncthreads();
+    if (threadIdx.x == 0 && S.failed) report(S.unsettled);
 }
 
 // ---- routing ----------------------------------------------------------------------------------------------------------
@@ -679,12 +680,12 @@ __device__ __forceinline__ uint32_t row_of(const MoeRouting& S, uint32_t e, uint
 __device__ __forceinline__ void moe_setup(MoeShared& S, uint32_t sharing)
 {
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (warp == 0 && lane == 0) {
-        for (uint32_t i = 0; i < kMoeMaxStages; ++i) { bar_init(smem_u32(&S.full[i]), 2 + sharing); bar_init(smem_u32(&S.empty[i]), 1); }
-        for (uint32_t i = 0; i < 2; ++i) { bar_init(smem_u32(&S.acc_full[i]), 1); bar_init(smem_u32(&S.acc_empty[i]), 4); }
-        S.failed = 0;
-        S.n_todo = 0;
+    if (warp == 0) {
+        if (lane < kMoeMaxStages) { bar_init(smem_u32(&S.copied[lane]), 1); bar_init(smem_u32(&S.full[lane]), 1 + sharing); bar_init(smem_u32(&S.empty[lane]), 1); }
+        if (lane < 2) { bar_init(smem_u32(&S.acc_full[lane]), 1); bar_init(smem_u32(&S.acc_empty[lane]), 4); }
+        if (lane == 0) S.failed = S.unsettled = S.n_todo = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        __syncwarp();
     }
     if (warp == 1) tmem_alloc<1>(smem_u32(&S.tmem), kMoeTmemCols);
     tc_fence_before();
@@ -830,7 +831,6 @@ moe_up_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ MoeP
     fence_async_shared();                        // the routing's shared memory becomes the stages'
     cluster_sync();                              // and no other block reads from it any more
     stream_weights<true, HALF, 3>(P, maps, S, cut_rows<true>(P.inter, S.R.n_passes, gridDim.x), base, gridDim.x, FinishUp{P, S});
-    __syncthreads();
     if (tid < 64 && tid >= 32) tmem_free<1>(S.tmem, kMoeTmemCols);
 }
 
@@ -859,7 +859,6 @@ moe_down_kernel(const __grid_constant__ MoeMaps maps, const __grid_constant__ Mo
     __syncthreads();
     const FinishDown<HALF> finish{P, S, n_passes};
     stream_weights<false, HALF, kHiddenPieces>(P, maps, S, cut_rows<false>(P.hidden, n_passes, gridDim.x), base, gridDim.x, finish);
-    __syncthreads();
     finish.add_up(tid, kMoeThreads);
     __syncthreads();
     if (tid < 64 && tid >= 32) tmem_free<1>(S.tmem, kMoeTmemCols);
@@ -942,7 +941,7 @@ static cudaError_t launch_moe(const MoeMaps& up, const MoeMaps& down, const MoeP
     return cudaLaunchKernelEx(&cfg, moe_down_kernel<HALF>, down, P);
 }
 
-zc_status moe_read_timeout(cudaStream_t st) { return read_timeout(st); }
+zc_status moe_read_marks(cudaStream_t st, uint32_t* marks) { return read_marks(st, marks); }
 
 }  // namespace zc
 
@@ -980,6 +979,7 @@ zc_status zc_fp8_moe(const zc_fp8_moe_layer* layer, uint32_t n_tokens, const voi
     P.pass = n_tokens <= 8 ? 8 : n_tokens <= 16 || n_tokens * layer->top_k <= 9 * layer->n_experts ? 16 : 32;
     P.spin_limit = test_knobs().spin_limit;
     P.skip_copy = test_knobs().skip_copy;
+    P.skip_math = test_knobs().skip_math;
     P.tokens = n_tokens;
     P.experts = layer->n_experts;
     P.top_k = layer->top_k;

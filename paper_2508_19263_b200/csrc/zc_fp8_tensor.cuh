@@ -8,12 +8,16 @@
 
 namespace zc {
 
-static __device__ unsigned int g_fp8_timeout;    // a wait of a kernel of this file's user gave up (one word per translation unit)
+// What kernels of this file's user left behind (one word per translation unit).
+static __device__ unsigned int g_fp8_timeout;
+constexpr uint32_t kMarkGaveUp = 1, kMarkSettled = 2, kMarkUnsettled = 4;
 
-// Every wait is bounded: on giving up the block is marked, and the other roles' waits end with it.
+// Every wait is bounded: on giving up the block is marked, and the other roles' waits end with it.  Blocks that copy into, or multiply
+// from, each other's shared memory are marked together: `other` is the place of the other block's mark (0: there is none).
 struct Waiter {
     uint32_t limit;
     volatile uint32_t* failed;
+    uint32_t other = 0;
     template <bool CLUSTER = false>
     __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const
     {
@@ -21,14 +25,48 @@ struct Waiter {
             if (CLUSTER ? bar_try_cluster(bar, parity) : bar_try(bar, parity)) return true;
             if (*failed) return false;
         }
-        *failed = 1;
-        atomicExch(&g_fp8_timeout, 1u);
+        give_up();
         return false;
+    }
+    __device__ __forceinline__ void give_up() const
+    {
+        *failed = 1;
+        if (other) asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(other), "r"(1u) : "memory");
     }
     // the same for all lanes of a converged warp at once
     __device__ __forceinline__ bool warp(uint32_t bar, uint32_t parity) const { return __all_sync(0xFFFFFFFFu, operator()(bar, parity)); }
+    // for two barriers' phases
+    __device__ __forceinline__ bool warp_both(uint32_t bar, uint32_t also, uint32_t parity) const
+    {
+        bool there = false;
+        for (uint32_t i = 0; i <= limit; ++i) {
+            there = bar_try(bar, parity) && bar_try(also, parity);
+            if (there || *failed) break;
+        }
+        if (!there) give_up();
+        return __all_sync(0xFFFFFFFFu, there);
+    }
     __device__ __forceinline__ bool warp_across(uint32_t bar, uint32_t parity) const { return __all_sync(0xFFFFFFFFu, operator()<true>(bar, parity)); }
 };
+
+// Copies and matrix instructions that are under way read and write a block's shared and tensor memory, which the next block may get when
+// this one ends, also when it gave up.  A block ends only once these have, or have been waited for as long as anything else: for phases
+// that they alone complete, whatever other roles do.
+__device__ __forceinline__ bool settled(uint32_t bar, uint32_t parity, uint32_t limit)
+{
+#pragma unroll 1
+    for (uint32_t i = 0; i <= limit; ++i)
+        if (bar_try(bar, parity)) return true;
+    return false;
+}
+// The same for the stage that is a lane's, where `st` is the next one to be used, in round `round`.
+__device__ __forceinline__ bool settled_stage(uint32_t first_bar, uint32_t lane, uint32_t stages, uint32_t st, uint32_t round, uint32_t limit)
+{
+    const uint32_t rounds = round + (lane < st);
+    return lane >= stages || rounds == 0 || settled(first_bar + 8 * lane, (rounds - 1) & 1, limit);
+}
+// One thread of a block that gave up, when all of its roles have ended.
+__device__ __forceinline__ void report(uint32_t unsettled) { atomicOr(&g_fp8_timeout, kMarkGaveUp | (unsettled ? kMarkUnsettled : kMarkSettled)); }
 
 // The scale bytes of steps first .. first + 3 of one row as a word; 127 (a factor of 1) where there is none.
 __device__ __forceinline__ uint32_t scale_word(const uint8_t* s, uint64_t ld, uint32_t square, uint32_t row, uint32_t rows, uint32_t first, uint32_t end)
@@ -47,14 +85,15 @@ __device__ __forceinline__ uint32_t scale_word(const uint8_t* s, uint64_t ld, ui
 // ---- host ----
 
 // Waits for the stream, reads and clears the calling translation unit's word.
-static zc_status read_timeout(cudaStream_t st)
+static zc_status read_marks(cudaStream_t st, uint32_t* marks)
 {
     unsigned int h = 0;
     const unsigned int zero = 0;
     if (cudaMemcpyFromSymbolAsync(&h, g_fp8_timeout, sizeof h, 0, cudaMemcpyDeviceToHost, st) != cudaSuccess) return ZC_E_CUDA;
     if (cudaMemcpyToSymbolAsync(g_fp8_timeout, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st) != cudaSuccess) return ZC_E_CUDA;
     if (cudaStreamSynchronize(st) != cudaSuccess) return ZC_E_CUDA;
-    return h ? ZC_E_DEVICE_TIMEOUT : ZC_OK;
+    *marks |= h;
+    return ZC_OK;
 }
 
 // A number that is worked out on a device's first use (0: it failed, and is tried again), kept per device.

@@ -277,7 +277,7 @@ uint64_t cost_bits(const uint64_t hist[256], const uint8_t len[256])
 namespace zc {
 TestKnobs& test_knobs()
 {
-    static TestKnobs k{kDefaultSpinLimit, 0, 0};
+    static TestKnobs k{kDefaultSpinLimit, 0, 0, 0, 0};
     return k;
 }
 }  // namespace zc
@@ -287,6 +287,8 @@ extern "C" {
 void zc_test_set_wait_limit(uint32_t polls) { test_knobs().spin_limit = polls ? polls : kDefaultSpinLimit; }
 void zc_test_stall_encoder(uint32_t first_ticket) { test_knobs().first_ticket = first_ticket; }
 void zc_test_stall_decoder(uint32_t on) { test_knobs().skip_copy = on ? 1u : 0u; }
+void zc_test_stall_math(uint32_t on) { test_knobs().skip_math = on ? 1u : 0u; }
+uint32_t zc_test_fp8_marks(void) { return test_knobs().fp8_marks; }
 
 int zc_test_debug_counts(uint32_t out[2])
 {

@@ -127,6 +127,8 @@ struct TestKnobs {
     uint32_t spin_limit;     // polls after which a bounded wait on the device gives up
     uint32_t first_ticket;   // first batch the encoder hands out (not 0: batch 0 is never packed, so every look-back stalls)
     uint32_t skip_copy;      // the decoder does not start the copies of the pieces it then waits for
+    uint32_t skip_math;    // zc_fp8_matmul and zc_fp8_moe copy their operands, but start no matrix instruction
+    uint32_t fp8_marks;      // what the last zc_fp8_status found
 };
 TestKnobs& test_knobs();
 // Development build (-DZC_DEBUG_CHECKS=1): each translation unit with kernels adds its counts of refused shared and
