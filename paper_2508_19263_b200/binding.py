@@ -610,7 +610,7 @@ def fp8_matmul(a: Fp8Matrix, b: Fp8Matrix, d_out: torch.Tensor, accumulate: bool
 
 
 def fp8_status(stream=None) -> int:
-    """zc_fp8_status: device status of the fp8_matmul calls on the current device since the last query."""
+    """zc_fp8_status: device status of the fp8_matmul and fp8_moe calls on the current device since the last query."""
     return int(_lib.zc_fp8_status(_stream_ptr(stream)))
 
 

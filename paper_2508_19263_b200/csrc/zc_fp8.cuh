@@ -34,7 +34,7 @@ inline zc_status check_matrix(const zc_fp8_matrix* m)
     return ZC_OK;
 }
 
-zc_status moe_read_marks(cudaStream_t st, uint32_t* marks);   // zc_fp8_status, for the kernels of zc_fp8_moe
+unsigned int* moe_marks_word();                           // what the kernels of zc_fp8_moe left for zc_fp8_status
 
 __device__ __forceinline__ float finite_abs(float v)
 {

@@ -941,7 +941,7 @@ static cudaError_t launch_moe(const MoeMaps& up, const MoeMaps& down, const MoeP
     return cudaLaunchKernelEx(&cfg, moe_down_kernel<HALF>, down, P);
 }
 
-zc_status moe_read_marks(cudaStream_t st, uint32_t* marks) { return read_marks(st, marks); }
+unsigned int* moe_marks_word() { return marks_word(); }
 
 }  // namespace zc
 

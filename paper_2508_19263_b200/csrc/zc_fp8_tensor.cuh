@@ -84,16 +84,11 @@ __device__ __forceinline__ uint32_t scale_word(const uint8_t* s, uint64_t ld, ui
 
 // ---- host ----
 
-// Waits for the stream, reads and clears the calling translation unit's word.
-static zc_status read_marks(cudaStream_t st, uint32_t* marks)
+// The calling translation unit's word on the current device; null on an error.
+static unsigned int* marks_word()
 {
-    unsigned int h = 0;
-    const unsigned int zero = 0;
-    if (cudaMemcpyFromSymbolAsync(&h, g_fp8_timeout, sizeof h, 0, cudaMemcpyDeviceToHost, st) != cudaSuccess) return ZC_E_CUDA;
-    if (cudaMemcpyToSymbolAsync(g_fp8_timeout, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st) != cudaSuccess) return ZC_E_CUDA;
-    if (cudaStreamSynchronize(st) != cudaSuccess) return ZC_E_CUDA;
-    *marks |= h;
-    return ZC_OK;
+    void* p = nullptr;
+    return cudaGetSymbolAddress(&p, g_fp8_timeout) == cudaSuccess ? (unsigned int*)p : nullptr;
 }
 
 // A number that is worked out on a device's first use (0: it failed, and is tried again), kept per device.
