@@ -106,8 +106,9 @@ __device__ __forceinline__ void put_columns(const MatmulParams& P, uint32_t base
     }
 }
 
-// One tile of 128 x 128 per block; the `gridDim.z` blocks of a cluster share a tile, each takes a part of the steps, and the
-// parts are added up through the cluster's shared memory in the order of the ranks.
+// One tile of 128 x 128 per block, one after the other along the grid's first axis (the only one with room for all rows that a matrix may
+// have); the `gridDim.z` blocks of a cluster share a tile, each takes a part of the steps, and the parts are added up through the
+// cluster's shared memory in the order of the ranks.
 constexpr size_t small_smem(uint32_t stages) { return 1024 + stages * 2 * kTileBytes + kScaleBufs * kScaleBufBytes + sizeof(MatmulShared); }
 constexpr uint32_t kSmallCols = 256;             // tensor memory: 128 accumulator columns, then two sets of 4 + 4 scale columns
 constexpr uint32_t kSmallScales = 128;
@@ -122,7 +123,7 @@ matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     MatmulShared* S = reinterpret_cast<MatmulShared*>(raw + (words_at - smem_u32(raw)) + kScaleBufs * kScaleBufBytes);
     const uint32_t warp = warp_index(), lane = threadIdx.x & 31;
     const uint32_t parts = gridDim.z, part = blockIdx.z;
-    const uint32_t m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
+    const uint32_t tile_m = blockIdx.x / P.tiles_n, m0 = tile_m * kTile, n0 = (blockIdx.x - tile_m * P.tiles_n) * kTile;
     const uint32_t lo = (uint32_t)((uint64_t)P.steps * part / parts), hi = (uint32_t)((uint64_t)P.steps * (part + 1) / parts);
     const Waiter wait{P.spin_limit, &S->failed};
 
@@ -601,7 +602,6 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
     P.skip_math = test_knobs().skip_math;
     P.tiles_m = (uint32_t)ceil_div(P.m, kTile);
     P.tiles_n = (uint32_t)ceil_div(P.n, kTile);
-    if (P.tiles_m > 65535) return ZC_E_TOO_LARGE;
     const uint64_t tiles = (uint64_t)P.tiles_m * P.tiles_n;
     const uint64_t large = ceil_div(P.m, 256) * ceil_div(P.n, 256);
     // for up to 128 tokens half of a pair's tile would be empty (16 x 14336 x 4096: 20.3 us in pairs, 14.8 in small tiles)
@@ -646,7 +646,7 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
     // one block per SM has all of the shared memory, two have half of it each (64 x 14336 x 4096: 15.2 us, 18.3 with half)
     P.stages = tiles * parts <= (uint64_t)sm_count() ? 6 : 3;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(P.tiles_n, P.tiles_m, parts);
+    cfg.gridDim = dim3((uint32_t)tiles, 1, parts);    // 2^24 at most: one of the two sides has a tile, or there are few
     cfg.blockDim = dim3(kMmThreads);
     cfg.dynamicSmemBytes = small_smem(P.stages);
     cfg.stream = st;

@@ -104,3 +104,16 @@ def test_linear_layer_of_a_training_step(tokens, n, k):
     assert torch.equal(y, (x.double() @ w.double().t()).float().bfloat16())
     assert torch.equal(dx, (dy.double() @ w.double()).float().bfloat16())
     assert torch.equal(dw, want.float())
+
+
+@pytest.mark.parametrize("n", [40, 300])
+def test_more_rows_than_a_grid_has_blocks_along_its_second_axis(n):
+    # 65536 tiles of 128 rows and a piece of one; 40 columns take the kernel of small tiles, 300 that of pairs
+    m, k = 65536 * 128 + 77, 32
+    a, va = matrix(m, k, zc.FMT_FP8_E4M3, 128, 81)
+    b, vb = matrix(n, k, zc.FMT_FP8_E4M3, 1, 82)
+    d = torch.full((m, n), 7.0, dtype=torch.float16, device=DEV)
+    zc.fp8_matmul(a, b, d)
+    for part in range(0, m, 1 << 20):
+        assert torch.equal(d[part: part + (1 << 20)], (va[part: part + (1 << 20)] @ vb.t()).half())
+    assert zc.fp8_status() == zc.OK
