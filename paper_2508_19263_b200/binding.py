@@ -638,6 +638,7 @@ class Fp8MoeLayer:
             if any(s != w for s, w, n in zip(t.stride(), want, t.shape) if n > 1):
                 raise ValueError(f"matrices follow one another with one row pitch: strides {t.stride()}")
         real, ptr, ld = _real_matrix(router, "router")
+        ld = ld if experts > 1 else -(-ld // 8) * 8              # a single row has no pitch of its own
         self.experts, self.hidden, self.inter, self.top_k, self.dtype = experts, hidden, inter, top_k, router.dtype
         self.tensors = (router, gate_up, gate_up_scales, down, down_scales)
         self.desc = Fp8MoeLayerDesc(ptr, gate_up.data_ptr(), gate_up_scales.data_ptr(), down.data_ptr(), down_scales.data_ptr(), ld,
