@@ -84,7 +84,8 @@ typedef enum zc_status {
     ZC_E_NOMEM = 6,             /* host allocation failed */
     ZC_E_DEVICE_TIMEOUT = 7,    /* a bounded wait inside a kernel gave up */
     ZC_E_NO_CODE = 8,           /* a symbol of the input has no code in the codebook */
-    ZC_E_TOO_LARGE = 9          /* the tensor needs more built-in scratch than zc_compress_noalloc has */
+    ZC_E_TOO_LARGE = 9          /* a size is above what the call takes; zc_compress_noalloc: the tensor needs more
+                                   built-in scratch than it has */
 } zc_status;
 
 typedef enum zc_format {
@@ -463,7 +464,7 @@ zc_status zc_fp8_quantize(zc_real in_type, const void* d_in, uint64_t ld_in, con
 
 /* Matrix product D = A B^T, or D += A B^T: D[m][n] = sum over k of A[m][k] * B[n][k], summed in FP32.
  * a, b        M x K and N x K; formats and block_rows may differ
- * d_out       M x N of out_type, row m begins at element m * ld_out
+ * d_out       M x N of out_type, row m begins at element m * ld_out; must not overlap the operands
  * accumulate  not 0: the product is added (in FP32, rounded once) to what d_out holds
  * A linear layer is x W^T (a = activations, b = weights); the gradient of its input is dy (W^T)^T and that of its
  * weights (dy^T)(x^T)^T, with the transposed matrices that zc_fp8_quantize makes.  K = 0 gives zeros.  The result
