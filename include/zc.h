@@ -469,8 +469,11 @@ zc_status zc_fp8_quantize(zc_real in_type, const void* d_in, uint64_t ld_in, con
  * A linear layer is x W^T (a = activations, b = weights); the gradient of its input is dy (W^T)^T and that of its
  * weights (dy^T)(x^T)^T, with the transposed matrices that zc_fp8_quantize makes.  K = 0 gives zeros.  The result
  * does not depend on other calls and is the same every time.  Asynchronous on cuda_stream; needs no workspace.
- * The sums are those of the tensor cores' FP32 accumulators: to nearest for some 4096 columns; beyond, sums of one sign
- * fall short by a few units in the last place (relative 6e-7 at 14336 columns, 5e-6 at 65536).
+ * The sums are those of the tensor cores' FP32 accumulators, which take 32 columns at a time and cut off what does not fit: a
+ * sum of terms of one sign falls short by less than a unit of it, as it is by then, for every 32 columns (relative
+ * 7e-7 at 1024 columns, 4e-6 at 4096, 1.5e-5 at 14336, 1.1e-4 at 65536; less for results of few tiles, whose k is cut into up to
+ * eight parts).  Where that is too much, products of parts of the columns are added up with accumulate, which rounds to
+ * nearest: fourteen parts of 1024 columns stay within 4e-6.
  * A wait inside the kernel that gives up leaves D undefined and is reported by zc_fp8_status.
  * Errors: INVALID_ARG (null or misaligned pointers, pitches, different K), UNSUPPORTED (types, formats), TOO_LARGE,
  * CUDA. */
@@ -486,8 +489,8 @@ zc_status zc_fp8_status(void* cuda_stream);
  *   logits = router x; the top_k largest (ties: the lowest index first; NaN counts as the lowest value); p = softmax
  *   over those top_k; y = sum over them of p_e * down_e (silu(gate_e x) * (up_e x)), silu(v) = v / (1 + exp(-v)).
  * The weights are FP8 with 128 x 128 blocks; every expert's matrix has scale bytes of its own, beginning with its first
- * row.  Only the experts that a token chose are read.  Sums are FP32, those of the router FP64 over parts of 64
- * columns.  x is used to 2^-25 of the largest magnitude of its 128 columns, and exactly where it is above 2^-17 of it; the
+ * row.  Only the experts that a token chose are read.  Sums are FP32, as zc_fp8_matmul's, those of the router FP64 over parts of
+ * 64 columns in FP32: experts whose logits are closer than 2^-20 of their terms' magnitudes may change places.  x is used to 2^-25 of the largest magnitude of its 128 columns, and exactly where it is above 2^-17 of it; the
  * hidden vector of an expert goes into the second product with 18 bits of precision, and to 2^-29 of the largest magnitude of
  * its 128 columns; an infinity in either gives NaN.  A wait inside a kernel that gives up leaves the outputs undefined and is reported by zc_fp8_status. */
 typedef struct zc_fp8_moe_layer {

@@ -117,3 +117,39 @@ def test_more_rows_than_a_grid_has_blocks_along_its_second_axis(n):
     for part in range(0, m, 1 << 20):
         assert torch.equal(d[part: part + (1 << 20)], (va[part: part + (1 << 20)] @ vb.t()).half())
     assert zc.fp8_status() == zc.OK
+
+
+def positive(r, k, g):
+    return zc.Fp8Matrix(torch.randint(0, 0x40, (r, k), generator=g, device=DEV, dtype=torch.uint8),
+                        torch.full((r, -(-k // 128)), 127, dtype=torch.uint8, device=DEV), zc.FMT_FP8_E4M3, 1)
+
+
+def short(k):
+    """What a sum of k positive products may be short by: less than a unit, 2^-23, of the sum as it is after every 32 columns.  The sum grows
+    evenly, so that is (k / 32 + 1) / 2 units of the whole; a product's deviation is 2.62 times its mean (that of the values of the 64 bytes
+    0 .. 0x3F 1.34 times), so the average of the sums on the way is off by 2.62 / sqrt(12 k) of the whole, against its half, six standard
+    deviations of which are 9.1 / sqrt(k)."""
+    return (k / 32 + 1) * 2.0 ** -24 * (1 + 9.1 / k ** 0.5)
+
+
+@pytest.mark.parametrize("k", [1024, 4096, 14336, 65536])
+@pytest.mark.parametrize("m,n", [(1600, 1792), (128, 128)])
+def test_sums_of_one_sign(m, n, k):
+    g = torch.Generator(device=DEV).manual_seed(71)
+    a, b = positive(m, k, g), positive(n, k, g)
+    want = a.elems.view(torch.float8_e4m3fn).double() @ b.elems.view(torch.float8_e4m3fn).double().t()
+    d = zc.fp8_matmul(a, b, torch.empty((m, n), device=DEV))
+    assert ((d.double() - want) / want).abs().max().item() <= short(k)
+
+
+def test_sums_of_one_sign_in_parts():
+    # fourteen parts of 1024 columns, added to nearest: half a unit, 2^-24, of the sum each
+    m, n, k, parts = 1600, 1792, 14336, 14
+    g = torch.Generator(device=DEV).manual_seed(72)
+    a, b = positive(m, k, g), positive(n, k, g)
+    want = a.elems.view(torch.float8_e4m3fn).double() @ b.elems.view(torch.float8_e4m3fn).double().t()
+    d = torch.zeros((m, n), device=DEV)
+    for i in range(parts):
+        x, y = (zc.Fp8Matrix(v.elems[:, i * 1024: (i + 1) * 1024], v.scales[:, i * 8: (i + 1) * 8], v.format, 1) for v in (a, b))
+        zc.fp8_matmul(x, y, d, accumulate=True)
+    assert ((d.double() - want) / want).abs().max().item() <= short(1024) + parts * 2.0 ** -24
