@@ -60,13 +60,13 @@ __device__ __forceinline__ void sts128(uint32_t addr, const uint32_t v[4])
 // ---- 32-byte global accesses (one sector per lane); 32-byte aligned ----
 __device__ __forceinline__ void ld_v8(const void* p, uint32_t v[8])
 {
-    asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(p));
 }
 __device__ __forceinline__ uint4 ld_stream_v4(const void* p)
 {
     uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 
@@ -87,7 +87,8 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr)
 // A kernel may be on the GPU, and set up its barriers and tensor memory, while the one before it in the stream ends; it
 // touches nothing that other kernels read or write before grid_wait(), which waits for all of them.  It lets the next one in
 // only after that, so that no more than two of a stream's kernels are there at a time and what the next one reads is not still
-// being read, and cached, by the one before this.
+// being read, and cached, by the one before this.  What it reads may have been written while it was there already, so its loads are
+// the ordinary ones, never those (`.nc`, __ldg) that take the memory to be unchanged for as long as the kernel is there.
 inline cudaLaunchAttribute launch_early()
 {
     cudaLaunchAttribute a{};

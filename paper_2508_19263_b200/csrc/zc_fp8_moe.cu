@@ -379,7 +379,7 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
                             if (UP) {
                                 const uint8_t* x = P.x + 2 * ((uint64_t)S.row_token[t.row + c + i] * P.ld_x + col);
                                 if (col + 4 <= cols) {
-                                    const uint2 v = __ldg(reinterpret_cast<const uint2*>(x));
+                                    const uint2 v = *reinterpret_cast<const uint2*>(x);
                                     raw[i].x = v.x;
                                     raw[i].y = v.y;
                                 } else {                     // a row may end where its buffer does

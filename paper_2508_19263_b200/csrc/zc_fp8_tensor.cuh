@@ -74,10 +74,10 @@ __device__ __forceinline__ uint32_t scale_word(const uint8_t* s, uint64_t ld, ui
     uint32_t w = 0x7F7F7F7Fu;
     if (row < rows) {
         const uint8_t* p = s + (uint64_t)(square ? row >> 7 : row) * ld + first;
-        if (first + 4 <= end && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return __ldg(reinterpret_cast<const uint32_t*>(p));
+        if (first + 4 <= end && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return *reinterpret_cast<const uint32_t*>(p);
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
-            if (first + i < end) w = (w & ~(0xFFu << (8 * i))) | ((uint32_t)__ldg(p + i) << (8 * i));
+            if (first + i < end) w = (w & ~(0xFFu << (8 * i))) | ((uint32_t)p[i] << (8 * i));
     }
     return w;
 }
