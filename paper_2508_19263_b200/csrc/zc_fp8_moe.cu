@@ -46,7 +46,7 @@ __host__ __device__ constexpr uint32_t stage_count(uint32_t pass, uint32_t piece
 {
     return kMoeStageSpace / stage_size(pass, pieces) < kMoeMaxStages ? kMoeStageSpace / stage_size(pass, pieces) : kMoeMaxStages;
 }
-static_assert(piece_rows(32, 4) <= 128 && stage_count(32, 4) == 6 && stage_count(8, 3) == 9, "stages");
+static_assert(piece_rows(16, 4) <= 128 && stage_count(16, 4) == 8 && stage_count(8, 3) == 9, "stages");
 
 struct MoeParams {
     const uint8_t *x, *router;                   // rows of BF16 or FP16
@@ -975,8 +975,9 @@ zc_status zc_fp8_moe(const zc_fp8_moe_layer* layer, uint32_t n_tokens, const voi
     P.down_scales = (const uint8_t*)layer->d_down_scales;
     P.idesc = instruction_of(layer->format, ZC_FMT_FP8_E4M3, 128, 0);
     // Tokens per reading of a tile: the stages that hold their pieces get larger and fewer with them (9 of 8 tokens, 8 of 16, 6 or 7 of 32), an expert
-    // that more tokens chose is read again, from the L2.  Above 9 tokens an expert on average many have more than 16.
-    P.pass = n_tokens <= 8 ? 8 : n_tokens <= 16 || n_tokens * layer->top_k <= 9 * layer->n_experts ? 16 : 32;
+    // that more tokens chose is read again, from the L2.  64 tokens, 2048 / 1024: with 64 experts, top 8, 117 us in passes of 16, 131 of 8, 125 of
+    // 32; with 32 experts, top 8 (16 an expert), 93, 114 and 103; with 16, top 4, 62.8, 71 and 66.
+    P.pass = n_tokens <= 8 ? 8 : 16;
     P.spin_limit = test_knobs().spin_limit;
     P.skip_copy = test_knobs().skip_copy;
     P.skip_math = test_knobs().skip_math;
