@@ -37,7 +37,7 @@ struct MatmulParams {
 
 // The scale words of four steps are a warp's own work, in turn with three others: each has the time of sixteen steps for the
 // latency of its loads, a buffer in shared memory, and sees every phase of the buffer's barrier.  (All four warps loading all
-// words straight into their quarters of tensor memory, a word ahead, took 498 us of a product that takes 349 without.)  Tensor
+// words straight into their quarters of tensor memory, a word ahead: 8192 x 14336 x 4096 took 498 us in short runs, 349 so.)  Tensor
 // memory has two sets of words.
 constexpr uint32_t kScaleBufs = 4;
 constexpr uint32_t kScaleBufBytes = 512 + 1024;  // 128 rows of A, up to 256 of B
@@ -539,9 +539,11 @@ constexpr uint32_t kAnswers = 1024;
 static __device__ unsigned int g_answers[kAnswers];
 __global__ void collect_kernel(unsigned int* product, unsigned int* layer, uint32_t at) { g_answers[at] = atomicExch(product, 0u) | atomicExch(layer, 0u); }
 
-// From this many tiles of 256 x 256 on, half of the GPU's pairs of blocks, a product goes to pairs; below, four times as many
-// tiles of 128 x 128 fill it better: 512 x 4096 x 4096 (32 tiles) takes 17.8 us in pairs, 16.0 in small tiles, 300 x 14336 x 4096
-// (112 tiles) 29.4 and 33.6, 1024 x 4096 x 1024 (64 tiles, 8 steps) 10.8 and 10.3.
+// From this many tiles of 256 x 256 on, half of the 74 pairs of blocks that the GPU has room for, a product goes to pairs; below, four
+// times as many tiles of 128 x 128 fill it better.  Pairs and small tiles, us: 512 x 4096 x 4096 (32 tiles) 16.4 and 14.1, 1024 x 2560 x 4096
+// (40) 17.6 and 18.4, 640 x 4096 x 4096 (48) 17.4 and 19.0, 300 x 14336 x 4096 (112) 33.0 and 34.8.  With few steps the start and end of
+// the larger tiles count for more, which the rule does not look at: 2048 x 1280 x 2048 (40 tiles, 16 steps) 12.4 and 11.7,
+// 1024 x 4096 x 1024 (64 tiles, 8 steps) 9.7 and 8.3.
 constexpr uint64_t kPairsFrom = 37;
 // Blocks of the large kernel that are on the GPU at once, in whole pairs.
 static uint32_t large_blocks()
@@ -604,7 +606,7 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
     P.tiles_n = (uint32_t)ceil_div(P.n, kTile);
     const uint64_t tiles = (uint64_t)P.tiles_m * P.tiles_n;
     const uint64_t large = ceil_div(P.m, 256) * ceil_div(P.n, 256);
-    // for up to 128 tokens half of a pair's tile would be empty (16 x 14336 x 4096: 20.3 us in pairs, 14.8 in small tiles)
+    // for up to 128 tokens half of a pair's tile would be empty (16 x 14336 x 4096: 21.6 us in pairs, 14.0 in small tiles; 128: 19.2 and 15.4)
     const bool pairs = P.m > 128 && P.n > 128 && large >= kPairsFrom;
     P.rows_a = pairs || P.m >= kTile ? kTile : (uint32_t)round_up(P.m, 8);
     P.rows_b = pairs || P.n >= kTile ? kTile : (uint32_t)round_up(P.n, 8);
@@ -638,12 +640,12 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
         return cudaLaunchKernelEx(&cfg, matmul_large_kernel, map_a, map_b, map_d, P) == cudaSuccess ? ZC_OK : ZC_E_CUDA;
     }
     P.idesc = instruction_of(a->format, b->format, 128, 128);
-    // Parts of k as long as there is an SM for each: 1 x 4096 x 4096 takes 13.2 us in 32 blocks, 8.3 in 128; 128 x 4096 x 4096 14.7 and
-    // 10.9.  Adding the parts up costs more the more rows there are, so these have 8 steps each at least, few rows 4
-    // (1024 x 1024 x 1024: 7.2 us in one part, 8.6 in two).
+    // Parts of k as long as there is an SM for each: 1 x 4096 x 4096 takes 12.2 us in 32 blocks, 6.6 in 128; 128 x 4096 x 4096 13.4 and
+    // 8.9.  Adding the parts up costs more the more rows there are, so these have 8 steps each at least, few rows 4
+    // (1024 x 1024 x 1024, 8 steps: 6.1 us in one part, 7.7 in two).
     uint32_t parts = 1;
     while (parts < 8 && tiles * parts * 2 <= (uint64_t)sm_count() && P.steps >= (P.m > 32 ? 16 : 8) * parts) parts *= 2;
-    // one block per SM has all of the shared memory, two have half of it each (64 x 14336 x 4096: 15.2 us, 18.3 with half)
+    // one block per SM has all of the shared memory, two have half of it each (64 x 14336 x 4096: 14.4 us, 18.0 with half)
     P.stages = tiles * parts <= (uint64_t)sm_count() ? 6 : 3;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((uint32_t)tiles, 1, parts);    // 2^24 at most: one of the two sides has a tile, or there are few

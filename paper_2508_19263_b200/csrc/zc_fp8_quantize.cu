@@ -61,7 +61,7 @@ struct Raw {
 
 // 16 consecutive elements, of which the first n exist (the others read as 0, which no maximum notices).  WIDE: 32-byte
 // loads are aligned.  Otherwise the aligned 16-byte pieces that hold the elements are loaded and shifted into place, where they lie
-// inside the matrix (777 x 11009 in FP16: 12.3 us with loads of single elements, 6.9 so).
+// inside the matrix (777 x 11009 in FP16: 12.3 us with loads of single elements, 6.5 so).
 template <typename T, bool WIDE>
 __device__ __forceinline__ Raw<T> load16(const QuantParams& P, const uint8_t* p, uint32_t n)
 {
