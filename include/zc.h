@@ -482,7 +482,7 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
 
 /* Waits for the stream, returns and clears what zc_fp8_matmul and zc_fp8_moe calls on the current device have left since
  * the last query, on whichever stream: ZC_OK or ZC_E_DEVICE_TIMEOUT.  Calls that are still running on other streams may report to
- * a later query.  Any thread may ask.  ZC_E_CUDA inside a stream capture, which stays as it was. */
+ * a later query.  Any thread may ask.  ZC_E_CUDA on a stream that is being captured; the capture goes on. */
 zc_status zc_fp8_status(void* cuda_stream);
 
 /* A mixture-of-experts layer for a few tokens (1 to ZC_FP8_MOE_MAX_TOKENS).  For a token x:

@@ -545,6 +545,17 @@ __global__ void collect_kernel(unsigned int* product, unsigned int* layer, uint3
 // the larger tiles count for more, which the rule does not look at: 2048 x 1280 x 2048 (40 tiles, 16 steps) 12.4 and 11.7,
 // 1024 x 4096 x 1024 (64 tiles, 8 steps) 9.7 and 8.3.
 constexpr uint64_t kPairsFrom = 37;
+// A plain launch, which says how it went itself: the runtime's last error may be that of another call.
+template <typename... Params, typename... Args>
+static cudaError_t launch(void (*kernel)(Params...), uint32_t grid, uint32_t block, cudaStream_t st, Args... args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+}
+
 // Blocks of the large kernel that are on the GPU at once, in whole pairs.
 static uint32_t large_blocks()
 {
@@ -586,8 +597,7 @@ zc_status zc_fp8_matmul(const zc_fp8_matrix* a, const zc_fp8_matrix* b, zc_real 
     P.m = (uint32_t)a->rows;
     P.n = (uint32_t)b->rows;
     if (a->cols == 0) {
-        if (!accumulate) zero_kernel<<<(uint32_t)std::min<uint64_t>(P.m, 1024), 256, 0, st>>>(P, width);
-        return cudaGetLastError() == cudaSuccess ? ZC_OK : ZC_E_CUDA;
+        return accumulate || launch(zero_kernel, (uint32_t)std::min<uint64_t>(P.m, 1024), 256, st, P, width) == cudaSuccess ? ZC_OK : ZC_E_CUDA;
     }
     P.sa = (const uint8_t*)a->d_scales;
     P.sb = (const uint8_t*)b->d_scales;
@@ -673,8 +683,7 @@ zc_status zc_fp8_status(void* cuda_stream)
     unsigned int *product = marks_word(), *layer = moe_marks_word(), marks = 0;
     if (!product || !layer) return ZC_E_CUDA;
     const uint32_t at = asked.fetch_add(1, std::memory_order_relaxed) % kAnswers;
-    collect_kernel<<<1, 1, 0, st>>>(product, layer, at);
-    if (cudaGetLastError() != cudaSuccess) return ZC_E_CUDA;
+    if (launch(collect_kernel, 1, 1, st, product, layer, at) != cudaSuccess) return ZC_E_CUDA;
     if (cudaMemcpyFromSymbolAsync(&marks, g_answers, sizeof marks, at * sizeof marks, cudaMemcpyDeviceToHost, st) != cudaSuccess) return ZC_E_CUDA;
     if (cudaStreamSynchronize(st) != cudaSuccess) return ZC_E_CUDA;
     test_knobs().fp8_marks = marks;
