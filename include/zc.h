@@ -489,8 +489,8 @@ zc_status zc_fp8_status(void* cuda_stream);
  *   logits = router x; the top_k largest (ties: the lowest index first; NaN counts as the lowest value); p = softmax
  *   over those top_k; y = sum over them of p_e * down_e (silu(gate_e x) * (up_e x)), silu(v) = v / (1 + exp(-v)).
  * The weights are FP8 with 128 x 128 blocks; every expert's matrix has scale bytes of its own, beginning with its first
- * row.  Only the experts that a token chose are read.  Sums are FP32, as zc_fp8_matmul's, those of the router FP64 over parts of
- * 64 columns in FP32: experts whose logits are closer than 2^-20 of their terms' magnitudes may change places.  x is used to 2^-25 of the largest magnitude of its 128 columns, and exactly where it is above 2^-17 of it; the
+ * row.  Only the experts that a token chose are read.  Sums are FP32, as zc_fp8_matmul's, those over inter of parts of 2048
+ * columns that are added to nearest, those of the router FP64 over parts of 64 columns in FP32: experts whose logits are closer than 2^-20 of their terms' magnitudes may change places.  x is used to 2^-25 of the largest magnitude of its 128 columns, and exactly where it is above 2^-17 of it; the
  * hidden vector of an expert goes into the second product with 18 bits of precision, and to 2^-29 of the largest magnitude of
  * its 128 columns; an infinity in either gives NaN.  A wait inside a kernel that gives up leaves the outputs undefined and is reported by zc_fp8_status. */
 typedef struct zc_fp8_moe_layer {

@@ -30,6 +30,10 @@ constexpr uint32_t kMaxRows = kMaxTokens * ZC_FP8_MOE_MAX_TOP_K;
 constexpr uint32_t kBuilders = 16;               // warps that make pieces
 constexpr uint32_t kMoeMaxStages = 9;
 constexpr uint32_t kMoeStageSpace = 208896;      // shared memory for stages: weights, pieces, 1 KiB of scale words each
+// Steps of down (2048 columns) after which the accumulator, which cuts off what does not fit every 32 columns, is added to the partial
+// result in FP32, to nearest: sums of one sign over 14336 columns are less than 6e-6 short, 1.3e-5 in one accumulator; y of experts 14336
+// wide is 5e-5 to 9e-5 from an FP32 form's (norm), 8e-5 to 1.4e-4 in one accumulator; in the same time.
+constexpr uint32_t kPartSteps = 16;
 constexpr uint32_t kMoeHeights = 5;              // tensor copies of 8, 16, 32, 64 and 128 rows
 // Tiles that complete a band at most: a block has up to 4 tiles per pass of an expert (8192 groups of rows in tiles of 16 on more than
 // 128 blocks) and 31 more, so it touches fewer bands than this; launch_moe refuses a GPU with so few SMs that it would not.
@@ -266,6 +270,7 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
     Tiles<UP> tiles(S.R, cut, rows, P.pass, blockIdx.x, blocks);
     Tile t;
     const uint32_t tmem = S.tmem;
+    const uint32_t most = UP ? steps : kPartSteps;
     // the stage of the present step and the parity of its round; `first`: no stage has been used yet
     uint32_t st = 0, round = 0;
     auto forward = [&] { if (++st == stages) { st = 0; ++round; } };
@@ -296,13 +301,17 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
         // nothing is copied into this block's shared memory any more, whether the block gave up or not
         if (!P.skip_copy && !settled_stage(smem_u32(S.copied), lane, stages, st, round, P.spin_limit)) S.failed = S.unsettled = 1;
     } else if (warp == 1 && !P.skip_math) {
-        uint32_t tile = 0;
+        uint32_t part = 0, k = steps;            // k: of the present tile, which is done
         bool ok = true;
-        while (ok && tiles.next(t)) {
-            const uint32_t buf = tile & 1, d = tmem + buf * 128;
+        while (ok) {
+            if (k == steps) {
+                if (!tiles.next(t)) break;
+                k = 0;
+            }
+            const uint32_t buf = part & 1, d = tmem + buf * 128, first = k, end = min(steps, k + most);
             const uint32_t idesc = P.idesc | ((piece_rows(t.count, PIECES) >> 3) << 17);
-            if (tile >= 2 && !(ok = wait.warp(smem_u32(&S.acc_empty[buf]), ((tile >> 1) - 1) & 1))) break;
-            for (uint32_t k = 0; k < steps; ++k, forward()) {
+            if (part >= 2 && !(ok = wait.warp(smem_u32(&S.acc_empty[buf]), ((part >> 1) - 1) & 1))) break;
+            for (; k < end; ++k, forward()) {
                 if (!(ok = wait.warp_both(smem_u32(&S.full[st]), smem_u32(&S.copied[st]), round & 1))) break;
                 tc_fence_after();
                 const uint32_t at = base + st * stage_bytes, sf = tmem + kMoeTmemScales + st * 8;
@@ -311,17 +320,17 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
                     tmem_copy_scales<1>(sf, at + scales_at);
                     tmem_copy_scales<1>(sf + 4, at + scales_at + 512);
 #pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j) mma_scaled<1>(d, da + 2 * j, db + 2 * j, idesc, sf, sf + 4, k | j);
+                    for (uint32_t j = 0; j < 4; ++j) mma_scaled<1>(d, da + 2 * j, db + 2 * j, idesc, sf, sf + 4, (k - first) | j);
                     mma_commit<1>(smem_u32(&S.empty[st]));
                 }
                 __syncwarp();
             }
             if (elect_one()) mma_commit<1>(smem_u32(&S.acc_full[buf]));
             __syncwarp();
-            ++tile;
+            ++part;
         }
         // nor do matrix instructions read from there
-        if (tile && lane == 0 && !settled(smem_u32(&S.acc_full[(tile - 1) & 1]), ((tile - 1) >> 1) & 1, P.spin_limit)) S.failed = S.unsettled = 1;
+        if (part && lane == 0 && !settled(smem_u32(&S.acc_full[(part - 1) & 1]), ((part - 1) >> 1) & 1, P.spin_limit)) S.failed = S.unsettled = 1;
     } else if (warp == 2) {
         // scale bytes of the weights, four steps at a time and four steps ahead; row r of the tile's operand is row 32 j + lane
         const uint32_t sld = steps, srows = (rows + 127) >> 7;
@@ -436,35 +445,40 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
         }
     } else if (warp >= 4) {
         const uint32_t quad = warp & 3;
-        uint32_t tile = 0;
-        while (tiles.next(t)) {
-            const uint32_t buf = tile & 1, padded = (t.count + 7) & ~7u;
+        uint32_t part = 0, k = steps;
+        while (true) {
+            if (k == steps) {
+                if (!tiles.next(t)) break;
+                k = 0;
+            }
+            const uint32_t buf = part & 1, padded = (t.count + 7) & ~7u;
             // the four warps go on, or stop, together: they meet at a barrier of their own
-            uint32_t ok = wait(smem_u32(&S.acc_full[buf]), (tile >> 1) & 1) && !*wait.failed;
+            uint32_t ok = wait(smem_u32(&S.acc_full[buf]), (part >> 1) & 1) && !*wait.failed;
             asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %0, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "+r"(ok) :: "memory");
             if (!ok) break;
             tc_fence_after();
             const uint32_t d = tmem + (quad * 32u << 16) + buf * 128;
             for (uint32_t c = 0; c < t.count; c += 8) {
-                float part[PIECES][8];
+                float piece[PIECES][8];
 #pragma unroll
-                for (uint32_t q = 0; q < PIECES; ++q) tmem_ld8(d + q * padded + c, part[q]);
+                for (uint32_t q = 0; q < PIECES; ++q) tmem_ld8(d + q * padded + c, piece[q]);
                 tmem_ld_wait();
                 // the smallest pieces first
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    float sum = part[PIECES - 1][i];
+                    float sum = piece[PIECES - 1][i];
 #pragma unroll
-                    for (int q = PIECES - 2; q >= 0; --q) sum += part[q][i];
-                    part[0][i] = sum;
+                    for (int q = PIECES - 2; q >= 0; --q) sum += piece[q][i];
+                    piece[0][i] = sum;
                 }
-                finish.store(t, c, quad, lane, part[0]);
+                finish.store(t, c, quad, lane, piece[0], k != 0);
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(smem_u32(&S.acc_empty[buf]));
-            finish.tile_done(t);
-            ++tile;
+            ++part;
+            k = min(steps, k + most);
+            if (k == steps) finish.tile_done(t);
         }
     }
     __syncwarp();
@@ -698,7 +712,7 @@ __device__ __forceinline__ void moe_setup(MoeShared& S, uint32_t sharing)
 struct FinishUp {
     const MoeParams& P;
     MoeShared& S;
-    __device__ __forceinline__ void store(const Tile& t, uint32_t c, uint32_t quad, uint32_t lane, const float v[8]) const
+    __device__ __forceinline__ void store(const Tile& t, uint32_t c, uint32_t quad, uint32_t lane, const float v[8], bool) const
     {
         const uint32_t row = (quad & 1) * 32 + lane, ch = t.group * 8 + row, mine = quad >> 1;     // gates' warps take tokens 0-3, ups' 4-7
         float* out = S.other[mine ^ 1][row];
@@ -724,13 +738,17 @@ struct FinishDown {
     const MoeParams& P;
     MoeShared& S;
     uint32_t n_passes;
-    __device__ __forceinline__ void store(const Tile& t, uint32_t c, uint32_t quad, uint32_t lane, const float v[8]) const
+    __device__ __forceinline__ void store(const Tile& t, uint32_t c, uint32_t quad, uint32_t lane, const float v[8], bool add) const
     {
         const uint32_t row = quad * 32 + lane, r = t.group * 8 + row;
         if (row >= t.groups * 8 || r >= P.hidden) return;
+        float* z = P.z + (uint64_t)(t.row + c) * P.hidden_pad + r;
+        float sum[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) sum[i] = c + i < t.count && add ? v[i] + z[(uint64_t)i * P.hidden_pad] : v[i];
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i)
-            if (c + i < t.count) P.z[(uint64_t)(t.row + c + i) * P.hidden_pad + r] = v[i];
+            if (c + i < t.count) z[(uint64_t)i * P.hidden_pad] = sum[i];
     }
     // The four warps: whoever completes a group's last pass adds its experts up, at the end, with all of the block's threads (they wait
     // for little but loads then: 128 threads took 16 us after the last product of 64 tokens).

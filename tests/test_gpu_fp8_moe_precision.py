@@ -51,3 +51,41 @@ def test_differences_of_neighbouring_hidden_values(dtype):
     off = both * (2.0 ** -21 + 2.0 ** -19 + 2.0 ** -21 + 2.0 ** -22) + 2 * 2.0 ** -29 * np.abs(h).max()
     t = torch.finfo(dtype)
     assert (np.abs(y - want) <= off + t.eps / 2 * (np.abs(want) + off) + t.smallest_normal * t.eps / 2).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_long_sums(dtype):
+    """Sums of positive products over 14336 - 128 inner channels, of which the last 128 take all but a trace off again: what is left shows
+    what the sums lose on the way, which the rounding of the result would hide otherwise.
+
+    gate is 32, so h = 32 up without a rounding, and up is an element of the weights: h goes into the product exactly.  The accumulators
+    cut off what does not fit, less than a unit, 2^-23, of the sum as it is after every 32 columns.  Over the 2048 columns of a part the sum grows
+    evenly: (64 + 1) / 2 units of what the part comes to, plus 9.1 / sqrt(2048) of that, six standard deviations of the average of the sums on the way (a
+    product of two of the elements deviates by 2.62 times its mean).  All parts come to the whole.  The last four instructions take it off: a unit
+    of the whole each.  The parts are added to nearest: half a unit each, and there are seven."""
+    hidden, inter, last = 256, 14336, 128
+    g = torch.Generator().manual_seed(43)
+    values = torch.arange(64, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
+    x = torch.zeros((1, hidden), dtype=dtype)
+    x[0, 0], x[0, 1] = 32.0, 1.0
+    gate_up = torch.zeros((1, 2, inter, hidden), dtype=torch.uint8)
+    gate_up[0, 0, :, 0] = ONE
+    up = torch.randint(0, 64, (inter,), generator=g, dtype=torch.uint8)
+    gate_up[0, 1, :, 1] = up
+    h = 32 * values[up.long()]
+    down = torch.randint(0, 64, (hidden, inter), generator=g, dtype=torch.uint8)
+    scales = torch.full((1, 2, inter // 128), 127, dtype=torch.uint8)
+    scales[0, :, -1] = 127 + 7                                               # the last block's elements count 128 times
+    whole = values[down[:, :-last].long()] @ h[:-last]
+    left = whole.clone()
+    for c in (inter - last + torch.argsort(h[-last:], descending=True)).tolist():
+        code = torch.searchsorted(values, left / (128 * h[c]).clamp(min=1e-9), right=True) - 1      # the largest element that does not take too much
+        down[:, c] = code.clamp(0, 63).to(torch.uint8) | 0x80
+        left -= values[code.clamp(0, 63)] * 128 * h[c]
+    assert bool((left >= 0).all()) and bool((left < 2.0 ** -12 * whole).all())
+    layer = zc.Fp8MoeLayer(torch.zeros((1, hidden), dtype=dtype, device=DEV), gate_up.to(DEV), torch.full((1, 2, inter // 128, 2), 127, dtype=torch.uint8, device=DEV),
+                           down[None].to(DEV), scales.to(DEV), 1)
+    y = run(layer, x.to(DEV)).double().cpu()[0]
+    off = whole * 2.0 ** -24 * (65 * (1 + 9.1 / 2048 ** 0.5) + 4 * 2 + 7)
+    t = torch.finfo(dtype)
+    assert bool(((y - left).abs() <= off + t.eps / 2 * (left + off) + t.smallest_normal * t.eps / 2).all()), ((y - left).abs() / whole * 2.0 ** 24).max()
