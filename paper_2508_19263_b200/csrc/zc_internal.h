@@ -2,6 +2,7 @@
 #pragma once
 #include <stdint.h>
 #include <stddef.h>
+#include <atomic>
 #include "zc.h"
 
 namespace zc {
@@ -128,7 +129,7 @@ struct TestKnobs {
     uint32_t first_ticket;   // first batch the encoder hands out (not 0: batch 0 is never packed, so every look-back stalls)
     uint32_t skip_copy;      // the decoder does not start the copies of the pieces it then waits for
     uint32_t skip_math;    // zc_fp8_matmul and zc_fp8_moe copy their operands, but start no matrix instruction
-    uint32_t fp8_marks;      // what the last zc_fp8_status found
+    std::atomic<uint32_t> fp8_marks;   // what the last zc_fp8_status found, on whichever thread
 };
 TestKnobs& test_knobs();
 // Development build (-DZC_DEBUG_CHECKS=1): each translation unit with kernels adds its counts of refused shared and
