@@ -271,7 +271,7 @@ __device__ __forceinline__ void stream_weights(const MoeParams& P, const MoeMaps
     Tile t;
     const uint32_t tmem = S.tmem;
     const uint32_t most = UP ? steps : kPartSteps;
-    // the stage of the present step and the parity of its round; `first`: no stage has been used yet
+    // the stage of the present step and its round
     uint32_t st = 0, round = 0;
     auto forward = [&] { if (++st == stages) { st = 0; ++round; } };
     auto free_stage = [&] { return round == 0 || wait(smem_u32(&S.empty[st]), (round - 1) & 1); };
