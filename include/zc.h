@@ -525,6 +525,97 @@ zc_status zc_fp8_moe(const zc_fp8_moe_layer* layer, uint32_t n_tokens, const voi
                      uint64_t ld_out, uint32_t* d_ids, float* d_weights, void* d_workspace, size_t workspace_bytes,
                      void* cuda_stream);
 
+/* ---- a quantised cache of keys and values --------------------------------------------------------
+ * (No counterpart in the paper, which compresses such caches: what a program keeps them in and reads them by.)  The keys and values
+ * of one layer lie in pages of page_tokens tokens: elements [n_pages][kv_heads][page_tokens][head_dim], the bytes of
+ * ZC_FMT_FP4_E2M1 (two elements a byte, the even one in the low half) or ZC_FMT_FP8_E4M3, and scale bytes s
+ * [n_pages][kv_heads][page_tokens][head_dim / 32], the bytes of ZC_FMT_SCALE_U8 in E8M0: an element stands for its value times
+ * 2^(s - 127), s = 255 for NaN.  No padding anywhere.  So a page, or the whole cache, goes through the codec as it is. */
+typedef struct zc_kv_cache {
+    void *d_k_elems, *d_k_scales, *d_v_elems, *d_v_scales;      /* 16-byte aligned */
+    uint64_t n_pages;           /* n_pages * kv_heads * page_tokens below 2^31 */
+    uint32_t page_tokens;       /* 16, 32, 64, 128 or 256 */
+    uint32_t kv_heads;          /* 1 .. ZC_KV_MAX_HEADS */
+    uint32_t head_dim;          /* 64 or 128 */
+    uint32_t format;            /* ZC_FMT_FP4_E2M1 or ZC_FMT_FP8_E4M3 */
+} zc_kv_cache;
+#define ZC_KV_MAX_HEADS 1024u
+
+/* The sequences of a call.  Their lengths and pages are read on the device, so that a captured call follows them.
+ * Rows: the tensors of a call hold the LAST tokens of the sequences, rows first[b] .. first[b + 1] - 1 those of sequence b; of its
+ * n = first[b + 1] - first[b] rows, row j is the token at position lens[b] - n + j.  lens counts them: they are in the cache or about
+ * to be written.  Rows before first[0] or from first[n_seqs] on belong to nobody: they are not read and, in results, left as they were.
+ * A row whose position is negative has no place in the cache: it is not stored, it is read as zeros, and a causal attention shows it
+ * nothing.
+ * What is wrong on the device is never followed: a length below 0 counts as 0, one above what the table's row has room for as that; a page
+ * outside 0 .. n_pages - 1 is not touched, its tokens are not stored, are read as zeros and are left out of the attention.
+ * zc_kv_status then says ZC_E_CORRUPT.  Table entries behind a sequence's last token are not read. */
+typedef struct zc_kv_batch {
+    const int32_t* d_page_table;   /* [n_seqs] rows of max_pages pages, row pitch ld_page_table elements */
+    const int32_t* d_lens;         /* [n_seqs] */
+    const int32_t* d_first;        /* [n_seqs + 1], not falling */
+    uint64_t ld_page_table;
+    uint64_t n_rows;               /* rows that the call's tensors have, below 2^31 */
+    uint32_t max_pages;            /* max_pages * page_tokens below 2^31 */
+    uint32_t n_seqs;               /* 0 .. ZC_KV_MAX_SEQS */
+    uint32_t max_new;              /* rows that a sequence is expected to have at most; decides only which kernels run, not what they compute */
+} zc_kv_batch;
+#define ZC_KV_MAX_SEQS 4096u
+
+/* A tensor [n_rows][heads][head_dim]: element (r, h, i) is at r * ld_row + h * ld_head + i.  Any alignment that the type has. */
+typedef struct zc_kv_tensor {
+    void* d;
+    uint64_t ld_row, ld_head;      /* elements, at least head_dim where there is more than one, below 2^39 */
+} zc_kv_tensor;
+
+/* Keys and values of the batch's rows into the cache.
+ * Scale of a block of 32 elements of a token's head: the least power of two 2^e, -127 <= e <= 127, with amax <= max * 2^e, max = 6 (FP4)
+ * or 448 (E4M3); e = -127 for a block of zeros.  Element: the value times 2^-e rounded to nearest even, with its sign, also of zero.
+ * FP4 has neither NaN nor infinities: a block with one gets the scale byte 255 and zeros, and is NaN when it is read.  In E4M3 amax is
+ * that of the finite elements, NaN stays NaN and an infinity becomes NaN.
+ * type     of k and v: any zc_real
+ * Two rows must not have the same place (sequences that share a page are fine as long as they write elsewhere).  Asynchronous.
+ * Errors: INVALID_ARG (null or misaligned pointers, pitches), UNSUPPORTED (types, formats, page_tokens, head_dim), TOO_LARGE, CUDA. */
+zc_status zc_kv_append(const zc_kv_cache* cache, const zc_kv_batch* batch, zc_real type, const zc_kv_tensor* k, const zc_kv_tensor* v,
+                       void* cuda_stream);
+
+/* The batch's rows out of the cache: values rounded to nearest even to `type` (exact in FP32; in BF16 all but the smallest subnormals are).
+ * k, v     one may be null: not wanted.  They must not overlap the cache or each other.  Asynchronous.
+ * Errors: as zc_kv_append. */
+zc_status zc_kv_read(const zc_kv_cache* cache, const zc_kv_batch* batch, zc_real type, const zc_kv_tensor* k, const zc_kv_tensor* v,
+                     void* cuda_stream);
+
+/* Attention over the cache: for row r of sequence b and query head h, with head h / (q_heads / kv_heads) of the cache,
+ *   x_t = scale * sum_i q[r][h][i] * K_t[i],  out[r][h] = sum_t softmax(x)_t * V_t,  lse[r][h] = log sum_t exp(x_t)
+ * over the tokens t of b that the row sees: all lens[b] of them, or where causal those up to its own position, and of these the last
+ * `window` where window > 0.  A row that sees nothing gets zeros and lse = -infinity.  What is in the cache where no row looks (behind the last
+ * token, outside the window) has no influence, whatever it is; NaN that a row sees makes NaN what depends on it. */
+typedef struct zc_kv_attention_args {
+    zc_kv_tensor q, out;           /* [n_rows][q_heads][head_dim] of `type`; must not overlap */
+    float* d_lse;                  /* [n_rows][q_heads], no padding; null: not wanted */
+    uint32_t type;                 /* ZC_REAL_BF16 or ZC_REAL_F16 */
+    uint32_t q_heads;              /* a multiple of kv_heads */
+    float scale;                   /* finite */
+    uint32_t causal;               /* 0 or 1 */
+    uint32_t window;               /* 0: none; only with causal */
+} zc_kv_attention_args;
+#define ZC_KV_MAX_GROUP 256u       /* query heads that share a head of the cache */
+
+/* Bytes of device scratch zc_kv_attention needs for up to q_heads query heads (it depends on neither lengths nor rows); 0 for arguments that it
+ * would refuse. */
+size_t zc_kv_attention_workspace_bytes(const zc_kv_cache* cache, const zc_kv_batch* batch, uint32_t q_heads);
+/* d_workspace  workspace_bytes >= zc_kv_attention_workspace_bytes(), 256-byte aligned, contents need not be initialised; calls that
+ *              overlap in time must not share it.  Asynchronous.  The result is the same every time.
+ * Errors: INVALID_ARG (null or misaligned pointers, pitches, q_heads, scale, causal, window), UNSUPPORTED (types, formats, page_tokens, head_dim),
+ * TOO_LARGE, BUFFER_TOO_SMALL (workspace), CUDA. */
+zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, const zc_kv_attention_args* args, void* d_workspace,
+                          size_t workspace_bytes, void* cuda_stream);
+
+/* Waits for the stream, returns and clears what zc_kv_* calls on the current device have left since the last query, on whichever stream:
+ * ZC_OK, ZC_E_DEVICE_TIMEOUT (a wait inside a kernel gave up; results are undefined) or ZC_E_CORRUPT (lengths or pages outside their ranges).
+ * Calls that are still running on other streams may report to a later query.  ZC_E_CUDA on a stream that is being captured; the capture goes on. */
+zc_status zc_kv_status(void* cuda_stream);
+
 const char* zc_strerror(zc_status s);
 
 #ifdef __cplusplus

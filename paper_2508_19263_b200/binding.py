@@ -70,6 +70,25 @@ class Fp8MoeLayerDesc(C.Structure):
                 ("format", C.c_uint32), ("real_type", C.c_uint32)]
 
 
+class KvCacheDesc(C.Structure):
+    _fields_ = [("d_k_elems", C.c_void_p), ("d_k_scales", C.c_void_p), ("d_v_elems", C.c_void_p), ("d_v_scales", C.c_void_p),
+                ("n_pages", C.c_uint64), ("page_tokens", C.c_uint32), ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("format", C.c_uint32)]
+
+
+class KvBatchDesc(C.Structure):
+    _fields_ = [("d_page_table", C.c_void_p), ("d_lens", C.c_void_p), ("d_first", C.c_void_p), ("ld_page_table", C.c_uint64),
+                ("n_rows", C.c_uint64), ("max_pages", C.c_uint32), ("n_seqs", C.c_uint32), ("max_new", C.c_uint32)]
+
+
+class KvTensorDesc(C.Structure):
+    _fields_ = [("d", C.c_void_p), ("ld_row", C.c_uint64), ("ld_head", C.c_uint64)]
+
+
+class KvAttentionArgs(C.Structure):
+    _fields_ = [("q", KvTensorDesc), ("out", KvTensorDesc), ("d_lse", C.c_void_p), ("type", C.c_uint32), ("q_heads", C.c_uint32),
+                ("scale", C.c_float), ("causal", C.c_uint32), ("window", C.c_uint32)]
+
+
 def _load():
     # ZC_LIBRARY: another build of the same library (the development build with in-kernel checks), for tests
     path = os.environ.get("ZC_LIBRARY") or _build.LIB
@@ -175,6 +194,15 @@ def _load():
     L.zc_fp8_moe_workspace_bytes.argtypes = [vp, C.c_uint32]
     L.zc_fp8_moe.restype = C.c_int
     L.zc_fp8_moe.argtypes = [vp, C.c_uint32, vp, C.c_uint64, vp, C.c_uint64, vp, vp, vp, C.c_size_t, vp]
+    for name in ("zc_kv_append", "zc_kv_read"):
+        getattr(L, name).restype = C.c_int
+        getattr(L, name).argtypes = [vp, vp, C.c_int, vp, vp, vp]
+    L.zc_kv_attention_workspace_bytes.restype = C.c_size_t
+    L.zc_kv_attention_workspace_bytes.argtypes = [vp, vp, C.c_uint32]
+    L.zc_kv_attention.restype = C.c_int
+    L.zc_kv_attention.argtypes = [vp, vp, vp, vp, C.c_size_t, vp]
+    L.zc_kv_status.restype = C.c_int
+    L.zc_kv_status.argtypes = [vp]
     L.zc_fp8_status.restype = C.c_int
     L.zc_fp8_status.argtypes = [vp]
     for name in ("zc_test_set_wait_limit", "zc_test_stall_encoder", "zc_test_stall_decoder", "zc_test_stall_math"):
@@ -674,6 +702,150 @@ def fp8_moe(layer: Fp8MoeLayer, d_x: torch.Tensor, d_out: torch.Tensor, d_worksp
     if status != OK:
         raise ZcError(status, "zc_fp8_moe")
     return d_out
+
+
+# ---- a quantised cache of keys and values ----
+
+class KvCache:
+    """zc_kv_cache: the keys and values of one layer in pages.  Elements uint8 [pages, kv_heads, page_tokens, head_dim / 2]
+    (FMT_FP4_E2M1) or [..., head_dim] (FMT_FP8_E4M3) and scale bytes uint8 [pages, kv_heads, page_tokens, head_dim / 32], all
+    contiguous.  Marshalled once; keeps its tensors alive."""
+
+    def __init__(self, k_elems: torch.Tensor, k_scales: torch.Tensor, v_elems: torch.Tensor, v_scales: torch.Tensor, fmt: int = FMT_FP4_E2M1):
+        if fmt not in (FMT_FP4_E2M1, FMT_FP8_E4M3):
+            raise ValueError("a cache is FMT_FP4_E2M1 or FMT_FP8_E4M3")
+        if any(t.dtype != torch.uint8 or t.dim() != 4 or not t.is_contiguous() for t in (k_elems, k_scales, v_elems, v_scales)):
+            raise ValueError("elements and scale bytes are contiguous uint8 tensors [pages, kv_heads, page_tokens, bytes]")
+        pages, heads, tokens, width = k_elems.shape
+        dim = width * (2 if fmt == FMT_FP4_E2M1 else 1)
+        if v_elems.shape != k_elems.shape or any(tuple(t.shape) != (pages, heads, tokens, dim // 32) for t in (k_scales, v_scales)):
+            raise ValueError(f"elements {tuple(k_elems.shape)}, {tuple(v_elems.shape)} and scales {tuple(k_scales.shape)}, {tuple(v_scales.shape)} do not belong together")
+        self.k_elems, self.k_scales, self.v_elems, self.v_scales, self.format = k_elems, k_scales, v_elems, v_scales, fmt
+        self.n_pages, self.kv_heads, self.page_tokens, self.head_dim = pages, heads, tokens, dim
+        self.desc = KvCacheDesc(k_elems.data_ptr(), k_scales.data_ptr(), v_elems.data_ptr(), v_scales.data_ptr(), pages, tokens, heads, dim, fmt)
+        self._ref = C.addressof(self.desc)
+        self._dev = k_elems.get_device()
+        if any(t.get_device() != self._dev for t in (k_scales, v_elems, v_scales)):
+            raise ValueError("the cache's tensors are on several devices")
+
+
+def kv_empty(n_pages: int, kv_heads: int, page_tokens: int, head_dim: int, fmt: int = FMT_FP4_E2M1, device="cuda") -> KvCache:
+    """A KvCache of new buffers, contents undefined."""
+    make = lambda width: torch.empty((n_pages, kv_heads, page_tokens, width), dtype=torch.uint8, device=device)  # noqa: E731
+    width = head_dim // 2 if fmt == FMT_FP4_E2M1 else head_dim
+    return KvCache(make(width), make(head_dim // 32), make(width), make(head_dim // 32), fmt)
+
+
+class KvBatch:
+    """zc_kv_batch: page_table int32 [sequences, pages] with contiguous rows, lens int32 [sequences], first int32 [sequences + 1], all read
+    on the device; max_new: rows that a sequence is expected to have at most (it decides which kernels run, not what they
+    compute).  Marshalled once; keeps its tensors alive."""
+
+    def __init__(self, page_table: torch.Tensor, lens: torch.Tensor, first: torch.Tensor, max_new: int = 1):
+        if any(t.dtype != torch.int32 for t in (page_table, lens, first)):
+            raise ValueError("page_table, lens and first are int32")
+        if page_table.dim() != 2 or (page_table.stride(1) != 1 and page_table.shape[1] > 1):
+            raise ValueError("page_table is a matrix with contiguous rows")
+        seqs, pages = page_table.shape
+        if tuple(lens.shape) != (seqs,) or tuple(first.shape) != (seqs + 1,) or not lens.is_contiguous() or not first.is_contiguous():
+            raise ValueError(f"lens and first are contiguous, of {seqs} and {seqs + 1} elements")
+        if not 0 <= max_new < 1 << 32:
+            raise ValueError("max_new is out of range")
+        self.page_table, self.lens, self.first, self.max_new, self.n_seqs = page_table, lens, first, max_new, seqs
+        pitch = page_table.stride(0) if seqs > 1 else max(page_table.stride(0), pages)
+        self._desc = (page_table.data_ptr(), lens.data_ptr(), first.data_ptr(), pitch)
+        self._made = {}
+        self._dev = lens.get_device()
+        if any(t.get_device() != self._dev for t in (page_table, first)):
+            raise ValueError("the batch's tensors are on several devices")
+
+    def _ref(self, n_rows: int):
+        """The descriptor for tensors of n_rows rows."""
+        made = self._made.get(n_rows)
+        if made is None:
+            if len(self._made) >= 8:
+                self._made.clear()
+            d = KvBatchDesc(*self._desc, n_rows, self.page_table.shape[1], self.n_seqs, self.max_new)
+            made = self._made[n_rows] = (C.addressof(d), d)
+        return made[0]
+
+
+def _kv_tensor(t: Optional[torch.Tensor], what: str, heads: int, dim: int) -> KvTensorDesc:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or stride[2] != 1:
+        raise ValueError(f"{what}: [rows, {heads}, {dim}] with contiguous heads is wanted, got shape {tuple(shape)}, strides {stride}")
+    return KvTensorDesc(t.data_ptr(), stride[0], stride[1])
+
+
+def _kv_rows(call, where: str, cache: KvCache, batch: KvBatch, d_k: Optional[torch.Tensor], d_v: Optional[torch.Tensor], stream):
+    one = d_k if d_k is not None else d_v
+    if one is None:
+        raise ValueError("neither keys nor values")
+    real = _REAL.get(one.dtype)
+    if real is None:
+        raise TypeError(f"float32, bfloat16 or float16 is wanted, got {one.dtype}")
+    descs, devs = [], [cache._dev, batch._dev]
+    for t, what in ((d_k, "d_k"), (d_v, "d_v")):
+        if t is not None:
+            if t.dtype != one.dtype or t.shape[0] != one.shape[0]:
+                raise ValueError("d_k and d_v are of one type and have the same rows")
+            descs.append(_kv_tensor(t, what, cache.kv_heads, cache.head_dim))
+            devs.append(t.get_device())
+        else:
+            descs.append(None)
+    dev = _same_device(*devs)
+    status = call(cache._ref, batch._ref(one.shape[0]), real, *[C.addressof(d) if d is not None else None for d in descs], _stream_of(stream, dev))
+    if status != OK:
+        raise ZcError(status, where)
+
+
+def kv_append(cache: KvCache, batch: KvBatch, d_k: torch.Tensor, d_v: torch.Tensor, stream=None) -> None:
+    """zc_kv_append: keys and values [rows, kv_heads, head_dim] of the batch's rows into the cache (asynchronous)."""
+    if d_k is None or d_v is None:
+        raise ValueError("keys and values are written together")
+    _kv_rows(_lib.zc_kv_append, "zc_kv_append", cache, batch, d_k, d_v, stream)
+
+
+def kv_read(cache: KvCache, batch: KvBatch, d_k: Optional[torch.Tensor], d_v: Optional[torch.Tensor], stream=None):
+    """zc_kv_read: the batch's rows out of the cache into d_k and / or d_v (asynchronous)."""
+    _kv_rows(_lib.zc_kv_read, "zc_kv_read", cache, batch, d_k, d_v, stream)
+    return d_k, d_v
+
+
+def kv_attention_workspace_bytes(cache: KvCache, batch: KvBatch, q_heads: int) -> int:
+    """zc_kv_attention_workspace_bytes."""
+    return int(_lib.zc_kv_attention_workspace_bytes(cache._ref, batch._ref(1), q_heads))
+
+
+def kv_attention(cache: KvCache, batch: KvBatch, d_q: torch.Tensor, d_out: torch.Tensor, d_workspace: torch.Tensor, scale: Optional[float] = None,
+                 causal: bool = True, window: int = 0, d_lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """zc_kv_attention: d_out[rows, q_heads, head_dim] = attention of d_q over the cache (asynchronous).  scale: 1 / sqrt(head_dim) where it is not
+    given; d_lse: float32 [rows, q_heads], contiguous, receives the logarithms of the sums."""
+    real = _REAL.get(d_q.dtype)
+    if real is None or d_out.dtype != d_q.dtype:
+        raise TypeError(f"d_q and d_out are bfloat16 or float16, got {d_q.dtype} and {d_out.dtype}")
+    rows, heads = d_q.shape[0], d_q.shape[1]
+    if d_out.shape != d_q.shape:
+        raise ValueError(f"d_q is {tuple(d_q.shape)}, d_out {tuple(d_out.shape)}")
+    args = KvAttentionArgs(_kv_tensor(d_q, "d_q", heads, cache.head_dim), _kv_tensor(d_out, "d_out", heads, cache.head_dim), None, real, heads,
+                           cache.head_dim ** -0.5 if scale is None else scale, causal, window)
+    devs = [cache._dev, batch._dev, d_q.get_device(), d_out.get_device(), d_workspace.get_device()]
+    if d_lse is not None:
+        if d_lse.dtype != torch.float32 or tuple(d_lse.shape) != (rows, heads) or not d_lse.is_contiguous():
+            raise ValueError(f"d_lse is contiguous float32 of shape {(rows, heads)}")
+        args.d_lse = d_lse.data_ptr()
+        devs.append(d_lse.get_device())
+    dev = _same_device(*devs)
+    status = _lib.zc_kv_attention(cache._ref, batch._ref(rows), C.addressof(args), d_workspace.data_ptr(),
+                                  d_workspace.numel() * d_workspace.element_size(), _stream_of(stream, dev))
+    if status != OK:
+        raise ZcError(status, "zc_kv_attention")
+    return d_out
+
+
+def kv_status(stream=None) -> int:
+    """zc_kv_status: device status of the kv_* calls on the current device since the last query."""
+    return int(_lib.zc_kv_status(_stream_ptr(stream)))
 
 
 def validate_container(p: Plan, h_container) -> int:
