@@ -1,102 +1,59 @@
-// Attention over a quantised key/value cache.
-//
-// The simplest kernel that is right: a warp has a row and a query head; a lane has a token of 32 for the products with the query, then a
-// 32nd of the head's width for the sum of the values.  Running maximum and sum, all in FP32.
+// Attention over a quantised key/value cache: arguments, choice of kernels, launches.
 #include <type_traits>
 
-#include "zc_kv.cuh"
+#include "zc_kv_stream.cuh"
 
 namespace zc {
 
-struct AttentionParams {
-    KvCache C;
-    KvBatch B;
-    KvTensor q, out;
-    float* lse;
-    uint32_t q_heads, group;
-    float scale;
-    uint32_t causal, window;
-};
-
-constexpr uint32_t kSimpleWarps = 4;
-
-template <typename T, bool FP4, uint32_t DIM>
-__global__ void __launch_bounds__(kSimpleWarps * 32) kv_attention_simple_kernel(const AttentionParams P)
+// The elements of a cache, a token's head a row, as boxes of up to 32 tokens of a page in the swizzle as wide as a row.
+static bool make_cache_map(CUtensorMap* map, const void* elems, uint64_t rows, uint32_t row_bytes, uint32_t box_rows)
 {
-    __shared__ float s_q[kSimpleWarps][DIM];
-    constexpr uint32_t kRowBytes = FP4 ? DIM / 2 : DIM, kBlocks = DIM / kKvBlock, kOwn = DIM / 32;
-    grid_wait();
-    grid_launch_dependents();
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint64_t item = (uint64_t)blockIdx.x * kSimpleWarps + warp;
-    const int row = (int)(item / P.q_heads);
-    const uint32_t head = (uint32_t)(item % P.q_heads), kv = head / P.group;
-    if ((uint32_t)row >= P.B.n_rows) return;
-    const int found = kv_find(P.B, row);
-    uint32_t b = found < 0 ? 0 : (uint32_t)found;
-    int pos;
-    if (!kv_position(P.B, row, b, pos)) return;
-    const int len = kv_len(P.B, b), to = P.causal ? pos + 1 : len, from = P.window ? max(0, to - (int)min(P.window, 0x7FFFFFFFu)) : 0;
-    const T* q = reinterpret_cast<const T*>(P.q.d + (uint64_t)row * P.q.ld_row + head * P.q.ld_head);
-    for (uint32_t i = lane; i < DIM; i += 32) s_q[warp][i] = (float)q[i];
-    __syncwarp();
-    float top = -INFINITY, sum = 0.0f, acc[kOwn] = {};
-    for (int t0 = from / 32 * 32; t0 < to; t0 += 32) {
-        const int t = t0 + (int)lane;
-        int page = t >= from && t < to ? kv_page(P.C, P.B, b, (uint32_t)t >> P.C.page_shift) : -1;
-        const uint64_t at = page < 0 ? 0 : ((((uint64_t)page * P.C.heads + kv) << P.C.page_shift) + (t & ((1 << P.C.page_shift) - 1)));
-        float x = -INFINITY;
-        if (page >= 0) {
-            const uint32_t* w = reinterpret_cast<const uint32_t*>(P.C.elems[0] + at * kRowBytes);
-            x = 0.0f;
-            for (uint32_t k = 0; k < kBlocks; ++k) {
-                float part = 0.0f;
-                for (uint32_t i = 0; i < kRowBytes / kBlocks / 4; ++i) {
-                    uint32_t h[4];
-                    const uint32_t word = w[k * (kRowBytes / kBlocks / 4) + i];
-                    if (FP4) fp4_to_half(word, h);
-                    else e4m3_to_half(word, h);
-                    for (uint32_t j = 0; j < (FP4 ? 4 : 2); ++j) {
-                        const float2 e = half_pair(h[j]);
-                        const uint32_t d = k * kKvBlock + i * (FP4 ? 8 : 4) + 2 * j;
-                        part = fmaf(e.x, s_q[warp][d], fmaf(e.y, s_q[warp][d + 1], part));
-                    }
-                }
-                x = fmaf(part, e8m0_value(P.C.scales[0][at * kBlocks + k]), x);
-            }
-            x *= P.scale;
-        }
-        float best = x;
-        for (int d = 16; d; d >>= 1) best = fmaxf(best, __shfl_xor_sync(0xFFFFFFFFu, best, d));
-        const bool bad = __any_sync(0xFFFFFFFFu, x != x);
-        const float next = fmaxf(top, best);
-        if (next == -INFINITY && !bad) continue;
-        const float shrink = top == -INFINITY ? 0.0f : expf(top - next), p = page >= 0 ? expf(x - next) : 0.0f;
-        top = next;
-        sum = sum * shrink + p;
-        for (uint32_t i = 0; i < kOwn; ++i) acc[i] *= shrink;
-        for (int j = 0; j < 32; ++j) {
-            const uint64_t there = __shfl_sync(0xFFFFFFFFu, at, j);
-            const float pj = __shfl_sync(0xFFFFFFFFu, p, j);
-            if (__shfl_sync(0xFFFFFFFFu, page, j) < 0) continue;
-            const uint32_t d = lane * kOwn;                                      // within a block: 2 or 4 of 32
-            const float s = e8m0_value(P.C.scales[1][there * kBlocks + d / kKvBlock]);
-            const uint32_t byte = FP4 ? d / 2 : d;
-            const uint32_t word = *reinterpret_cast<const uint32_t*>(P.C.elems[1] + there * kRowBytes + byte / 4 * 4) >> (8 * (byte & 3));
-            uint32_t h[4];
-            if (FP4) fp4_to_half(word, h);
-            else e4m3_to_half(word, h);
-            for (uint32_t i = 0; i < kOwn; i += 2) {
-                const float2 v = half_pair(h[i / 2]);
-                acc[i] = fmaf(pj, v.x * s, acc[i]);
-                acc[i + 1] = fmaf(pj, v.y * s, acc[i + 1]);
-            }
-        }
-    }
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-    T* out = reinterpret_cast<T*>(P.out.d + (uint64_t)row * P.out.ld_row + head * P.out.ld_head);
-    for (uint32_t i = 0; i < kOwn; ++i) out[lane * kOwn + i] = T(sum == 0.0f ? 0.0f : acc[i] / sum);
-    if (P.lse && lane == 0) P.lse[(uint64_t)row * P.q_heads + head] = sum == 0.0f ? -INFINITY : top + logf(sum);
+    const cuuint64_t dims[2] = {row_bytes, rows}, pitch[1] = {row_bytes};
+    const cuuint32_t box[2] = {row_bytes, box_rows}, step[2] = {1, 1};
+    const CUtensorMapSwizzle swizzle = row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
+    return encode_fn() && encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(elems), dims, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                                      CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static uint32_t multiprocessors()
+{
+    static OncePerDevice once;
+    return once([]() -> uint32_t {
+        int dev = 0, n = 0;
+        return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess ? (uint32_t)n : 0;
+    });
+}
+
+// without a device (argument checks): as many as any has
+static uint32_t multiprocessors_or_most()
+{
+    const uint32_t n = multiprocessors();
+    return n ? n : 256;
+}
+
+template <typename S>
+static size_t stream_workspace(uint32_t blocks)
+{
+    return (blocks * sizeof(BlockEnd) + 255) / 256 * 256 + (size_t)blocks * 2 * S::kCols * (S::kDim + 2) * 4;
+}
+
+template <typename S>
+static cudaError_t launch_stream(const AttentionParams& P, const CUtensorMap& keys, const CUtensorMap& values, uint32_t blocks, cudaStream_t st)
+{
+    static OncePerDevice ready;
+    if (!ready([]() -> uint32_t { return cudaFuncSetAttribute(kv_stream_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem) == cudaSuccess; })) return cudaErrorUnknown;
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at[1] = {launch_early()};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(S::kWarps * 32);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_stream_kernel<S>, P, keys, values)) return e;
+    cfg.blockDim = dim3(S::kCols * S::kDim / 4);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, kv_join_kernel<S>, P, blocks);
 }
 
 }  // namespace zc
@@ -108,7 +65,7 @@ extern "C" {
 size_t zc_kv_attention_workspace_bytes(const zc_kv_cache* cache, const zc_kv_batch* batch, uint32_t q_heads)
 {
     if (check_cache(cache) || check_batch(cache, batch) || q_heads == 0 || q_heads % cache->kv_heads || q_heads / cache->kv_heads > ZC_KV_MAX_GROUP) return 0;
-    return 256;
+    return cache->head_dim == 128 ? stream_workspace<StreamShape<true, 128, 2>>(multiprocessors_or_most()) : stream_workspace<StreamShape<true, 64, 2>>(multiprocessors_or_most());
 }
 
 zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, const zc_kv_attention_args* args, void* d_workspace,
@@ -136,25 +93,33 @@ zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, co
     P.lse = args->d_lse;
     P.q_heads = args->q_heads;
     P.group = args->q_heads / cache->kv_heads;
-    P.scale = args->scale;
+    P.scale_log2 = args->scale * 1.44269504f;
     P.causal = args->causal;
     P.window = args->window;
-    auto run = [&](auto value, auto fp4, auto dim) {
-        cudaLaunchConfig_t cfg{};
-        cudaLaunchAttribute at[1] = {launch_early()};
-        cfg.blockDim = dim3(kSimpleWarps * 32);
-        cfg.gridDim = dim3((uint32_t)ceil_div((uint64_t)P.B.n_rows * P.q_heads, kSimpleWarps));
-        cfg.stream = (cudaStream_t)cuda_stream;
-        cfg.attrs = at;
-        cfg.numAttrs = 1;
-        return cudaLaunchKernelEx(&cfg, kv_attention_simple_kernel<decltype(value), decltype(fp4)::value, decltype(dim)::value>, P);
+    P.workspace = (uint8_t*)d_workspace;
+    P.half_type = args->type == ZC_REAL_F16;
+    P.q_wide = reinterpret_cast<uintptr_t>(P.q.d) % 8 == 0 && P.q.ld_row % 8 == 0 && P.q.ld_head % 8 == 0;
+    P.out_wide = reinterpret_cast<uintptr_t>(P.out.d) % 8 == 0 && P.out.ld_row % 8 == 0 && P.out.ld_head % 8 == 0;
+    P.most_rows = 0xFFFFFFFFu;
+    P.spin_limit = test_knobs().spin_limit;
+    P.skip_copy = test_knobs().skip_copy;
+    const uint32_t blocks = multiprocessors();
+    if (!blocks) return ZC_E_CUDA;
+    const uint32_t row_bytes = cache->format == ZC_FMT_FP4_E2M1 ? cache->head_dim / 2 : cache->head_dim;
+    const uint64_t rows = std::max<uint64_t>(1, cache->n_pages * cache->kv_heads * cache->page_tokens);
+    CUtensorMap maps[2];
+    for (int side = 0; side < 2; ++side)                         // without pages nothing is read, but the descriptor wants an address
+        if (!make_cache_map(&maps[side], cache->n_pages ? P.C.elems[side] : P.workspace, rows, row_bytes, std::min(cache->page_tokens, kStepTokens))) return ZC_E_CUDA;
+    auto run = [&](auto fp4, auto dim) {
+        using One = StreamShape<decltype(fp4)::value, decltype(dim)::value, 1>;
+        using Two = StreamShape<decltype(fp4)::value, decltype(dim)::value, 2>;
+        const bool few = (uint64_t)P.group * std::max(1u, batch->max_new) <= 8;
+        return few ? launch_stream<One>(P, maps[0], maps[1], blocks, (cudaStream_t)cuda_stream) : launch_stream<Two>(P, maps[0], maps[1], blocks, (cudaStream_t)cuda_stream);
     };
-    auto dims = [&](auto value, auto fp4) {
-        return cache->head_dim == 128 ? run(value, fp4, std::integral_constant<uint32_t, 128>()) : run(value, fp4, std::integral_constant<uint32_t, 64>());
+    auto dims = [&](auto fp4) {
+        return cache->head_dim == 128 ? run(fp4, std::integral_constant<uint32_t, 128>()) : run(fp4, std::integral_constant<uint32_t, 64>());
     };
-    auto formats = [&](auto value) { return cache->format == ZC_FMT_FP4_E2M1 ? dims(value, std::true_type()) : dims(value, std::false_type()); };
-    const cudaError_t e = args->type == ZC_REAL_BF16 ? formats(__nv_bfloat16()) : formats(__half());
-    return e == cudaSuccess ? ZC_OK : ZC_E_CUDA;
+    return (cache->format == ZC_FMT_FP4_E2M1 ? dims(std::true_type()) : dims(std::false_type())) == cudaSuccess ? ZC_OK : ZC_E_CUDA;
 }
 
 }  // extern "C"
