@@ -34,7 +34,7 @@ static uint32_t multiprocessors_or_most()
 template <typename S>
 static size_t stream_workspace(uint32_t blocks)
 {
-    return (blocks * sizeof(BlockEnd) + 255) / 256 * 256 + (size_t)blocks * 2 * S::kCols * (S::kDim + 2) * 4;
+    return (blocks * sizeof(BlockEnd) + 255) / 256 * 256 + (size_t)blocks * (2 * S::kCols * (S::kDim + 2) + S::kWarps * S::kPart) * 4;
 }
 
 template <typename S>
@@ -51,7 +51,7 @@ static cudaError_t launch_stream(const AttentionParams& P, const CUtensorMap& ke
     cfg.attrs = at;
     cfg.numAttrs = 1;
     if (const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_stream_kernel<S>, P, keys, values)) return e;
-    cfg.blockDim = dim3(S::kCols * S::kDim / 4);
+    cfg.blockDim = dim3(S::kCols * 32);
     cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, kv_join_kernel<S>, P, blocks);
 }
@@ -65,7 +65,9 @@ extern "C" {
 size_t zc_kv_attention_workspace_bytes(const zc_kv_cache* cache, const zc_kv_batch* batch, uint32_t q_heads)
 {
     if (check_cache(cache) || check_batch(cache, batch) || q_heads == 0 || q_heads % cache->kv_heads || q_heads / cache->kv_heads > ZC_KV_MAX_GROUP) return 0;
-    return cache->head_dim == 128 ? stream_workspace<StreamShape<true, 128, 2>>(multiprocessors_or_most()) : stream_workspace<StreamShape<true, 64, 2>>(multiprocessors_or_most());
+    const uint32_t n = multiprocessors_or_most();
+    return cache->head_dim == 128 ? std::max(stream_workspace<StreamShape<true, 128, 1>>(n), stream_workspace<StreamShape<true, 128, 2>>(n))
+                                  : std::max(stream_workspace<StreamShape<true, 64, 1>>(n), stream_workspace<StreamShape<true, 64, 2>>(n));
 }
 
 zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, const zc_kv_attention_args* args, void* d_workspace,
@@ -109,7 +111,7 @@ zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, co
     const uint64_t rows = std::max<uint64_t>(1, cache->n_pages * cache->kv_heads * cache->page_tokens);
     CUtensorMap maps[2];
     for (int side = 0; side < 2; ++side)                         // without pages nothing is read, but the descriptor wants an address
-        if (!make_cache_map(&maps[side], cache->n_pages ? P.C.elems[side] : P.workspace, rows, row_bytes, std::min(cache->page_tokens, kStepTokens))) return ZC_E_CUDA;
+        if (!make_cache_map(&maps[side], cache->n_pages ? P.C.elems[side] : P.workspace, rows, row_bytes, std::min(cache->page_tokens, row_bytes == 128 ? 32u : 64u))) return ZC_E_CUDA;
     auto run = [&](auto fp4, auto dim) {
         using One = StreamShape<decltype(fp4)::value, decltype(dim)::value, 1>;
         using Two = StreamShape<decltype(fp4)::value, decltype(dim)::value, 2>;

@@ -5,8 +5,6 @@
 
 namespace zc {
 
-constexpr uint32_t kStepTokens = 32;
-
 struct AttentionParams {
     KvCache C;
     KvBatch B;
@@ -22,10 +20,16 @@ struct AttentionParams {
     uint32_t spin_limit, skip_copy;
 };
 
+// An item's columns, as whoever joins its parts needs them.
+struct ItemColumns {
+    int row0;
+    uint32_t head, first, count;             // columns first .. first + count - 1
+};
 // What a block leaves of the item that begins in it and goes on in the next ones.
 struct BlockEnd {
     unsigned long long to, total;
-    uint32_t b, item, there, pad;
+    ItemColumns columns;
+    uint32_t there, pad[3];
 };
 
 __device__ __forceinline__ float exp2_fast(float x)
@@ -48,6 +52,7 @@ __device__ __forceinline__ float lds_f1(uint32_t a) { return __uint_as_float(lds
 __device__ __forceinline__ void lds_f2(uint32_t a, float v[2]) { asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(a) : "memory"); }
 __device__ __forceinline__ void lds_f4(uint32_t a, float v[4]) { asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(a) : "memory"); }
 __device__ __forceinline__ void sts16(uint32_t a, uint32_t v) { asm volatile("st.shared.u16 [%0], %1;" :: "r"(a), "h"((uint16_t)v) : "memory"); }
+__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.b32 [%0], {%1,%2};" :: "r"(a), "r"(x), "r"(y) : "memory"); }
 __device__ __forceinline__ void sts_f1(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;" :: "r"(a), "f"(v) : "memory"); }
 __device__ __forceinline__ void sts_f2(uint32_t a, const float* v) { asm volatile("st.shared.v2.f32 [%0], {%1,%2};" :: "r"(a), "f"(v[0]), "f"(v[1]) : "memory"); }
 __device__ __forceinline__ void sts_f4(uint32_t a, const float* v) { asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" :: "r"(a), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory"); }
@@ -86,7 +91,7 @@ struct SeqSpan {
     uint32_t tiles, steps;
     __device__ __forceinline__ unsigned long long cost(uint32_t heads) const { return (unsigned long long)tiles * heads * steps; }
 };
-template <uint32_t COLS>
+template <uint32_t COLS, uint32_t STEP>
 __device__ __forceinline__ SeqSpan stream_span(const AttentionParams& P, uint32_t b)
 {
     SeqSpan s{};
@@ -94,14 +99,14 @@ __device__ __forceinline__ SeqSpan stream_span(const AttentionParams& P, uint32_
     if (b < P.B.n_seqs) {
         s.r.load(P, b);
         if ((uint32_t)s.r.n <= P.most_rows) s.tiles = (uint32_t)(((unsigned long long)s.r.n * P.group + COLS - 1) / COLS);
-        const uint32_t first = (uint32_t)s.r.from / kStepTokens, last = ((uint32_t)s.r.to + kStepTokens - 1) / kStepTokens;
+        const uint32_t first = (uint32_t)s.r.from / STEP, last = ((uint32_t)s.r.to + STEP - 1) / STEP;
         s.steps = last > first ? last - first : 1;         // at least one, that rows which see nothing get their zeros
     }
     return s;
 }
 
 // Where a warp is.  All lanes have the same.
-template <uint32_t COLS>
+template <uint32_t COLS, uint32_t STEP>
 struct Cursor : SeqRows {
     uint32_t b, item, head, tile, step, steps, tiles;
     __device__ __forceinline__ void take(const SeqSpan& s)
@@ -128,7 +133,7 @@ struct Cursor : SeqRows {
         take(s);
         place();
     }
-    __device__ __forceinline__ uint32_t token() const { return ((uint32_t)from / kStepTokens + step) * kStepTokens; }
+    __device__ __forceinline__ uint32_t token() const { return ((uint32_t)from / STEP + step) * STEP; }
     __device__ __forceinline__ bool last() const { return step + 1 == steps; }
     __device__ __forceinline__ void next(const AttentionParams& P, SeqSpan& s)
     {
@@ -138,20 +143,15 @@ struct Cursor : SeqRows {
         item = 0;
         while (true) {
             if (++b >= P.B.n_seqs) return;
-            if ((b & 31) == 0) s = stream_span<COLS>(P, b + (threadIdx.x & 31));
+            if ((b & 31) == 0) s = stream_span<COLS, STEP>(P, b + (threadIdx.x & 31));
             if (__shfl_sync(0xFFFFFFFFu, s.tiles, b & 31)) break;
         }
         take(s);
         place();
     }
-    // the same item without the lanes' help
-    __device__ __forceinline__ void set_item(const AttentionParams& P, uint32_t b_, uint32_t item_)
+    __device__ __forceinline__ ItemColumns columns(const AttentionParams& P) const
     {
-        b = b_;
-        item = item_;
-        load(P, b);
-        tiles = (uint32_t)(((unsigned long long)n * P.group + COLS - 1) / COLS);
-        place();
+        return ItemColumns{row0, head, tile * COLS, min(COLS, (uint32_t)n * P.group - tile * COLS)};
     }
     __device__ __forceinline__ bool has(const AttentionParams& P, uint32_t col) const { return col < (uint32_t)n * P.group; }
     __device__ __forceinline__ void column_limits(const AttentionParams& P, uint32_t col, int& lo, int& hi) const
@@ -193,14 +193,18 @@ __device__ __forceinline__ void store_out(const AttentionParams& P, uint8_t* out
         for (uint32_t k = 0; k < N; ++k) reinterpret_cast<uint16_t*>(out)[k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
     }
 }
-// Four neighbours of a column's joined sums.
-template <typename CURSOR>
-__device__ __forceinline__ void finish_column(const AttentionParams& P, const CURSOR& c, uint32_t col, uint32_t d, const float sums[4], float top, float weight)
+// A joined column: a lane has N neighbours from d on.
+template <uint32_t N>
+__device__ __forceinline__ void finish_column(const AttentionParams& P, const ItemColumns& c, uint32_t in_tile, uint32_t d, const float* sums, float top, float weight)
 {
     const float norm = weight == 0.0f ? 0.0f : 1.0f / weight;
-    const float v[4] = {sums[0] * norm, sums[1] * norm, sums[2] * norm, sums[3] * norm};
-    store_out<4>(P, c.out(P, col), d, v);
-    if (P.lse && d == 0) P.lse[c.lse(P, col)] = lse_of(top, weight);
+    float v[N];
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k) v[k] = sums[k] * norm;
+    const uint32_t col = c.first + in_tile, head = c.head * P.group + col % P.group;
+    const uint64_t row = (uint64_t)c.row0 + col / P.group;
+    store_out<N>(P, P.out.d + row * P.out.ld_row + head * P.out.ld_head, d, v);
+    if (P.lse && d == 0) P.lse[row * P.q_heads + head] = lse_of(top, weight);
 }
 
 // Two neighbours of a query as FP32.

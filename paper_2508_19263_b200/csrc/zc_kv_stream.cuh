@@ -1,7 +1,7 @@
 // Attention of a few rows over a long cache: the cache's bytes bound it.
 //
 // Columns: the rows of a sequence times the query heads that share a head of the cache; kCols of them make an item with that head.  A step
-// is 32 tokens of an item.  All steps of a call, in order, are cut into as many equal runs as there are warps on the GPU; a warp goes
+// is 64 tokens (32 where they are 128 bytes) of an item.  All steps of a call, in order, are cut into as many equal runs as there are warps on the GPU; a warp goes
 // through its run by itself: copies, two barriers, matrix instructions, running maximum and sum, nothing shared with other warps until its end.  So long
 // sequences are split, short ones are not, and nobody waits for the longest.  An item that lies in one run is finished by its warp; the
 // parts of the others are joined, in order, first in the block, then, where an item goes on in the next block, by a second kernel.
@@ -10,11 +10,11 @@
 // O^T += V^T P^T with 16 of the head's width as rows, 16 tokens as the sum's axis.  Both operands from the cache come out of shared memory
 // as they are, by ldmatrix (transposed for V), and become FP16 in registers (one conversion for two elements, exact).  The order in which the
 // sum over a head's width goes is free, so Q is laid out in the order in which ldmatrix gives K's nibbles.
-//   Keys' scales multiply the FP32 sums of each 32 products.  Values' scales multiply the elements, as 2^(s - R + kLift) with R the largest scale
-// byte that the item's run has met: exact unless a scale is 2^-35 (E4M3: 2^-22) of the largest, and off by at most 2^-25 of a unit that is 2^-kLift of it then.
+//   Keys' scales multiply the FP32 sums of each 32 products, values' scales the weights: a block of 32 of the head's width has weights of its own,
+// 2^(s - R) times the softmax's, R the largest scale byte that the item's run has met.  So elements go into the products as they are.
 //   Queries become FP16 over a power of two that brings the row's largest to 2^14 .. 2^15: BF16's eight bits are kept down to 2^-31 of it.
 //   Weights are 2^(x - max + 15), in FP32 for the sum, rounded to FP16 for the product with V: off by at most 2^-12 of it where it is above 2^-29 of the
-// largest, by 2^-40 of the largest below.
+// largest (the scale's power of two counted in), by 2^-40 of the largest below.
 #pragma once
 #include <type_traits>
 
@@ -28,28 +28,41 @@ struct StreamShape {
     static constexpr uint32_t kDim = DIM_, kNt = NT_, kCols = 8 * NT_;
     static constexpr uint32_t kRow = kFp4 ? kDim / 2 : kDim;               // bytes of a token's head
     static constexpr uint32_t kBlocks = kDim / kKvBlock, kChunks = kRow / 16;
-    static constexpr uint32_t kTile = kStepTokens * kRow;                    // keys or values of a step
-    static constexpr uint32_t kStage = 2 * kTile, kScales = kStepTokens * kBlocks;
+    // Tokens of a step.  What a step costs whatever its tokens (copies, barrier, maxima over the warp) is a third of it at 32.
+    static constexpr uint32_t kStep = kRow == 128 ? 32 : 64, kOwn = kStep / 32, kGroups = kStep / 16;
+    static constexpr uint32_t kTile = kStep * kRow;                          // keys or values of a step
+    static constexpr uint32_t kStage = 2 * kTile, kScales = kStep * kBlocks;
     static constexpr uint32_t kTiles = kDim / 16;                            // of 16 of the head's width
-    // 16 warps of 128 registers where two stages each and the parts fit into shared memory, else 8 of up to 255
-    static constexpr uint32_t kWarps = NT_ == 1 && kRow <= 64 ? 16 : 8;
-    static constexpr uint32_t kStages = kRow == 32 ? 4 : NT_ == 2 && kRow == 64 ? 4 : 2;
-    static constexpr int kLift = kFp4 ? 12 : 6;                              // 6 * 2^12 and 448 * 2^6 are FP16 numbers
+    // 12 warps of 168 registers where 8 columns are all, 8 of 255 for 16
+    static constexpr uint32_t kWarps = NT_ == 1 ? 12 : 8, kStages = kRow == 32 ? 3 : 2;
+    using Place = Cursor<kCols, kStep>;
     // a part: sums [kCols][kDim + 4] (the padding spreads lanes over the banks), largest logits [kCols], sums of weights [kCols]
     static constexpr uint32_t kPartLd = kDim + 4, kPart = kCols * (kPartLd + 2);
     // shared memory of a warp
     static constexpr uint32_t kRing = kStages * kStage, kRingScales = kStages * 2 * kScales;
-    static constexpr uint32_t kFactors = kStepTokens * kBlocks * 4;          // of keys (FP32); of values (pairs of FP16) half of it
-    static constexpr uint32_t kWarpBytes = kRing + kRingScales + kFactors + kFactors / 2 + kPart * 4;
+    static constexpr uint32_t kFactors = kStep * kBlocks * 4;                // of keys (FP32), then of values (FP16, twice)
+    // logits of 16 tokens, a lane's four a piece of 16 bytes: where their keys were, if they fit there
+    static constexpr bool kLogitsOver = 16 * kRow >= kNt * 512;
+    static constexpr uint32_t kLogitsLd = kLogitsOver ? 16 * kRow : kNt * 512;
+    static constexpr uint32_t kWarpBytes = kRing + kRingScales + kFactors + (kLogitsOver ? 0 : kGroups * kLogitsLd);
     static constexpr uint32_t kSmem = kWarps * kWarpBytes + 1024;
+    static_assert(kWarps <= 16, "a lane for each part of a block");
     static_assert(kPart * 4 <= kRing, "a run's last part goes where its copies were");
     static_assert(kSmem <= kMaxSmem - 2048, "shared memory");
 };
 
+// Where the run-th of `runs` equal shares begins.
+__device__ __forceinline__ unsigned long long share(unsigned long long total, uint32_t run, uint32_t runs)
+{
+    const unsigned long long all = total * run;               // below 2^63: 2^49 steps in 2^13 runs
+    return all >> 32 ? all / runs : (uint32_t)all / runs;
+}
+
 // A part of an item that a warp leaves to the block.
 struct StreamEntry {
     unsigned long long from, to;           // the item's steps among all
-    uint32_t b, item, there;
+    ItemColumns columns;
+    uint32_t there;
 };
 
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t w[4])
@@ -87,24 +100,31 @@ __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t chunk)
 // Two tokens' elements of the cache, 16 bits each (the first token's in the low half), as pairs (first, second) of FP16: 4 in FP4, 2 in E4M3.
 __device__ __forceinline__ void pairs_fp4(uint32_t w, uint32_t h[4])
 {
-    const uint32_t even = (w & 0x0F0F0F0Fu) | ((w >> 12) & 0xF0F0F0F0u);        // byte 0: nibble 0 of both, byte 1: nibble 2
-    const uint32_t odd = (w & 0xF0F0F0F0u) | ((w << 12) & 0x0F0F0F0Fu);         // byte 2: nibble 1 of both, byte 3: nibble 3
+    uint32_t even, odd;                                                       // byte 0: nibble 0 of both, byte 1: nibble 2; byte 2: nibble 1, byte 3: nibble 3
+    asm("lop3.b32 %0, %1, %2, 0x0F0F0F0F, 0xE4;" : "=r"(even) : "r"(w), "r"(w >> 12));         // the mask's bits of the first, the others of the second
+    asm("lop3.b32 %0, %1, %2, 0x0F0F0F0F, 0xD8;" : "=r"(odd) : "r"(w), "r"(w << 12));          // the other way round
     asm("{\n\t.reg .b8 b0, b1, b2, b3, c0, c1, c2, c3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\tmov.b32 {c0, c1, c2, c3}, %5;\n\t"
         "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, c2;\n\tcvt.rn.f16x2.e2m1x2 %2, b1;\n\tcvt.rn.f16x2.e2m1x2 %3, c3;\n\t}"
         : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(even), "r"(odd));
 }
 __device__ __forceinline__ void pairs_e4m3(uint32_t w, uint32_t h[2]) { e4m3_to_half(__byte_perm(w, 0, 0x3120), h); }
 
-// 2^(s - ref + lift) in FP16; 255 gives NaN.
-__device__ __forceinline__ uint32_t value_factor(uint32_t s, uint32_t ref, int lift)
+// D = A B for m16n8k16; `zero` holds zeros
+__device__ __forceinline__ void mma_f16_first(float c[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, const float zero[4])
 {
-    const int e = (int)s - (int)ref + lift + 15;
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(zero[0]), "f"(zero[1]), "f"(zero[2]), "f"(zero[3]));
+}
+// 2^(s - ref) in FP16, s <= ref; NaN for 255.
+__device__ __forceinline__ uint32_t value_factor(uint32_t s, uint32_t ref)
+{
+    const int e = (int)s - (int)ref + 15;
     return s == 255 ? 0x7E00u : e > 0 ? (uint32_t)e << 10 : 0x400u >> min(1 - e, 31);
 }
 
 // Query of a column in the order of the keys' elements in a lane's registers, in FP16 times 2^k; factor: what makes a logit of a product.
 template <typename S>
-__device__ __forceinline__ void load_queries(const AttentionParams& P, const Cursor<S::kCols>& c, uint32_t col, uint32_t i, uint32_t q[S::kDim / 8], float& factor)
+__device__ __forceinline__ void load_queries(const AttentionParams& P, const typename S::Place& c, uint32_t col, uint32_t i, uint32_t q[S::kDim / 8], float& factor)
 {
 #pragma unroll
     for (uint32_t k = 0; k < S::kDim / 8; ++k) q[k] = 0;
@@ -127,25 +147,62 @@ __device__ __forceinline__ void load_queries(const AttentionParams& P, const Cur
     most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
     most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
     const int k = query_lift(most);
-    const float lift = power_of_two(k);
+    const float lift = copysignf(power_of_two(k), P.scale_log2);
 #pragma unroll
     for (uint32_t j = 0; j < S::kDim / 8; ++j) {
         const float2 f = query_pair(P, q[j]);
         q[j] = pack_half(f.x * lift, f.y * lift);
     }
-    factor = ldexpf(P.scale_log2, -k);
+    // above 0, that the largest product is the largest logit and -infinity stays: the scale's sign is with the queries
+    factor = fmaxf(ldexpf(fabsf(P.scale_log2), -k), 1.17549435e-38f);
 }
 template <typename S>
 __device__ __forceinline__ float* partial_of(const AttentionParams& P, uint32_t blocks, uint32_t block, uint32_t slot)
 {
     return reinterpret_cast<float*>(P.workspace + ((size_t)blocks * sizeof(BlockEnd) + 255) / 256 * 256) + (size_t)(2 * block + slot) * (S::kCols * (S::kDim + 2));
 }
-// Where a warp's part lies: its first one in a place of its own, its last one where its copies were.
 template <typename S>
-__device__ __forceinline__ uint32_t part_of(uint32_t base, uint32_t entry)
+__device__ __forceinline__ float* part_in_workspace(const AttentionParams& P, uint32_t warp)
 {
-    const uint32_t warp = entry >> 1;
-    return entry & 1 ? base + warp * S::kRing : base + S::kWarps * S::kRing + warp * (S::kWarpBytes - S::kRing) + (S::kWarpBytes - S::kRing - S::kPart * 4);
+    return partial_of<S>(P, gridDim.x, gridDim.x, 0) + (size_t)warp * S::kPart;
+}
+// The joined sums of a column whose parts begin at part(k), 0 <= k < count, all lanes together: a lane has kDim / 32 neighbours.
+// `at` and `weights` say where in a part the largest logit and the sum of weights of the column are, `sums` where its sums begin.
+template <typename S, typename PART>
+__device__ __forceinline__ void join_parts(uint32_t count, PART part, uint32_t sums, uint32_t at, uint32_t weights, float v[S::kDim / 32], float& best, float& weight)
+{
+    constexpr uint32_t N = S::kDim / 32;
+    const uint32_t lane = threadIdx.x & 31;
+    best = -INFINITY;
+    weight = 0.0f;
+#pragma unroll
+    for (uint32_t n = 0; n < N; ++n) v[n] = 0.0f;
+    for (uint32_t k0 = 0; k0 < count; k0 += 32) {
+        // a lane has a part
+        const float* mine = k0 + lane < count ? part(k0 + lane) : nullptr;
+        const float t = mine ? mine[at] : -INFINITY, w = mine ? mine[weights] : 0.0f;
+        float next = t;
+        for (int d = 16; d; d >>= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, d));
+        next = fmaxf(next, best);
+        const float off = next == -INFINITY ? 0.0f : next, old = exp2_fast(best - off), now = exp2_fast(t - off);
+        best = next;
+        float sum = w * now;
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+        weight = fmaf(weight, old, sum);
+#pragma unroll
+        for (uint32_t n = 0; n < N; ++n) v[n] *= old;
+        const uint32_t some = min(32u, count - k0);
+#pragma unroll 8
+        for (uint32_t k = 0; k < some; ++k) {
+            const float* p = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(mine), k)) + sums + lane * N;
+            const float f = __shfl_sync(0xFFFFFFFFu, now, k);
+            float x[N];
+            if (N == 4) { const float4 y = *reinterpret_cast<const float4*>(p); x[0] = y.x; x[1] = y.y; x[N - 2] = y.z; x[N - 1] = y.w; }
+            else { const float2 y = *reinterpret_cast<const float2*>(p); x[0] = y.x; x[1] = y.y; }
+#pragma unroll
+            for (uint32_t n = 0; n < N; ++n) v[n] = fmaf(x[n], f, v[n]);
+        }
+    }
 }
 
 template <typename S>
@@ -155,13 +212,14 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
     __shared__ __align__(8) uint64_t s_full[S::kWarps * S::kStages];
     __shared__ unsigned long long s_cost[ZC_KV_MAX_SEQS / 32];
     __shared__ StreamEntry s_entry[S::kWarps * 2];
+    __shared__ uint8_t s_order[S::kWarps][32];
     __shared__ volatile uint32_t s_failed;
     constexpr uint32_t kAll = 0xFFFFFFFFu;
     const uint32_t lane = threadIdx.x & 31, warp = warp_index(), g = lane >> 2, i = lane & 3;
     // the swizzle goes by address bits: the rings begin on 1024 bytes
     const uint32_t base = (smem_u32(smem) + 1023) & ~1023u;
     const uint32_t ring = base + warp * S::kRing, rest = base + S::kWarps * S::kRing + warp * (S::kWarpBytes - S::kRing);
-    const uint32_t ring_scales = rest, key_factors = rest + S::kRingScales, value_factors = key_factors + S::kFactors, first_part = value_factors + S::kFactors / 2;
+    const uint32_t ring_scales = rest, factors = rest + S::kRingScales;
     const uint32_t bars = smem_u32(s_full) + warp * S::kStages * 8;
     if (lane < S::kStages) bar_init(bars + 8 * lane, 1);
     if (lane < 2) s_entry[2 * warp + lane].there = 0;
@@ -176,11 +234,11 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
 
     // ---- which steps are this warp's ----
     const uint32_t chunks = (P.B.n_seqs + 31) / 32;
-    SeqSpan span = stream_span<S::kCols>(P, lane);
+    SeqSpan span = stream_span<S::kCols, S::kStep>(P, lane);
     unsigned long long total = 0, before = 0, cost = span.cost(P.C.heads);
     if (chunks > 1) {
         for (uint32_t c = warp; c < chunks; c += S::kWarps) {
-            unsigned long long sum = stream_span<S::kCols>(P, 32 * c + lane).cost(P.C.heads);
+            unsigned long long sum = stream_span<S::kCols, S::kStep>(P, 32 * c + lane).cost(P.C.heads);
             for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kAll, sum, d);
             if (lane == 0) s_cost[c] = sum;
         }
@@ -191,9 +249,9 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
         __syncthreads();
     }
     for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(kAll, total, d);
-    const unsigned long long runs = (unsigned long long)gridDim.x * S::kWarps, run = (unsigned long long)blockIdx.x * S::kWarps + warp;
-    const unsigned long long from = total * run / runs, to = total * (run + 1) / runs;
-    const unsigned long long block_from = total * ((unsigned long long)blockIdx.x * S::kWarps) / runs, block_to = total * ((unsigned long long)(blockIdx.x + 1) * S::kWarps) / runs;
+    const uint32_t runs = gridDim.x * S::kWarps, run = blockIdx.x * S::kWarps + warp;
+    const unsigned long long from = share(total, run, runs), to = share(total, run + 1, runs);
+    const unsigned long long block_from = share(total, blockIdx.x, gridDim.x), block_to = share(total, blockIdx.x + 1, gridDim.x);
 
     // ---- the place of step `from`: sequence, item of the sequence, step of the item ----
     uint32_t b = 0, item = 0, step = 0;
@@ -202,7 +260,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
         uint32_t c = 0;
         if (chunks > 1) {
             while (before + s_cost[c] <= from) before += s_cost[c++];
-            span = stream_span<S::kCols>(P, 32 * c + lane);
+            span = stream_span<S::kCols, S::kStep>(P, 32 * c + lane);
             cost = span.cost(P.C.heads);
         }
         unsigned long long upto = cost;                  // inclusive sums over the lanes
@@ -214,21 +272,22 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
         b = 32 * c + k;
         const unsigned long long inside = from - before - __shfl_sync(kAll, upto - cost, k);
         const uint32_t steps = __shfl_sync(kAll, span.steps, k);
-        item = (uint32_t)(inside / steps);
-        step = (uint32_t)(inside % steps);
+        item = (uint32_t)(inside >> 32 ? inside / steps : (uint32_t)inside / steps);
+        step = (uint32_t)(inside - (unsigned long long)item * steps);
         item_from = from - step;
     }
 
     // ---- copies: one cursor runs ahead ----
     const Waiter wait{P.spin_limit, &s_failed};
-    Cursor<S::kCols> ahead;
+    typename S::Place ahead;
     ahead.set(span, b, item, step);
     SeqSpan at_span = span;                              // `ahead` may come to the next 32 sequences before
     uint32_t place_base = 0xFFFFFFFFu, place_seq = 0xFFFFFFFFu;
     int pages = 0;
-    uint32_t missing = 0;                                 // two bits a stage: its tokens 0..15 and 16..31 have no page
-    const unsigned long long count = to - from;
-    unsigned long long sent = 0;
+    uint32_t missing = 0;                                 // kGroups bits a stage: groups of 16 tokens that have no page
+    const uint32_t count = (uint32_t)(to - from);        // 2^32 steps a warp would take days
+    uint32_t sent = 0;
+    const uint32_t piece_tokens = min(1u << P.C.page_shift, S::kStep), pieces = S::kStep / piece_tokens;
     auto send = [&](uint32_t st) {
         // the pages of the next 32 places are kept in the lanes
         const uint32_t t0 = ahead.token(), place = t0 >> P.C.page_shift;
@@ -238,27 +297,23 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
             const uint32_t mine = place_base + lane;
             pages = mine < P.B.max_pages && (mine << P.C.page_shift) < (uint32_t)ahead.to && ((mine + 1) << P.C.page_shift) > (uint32_t)ahead.from ? kv_page(P.C, P.B, ahead.b, mine) : -1;
         }
-        const uint32_t half = P.C.page_shift == 4;         // pages of 16 tokens: two a step
-        const int page0 = __shfl_sync(kAll, pages, place & 31), page1 = __shfl_sync(kAll, pages, (place + half) & 31);
-        const bool go0 = page0 >= 0, go1 = half ? page1 >= 0 && place + 1 - place_base < 32 : go0;
-        missing = (missing & ~(3u << (2 * st))) | ((go0 ? 0u : 1u) | (go1 ? 0u : 2u)) << (2 * st);
-        const uint32_t bytes = ((go0 ? 16u : 0u) + (go1 ? 16u : 0u)) * 2 * (S::kRow + S::kBlocks);
-        if (elect_one()) {
-            const uint32_t bar = bars + 8 * st, head = ahead.head;
-            bar_expect(bar, bytes);
-            const uint32_t to_keys = ring + st * S::kStage, to_scales = ring_scales + st * 2 * S::kScales;
-            auto part = [&](int page, uint32_t at, uint32_t tokens) {
-                const uint32_t row = (((uint32_t)page * P.C.heads + head) << P.C.page_shift) + ((t0 + at) & ((1u << P.C.page_shift) - 1));
+        const uint32_t bar = bars + 8 * st, to_keys = ring + st * S::kStage, to_scales = ring_scales + st * 2 * S::kScales;
+        const uint32_t there = __ballot_sync(kAll, pages >= 0) >> (place & 31), have = there & ((1u << pieces) - 1);
+        if (elect_one()) bar_expect(bar, __popc(have) * piece_tokens * 2 * (S::kRow + S::kBlocks));
+        missing &= ~(((1u << S::kGroups) - 1) << (S::kGroups * st));
+        for (uint32_t k = 0; k < pieces; ++k) {
+            const int page = __shfl_sync(kAll, pages, (place + k) & 31);
+            const uint32_t at = k * piece_tokens;
+            if (page < 0) {
+                missing |= ((1u << (piece_tokens / 16)) - 1) << (S::kGroups * st + at / 16);
+                continue;
+            }
+            const uint32_t row = (((uint32_t)page * P.C.heads + ahead.head) << P.C.page_shift) + (t0 & ((1u << P.C.page_shift) - 1));
+            if (!P.skip_copy && elect_one()) {
                 tensor_copy<1>(to_keys + at * S::kRow, &key_map, 0, (int)row, bar);
                 tensor_copy<1>(to_keys + S::kTile + at * S::kRow, &value_map, 0, (int)row, bar);
-                bulk_copy(to_scales + at * S::kBlocks, P.C.scales[0] + (uint64_t)row * S::kBlocks, tokens * S::kBlocks, bar);
-                bulk_copy(to_scales + S::kScales + at * S::kBlocks, P.C.scales[1] + (uint64_t)row * S::kBlocks, tokens * S::kBlocks, bar);
-            };
-            if (!P.skip_copy) {
-                if (half) {
-                    if (go0) part(page0, 0, 16);
-                    if (go1) part(page1, 16, 16);
-                } else if (go0) part(page0, 0, 32);
+                bulk_copy(to_scales + at * S::kBlocks, P.C.scales[0] + (uint64_t)row * S::kBlocks, piece_tokens * S::kBlocks, bar);
+                bulk_copy(to_scales + S::kScales + at * S::kBlocks, P.C.scales[1] + (uint64_t)row * S::kBlocks, piece_tokens * S::kBlocks, bar);
             }
         }
         __syncwarp();
@@ -270,15 +325,25 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
         if (sent < count) send(st);
 
     // ---- the steps ----
-    Cursor<S::kCols> at;
+    typename S::Place at;
     at.set(at_span, b, item, step);
     float acc[S::kNt][S::kTiles][4], top[S::kNt][2], sum[S::kNt][2], factor[S::kNt][2];
     uint32_t q[S::kNt][S::kDim / 8];
     int lo[S::kNt][2], hi[S::kNt][2], lo_most = 0, hi_least = 0;
+    // where a lane's rows for ldmatrix begin: swizzled by the lane alone, 16 tokens further the same
+    uint32_t key_at[S::kChunks / 2], value_at[S::kChunks / 2];
+#pragma unroll
+    for (uint32_t c = 0; c < S::kChunks; c += 2) {
+        key_at[c / 2] = swizzled<S::kRow>((lane & 7) + 8 * ((lane >> 3) & 1), c + (lane >> 4));
+        value_at[c / 2] = swizzled<S::kRow>((lane & 7) + 8 * (lane >> 4), c + ((lane >> 3) & 1));
+    }
+    float zero[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) asm volatile("mov.b32 %0, 0;" : "=f"(zero[k]));
     uint32_t ref = 0;
     bool fresh = true, ok = true;
     uint32_t st = 0, parity = 0;
-    for (unsigned long long done = 0; done < count; ++done) {
+    for (uint32_t done = 0; done < count; ++done) {
         if (fresh) {
             // the item's columns: queries, limits
             fresh = false;
@@ -310,87 +375,77 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
         }
         if (!wait.warp(bars + 8 * st, parity)) { ok = false; break; }
         const uint32_t keys = ring + st * S::kStage, values = keys + S::kTile, scales = ring_scales + st * 2 * S::kScales;
+        const uint32_t logits = S::kLogitsOver ? keys : factors + S::kFactors;
         const int t0 = (int)at.token();
-        const uint32_t gone = (missing >> (2 * st)) & 3;
-        const bool plain = t0 >= lo_most && t0 + (int)kStepTokens <= hi_least && gone == 0;
+        const uint32_t gone = (missing >> (S::kGroups * st)) & ((1u << S::kGroups) - 1);
+        const bool plain = t0 >= lo_most && t0 + (int)S::kStep <= hi_least && gone == 0;
 
-        // scales: a lane has a token
-        uint32_t ks, vs;
-        if (S::kBlocks == 4) { ks = lds32(scales + 4 * lane); vs = lds32(scales + S::kScales + 4 * lane); }
-        else { ks = lds16(scales + 2 * lane); vs = lds16(scales + S::kScales + 2 * lane); }
-        bool hidden = false;
-        uint32_t poisoned = 0;                           // tokens with NaN in their values that not every column sees
+        // scales: a lane has every 32nd token
+        uint32_t ks[S::kOwn], vs[S::kOwn], hidden = 0, poisoned[S::kOwn] = {};     // poisoned: tokens with NaN in their values that not every column sees
+#pragma unroll
+        for (uint32_t j = 0; j < S::kOwn; ++j) {
+            if (S::kBlocks == 4) { ks[j] = lds32(scales + 4 * (32 * j + lane)); vs[j] = lds32(scales + S::kScales + 4 * (32 * j + lane)); }
+            else { ks[j] = lds16(scales + 2 * (32 * j + lane)); vs[j] = lds16(scales + S::kScales + 2 * (32 * j + lane)); }
+        }
         if (!plain) {
-            const int t = t0 + (int)lane;
-            hidden = t < at.from || t >= at.to || (gone >> (lane >> 4)) & 1;
-            bool nan = false;
 #pragma unroll
-            for (uint32_t k = 0; k < S::kBlocks; ++k) nan |= ((vs >> (8 * k)) & 0xFF) == 255;
-            if (!S::kFp4) {
+            for (uint32_t j = 0; j < S::kOwn; ++j) {
+                const uint32_t r = 32 * j + lane;
+                const int t = t0 + (int)r;
+                bool hide = t < at.from || t >= at.to || (gone >> (r >> 4)) & 1, nan = false;
 #pragma unroll
-                for (uint32_t c = 0; c < S::kChunks; ++c) {
-                    const uint4 w = lds128(values + swizzled<S::kRow>(lane, c));
-                    nan |= nan_bytes(w.x) || nan_bytes(w.y) || nan_bytes(w.z) || nan_bytes(w.w);
+                for (uint32_t k = 0; k < S::kBlocks; ++k) nan |= ((vs[j] >> (8 * k)) & 0xFF) == 255;
+                if (!S::kFp4) {
+#pragma unroll
+                    for (uint32_t c = 0; c < S::kChunks; ++c) {
+                        const uint4 w = lds128(values + swizzled<S::kRow>(r, c));
+                        nan |= nan_bytes(w.x) || nan_bytes(w.y) || nan_bytes(w.z) || nan_bytes(w.w);
+                    }
+                }
+                nan = nan && !hide && !(t >= lo_most && t < hi_least);
+                poisoned[j] = __ballot_sync(kAll, nan);
+                hide |= nan;
+                if (hide) {
+                    hidden |= 1u << j;
+                    vs[j] = 0;
+                    if (!S::kFp4) {
+                        const uint32_t none[4] = {};
+#pragma unroll
+                        for (uint32_t c = 0; c < S::kChunks; ++c) sts128(values + swizzled<S::kRow>(r, c), none);
+                        fence_async_shared();            // the next copy comes here
+                    }
                 }
             }
-            nan = nan && !hidden && !(t >= lo_most && t < hi_least);
-            poisoned = __ballot_sync(kAll, nan);
-            hidden |= nan;
-            if (!S::kFp4 && hidden) {
-                const uint32_t zero[4] = {};
-#pragma unroll
-                for (uint32_t c = 0; c < S::kChunks; ++c) sts128(values + swizzled<S::kRow>(lane, c), zero);
-                fence_async_shared();                    // the next copy comes here
-            }
         }
-        {
-            // keys: FP32 factors
-            float f[4];
+        // keys' scales, [token][block] in FP32
 #pragma unroll
-            for (uint32_t k = 0; k < S::kBlocks; ++k) f[k] = e8m0_value((ks >> (8 * k)) & 0xFF);
-            if (S::kBlocks == 4) sts_f4(key_factors + 16 * lane, f);
-            else sts_f2(key_factors + 8 * lane, f);
-            // values: over the largest scale so far
-            uint32_t s[S::kBlocks], most = 0;
+        for (uint32_t j = 0; j < S::kOwn; ++j) {
+            uint32_t f[4];
 #pragma unroll
-            for (uint32_t k = 0; k < S::kBlocks; ++k) {
-                s[k] = (vs >> (8 * k)) & 0xFF;
-                if (s[k] != 255) most = max(most, s[k]);
-            }
-            most = __reduce_max_sync(kAll, hidden ? 0u : most);
-            if (most > ref) {
-                const float shrink = ldexpf(1.0f, max((int)ref - (int)most, -200));
-                ref = most;
-#pragma unroll
-                for (uint32_t t = 0; t < S::kNt; ++t)
-#pragma unroll
-                    for (uint32_t m = 0; m < S::kTiles; ++m)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) acc[t][m][k] *= shrink;
-            }
-            // [token / 2][block] pairs of two tokens
-#pragma unroll
-            for (uint32_t k = 0; k < S::kBlocks; ++k)
-                sts16(value_factors + ((lane >> 1) * S::kBlocks + k) * 4 + (lane & 1) * 2, hidden ? 0u : value_factor(s[k], ref, S::kLift));
-            __syncwarp();
+            for (uint32_t k = 0; k < S::kBlocks; ++k) f[k] = __float_as_uint(e8m0_value((ks[j] >> (8 * k)) & 0xFF));
+            if (S::kBlocks == 4) sts128(factors + 16 * (32 * j + lane), f);
+            else sts64(factors + 8 * (32 * j + lane), f[0], f[1]);
         }
+        __syncwarp();
 
-        // logits of 32 tokens: p[t][m][..], m 16 tokens, rows g and g + 8, columns 2i and 2i + 1
-        float p[S::kNt][2][4];
+        // logits, 16 tokens at a time: rows g and g + 8, columns 2i and 2i + 1.  They wait for the step's maximum where their keys were.
+        float best[S::kNt][2];
 #pragma unroll
-        for (uint32_t m = 0; m < 2; ++m) {
-            float f[2][4];
+        for (uint32_t t = 0; t < S::kNt; ++t) best[t][0] = best[t][1] = -INFINITY;
+#pragma unroll 2
+        for (uint32_t m = 0; m < S::kGroups; ++m) {
+            float f[2][4], p[S::kNt][4];
             const uint32_t row = 16 * m + g;
-            if (S::kBlocks == 4) { lds_f4(key_factors + 16 * row, f[0]); lds_f4(key_factors + 16 * (row + 8), f[1]); }
-            else { lds_f2(key_factors + 8 * row, f[0]); lds_f2(key_factors + 8 * (row + 8), f[1]); }
+            if (S::kBlocks == 4) { lds_f4(factors + 16 * row, f[0]); lds_f4(factors + 16 * (row + 8), f[1]); }
+            else { lds_f2(factors + 8 * row, f[0]); lds_f2(factors + 8 * (row + 8), f[1]); }
 #pragma unroll
             for (uint32_t t = 0; t < S::kNt; ++t)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) p[t][m][k] = 0.0f;
+                for (int k = 0; k < 4; ++k) p[t][k] = 0.0f;
 #pragma unroll
             for (uint32_t c = 0; c < S::kChunks; c += 2) {
                 uint32_t w[4];
-                ldmatrix4(keys + swizzled<S::kRow>(16 * m + (lane & 7) + 8 * ((lane >> 3) & 1), c + (lane >> 4)), w);
+                ldmatrix4(keys + m * (16 * S::kRow) + key_at[c / 2], w);
 #pragma unroll
                 for (uint32_t h = 0; h < (S::kFp4 ? 2 : 1); ++h) {
                     uint32_t a[8];                       // rows g, g + 8 of the first four pairs, then of the next
@@ -412,55 +467,67 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                     const uint32_t block = S::kFp4 ? c + h : c / 2;
 #pragma unroll
                     for (uint32_t t = 0; t < S::kNt; ++t) {
-                        float d[4] = {};
-                        mma_f16(d, a[0], a[1], a[2], a[3], q[t][4 * block], q[t][4 * block + 1]);
+                        float d[4];
+                        mma_f16_first(d, a[0], a[1], a[2], a[3], q[t][4 * block], q[t][4 * block + 1], zero);
                         mma_f16(d, a[4], a[5], a[6], a[7], q[t][4 * block + 2], q[t][4 * block + 3]);
-                        p[t][m][0] = fmaf(d[0], f[0][block], p[t][m][0]);
-                        p[t][m][1] = fmaf(d[1], f[0][block], p[t][m][1]);
-                        p[t][m][2] = fmaf(d[2], f[1][block], p[t][m][2]);
-                        p[t][m][3] = fmaf(d[3], f[1][block], p[t][m][3]);
+                        p[t][0] = fmaf(d[0], f[0][block], p[t][0]);
+                        p[t][1] = fmaf(d[1], f[0][block], p[t][1]);
+                        p[t][2] = fmaf(d[2], f[1][block], p[t][2]);
+                        p[t][3] = fmaf(d[3], f[1][block], p[t][3]);
                     }
+                }
+            }
+            __syncwarp();
+#pragma unroll
+            for (uint32_t t = 0; t < S::kNt; ++t) {
+                best[t][0] = fmaxf(best[t][0], fmaxf(p[t][0], p[t][2]));
+                best[t][1] = fmaxf(best[t][1], fmaxf(p[t][1], p[t][3]));
+                sts_f4(logits + (m * S::kLogitsLd + t * 512) + 16 * lane, p[t]);
+            }
+        }
+
+        if (!plain) {
+            // what a column does not see
+#pragma unroll
+            for (uint32_t t = 0; t < S::kNt; ++t) {
+                best[t][0] = best[t][1] = -INFINITY;
+#pragma unroll 1
+                for (uint32_t m = 0; m < S::kGroups; ++m) {
+                    const uint32_t nan = (m < 2 ? poisoned[0] : poisoned[S::kOwn - 1]) >> (16 * (m & 1)), where = logits + (m * S::kLogitsLd + t * 512) + 16 * lane;
+                    float p[4];
+                    lds_f4(where, p);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t r = g + 8 * (k >> 1);
+                        const int tok = t0 + (int)(16 * m + r);
+                        const bool seen = tok >= lo[t][k & 1] && tok < hi[t][k & 1] && !((gone >> m) & 1);
+                        if ((nan >> r) & 1) p[k] = __int_as_float(0x7FFFFFFF);
+                        if (!seen) p[k] = -INFINITY;
+                        best[t][k & 1] = fmaxf(best[t][k & 1], p[k]);
+                    }
+                    sts_f4(where, p);
                 }
             }
         }
 
-        // weights
+        // the largest so far, a power of two over it
         bool grew = false;
-        float shrink[S::kNt][2];
+        float shrink[S::kNt][2], off[S::kNt][2];
 #pragma unroll
-        for (uint32_t t = 0; t < S::kNt; ++t) {
-#pragma unroll
-            for (uint32_t m = 0; m < 2; ++m)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    p[t][m][k] *= factor[t][k & 1];
-                    if (!plain) {
-                        const uint32_t r = 16 * m + g + 8 * (k >> 1);
-                        const int tok = t0 + (int)r;
-                        const bool seen = tok >= lo[t][k & 1] && tok < hi[t][k & 1] && !((gone >> m) & 1);
-                        if (!seen) p[t][m][k] = -INFINITY;
-                        else if ((poisoned >> r) & 1) p[t][m][k] = __int_as_float(0x7FFFFFFF);
-                    }
-                }
+        for (uint32_t t = 0; t < S::kNt; ++t)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                float best = fmaxf(fmaxf(p[t][0][k], p[t][0][k + 2]), fmaxf(p[t][1][k], p[t][1][k + 2]));
-                best = fmaxf(best, __shfl_xor_sync(kAll, best, 4));
-                best = fmaxf(best, __shfl_xor_sync(kAll, best, 8));
-                best = fmaxf(best, __shfl_xor_sync(kAll, best, 16));
-                grew |= best > top[t][k];
-                best = fmaxf(best, top[t][k]);
-                shrink[t][k] = best == -INFINITY ? 1.0f : exp2_fast(top[t][k] - best);
-                top[t][k] = best;
-                const float off = best == -INFINITY ? 0.0f : best - 15.0f;
-#pragma unroll
-                for (uint32_t m = 0; m < 2; ++m) {
-                    p[t][m][k] = exp2_fast(p[t][m][k] - off);
-                    p[t][m][k + 2] = exp2_fast(p[t][m][k + 2] - off);
-                }
-                sum[t][k] = sum[t][k] * shrink[t][k] + ((p[t][0][k] + p[t][0][k + 2]) + (p[t][1][k] + p[t][1][k + 2]));
+                float x = best[t][k];
+                x = fmaxf(x, __shfl_xor_sync(kAll, x, 4));
+                x = fmaxf(x, __shfl_xor_sync(kAll, x, 8));
+                x = fmaxf(x, __shfl_xor_sync(kAll, x, 16)) * factor[t][k];
+                grew |= x > top[t][k];
+                x = fmaxf(x, top[t][k]);
+                shrink[t][k] = x == -INFINITY ? 1.0f : exp2_fast(top[t][k] - x);
+                top[t][k] = x;
+                off[t][k] = x == -INFINITY ? 15.0f : 15.0f - x;
+                sum[t][k] *= shrink[t][k];
             }
-        }
         if (__any_sync(kAll, grew)) {
 #pragma unroll
             for (uint32_t t = 0; t < S::kNt; ++t)
@@ -470,26 +537,89 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                     for (int k = 0; k < 4; ++k) acc[t][m][k] *= shrink[t][k & 1];
         }
 
-        // weighted values, 16 tokens at a time
+        {
+            // values' scales over the largest so far, [token][block] in FP16, twice in a word; every lane is done with the keys'
+            __syncwarp();
+            uint32_t v01[S::kOwn], v23[S::kOwn], mine = 0, least = 255;
+            bool odd = false;
 #pragma unroll
-        for (uint32_t m = 0; m < 2; ++m) {
-            uint32_t pb[S::kNt][2];
+            for (uint32_t j = 0; j < S::kOwn; ++j) {
+                v01[j] = __byte_perm(vs[j], 0, 0x4140);
+                v23[j] = S::kBlocks == 4 ? __byte_perm(vs[j], 0, 0x4342) : v01[j];
+                const uint32_t most2 = __vmaxu2(v01[j], v23[j]), least2 = __vminu2(v01[j], v23[j]);
+                mine = max(mine, max(most2 & 0xFFFFu, most2 >> 16));
+                least = min(least, min(least2 & 0xFFFFu, least2 >> 16));
+            }
+            if (mine == 255) {
+                odd = true;
+                mine = 0;
+#pragma unroll
+                for (uint32_t j = 0; j < S::kOwn; ++j)
+#pragma unroll
+                    for (uint32_t k = 0; k < S::kBlocks; ++k)
+                        if (((vs[j] >> (8 * k)) & 0xFF) != 255) mine = max(mine, (vs[j] >> (8 * k)) & 0xFF);
+            }
+            const uint32_t most = __reduce_max_sync(kAll, mine);
+            if (most > ref) {
+                const float shrink = ldexpf(1.0f, max((int)ref - (int)most, -200));
+                ref = most;
+#pragma unroll
+                for (uint32_t t = 0; t < S::kNt; ++t)
+#pragma unroll
+                    for (uint32_t m = 0; m < S::kTiles; ++m)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc[t][m][k] *= shrink;
+            }
+            const uint32_t off = (ref - 15) * 0x10001u;                       // no half borrows from the other: s + 15 > ref
+            const bool quick = !odd && !hidden && least + 14 >= ref;
+#pragma unroll
+            for (uint32_t j = 0; j < S::kOwn; ++j) {
+                uint32_t f[4];
+                if (quick) {
+                    const uint32_t f01 = (v01[j] - off) << 10, f23 = (v23[j] - off) << 10;
+                    f[0] = __byte_perm(f01, 0, 0x1010);
+                    f[1] = __byte_perm(f01, 0, 0x3232);
+                    f[2] = __byte_perm(f23, 0, 0x1010);
+                    f[3] = __byte_perm(f23, 0, 0x3232);
+                } else {
+#pragma unroll
+                    for (uint32_t k = 0; k < S::kBlocks; ++k) f[k] = (hidden >> j) & 1 ? 0u : value_factor((vs[j] >> (8 * k)) & 0xFF, ref) * 0x10001u;
+                }
+                if (S::kBlocks == 4) sts128(factors + 16 * (32 * j + lane), f);
+                else sts64(factors + 8 * (32 * j + lane), f[0], f[1]);
+            }
+            __syncwarp();
+        }
+
+        // weights and weighted values, 16 tokens at a time
+#pragma unroll 2
+        for (uint32_t m = 0; m < S::kGroups; ++m) {
+            uint32_t f[2][4], pb[S::kNt][S::kBlocks][2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {                  // tokens g and g + 8
+                const uint32_t where = factors + (16 * m + 8 * k + g) * S::kBlocks * 4;
+                if (S::kBlocks == 4) { const uint4 v = lds128(where); f[k][0] = v.x; f[k][1] = v.y; f[k][2] = v.z; f[k][3] = v.w; }
+                else lds64(where, f[k][0], f[k][1]);
+            }
 #pragma unroll
             for (uint32_t t = 0; t < S::kNt; ++t) {
-                pb[t][0] = transpose8x8(pack_half(p[t][m][0], p[t][m][1]));
-                pb[t][1] = transpose8x8(pack_half(p[t][m][2], p[t][m][3]));
-            }
-            uint32_t f[2][4];                              // of tokens 2i, 2i + 1 and 2i + 8, 2i + 9
+                float p[4];
+                lds_f4(logits + (m * S::kLogitsLd + t * 512) + 16 * lane, p);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint32_t where = value_factors + (8 * m + 4 * k + i) * S::kBlocks * 4;
-                if (S::kBlocks == 4) { const uint4 v = lds128(where); f[k][0] = v.x; f[k][1] = v.y; f[k][2] = v.z; f[k][3] = v.w; }
-                else { lds64(where, f[k][0], f[k][1]); }
+                for (int k = 0; k < 4; ++k) p[k] = exp2_fast(fmaf(p[k], factor[t][k & 1], off[t][k & 1]));
+                sum[t][0] += p[0] + p[2];
+                sum[t][1] += p[1] + p[3];
+                const uint32_t w0 = pack_half(p[0], p[1]), w1 = pack_half(p[2], p[3]);
+#pragma unroll
+                for (uint32_t k = 0; k < S::kBlocks; ++k) {
+                    pb[t][k][0] = transpose8x8(mul_half2(w0, f[0][k]));
+                    pb[t][k][1] = transpose8x8(mul_half2(w1, f[1][k]));
+                }
             }
 #pragma unroll
             for (uint32_t c = 0; c < S::kChunks; c += 2) {
                 uint32_t w[4];                             // chunk c, c + 1 of the first eight tokens, then of the next
-                ldmatrix4_trans(values + swizzled<S::kRow>(16 * m + 8 * (lane >> 4) + (lane & 7), c + ((lane >> 3) & 1)), w);
+                ldmatrix4_trans(values + m * (16 * S::kRow) + value_at[c / 2], w);
 #pragma unroll
                 for (uint32_t h = 0; h < 2; ++h) {
                     const uint32_t block = S::kFp4 ? c + h : c / 2;
@@ -498,15 +628,14 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                     if (S::kFp4) { pairs_fp4(w[h], x); pairs_fp4(w[h + 2], y); }
                     else { pairs_e4m3(w[h], x); pairs_e4m3(w[h + 2], y); }
 #pragma unroll
-                    for (uint32_t k = 0; k < kPairs; ++k) { x[k] = mul_half2(x[k], f[0][block]); y[k] = mul_half2(y[k], f[1][block]); }
-#pragma unroll
                     for (uint32_t u = 0; u < kPairs / 2; ++u)
 #pragma unroll
                         for (uint32_t t = 0; t < S::kNt; ++t)
-                            mma_f16(acc[t][(c + h) * (kPairs / 2) + u], x[2 * u], x[2 * u + 1], y[2 * u], y[2 * u + 1], pb[t][0], pb[t][1]);
+                            mma_f16(acc[t][(c + h) * (kPairs / 2) + u], x[2 * u], x[2 * u + 1], y[2 * u], y[2 * u + 1], pb[t][block][0], pb[t][block][1]);
                 }
             }
         }
+        if (S::kLogitsOver) fence_async_shared();        // the next copy comes where the logits were
         __syncwarp();                                    // everybody is done with the stage
         const uint32_t used = st;
         if (++st == S::kStages) { st = 0; parity ^= 1; }
@@ -523,9 +652,9 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                     for (int d = 4; d < 32; d <<= 1) sum[t][k] += __shfl_xor_sync(kAll, sum[t][k], d);
             const bool whole = item_from >= from && item_to <= to;
             const float unit = e8m0_value(ref);
-            constexpr float kDown = 1.0f / (float)(1u << (S::kLift)) / 32768.0f;       // the weights' 2^15 goes here, once
-            const uint32_t slot = item_from < from ? 0u : 1u;            // a run's first part is of an item that began before it
-            const uint32_t where = slot == 0 ? first_part : ring;
+            constexpr float kDown = 1.0f / 32768.0f;       // the weights' 2^15 goes here, once
+            const uint32_t slot = done + 1 == count ? 1u : 0u;           // the run's last part goes where its copies were, an earlier one (there is one at most) to the workspace
+            float* early = part_in_workspace<S>(P, blockIdx.x * S::kWarps + warp);
 #pragma unroll
             for (uint32_t t = 0; t < S::kNt; ++t) {
 #pragma unroll
@@ -540,7 +669,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                     }
 #pragma unroll
                     for (uint32_t m = 0; m < S::kTiles; m += S::kFp4 ? 2 : 1) {
-                        constexpr uint32_t kOwn = S::kFp4 ? 4 : 2;         // neighbours of the head's width
+                        constexpr uint32_t kSide = S::kFp4 ? 4 : 2;        // neighbours of the head's width
                         float v[4];
                         v[0] = acc[t][m][k] * kDown * unit * norm;
                         v[1] = acc[t][m][k + 2] * kDown * unit * norm;
@@ -548,16 +677,23 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                             v[2] = acc[t][m + 1][k] * kDown * unit * norm;
                             v[3] = acc[t][m + 1][k + 2] * kDown * unit * norm;
                         }
-                        const uint32_t d = 16 * m + kOwn * g;
-                        if (out) store_out<kOwn>(P, out, d, v);
+                        const uint32_t d = 16 * m + kSide * g;
+                        if (out) store_out<kSide>(P, out, d, v);
                         else if (!whole) {
-                            if (S::kFp4) sts_f4(where + (in_tile * S::kPartLd + d) * 4, v);
-                            else sts_f2(where + (in_tile * S::kPartLd + d) * 4, v);
+                            if (slot == 0) {
+                                for (uint32_t n = 0; n < kSide; ++n) early[in_tile * S::kPartLd + d + n] = v[n];
+                            } else if (S::kFp4) sts_f4(ring + (in_tile * S::kPartLd + d) * 4, v);
+                            else sts_f2(ring + (in_tile * S::kPartLd + d) * 4, v);
                         }
                     }
                     if (!whole && g == 0) {
-                        sts_f1(where + (S::kCols * S::kPartLd + in_tile) * 4, top[t][k]);
-                        sts_f1(where + (S::kCols * S::kPartLd + S::kCols + in_tile) * 4, total_weight);
+                        if (slot == 0) {
+                            early[S::kCols * S::kPartLd + in_tile] = top[t][k];
+                            early[S::kCols * S::kPartLd + S::kCols + in_tile] = total_weight;
+                        } else {
+                            sts_f1(ring + (S::kCols * S::kPartLd + in_tile) * 4, top[t][k]);
+                            sts_f1(ring + (S::kCols * S::kPartLd + S::kCols + in_tile) * 4, total_weight);
+                        }
                     }
                 }
             }
@@ -565,8 +701,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                 StreamEntry& e = s_entry[2 * warp + slot];
                 e.from = item_from;
                 e.to = item_to;
-                e.b = at.b;
-                e.item = at.item;
+                e.columns = at.columns(P);
                 e.there = 1;
             }
             item_from = item_to;
@@ -576,9 +711,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
     }
     if (!ok) {
         // copies under way end, or are waited for as long as anything else, before the block does
-        const unsigned long long open = sent;
         for (uint32_t s = 0; s < S::kStages; ++s)
-            if (open > s) settled(bars + 8 * s, (uint32_t)((open - 1 - s) / S::kStages) & 1, P.spin_limit);
+            if (sent > s) settled(bars + 8 * s, ((sent - 1 - s) / S::kStages) & 1, P.spin_limit);
         if (lane == 0) atomicOr(P.B.marks, kKvGaveUp);
     }
     __syncthreads();
@@ -588,83 +722,77 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
         return;
     }
 
-    // ---- the block's parts, in order ----
+    // ---- the block's parts, in order: a warp has a column of an item ----
+    const uint8_t* rings = smem + (base - smem_u32(smem));
+    uint32_t parts = 0;
+    {
+        const bool there = lane < 2 * S::kWarps && s_entry[lane].there;
+        const uint32_t mask = __ballot_sync(kAll, there);
+        if (there) s_order[warp][__popc(mask & ((1u << lane) - 1))] = (uint8_t)lane;
+        parts = __popc(mask);
+        __syncwarp();
+    }
+    const uint8_t* order = s_order[warp];
     bool goes_on = false;
-    for (uint32_t e = 0; e < 2 * S::kWarps;) {
-        if (!s_entry[e].there) { ++e; continue; }
-        const StreamEntry one = s_entry[e];
-        uint32_t end = e + 1;
-        while (end < 2 * S::kWarps && (!s_entry[end].there || s_entry[end].from == one.from)) ++end;
-        const bool whole = one.from >= block_from && one.to <= block_to, begins = one.from >= block_from;
-        Cursor<S::kCols> c;
-        c.set_item(P, one.b, one.item);
-        for (uint32_t k = threadIdx.x; k < S::kCols * S::kDim / 4; k += S::kWarps * 32) {
-            const uint32_t in_tile = k / (S::kDim / 4), d = k % (S::kDim / 4) * 4, col = c.tile * S::kCols + in_tile;
-            float best = -INFINITY;
-            for (uint32_t j = e; j < end; ++j)
-                if (s_entry[j].there) best = fmaxf(best, lds_f1(part_of<S>(base, j) + (S::kCols * S::kPartLd + in_tile) * 4));
-            const float off = best == -INFINITY ? 0.0f : best;
-            float v[4] = {}, weight = 0.0f;
-            for (uint32_t j = e; j < end; ++j) {
-                if (!s_entry[j].there) continue;
-                const uint32_t part = part_of<S>(base, j);
-                const float w = exp2_fast(lds_f1(part + (S::kCols * S::kPartLd + in_tile) * 4) - off);
-                float x[4];
-                lds_f4(part + (in_tile * S::kPartLd + d) * 4, x);
-#pragma unroll
-                for (int n = 0; n < 4; ++n) v[n] = fmaf(x[n], w, v[n]);
-                weight = fmaf(lds_f1(part + (S::kCols * S::kPartLd + S::kCols + in_tile) * 4), w, weight);
-            }
-            if (whole) {
-                if (c.has(P, col)) finish_column(P, c, col, d, v, best, weight);
-            } else {
+    uint32_t unit = 0;
+    for (uint32_t e = 0; e < parts;) {
+        const StreamEntry& entry = s_entry[order[e]];
+        const unsigned long long item_at = entry.from, item_to = entry.to;
+        uint32_t count = 1;
+        while (e + count < parts && s_entry[order[e + count]].from == item_at) ++count;
+        const bool begins = item_at >= block_from, whole = begins && item_to <= block_to;
+        const ItemColumns columns = entry.columns;
+        if (!whole && begins) {
+            goes_on = true;
+            if (threadIdx.x == 0) *ends = BlockEnd{item_to, total, columns, 1, {}};
+        }
+        for (uint32_t in_tile = 0; in_tile < columns.count; ++in_tile, ++unit) {
+            if (unit % S::kWarps != warp) continue;
+            auto part = [&](uint32_t k) -> const float* {
+                const uint32_t at = order[e + k];
+                return at & 1 ? reinterpret_cast<const float*>(rings + (at >> 1) * S::kRing) : part_in_workspace<S>(P, blockIdx.x * S::kWarps + (at >> 1));
+            };
+            float v[S::kDim / 32], best, weight;
+            join_parts<S>(count, part, in_tile * S::kPartLd, S::kCols * S::kPartLd + in_tile, S::kCols * S::kPartLd + S::kCols + in_tile, v, best, weight);
+            constexpr uint32_t N = S::kDim / 32;
+            if (whole) finish_column<N>(P, columns, in_tile, lane * N, v, best, weight);
+            else {
                 float* to_part = partial_of<S>(P, gridDim.x, blockIdx.x, begins ? 1 : 0);
-                *reinterpret_cast<float4*>(to_part + in_tile * S::kDim + d) = make_float4(v[0], v[1], v[2], v[3]);
-                if (d == 0) {
+                if (N == 4) *reinterpret_cast<float4*>(to_part + in_tile * S::kDim + lane * N) = make_float4(v[0], v[1], v[N - 2], v[N - 1]);
+                else *reinterpret_cast<float2*>(to_part + in_tile * S::kDim + lane * N) = make_float2(v[0], v[1]);
+                if (lane == 0) {
                     to_part[S::kCols * S::kDim + in_tile] = best;
                     to_part[S::kCols * S::kDim + S::kCols + in_tile] = weight;
                 }
             }
         }
-        if (!whole && begins) {
-            goes_on = true;
-            if (threadIdx.x == 0) *ends = BlockEnd{one.to, total, one.b, one.item, 1, 0};
-        }
-        e = end;
+        e += count;
     }
     if (!goes_on && threadIdx.x == 0) ends->there = 0;
 }
 
-// The items that go on from one block to the next: a block for each block that an item begins and does not end in.
+// The items that go on from one block to the next: a block for each block that an item begins and does not end in, a warp for each column.
 template <typename S>
-__global__ void __launch_bounds__(S::kCols * S::kDim / 4) kv_join_kernel(const AttentionParams P, uint32_t blocks)
+__global__ void __launch_bounds__(S::kCols * 32) kv_join_kernel(const AttentionParams P, uint32_t blocks)
 {
     grid_wait();
     grid_launch_dependents();
     const BlockEnd end = reinterpret_cast<const BlockEnd*>(P.workspace)[blockIdx.x];
-    if (!end.there) return;
-    Cursor<S::kCols> c;
-    c.set_item(P, end.b, end.item);
-    const uint32_t in_tile = threadIdx.x / (S::kDim / 4), d = threadIdx.x % (S::kDim / 4) * 4, col = c.tile * S::kCols + in_tile;
-    const unsigned long long runs = (unsigned long long)blocks * S::kWarps;
-    // the last block whose steps begin before the item's end
-    uint32_t last = blockIdx.x;
-    while (last + 1 < blocks && end.total * ((unsigned long long)(last + 1) * S::kWarps) / runs < end.to) ++last;
-    float best = -INFINITY, weight = 0.0f, v[4] = {};
-    for (uint32_t k = blockIdx.x; k <= last; ++k) {
-        if (k > blockIdx.x && end.total * ((unsigned long long)(k + 1) * S::kWarps) / runs == end.total * ((unsigned long long)k * S::kWarps) / runs) continue;     // no steps
-        const float* part = partial_of<S>(P, blocks, k, k == blockIdx.x ? 1 : 0);
-        const float4 x = *reinterpret_cast<const float4*>(part + in_tile * S::kDim + d);
-        const float t = part[S::kCols * S::kDim + in_tile], w = part[S::kCols * S::kDim + S::kCols + in_tile];
-        const float next = fmaxf(best, t), off = next == -INFINITY ? 0.0f : next, old = exp2_fast(best - off), now = exp2_fast(t - off);
-        best = next;
-        v[0] = v[0] * old + x.x * now;
-        v[1] = v[1] * old + x.y * now;
-        v[2] = v[2] * old + x.z * now;
-        v[3] = v[3] * old + x.w * now;
-        weight = weight * old + w * now;
-    }
-    if (c.has(P, col)) finish_column(P, c, col, d, v, best, weight);
+    const uint32_t lane = threadIdx.x & 31, in_tile = threadIdx.x >> 5;
+    if (!end.there || in_tile >= end.columns.count) return;
+    // up to the last block whose steps begin before the item's end; with fewer steps than blocks some have none, and no part
+    const uint32_t last = (uint32_t)((end.to * blocks - 1) / end.total);
+    const bool gaps = end.total < blocks;
+    const uint32_t count = gaps ? (uint32_t)(end.to - share(end.total, blockIdx.x, blocks)) : last - blockIdx.x + 1;
+    auto part = [&](uint32_t k) -> const float* {
+        // with gaps a block has one step at most: the k-th next step's block is the last that begins at or before it
+        const uint32_t block = k == 0 ? blockIdx.x : gaps ? (uint32_t)(((share(end.total, blockIdx.x, blocks) + k + 1) * blocks - 1) / end.total) : blockIdx.x + k;
+        return partial_of<S>(P, blocks, block, k == 0 ? 1 : 0);
+    };
+    constexpr uint32_t N = S::kDim / 32;
+    float v[N], best, weight;
+    join_parts<S>(count, part, in_tile * S::kDim, S::kCols * S::kDim + in_tile, S::kCols * S::kDim + S::kCols + in_tile, v, best, weight);
+    finish_column<N>(P, end.columns, in_tile, lane * N, v, best, weight);
 }
 
 }  // namespace zc
