@@ -24,7 +24,7 @@ UNITS = [("zc_host.cpp", [], "zc_host.cpp.o"), ("zc_hist.cu", [], "zc_hist.cu.o"
          ("zc_kv_attention.cu", [], "zc_kv_attention.cu.o")] + \
         [("zc_encode_fmt.cu", [f"-DZC_ENC_FMT={k}"], f"zc_encode.fmt{k}.o") for k in (1, 2, 3, 4)] + \
         [("zc_decode.cu", [f"-DZC_DEC_PART={k}"], f"zc_decode.part{k}.o") for k in (1, 2, 3, 4)]
-HEADERS = ["zc_internal.h", "zc_bits.cuh", "zc_device.cuh", "zc_encode.cuh", "zc_fp8.cuh", "zc_fp8_tensor.cuh", "zc_kv.cuh", "zc_kv_attention.cuh", "zc_kv_stream.cuh"]
+HEADERS = ["zc_internal.h", "zc_bits.cuh", "zc_device.cuh", "zc_encode.cuh", "zc_fp8.cuh", "zc_fp8_tensor.cuh", "zc_kv.cuh", "zc_kv_attention.cuh", "zc_kv_stream.cuh", "zc_kv_prompt.cuh"]
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 
 

@@ -1,7 +1,7 @@
 // Attention over a quantised key/value cache: arguments, choice of kernels, launches.
 #include <type_traits>
 
-#include "zc_kv_stream.cuh"
+#include "zc_kv_prompt.cuh"
 
 namespace zc {
 
@@ -31,10 +31,22 @@ static uint32_t multiprocessors_or_most()
     return n ? n : 256;
 }
 
+// What blocks leave to the joining kernel, and what warps of a block leave to the block.
 template <typename S>
-static size_t stream_workspace(uint32_t blocks)
+static size_t workspace_of(uint32_t blocks, uint32_t early_floats)
 {
-    return (blocks * sizeof(BlockEnd) + 255) / 256 * 256 + (size_t)blocks * (2 * S::kCols * (S::kDim + 2) + S::kWarps * S::kPart) * 4;
+    return (blocks * sizeof(BlockEnd) + 255) / 256 * 256 + ((size_t)blocks * 2 * S::kCols * (S::kDim + 2) + early_floats) * 4;
+}
+template <typename S>
+static size_t stream_workspace(uint32_t blocks) { return workspace_of<S>(blocks, blocks * S::kWarps * S::kPart); }
+
+template <typename S>
+static cudaError_t launch_join(const AttentionParams& P, uint32_t blocks, cudaLaunchConfig_t cfg)
+{
+    cfg.gridDim = dim3(blocks, S::kCols / 8);
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, kv_join_kernel<S>, P, blocks);
 }
 
 template <typename S>
@@ -51,10 +63,30 @@ static cudaError_t launch_stream(const AttentionParams& P, const CUtensorMap& ke
     cfg.attrs = at;
     cfg.numAttrs = 1;
     if (const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_stream_kernel<S>, P, keys, values)) return e;
-    cfg.blockDim = dim3(S::kCols * 32);
-    cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, kv_join_kernel<S>, P, blocks);
+    return launch_join<S>(P, blocks, cfg);
 }
+
+template <typename S>
+static cudaError_t launch_prompt(const AttentionParams& P, uint32_t blocks, cudaStream_t st)
+{
+    static OncePerDevice ready;
+    if (!ready([]() -> uint32_t {
+            return cudaFuncSetAttribute(kv_prompt_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem) == cudaSuccess &&
+                   cudaFuncSetAttribute(kv_prompt_kernel<S>, cudaFuncAttributePreferredSharedMemoryCarveout, 100) == cudaSuccess; })) return cudaErrorUnknown;
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at[1] = {launch_early()};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(S::kThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_prompt_kernel<S>, P)) return e;
+    return launch_join<S>(P, blocks, cfg);
+}
+
+// Columns (rows times heads that share a head of the cache) up to which a sequence goes to the kernel of few rows.
+constexpr uint32_t kFewColumns = 16;
 
 }  // namespace zc
 
@@ -66,8 +98,12 @@ size_t zc_kv_attention_workspace_bytes(const zc_kv_cache* cache, const zc_kv_bat
 {
     if (check_cache(cache) || check_batch(cache, batch) || q_heads == 0 || q_heads % cache->kv_heads || q_heads / cache->kv_heads > ZC_KV_MAX_GROUP) return 0;
     const uint32_t n = multiprocessors_or_most();
-    return cache->head_dim == 128 ? std::max(stream_workspace<StreamShape<true, 128, 1>>(n), stream_workspace<StreamShape<true, 128, 2>>(n))
-                                  : std::max(stream_workspace<StreamShape<true, 64, 1>>(n), stream_workspace<StreamShape<true, 64, 2>>(n));
+    const bool wide = cache->head_dim == 128;
+    size_t bytes = wide ? std::max(stream_workspace<StreamShape<true, 128, 1>>(n), stream_workspace<StreamShape<true, 128, 2>>(n))
+                        : std::max(stream_workspace<StreamShape<true, 64, 1>>(n), stream_workspace<StreamShape<true, 64, 2>>(n));
+    if ((uint64_t)(q_heads / cache->kv_heads) * std::max(1u, batch->max_new) > kFewColumns)
+        bytes = std::max(bytes, wide ? workspace_of<PromptShape<true, 128>>(2 * n, 0) : workspace_of<PromptShape<true, 64>>(2 * n, 0));
+    return bytes;
 }
 
 zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, const zc_kv_attention_args* args, void* d_workspace,
@@ -105,6 +141,7 @@ zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, co
     P.most_rows = 0xFFFFFFFFu;
     P.spin_limit = test_knobs().spin_limit;
     P.skip_copy = test_knobs().skip_copy;
+    P.skip_math = test_knobs().skip_math;
     const uint32_t blocks = multiprocessors();
     if (!blocks) return ZC_E_CUDA;
     const uint32_t row_bytes = cache->format == ZC_FMT_FP4_E2M1 ? cache->head_dim / 2 : cache->head_dim;
@@ -115,8 +152,15 @@ zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, co
     auto run = [&](auto fp4, auto dim) {
         using One = StreamShape<decltype(fp4)::value, decltype(dim)::value, 1>;
         using Two = StreamShape<decltype(fp4)::value, decltype(dim)::value, 2>;
-        const bool few = (uint64_t)P.group * std::max(1u, batch->max_new) <= 8;
-        return few ? launch_stream<One>(P, maps[0], maps[1], blocks, (cudaStream_t)cuda_stream) : launch_stream<Two>(P, maps[0], maps[1], blocks, (cudaStream_t)cuda_stream);
+        using Many = PromptShape<decltype(fp4)::value, decltype(dim)::value>;
+        cudaStream_t st = (cudaStream_t)cuda_stream;
+        const uint64_t columns = (uint64_t)P.group * std::max(1u, batch->max_new);
+        if (columns <= 8) return launch_stream<One>(P, maps[0], maps[1], blocks, st);
+        if (columns <= kFewColumns) return launch_stream<Two>(P, maps[0], maps[1], blocks, st);
+        // a sequence alone has the rows that are expected; of several some may have few
+        if (batch->n_seqs > 1) P.most_rows = kFewColumns / P.group;
+        if (const cudaError_t e = launch_prompt<Many>(P, Many::kBlocksPerSm * blocks, st)) return e;
+        return batch->n_seqs > 1 && P.most_rows ? launch_stream<Two>(P, maps[0], maps[1], blocks, st) : cudaSuccess;
     };
     auto dims = [&](auto fp4) {
         return cache->head_dim == 128 ? run(fp4, std::integral_constant<uint32_t, 128>()) : run(fp4, std::integral_constant<uint32_t, 64>());

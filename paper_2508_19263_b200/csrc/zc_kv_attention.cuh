@@ -16,8 +16,8 @@ struct AttentionParams {
     uint32_t causal, window;
     uint32_t half_type;                 // queries and results in FP16, else BF16
     uint32_t q_wide, out_wide;          // four neighbours begin on 8 bytes
-    uint32_t most_rows;                 // sequences of more rows are another kernel's
-    uint32_t spin_limit, skip_copy;
+    uint32_t most_rows;                 // sequences of up to so many rows are for the kernel of few rows, the others for that of many; all ones: all are
+    uint32_t spin_limit, skip_copy, skip_math;
 };
 
 // An item's columns, as whoever joins its parts needs them.

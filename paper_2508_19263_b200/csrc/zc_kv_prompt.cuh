@@ -1,0 +1,582 @@
+// Attention of many rows over a cache: the tensor cores and the exponentials bound it.
+//
+// Columns of a sequence and a head (rows times the query heads that share it) are cut into tiles of 128, the rows of one matrix instruction; a tile
+// with a head is an item, a step is 128 tokens of an item.  As in the other kernel all steps in order are cut into equal runs, here one for each of
+// two blocks an SM, and parts of items are joined by a second kernel.  Two blocks an SM because a block goes through product, softmax and product
+// one after the other: while one is at its softmax the other's products have the tensor cores.
+//
+// Roles: four warps have a row a thread (maxima, exponentials, sums, the weights into tensor memory, results); four have a token a thread and write
+// keys and values as FP16 into shared memory; one issues the matrix instructions.
+//   S = Q K^T: both operands in shared memory, 128-byte swizzle, the head's width fastest.  O += P V: P in tensor memory, in S's place; V as it is written,
+// the head's width fastest, which for this product is the outer axis.  S and O, FP32, are 256 of tensor memory's columns, half of them for each block.
+//   Keys and values are element * 2^(s - R + kLift), R the largest scale byte that the item has met, for keys and for values: exact unless a scale is 2^-35 (E4M3:
+// 2^-22) of the largest, off by at most 2^-25 / 2^kLift of 2^R then.  Queries as in the other kernel.
+//   Weights are 2^(x - m + 14) with m at most 1 below the row's largest so far: so the sums in tensor memory are only touched when it grows by more than
+// a factor of 2.  They are rounded to FP16: off by at most 2^-12 of it down to 2^-28 of the largest, by 2^-39 of the largest below; the sum of weights is FP32.
+#pragma once
+#include "zc_kv_stream.cuh"
+
+namespace zc {
+
+template <bool FP4_, uint32_t DIM_>
+struct PromptShape {
+    static constexpr bool kFp4 = FP4_;
+    static constexpr uint32_t kDim = DIM_, kCols = 128, kStep = 128;
+    static constexpr uint32_t kRow = kFp4 ? kDim / 2 : kDim, kBlocks = kDim / kKvBlock;
+    static constexpr int kLift = kFp4 ? 12 : 6;                              // 6 * 2^12 and 448 * 2^6 are FP16 numbers
+    static constexpr uint32_t kTile = 128 * kDim * 2;                        // Q, K, V: 128 rows of FP16, pieces of 64 of the head's width one after the other
+    static constexpr uint32_t kSmem = 3 * kTile + 1024;
+    static constexpr uint32_t kThreads = 288, kBlocksPerSm = 2;
+    static constexpr uint32_t kS = 0, kO = 128, kTmem = 256;                 // columns
+};
+
+// Where a role is; the same in all of a block's threads.
+struct PromptCursor : SeqRows {
+    uint32_t b, tile, head, tiles, step, steps, first_step;
+    __device__ __forceinline__ void tile_span(const AttentionParams& P, uint32_t t, uint32_t& first, uint32_t& count) const
+    {
+        const uint32_t cols = (uint32_t)n * P.group, last = min(cols, (t + 1) * 128) - 1;
+        int lo, hi, skip;
+        limits(P, (int)(last / P.group), skip, hi);
+        limits(P, (int)(t * 128 / P.group), lo, skip);
+        hi = min(max(hi, 0), len);
+        first = (uint32_t)lo / 128;
+        const uint32_t end = ((uint32_t)hi + 127) / 128;
+        count = end > first ? end - first : 1;             // at least one, that rows which see nothing get their zeros
+    }
+    __device__ __forceinline__ void sequence(const AttentionParams& P, uint32_t b_)
+    {
+        b = b_;
+        load(P, b);
+        tiles = (uint32_t)n > P.most_rows || P.most_rows == 0xFFFFFFFFu ? (uint32_t)(((unsigned long long)n * P.group + 127) / 128) : 0;
+    }
+    __device__ __forceinline__ void next_item(const AttentionParams& P)
+    {
+        step = 0;
+        if (++head < P.C.heads) return;
+        head = 0;
+        if (++tile >= tiles) {
+            tile = 0;
+            do {
+                if (b + 1 >= P.B.n_seqs) return;
+                sequence(P, b + 1);
+            } while (tiles == 0);
+        }
+        tile_span(P, tile, first_step, steps);
+    }
+    __device__ __forceinline__ ItemColumns columns(const AttentionParams& P) const { return ItemColumns{row0, head, tile * 128, min(128u, (uint32_t)n * P.group - tile * 128)}; }
+};
+
+__device__ __forceinline__ void mma_ss_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void mma_ts_f16(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+// 32 columns of a warp's 32 lanes; not complete before tmem_ld_wait
+__device__ __forceinline__ void tmem_ld32_async(uint32_t addr, float v[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+                   "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+                   "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+                   "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t v[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 :: "r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+                    "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const float v[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 :: "r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]),
+                    "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]),
+                    "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]),
+                    "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// A tile whose rows are tokens and whose outer axis for the product is the head's width: pieces of 64 of it 128 rows * 128 bytes apart, groups of 8 rows 1024 bytes.
+__device__ __forceinline__ uint64_t outer_desc(uint32_t addr)
+{
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(16384 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// Where 16 bytes (8 of the head's width) of a row of a tile are.
+__device__ __forceinline__ uint32_t tile_at(uint32_t row, uint32_t chunk) { return (chunk >> 3) * 16384 + row * 128 + (((chunk ^ row) & 7) << 4); }
+
+// 2^(s - ref + lift) in FP16, twice; NaN for 255.
+__device__ __forceinline__ uint32_t element_factor(uint32_t s, uint32_t ref, int lift)
+{
+    const int e = (int)s - (int)ref + lift + 15;
+    return (s == 255 ? 0x7E00u : e > 0 ? (uint32_t)e << 10 : 0x400u >> min(1 - e, 31)) * 0x10001u;
+}
+
+// One token's elements, raw in w, into its row of a tile.
+template <typename S>
+__device__ __forceinline__ void write_row(uint32_t tile, uint32_t row, const uint4* w, uint32_t scales, uint32_t ref, bool hidden)
+{
+#pragma unroll
+    for (uint32_t k = 0; k < S::kBlocks; ++k) {
+        const uint32_t f = hidden ? 0u : element_factor((scales >> (8 * k)) & 0xFF, ref, S::kLift);
+        if (S::kFp4) {
+            const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                uint32_t h[4];
+                fp4_to_half(x[j], h);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[i] = mul_half2(h[i], f);
+                sts128(tile + tile_at(row, 4 * k + j), h);
+            }
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                const uint4 v = w[2 * k + j / 2];
+                const uint32_t x0 = j & 1 ? v.z : v.x, x1 = j & 1 ? v.w : v.y;
+                uint32_t h[4];
+                e4m3_to_half(x0, h);
+                e4m3_to_half(x1, h + 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[i] = hidden ? 0u : mul_half2(h[i], f);
+                sts128(tile + tile_at(row, 4 * k + j), h);
+            }
+        }
+    }
+}
+
+template <typename S>
+__global__ void __launch_bounds__(S::kThreads, S::kBlocksPerSm) kv_prompt_kernel(const AttentionParams P)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ __align__(8) uint64_t s_bars[9];
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile uint32_t s_failed;
+    __shared__ unsigned long long s_total, s_item_from;
+    __shared__ uint32_t s_start[4];                       // sequence, tile, head, step
+    __shared__ uint32_t s_most[2][2][4];                  // by step parity, keys and values, by warp: largest scale bytes
+    __shared__ uint32_t s_ref[2][2];                      // by step parity: what keys and values are over
+    __shared__ uint32_t s_gone[2][4], s_poisoned[2][4];   // by step parity: tokens without a page; with NaN in their values that not every row sees
+    constexpr uint32_t kAll = 0xFFFFFFFFu;
+    const uint32_t lane = threadIdx.x & 31, warp = warp_index();
+    const uint32_t base = (smem_u32(smem) + 1023) & ~1023u, q_tile = base, k_tile = base + S::kTile, v_tile = base + 2 * S::kTile;
+    const uint32_t bars = smem_u32(s_bars);
+    // queries written; keys written (m_full: largest scales known); product done (softmax, keys free); values written; weights written; second product done
+    const uint32_t q_full = bars, k_full = bars + 8, s_full = bars + 16, v_full = bars + 24, p_full = bars + 32, o_full = bars + 40, k_free = bars + 48, v_free = bars + 56, m_full = bars + 64;
+    if (threadIdx.x == 0) {
+        s_failed = 0;
+        bar_init(q_full, 128);
+        bar_init(k_full, 128);
+        bar_init(s_full, 1);
+        bar_init(v_full, 128);
+        bar_init(p_full, 128);
+        bar_init(o_full, 1);
+        bar_init(k_free, 1);
+        bar_init(v_free, 1);
+        bar_init(m_full, 4);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) tmem_alloc<1>(smem_u32(&s_tmem), S::kTmem);
+    grid_wait();
+    grid_launch_dependents();
+
+    // ---- which steps are this block's: every tile of every sequence is looked at, 32 at a time ----
+    if (warp == 0) {
+        unsigned long long total = 0;
+        for (int pass = 0; pass < 2; ++pass) {
+            const unsigned long long from = pass ? share(total, blockIdx.x, gridDim.x) : 0;
+            unsigned long long before = 0;
+            bool found = false;
+            PromptCursor many{};                          // a lane has one of 32 sequences
+            for (uint32_t b = 0; b < P.B.n_seqs && !found; ++b) {
+                if ((b & 31) == 0) {
+                    many.tiles = 0;
+                    if (b + lane < P.B.n_seqs) many.sequence(P, b + lane);
+                }
+                PromptCursor c;
+                c.tiles = __shfl_sync(kAll, many.tiles, b & 31);
+                if (c.tiles == 0) continue;
+                c.n = __shfl_sync(kAll, many.n, b & 31);
+                c.len = __shfl_sync(kAll, many.len, b & 31);
+                for (uint32_t t0 = 0; t0 < c.tiles; t0 += 32) {
+                    uint32_t first = 0, count = 0;
+                    if (t0 + lane < c.tiles) c.tile_span(P, t0 + lane, first, count);
+                    unsigned long long upto = (unsigned long long)count * P.C.heads;
+                    for (int d = 1; d < 32; d <<= 1) {
+                        const unsigned long long o = __shfl_up_sync(kAll, upto, d);
+                        if ((int)lane >= d) upto += o;
+                    }
+                    const unsigned long long sum = __shfl_sync(kAll, upto, 31);
+                    if (pass && before + sum > from) {
+                        const uint32_t k = __ffs(__ballot_sync(kAll, before + upto > from)) - 1;
+                        const uint32_t steps = __shfl_sync(kAll, count, k);
+                        const unsigned long long inside = from - before - (__shfl_sync(kAll, upto, k) - (unsigned long long)steps * P.C.heads);
+                        if (lane == 0) {
+                            const uint32_t head = (uint32_t)inside / steps, step = (uint32_t)inside % steps;
+                            s_start[0] = b;
+                            s_start[1] = t0 + k;
+                            s_start[2] = head;
+                            s_start[3] = step;
+                            s_item_from = from - step;
+                        }
+                        found = true;
+                        break;
+                    }
+                    before += sum;
+                }
+            }
+            if (!pass) total = before;
+        }
+        if (lane == 0) s_total = total;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const unsigned long long total = s_total, from = share(total, blockIdx.x, gridDim.x), to = share(total, blockIdx.x + 1, gridDim.x);
+    const uint32_t count = (uint32_t)(to - from), tmem = s_tmem;
+    const Waiter wait{P.spin_limit, &s_failed};
+    PromptCursor c;
+    if (count) {
+        c.sequence(P, s_start[0]);
+        c.tile = s_start[1];
+        c.head = s_start[2];
+        c.step = s_start[3];
+        c.tile_span(P, c.tile, c.first_step, c.steps);
+    }
+    BlockEnd* ends = reinterpret_cast<BlockEnd*>(P.workspace) + blockIdx.x;
+    uint32_t issued = 0;                                   // of the issuing warp: steps whose first, and second, product were issued
+    uint32_t issued2 = 0;
+
+    if (warp == 8) {
+        // ---- matrix instructions ----
+        const uint32_t qk = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);                               // FP16 operands, FP32 sums
+        const uint32_t pv = (1u << 4) | (1u << 16) | ((S::kDim >> 3) << 17) | ((128u >> 4) << 24);               // the second operand by its outer axis
+        uint32_t items = 0;
+        bool fresh = true;
+        for (uint32_t j = 0; j < count; ++j) {
+            if (fresh && !wait.warp(q_full, items & 1)) break;
+            if (!wait.warp(k_full, j & 1)) break;
+            // the product goes where the last step's weights are
+            if (j && !wait.warp(o_full, (j - 1) & 1)) break;
+            tc_fence_after();
+            if (P.skip_math) { wait.give_up(); break; }
+            if (elect_one()) {
+#pragma unroll
+                for (uint32_t k = 0; k < S::kDim / 16; ++k) {
+                    const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
+                    mma_ss_f16(tmem + S::kS, operand_desc(q_tile + off), operand_desc(k_tile + off), qk, k != 0);
+                }
+                mma_commit<1>(s_full);
+                mma_commit<1>(k_free);
+            }
+            __syncwarp();
+            ++issued;
+            if (!wait.warp(v_full, j & 1) || !wait.warp(p_full, j & 1)) break;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) mma_ts_f16(tmem + S::kO, tmem + S::kS + 8 * k, outer_desc(v_tile + k * 2048), pv, !(fresh && k == 0));
+                mma_commit<1>(o_full);
+                mma_commit<1>(v_free);
+            }
+            __syncwarp();
+            ++issued2;
+            fresh = false;
+            if (++c.step == c.steps) {
+                c.next_item(P);
+                fresh = true;
+                ++items;
+            }
+        }
+    } else if (warp >= 4) {
+        // ---- keys and values: a thread has a token ----
+        const uint32_t row = threadIdx.x - 128, group = row >> 5;
+        PromptCursor ahead = c;
+        constexpr uint32_t kWords = S::kRow / 16;
+        uint4 kw[kWords], vw[kWords];
+        uint32_t ks = 0, vs = 0;
+        int page = -1, next_page = -1;
+        auto find_page = [&](const PromptCursor& a) -> int {
+            const uint32_t t = (a.first_step + a.step) * 128 + row;
+            int lo, hi, skip;
+            const uint32_t cols = (uint32_t)a.n * P.group;
+            a.limits(P, (int)(a.tile * 128 / P.group), lo, skip);
+            a.limits(P, (int)((min(cols, a.tile * 128 + 128) - 1) / P.group), skip, hi);
+            return (int)t >= lo && (int)t < hi && t < (uint32_t)a.len ? kv_page(P.C, P.B, a.b, t >> P.C.page_shift) : -2;     // -2: nobody sees the token
+        };
+        auto load = [&](const PromptCursor& a, int pg) {
+            const uint32_t t = (a.first_step + a.step) * 128 + row;
+            if (pg >= 0) {
+                const uint64_t at = (((uint64_t)pg * P.C.heads + a.head) << P.C.page_shift) + (t & ((1u << P.C.page_shift) - 1));
+                const uint4 *k = reinterpret_cast<const uint4*>(P.C.elems[0] + at * S::kRow), *v = reinterpret_cast<const uint4*>(P.C.elems[1] + at * S::kRow);
+#pragma unroll
+                for (uint32_t i = 0; i < kWords; ++i) { kw[i] = k[i]; vw[i] = v[i]; }
+                if (S::kBlocks == 4) {
+                    ks = *reinterpret_cast<const uint32_t*>(P.C.scales[0] + at * 4);
+                    vs = *reinterpret_cast<const uint32_t*>(P.C.scales[1] + at * 4);
+                } else {
+                    ks = *reinterpret_cast<const uint16_t*>(P.C.scales[0] + at * 2);
+                    vs = *reinterpret_cast<const uint16_t*>(P.C.scales[1] + at * 2);
+                }
+            }
+        };
+        auto advance = [&](PromptCursor& a) { if (++a.step == a.steps) a.next_item(P); };
+        uint32_t k_ref = 0, v_ref = 0;
+        if (count) {
+            page = find_page(c);
+            load(c, page);
+            advance(ahead);
+            if (count > 1) next_page = find_page(ahead);
+        }
+        for (uint32_t j = 0; j < count; ++j) {
+            const uint32_t par = j & 1;
+            if (j && c.step == 0) k_ref = v_ref = 0;
+            const bool hidden = page < 0;
+            // the largest scales
+            uint32_t km = 0, vm = 0;
+            bool nan = false;
+            if (!hidden) {
+#pragma unroll
+                for (uint32_t k = 0; k < S::kBlocks; ++k) {
+                    const uint32_t a = (ks >> (8 * k)) & 0xFF, b = (vs >> (8 * k)) & 0xFF;
+                    if (a != 255) km = max(km, a);
+                    if (b != 255) vm = max(vm, b);
+                    nan |= b == 255;
+                }
+                if (!S::kFp4) {
+#pragma unroll
+                    for (uint32_t i = 0; i < kWords; ++i) nan |= nan_bytes(vw[i].x) || nan_bytes(vw[i].y) || nan_bytes(vw[i].z) || nan_bytes(vw[i].w);
+                }
+            }
+            if (nan) {
+                // NaN that every row of the tile sees goes through the product, else the rows that see it are told
+                const int t = (int)((c.first_step + c.step) * 128 + row);
+                int lo, hi, skip;
+                c.limits(P, (int)(c.tile * 128 / P.group), skip, hi);
+                c.limits(P, (int)((min((uint32_t)c.n * P.group, c.tile * 128 + 128) - 1) / P.group), lo, skip);
+                nan = t < lo || t >= hi;
+            }
+            km = __reduce_max_sync(kAll, km);
+            vm = __reduce_max_sync(kAll, vm);
+            const uint32_t gone = __ballot_sync(kAll, page == -1), poisoned = __ballot_sync(kAll, nan);
+            if (lane == 0) {
+                s_most[par][0][group] = km;
+                s_most[par][1][group] = vm;
+                s_gone[par][group] = gone;
+                s_poisoned[par][group] = poisoned;
+                bar_arrive(m_full);
+            }
+            if (!wait.warp(m_full, par)) break;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                k_ref = max(k_ref, s_most[par][0][k]);
+                v_ref = max(v_ref, s_most[par][1][k]);
+            }
+            if (row == 0) { s_ref[par][0] = k_ref; s_ref[par][1] = v_ref; }
+            if (j && !wait.warp(k_free, (j - 1) & 1)) break;
+            write_row<S>(k_tile, row, kw, ks, k_ref, hidden);
+            fence_async_shared();
+            bar_arrive(k_full);
+            if (j && !wait.warp(v_free, (j - 1) & 1)) break;
+            write_row<S>(v_tile, row, vw, vs, v_ref, hidden || nan);
+            fence_async_shared();
+            bar_arrive(v_full);
+            // the next step's elements are on their way while this one's are multiplied, its pages a step earlier
+            advance(c);
+            page = next_page;
+            if (j + 1 < count) load(c, page);
+            if (j + 2 < count) {
+                advance(ahead);
+                next_page = find_page(ahead);
+            }
+        }
+    } else {
+        // ---- rows: a thread has one ----
+        const uint32_t row = threadIdx.x, lanes = (warp * 32) << 16;
+        unsigned long long item_from = s_item_from;
+        float factor = 0.0f, top = -INFINITY, sum = 0.0f;
+        int lo = 0, hi = 0x7FFFFFFF, lo_most = 0, hi_least = 0;
+        uint32_t col = 0, v_ref = 0;
+        bool fresh = true, goes_on = false;
+        for (uint32_t j = 0; j < count; ++j) {
+            const uint32_t par = j & 1;
+            if (fresh) {
+                col = c.tile * 128 + row;
+                const uint32_t cols = (uint32_t)c.n * P.group;
+                int skip;
+                lo = 0;
+                hi = 0x7FFFFFFF;
+                if (col < cols) c.limits(P, (int)(col / P.group), lo, hi);
+                c.limits(P, (int)((min(cols, c.tile * 128 + 128) - 1) / P.group), lo_most, skip);
+                c.limits(P, (int)(c.tile * 128 / P.group), skip, hi_least);
+                hi_least = min(hi_least, c.len);
+                // the query over a power of two, in FP16; twice read, the second time out of the L1
+                const uint8_t* q = P.q.d + (uint64_t)(c.row0 + col / P.group) * P.q.ld_row + (uint64_t)(c.head * P.group + col % P.group) * P.q.ld_head;
+                float most = 0.0f;
+                if (col < cols)
+                    for (uint32_t k = 0; k < S::kDim / 4; ++k) {
+                        const uint2 w = query_four(P, q + 8 * k);
+                        const float2 a = query_pair(P, w.x), b = query_pair(P, w.y);
+                        most = fmaxf(fmaxf(most, fmaxf(fabsf(a.x), fabsf(a.y))), fmaxf(fabsf(b.x), fabsf(b.y)));
+                    }
+                const int up = query_lift(most);
+                const float lift = copysignf(power_of_two(up), P.scale_log2);
+                for (uint32_t k = 0; k < S::kDim / 8; ++k) {
+                    uint32_t h[4] = {};
+                    if (col < cols) {
+                        const uint2 w0 = query_four(P, q + 16 * k), w1 = query_four(P, q + 16 * k + 8);
+                        const float2 a = query_pair(P, w0.x), b = query_pair(P, w0.y), d = query_pair(P, w1.x), e = query_pair(P, w1.y);
+                        h[0] = pack_half(a.x * lift, a.y * lift);
+                        h[1] = pack_half(b.x * lift, b.y * lift);
+                        h[2] = pack_half(d.x * lift, d.y * lift);
+                        h[3] = pack_half(e.x * lift, e.y * lift);
+                    }
+                    sts128(q_tile + tile_at(row, k), h);
+                }
+                factor = ldexpf(fabsf(P.scale_log2), -up);
+                fence_async_shared();
+                bar_arrive(q_full);
+                top = -INFINITY;
+                sum = 0.0f;
+            }
+            if (!wait.warp(s_full, par)) break;
+            tc_fence_after();
+            const int t0 = (int)((c.first_step + c.step) * 128);
+            const uint32_t k_ref = s_ref[par][0], new_ref = s_ref[par][1];
+            const bool plain = t0 >= lo_most && t0 + 128 <= hi_least && (s_gone[par][0] | s_gone[par][1] | s_gone[par][2] | s_gone[par][3]) == 0;
+            // above 0, that the largest product is the largest logit and -infinity stays
+            const float f = fmaxf(factor * ldexpf(1.0f, (int)k_ref - 127 - S::kLift), 1.17549435e-38f);
+            const uint32_t s_at = tmem + S::kS + lanes;
+            auto hide = [&](float* v, uint32_t chunk) {
+                const uint32_t gone = s_gone[par][chunk], poisoned = s_poisoned[par][chunk];
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    const int t = t0 + (int)chunk * 32 + k;
+                    if ((poisoned >> k) & 1) v[k] = __int_as_float(0x7FFFFFFF);
+                    if (t < lo || t >= hi || t >= c.len || ((gone >> k) & 1)) v[k] = -INFINITY;
+                }
+            };
+            float best = -INFINITY;
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) {
+                float v[32];
+                tmem_ld32_async(s_at + 32 * k, v);
+                tmem_ld_wait();
+                if (!plain) hide(v, k);
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) best = fmaxf(best, fmaxf(v[i], v[i + 1]));
+            }
+            best *= f;
+            // the sums in tensor memory are over 2^top of the weights and 2^v_ref of the values
+            float shrink = 1.0f;
+            if (best > top + 1.0f) {
+                shrink = exp2_fast(top - best);
+                top = best;
+            }
+            sum *= shrink;
+            if (!fresh && new_ref != v_ref) shrink *= ldexpf(1.0f, max((int)v_ref - (int)new_ref, -200));
+            if (!fresh && __any_sync(kAll, shrink != 1.0f)) {
+#pragma unroll 1
+                for (uint32_t k = 0; k < S::kDim / 32; ++k) {
+                    float v[32];
+                    tmem_ld32_async(tmem + S::kO + lanes + 32 * k, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] *= shrink;
+                    tmem_st32(tmem + S::kO + lanes + 32 * k, v);
+                }
+            }
+            v_ref = new_ref;
+            fresh = false;
+            const float off = top == -INFINITY ? 14.0f : 14.0f - top;
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) {
+                float v[32];
+                uint32_t h[16];
+                tmem_ld32_async(s_at + 32 * k, v);
+                tmem_ld_wait();
+                if (!plain) hide(v, k);
+                float more[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float a = exp2_fast(fmaf(v[2 * i], f, off)), b = exp2_fast(fmaf(v[2 * i + 1], f, off));
+                    more[0] += a;
+                    more[1] += b;
+                    h[i] = pack_half(a, b);
+                }
+                sum += more[0] + more[1];
+                tmem_st16(s_at + 16 * k, h);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            bar_arrive(p_full);
+
+            const bool item_ends = c.step + 1 == c.steps;
+            if (item_ends || j + 1 == count) {
+                if (!wait.warp(o_full, par)) break;
+                tc_fence_after();
+                const unsigned long long item_to = item_from + c.steps;
+                const bool begins = item_from >= from, whole = begins && item_to <= to;
+                const float weight = sum * (1.0f / 16384.0f);
+                const float unit = e8m0_value(v_ref), norm = whole ? (weight == 0.0f ? 0.0f : 1.0f / weight) : 1.0f;
+                constexpr float kDown = 1.0f / 16384.0f / (float)(1u << S::kLift);
+                const bool mine = col < (uint32_t)c.n * P.group;
+                const uint32_t head = c.head * P.group + col % P.group;
+                const uint64_t out_row = (uint64_t)c.row0 + col / P.group;
+                uint8_t* out = P.out.d + out_row * P.out.ld_row + head * P.out.ld_head;
+                float* part = partial_of<S>(P, gridDim.x, blockIdx.x, begins ? 1 : 0);
+#pragma unroll 1
+                for (uint32_t k = 0; k < S::kDim / 32; ++k) {
+                    float v[32];
+                    tmem_ld32_async(tmem + S::kO + lanes + 32 * k, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = v[i] * kDown * unit * norm;
+                    if (!mine) continue;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        if (whole) store_out<4>(P, out, 32 * k + i, v + i);
+                        else *reinterpret_cast<float4*>(part + row * S::kDim + 32 * k + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    }
+                }
+                if (mine && whole && P.lse) P.lse[out_row * P.q_heads + head] = lse_of(top, weight);
+                if (!whole) {
+                    part[S::kCols * S::kDim + row] = top;
+                    part[S::kCols * S::kDim + S::kCols + row] = weight;
+                    if (begins) {
+                        goes_on = true;
+                        if (row == 0) *ends = BlockEnd{item_to, total, c.columns(P), 1, {}};
+                    }
+                }
+                tc_fence_before();                         // read before the next item's products
+                item_from = item_to;
+            }
+            if (++c.step == c.steps) {
+                c.next_item(P);
+                fresh = true;
+            }
+        }
+        if (row == 0 && !goes_on) ends->there = 0;
+    }
+    __syncthreads();
+    if (warp == 8) {
+        // products under way end, or are waited for as long as anything else, before the block and its memories are given back
+        if (s_failed) {
+            if (issued) settled(s_full, (issued - 1) & 1, P.spin_limit);
+            if (issued2) settled(o_full, (issued2 - 1) & 1, P.spin_limit);
+            if (lane == 0) {
+                atomicOr(P.B.marks, kKvGaveUp);
+                ends->there = 0;
+            }
+        }
+        tc_fence_after();
+        tmem_free<1>(tmem, S::kTmem);
+    }
+}
+
+}  // namespace zc

@@ -192,15 +192,22 @@ __device__ __forceinline__ void join_parts(uint32_t count, PART part, uint32_t s
 #pragma unroll
         for (uint32_t n = 0; n < N; ++n) v[n] *= old;
         const uint32_t some = min(32u, count - k0);
-#pragma unroll 8
-        for (uint32_t k = 0; k < some; ++k) {
-            const float* p = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(mine), k)) + sums + lane * N;
-            const float f = __shfl_sync(0xFFFFFFFFu, now, k);
-            float x[N];
-            if (N == 4) { const float4 y = *reinterpret_cast<const float4*>(p); x[0] = y.x; x[1] = y.y; x[N - 2] = y.z; x[N - 1] = y.w; }
-            else { const float2 y = *reinterpret_cast<const float2*>(p); x[0] = y.x; x[1] = y.y; }
+        constexpr uint32_t kAtOnce = 16;                       // reads under way
+        for (uint32_t k1 = 0; k1 < some; k1 += kAtOnce) {
+            float x[kAtOnce][N];
 #pragma unroll
-            for (uint32_t n = 0; n < N; ++n) v[n] = fmaf(x[n], f, v[n]);
+            for (uint32_t k = 0; k < kAtOnce; ++k) {
+                const float* p = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(mine), min(k1 + k, some - 1))) + sums + lane * N;
+                if (N == 4) { const float4 y = *reinterpret_cast<const float4*>(p); x[k][0] = y.x; x[k][1] = y.y; x[k][N - 2] = y.z; x[k][N - 1] = y.w; }
+                else { const float2 y = *reinterpret_cast<const float2*>(p); x[k][0] = y.x; x[k][1] = y.y; }
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < kAtOnce; ++k) {
+                const float f = __shfl_sync(0xFFFFFFFFu, now, (k1 + k) & 31);
+                if (k1 + k < some)
+#pragma unroll
+                    for (uint32_t n = 0; n < N; ++n) v[n] = fmaf(x[k][n], f, v[n]);
+            }
         }
     }
 }
@@ -771,17 +778,18 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
     if (!goes_on && threadIdx.x == 0) ends->there = 0;
 }
 
-// The items that go on from one block to the next: a block for each block that an item begins and does not end in, a warp for each column.
+// The items that go on from one block to the next: a block for each eight columns of the item that begins and does not end in a block, a warp a column.
 template <typename S>
-__global__ void __launch_bounds__(S::kCols * 32) kv_join_kernel(const AttentionParams P, uint32_t blocks)
+__global__ void __launch_bounds__(256) kv_join_kernel(const AttentionParams P, uint32_t blocks)
 {
     grid_wait();
     grid_launch_dependents();
     const BlockEnd end = reinterpret_cast<const BlockEnd*>(P.workspace)[blockIdx.x];
-    const uint32_t lane = threadIdx.x & 31, in_tile = threadIdx.x >> 5;
+    const uint32_t lane = threadIdx.x & 31, in_tile = blockIdx.y * 8 + (threadIdx.x >> 5);
     if (!end.there || in_tile >= end.columns.count) return;
     // up to the last block whose steps begin before the item's end; with fewer steps than blocks some have none, and no part
-    const uint32_t last = (uint32_t)((end.to * blocks - 1) / end.total);
+    const unsigned long long all = end.to * blocks - 1;
+    const uint32_t last = all >> 32 ? (uint32_t)(all / end.total) : (uint32_t)all / (uint32_t)end.total;
     const bool gaps = end.total < blocks;
     const uint32_t count = gaps ? (uint32_t)(end.to - share(end.total, blockIdx.x, blocks)) : last - blockIdx.x + 1;
     auto part = [&](uint32_t k) -> const float* {
