@@ -71,8 +71,7 @@ static cudaError_t launch_prompt(const AttentionParams& P, uint32_t blocks, cuda
 {
     static OncePerDevice ready;
     if (!ready([]() -> uint32_t {
-            return cudaFuncSetAttribute(kv_prompt_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem) == cudaSuccess &&
-                   cudaFuncSetAttribute(kv_prompt_kernel<S>, cudaFuncAttributePreferredSharedMemoryCarveout, 100) == cudaSuccess; })) return cudaErrorUnknown;
+            return cudaFuncSetAttribute(kv_prompt_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem) == cudaSuccess; })) return cudaErrorUnknown;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute at[1] = {launch_early()};
     cfg.gridDim = dim3(blocks);
@@ -86,7 +85,7 @@ static cudaError_t launch_prompt(const AttentionParams& P, uint32_t blocks, cuda
 }
 
 // Columns (rows times heads that share a head of the cache) up to which a sequence goes to the kernel of few rows.
-constexpr uint32_t kFewColumns = 16;
+constexpr uint32_t kFewColumns = 32;
 
 }  // namespace zc
 
@@ -102,7 +101,7 @@ size_t zc_kv_attention_workspace_bytes(const zc_kv_cache* cache, const zc_kv_bat
     size_t bytes = wide ? std::max(stream_workspace<StreamShape<true, 128, 1>>(n), stream_workspace<StreamShape<true, 128, 2>>(n))
                         : std::max(stream_workspace<StreamShape<true, 64, 1>>(n), stream_workspace<StreamShape<true, 64, 2>>(n));
     if ((uint64_t)(q_heads / cache->kv_heads) * std::max(1u, batch->max_new) > kFewColumns)
-        bytes = std::max(bytes, wide ? workspace_of<PromptShape<true, 128>>(2 * n, 0) : workspace_of<PromptShape<true, 64>>(2 * n, 0));
+        bytes = std::max(bytes, wide ? workspace_of<PromptShape<true, 128>>(n, 0) : workspace_of<PromptShape<true, 64>>(n, 0));
     return bytes;
 }
 
@@ -159,7 +158,7 @@ zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, co
         if (columns <= kFewColumns) return launch_stream<Two>(P, maps[0], maps[1], blocks, st);
         // a sequence alone has the rows that are expected; of several some may have few
         if (batch->n_seqs > 1) P.most_rows = kFewColumns / P.group;
-        if (const cudaError_t e = launch_prompt<Many>(P, Many::kBlocksPerSm * blocks, st)) return e;
+        if (const cudaError_t e = launch_prompt<Many>(P, blocks, st)) return e;
         return batch->n_seqs > 1 && P.most_rows ? launch_stream<Two>(P, maps[0], maps[1], blocks, st) : cudaSuccess;
     };
     auto dims = [&](auto fp4) {

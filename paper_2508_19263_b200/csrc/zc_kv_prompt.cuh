@@ -1,14 +1,14 @@
 // Attention of many rows over a cache: the tensor cores and the exponentials bound it.
 //
-// Columns of a sequence and a head (rows times the query heads that share it) are cut into tiles of 128, the rows of one matrix instruction; a tile
-// with a head is an item, a step is 128 tokens of an item.  As in the other kernel all steps in order are cut into equal runs, here one for each of
-// two blocks an SM, and parts of items are joined by a second kernel.  Two blocks an SM because a block goes through product, softmax and product
-// one after the other: while one is at its softmax the other's products have the tensor cores.
+// Columns of a sequence and a head (rows times the query heads that share it) are cut into tiles of 256, two matrix instructions' rows; a tile
+// with a head is an item, a step is 128 tokens of an item.  As in the other kernel all steps in order are cut into equal runs, here one for each block
+// (a block an SM), and parts of items are joined by a second kernel.
 //
-// Roles: four warps have a row a thread (maxima, exponentials, sums, the weights into tensor memory, results); four have a token a thread and write
-// keys and values as FP16 into shared memory; one issues the matrix instructions.
+// Roles: twice four warps have a row of a half of the tile a thread (maxima, exponentials, sums, the weights into tensor memory, results); four have a token a
+// thread and write keys and values as FP16 into shared memory, up to two steps ahead; one issues the matrix instructions.  The halves are half a step apart:
+// while one is at its softmax the other's products have the tensor cores, and both use what the four warps have made of the cache.
 //   S = Q K^T: both operands in shared memory, 128-byte swizzle, the head's width fastest.  O += P V: P in tensor memory, in S's place; V as it is written,
-// the head's width fastest, which for this product is the outer axis.  S and O, FP32, are 256 of tensor memory's columns, half of them for each block.
+// the head's width fastest, which for this product is the outer axis.  S and O, FP32, of both halves are all of tensor memory's 512 columns (head_dim 128).
 //   Keys and values are element * 2^(s - R + kLift), R the largest scale byte that the item has met, for keys and for values: exact unless a scale is 2^-35 (E4M3:
 // 2^-22) of the largest, off by at most 2^-25 / 2^kLift of 2^R then.  Queries as in the other kernel.
 //   Weights are 2^(x - m + 14) with m at most 1 below the row's largest so far: so the sums in tensor memory are only touched when it grows by more than
@@ -21,13 +21,13 @@ namespace zc {
 template <bool FP4_, uint32_t DIM_>
 struct PromptShape {
     static constexpr bool kFp4 = FP4_;
-    static constexpr uint32_t kDim = DIM_, kCols = 128, kStep = 128;
+    static constexpr uint32_t kDim = DIM_, kCols = 256, kStep = 128;
     static constexpr uint32_t kRow = kFp4 ? kDim / 2 : kDim, kBlocks = kDim / kKvBlock;
     static constexpr int kLift = kFp4 ? 12 : 6;                              // 6 * 2^12 and 448 * 2^6 are FP16 numbers
-    static constexpr uint32_t kTile = 128 * kDim * 2;                        // Q, K, V: 128 rows of FP16, pieces of 64 of the head's width one after the other
-    static constexpr uint32_t kSmem = 3 * kTile + 1024;
-    static constexpr uint32_t kThreads = 288, kBlocksPerSm = 2;
-    static constexpr uint32_t kS = 0, kO = 128, kTmem = 256;                 // columns
+    static constexpr uint32_t kTile = 128 * kDim * 2;                        // 128 rows of FP16, pieces of 64 of the head's width one after the other
+    static constexpr uint32_t kSmem = 6 * kTile + 1024;                      // queries of both halves; keys and values of two steps
+    static constexpr uint32_t kThreads = 13 * 32;
+    static constexpr uint32_t kHalf = 256, kO = 128, kTmem = 512;            // columns: of a half S, then O
 };
 
 // Where a role is; the same in all of a block's threads.
@@ -35,10 +35,10 @@ struct PromptCursor : SeqRows {
     uint32_t b, tile, head, tiles, step, steps, first_step;
     __device__ __forceinline__ void tile_span(const AttentionParams& P, uint32_t t, uint32_t& first, uint32_t& count) const
     {
-        const uint32_t cols = (uint32_t)n * P.group, last = min(cols, (t + 1) * 128) - 1;
+        const uint32_t cols = (uint32_t)n * P.group, last = min(cols, (t + 1) * 256) - 1;
         int lo, hi, skip;
         limits(P, (int)(last / P.group), skip, hi);
-        limits(P, (int)(t * 128 / P.group), lo, skip);
+        limits(P, (int)(t * 256 / P.group), lo, skip);
         hi = min(max(hi, 0), len);
         first = (uint32_t)lo / 128;
         const uint32_t end = ((uint32_t)hi + 127) / 128;
@@ -48,7 +48,7 @@ struct PromptCursor : SeqRows {
     {
         b = b_;
         load(P, b);
-        tiles = (uint32_t)n > P.most_rows || P.most_rows == 0xFFFFFFFFu ? (uint32_t)(((unsigned long long)n * P.group + 127) / 128) : 0;
+        tiles = (uint32_t)n > P.most_rows || P.most_rows == 0xFFFFFFFFu ? (uint32_t)(((unsigned long long)n * P.group + 255) / 256) : 0;
     }
     __device__ __forceinline__ void next_item(const AttentionParams& P)
     {
@@ -64,7 +64,8 @@ struct PromptCursor : SeqRows {
         }
         tile_span(P, tile, first_step, steps);
     }
-    __device__ __forceinline__ ItemColumns columns(const AttentionParams& P) const { return ItemColumns{row0, head, tile * 128, min(128u, (uint32_t)n * P.group - tile * 128)}; }
+    __device__ __forceinline__ ItemColumns columns(const AttentionParams& P) const { return ItemColumns{row0, head, tile * 256, columns_left(P)}; }
+    __device__ __forceinline__ uint32_t columns_left(const AttentionParams& P) const { return min(256u, (uint32_t)n * P.group - tile * 256); }
 };
 
 __device__ __forceinline__ void mma_ss_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add)
@@ -150,38 +151,55 @@ __device__ __forceinline__ void write_row(uint32_t tile, uint32_t row, const uin
     }
 }
 
+// Two numbers at once.
+__device__ __forceinline__ void fma_pair(float& x, float& y, float m, float a)
+{
+    asm("{\n\t.reg .b64 v, w, z;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\tfma.rn.f32x2 v, v, w, z;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "+f"(x), "+f"(y) : "f"(m), "f"(a));
+}
+__device__ __forceinline__ void add_pair(float& x, float& y, float a, float b)
+{
+    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %3};\n\tadd.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void mul_pair(float& x, float& y, float m)
+{
+    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\tmul.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}" : "+f"(x), "+f"(y) : "f"(m));
+}
+
 template <typename S>
-__global__ void __launch_bounds__(S::kThreads, S::kBlocksPerSm) kv_prompt_kernel(const AttentionParams P)
+__global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const AttentionParams P)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ __align__(8) uint64_t s_bars[9];
+    __shared__ __align__(8) uint64_t s_bars[15];
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_failed;
     __shared__ unsigned long long s_total, s_item_from;
     __shared__ uint32_t s_start[4];                       // sequence, tile, head, step
-    __shared__ uint32_t s_most[2][2][4];                  // by step parity, keys and values, by warp: largest scale bytes
-    __shared__ uint32_t s_ref[2][2];                      // by step parity: what keys and values are over
-    __shared__ uint32_t s_gone[2][4], s_poisoned[2][4];   // by step parity: tokens without a page; with NaN in their values that not every row sees
+    // by step parity:
+    __shared__ uint32_t s_most[2][2][4];                  // largest scale bytes of keys and values, by warp
+    __shared__ uint32_t s_ref[2][2];                      // what keys and values are over
+    __shared__ uint32_t s_gone[2][4], s_poisoned[2][4];   // tokens without a page; with NaN in their values that not every row sees
     constexpr uint32_t kAll = 0xFFFFFFFFu;
     const uint32_t lane = threadIdx.x & 31, warp = warp_index();
-    const uint32_t base = (smem_u32(smem) + 1023) & ~1023u, q_tile = base, k_tile = base + S::kTile, v_tile = base + 2 * S::kTile;
+    const uint32_t base = (smem_u32(smem) + 1023) & ~1023u, q_tile = base, k_tile = base + 2 * S::kTile, v_tile = base + 4 * S::kTile;
     const uint32_t bars = smem_u32(s_bars);
-    // queries written; keys written (m_full: largest scales known); product done (softmax, keys free); values written; weights written; second product done
-    const uint32_t q_full = bars, k_full = bars + 8, s_full = bars + 16, v_full = bars + 24, p_full = bars + 32, o_full = bars + 40, k_free = bars + 48, v_free = bars + 56, m_full = bars + 64;
+    // of each half: queries written; first product done; weights written; second product done.  Of each step parity: keys written; values written; both used; scales known
+    const uint32_t q_full = bars, s_full = bars + 16, p_full = bars + 32, o_full = bars + 48, k_full = bars + 64, v_full = bars + 80, kv_free = bars + 96, m_full = bars + 112;
     if (threadIdx.x == 0) {
         s_failed = 0;
-        bar_init(q_full, 128);
-        bar_init(k_full, 128);
-        bar_init(s_full, 1);
-        bar_init(v_full, 128);
-        bar_init(p_full, 128);
-        bar_init(o_full, 1);
-        bar_init(k_free, 1);
-        bar_init(v_free, 1);
+        for (uint32_t x = 0; x < 2; ++x) {
+            bar_init(q_full + 8 * x, 128);
+            bar_init(s_full + 8 * x, 1);
+            bar_init(p_full + 8 * x, 128);
+            bar_init(o_full + 8 * x, 1);
+            bar_init(k_full + 8 * x, 128);
+            bar_init(v_full + 8 * x, 128);
+            bar_init(kv_free + 8 * x, 1);
+        }
         bar_init(m_full, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8) tmem_alloc<1>(smem_u32(&s_tmem), S::kTmem);
+    if (warp == 12) tmem_alloc<1>(smem_u32(&s_tmem), S::kTmem);
     grid_wait();
     grid_launch_dependents();
 
@@ -249,53 +267,70 @@ __global__ void __launch_bounds__(S::kThreads, S::kBlocksPerSm) kv_prompt_kernel
         c.tile_span(P, c.tile, c.first_step, c.steps);
     }
     BlockEnd* ends = reinterpret_cast<BlockEnd*>(P.workspace) + blockIdx.x;
-    uint32_t issued = 0;                                   // of the issuing warp: steps whose first, and second, product were issued
-    uint32_t issued2 = 0;
+    uint32_t first_done[2] = {}, second_done[2] = {};      // of the issuing warp: products issued, of each half
 
-    if (warp == 8) {
+    if (warp == 12) {
         // ---- matrix instructions ----
         const uint32_t qk = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);                               // FP16 operands, FP32 sums
         const uint32_t pv = (1u << 4) | (1u << 16) | ((S::kDim >> 3) << 17) | ((128u >> 4) << 24);               // the second operand by its outer axis
-        uint32_t items = 0;
-        bool fresh = true;
-        for (uint32_t j = 0; j < count; ++j) {
-            if (fresh && !wait.warp(q_full, items & 1)) break;
-            if (!wait.warp(k_full, j & 1)) break;
-            // the product goes where the last step's weights are
-            if (j && !wait.warp(o_full, (j - 1) & 1)) break;
+        uint32_t items[2] = {};
+        // a half's first product for step j; `fresh`: of a new item
+        auto first = [&](uint32_t x, uint32_t j, bool fresh) -> bool {
+            if (fresh && !wait.warp(q_full + 8 * x, items[x]++ & 1)) return false;
+            if (!wait.warp(k_full + 8 * (j & 1), (j >> 1) & 1)) return false;
             tc_fence_after();
-            if (P.skip_math) { wait.give_up(); break; }
+            if (P.skip_math) { wait.give_up(); return false; }
             if (elect_one()) {
 #pragma unroll
                 for (uint32_t k = 0; k < S::kDim / 16; ++k) {
                     const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
-                    mma_ss_f16(tmem + S::kS, operand_desc(q_tile + off), operand_desc(k_tile + off), qk, k != 0);
+                    mma_ss_f16(tmem + x * S::kHalf, operand_desc(q_tile + x * S::kTile + off), operand_desc(k_tile + (j & 1) * S::kTile + off), qk, k != 0);
                 }
-                mma_commit<1>(s_full);
-                mma_commit<1>(k_free);
+                mma_commit<1>(s_full + 8 * x);
             }
             __syncwarp();
-            ++issued;
-            if (!wait.warp(v_full, j & 1) || !wait.warp(p_full, j & 1)) break;
-            tc_fence_after();
-            if (elect_one()) {
-#pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) mma_ts_f16(tmem + S::kO, tmem + S::kS + 8 * k, outer_desc(v_tile + k * 2048), pv, !(fresh && k == 0));
-                mma_commit<1>(o_full);
-                mma_commit<1>(v_free);
-            }
-            __syncwarp();
-            ++issued2;
-            fresh = false;
-            if (++c.step == c.steps) {
-                c.next_item(P);
-                fresh = true;
-                ++items;
-            }
+            ++first_done[x];
+            return true;
+        };
+        uint32_t halves = 0;
+        bool ok = true, fresh = true;
+        if (count) {
+            halves = c.columns_left(P) > 128 ? 2 : 1;
+            for (uint32_t x = 0; x < halves && ok; ++x) ok = first(x, 0, true);
         }
-    } else if (warp >= 4) {
+        for (uint32_t j = 0; j < count && ok; ++j) {
+            PromptCursor n = c;
+            const bool item_ends = c.step + 1 == c.steps;
+            if (item_ends) n.next_item(P);
+            else ++n.step;
+            const uint32_t next_halves = item_ends && j + 1 < count ? (n.columns_left(P) > 128 ? 2 : 1) : halves;
+            for (uint32_t x = 0; x < 2 && ok; ++x) {
+                if (x < halves) {
+                    if (!wait.warp(v_full + 8 * (j & 1), (j >> 1) & 1) || !wait.warp(p_full + 8 * x, second_done[x] & 1)) { ok = false; break; }
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (uint32_t k = 0; k < 8; ++k)
+                            mma_ts_f16(tmem + x * S::kHalf + S::kO, tmem + x * S::kHalf + 8 * k, outer_desc(v_tile + (j & 1) * S::kTile + k * 2048), pv, !(fresh && k == 0));
+                        mma_commit<1>(o_full + 8 * x);
+                        if (x + 1 == halves) mma_commit<1>(kv_free + 8 * (j & 1));
+                    }
+                    __syncwarp();
+                    ++second_done[x];
+                }
+                if (j + 1 < count && x < next_halves) {
+                    // the product goes where the last step's weights are
+                    if (second_done[x] && !wait.warp(o_full + 8 * x, (second_done[x] - 1) & 1)) { ok = false; break; }
+                    ok = first(x, j + 1, item_ends);
+                }
+            }
+            halves = next_halves;
+            fresh = item_ends;
+            c = n;
+        }
+    } else if (warp >= 8) {
         // ---- keys and values: a thread has a token ----
-        const uint32_t row = threadIdx.x - 128, group = row >> 5;
+        const uint32_t row = threadIdx.x - 256, group = row >> 5;
         PromptCursor ahead = c;
         constexpr uint32_t kWords = S::kRow / 16;
         uint4 kw[kWords], vw[kWords];
@@ -304,9 +339,8 @@ __global__ void __launch_bounds__(S::kThreads, S::kBlocksPerSm) kv_prompt_kernel
         auto find_page = [&](const PromptCursor& a) -> int {
             const uint32_t t = (a.first_step + a.step) * 128 + row;
             int lo, hi, skip;
-            const uint32_t cols = (uint32_t)a.n * P.group;
-            a.limits(P, (int)(a.tile * 128 / P.group), lo, skip);
-            a.limits(P, (int)((min(cols, a.tile * 128 + 128) - 1) / P.group), skip, hi);
+            a.limits(P, (int)(a.tile * 256 / P.group), lo, skip);
+            a.limits(P, (int)((a.tile * 256 + a.columns_left(P) - 1) / P.group), skip, hi);
             return (int)t >= lo && (int)t < hi && t < (uint32_t)a.len ? kv_page(P.C, P.B, a.b, t >> P.C.page_shift) : -2;     // -2: nobody sees the token
         };
         auto load = [&](const PromptCursor& a, int pg) {
@@ -335,6 +369,8 @@ __global__ void __launch_bounds__(S::kThreads, S::kBlocksPerSm) kv_prompt_kernel
         }
         for (uint32_t j = 0; j < count; ++j) {
             const uint32_t par = j & 1;
+            // the step before the last is over: its keys, values, and what is said of them
+            if (j >= 2 && !wait.warp(kv_free + 8 * par, ((j >> 1) - 1) & 1)) break;
             if (j && c.step == 0) k_ref = v_ref = 0;
             const bool hidden = page < 0;
             // the largest scales
@@ -357,8 +393,8 @@ __global__ void __launch_bounds__(S::kThreads, S::kBlocksPerSm) kv_prompt_kernel
                 // NaN that every row of the tile sees goes through the product, else the rows that see it are told
                 const int t = (int)((c.first_step + c.step) * 128 + row);
                 int lo, hi, skip;
-                c.limits(P, (int)(c.tile * 128 / P.group), skip, hi);
-                c.limits(P, (int)((min((uint32_t)c.n * P.group, c.tile * 128 + 128) - 1) / P.group), lo, skip);
+                c.limits(P, (int)(c.tile * 256 / P.group), skip, hi);
+                c.limits(P, (int)((c.tile * 256 + c.columns_left(P) - 1) / P.group), lo, skip);
                 nan = t < lo || t >= hi;
             }
             km = __reduce_max_sync(kAll, km);
@@ -378,14 +414,12 @@ __global__ void __launch_bounds__(S::kThreads, S::kBlocksPerSm) kv_prompt_kernel
                 v_ref = max(v_ref, s_most[par][1][k]);
             }
             if (row == 0) { s_ref[par][0] = k_ref; s_ref[par][1] = v_ref; }
-            if (j && !wait.warp(k_free, (j - 1) & 1)) break;
-            write_row<S>(k_tile, row, kw, ks, k_ref, hidden);
+            write_row<S>(k_tile + par * S::kTile, row, kw, ks, k_ref, hidden);
             fence_async_shared();
-            bar_arrive(k_full);
-            if (j && !wait.warp(v_free, (j - 1) & 1)) break;
-            write_row<S>(v_tile, row, vw, vs, v_ref, hidden || nan);
+            bar_arrive(k_full + 8 * par);
+            write_row<S>(v_tile + par * S::kTile, row, vw, vs, v_ref, hidden || nan);
             fence_async_shared();
-            bar_arrive(v_full);
+            bar_arrive(v_full + 8 * par);
             // the next step's elements are on their way while this one's are multiplied, its pages a step earlier
             advance(c);
             page = next_page;
@@ -396,179 +430,183 @@ __global__ void __launch_bounds__(S::kThreads, S::kBlocksPerSm) kv_prompt_kernel
             }
         }
     } else {
-        // ---- rows: a thread has one ----
-        const uint32_t row = threadIdx.x, lanes = (warp * 32) << 16;
+        // ---- rows of a half: a thread has one ----
+        const uint32_t half = warp >> 2, row = threadIdx.x & 127, at = tmem + half * S::kHalf + (((warp & 3) * 32) << 16);
+        const uint32_t my_s = s_full + 8 * half, my_p = p_full + 8 * half, my_o = o_full + 8 * half;
         unsigned long long item_from = s_item_from;
         float factor = 0.0f, top = -INFINITY, sum = 0.0f;
         int lo = 0, hi = 0x7FFFFFFF, lo_most = 0, hi_least = 0;
-        uint32_t col = 0, v_ref = 0;
+        uint32_t col = 0, v_ref = 0, turns = 0;               // turns: steps in which the half had rows
         bool fresh = true, goes_on = false;
         for (uint32_t j = 0; j < count; ++j) {
-            const uint32_t par = j & 1;
-            if (fresh) {
-                col = c.tile * 128 + row;
-                const uint32_t cols = (uint32_t)c.n * P.group;
-                int skip;
-                lo = 0;
-                hi = 0x7FFFFFFF;
-                if (col < cols) c.limits(P, (int)(col / P.group), lo, hi);
-                c.limits(P, (int)((min(cols, c.tile * 128 + 128) - 1) / P.group), lo_most, skip);
-                c.limits(P, (int)(c.tile * 128 / P.group), skip, hi_least);
-                hi_least = min(hi_least, c.len);
-                // the query over a power of two, in FP16; twice read, the second time out of the L1
-                const uint8_t* q = P.q.d + (uint64_t)(c.row0 + col / P.group) * P.q.ld_row + (uint64_t)(c.head * P.group + col % P.group) * P.q.ld_head;
-                float most = 0.0f;
-                if (col < cols)
-                    for (uint32_t k = 0; k < S::kDim / 4; ++k) {
-                        const uint2 w = query_four(P, q + 8 * k);
-                        const float2 a = query_pair(P, w.x), b = query_pair(P, w.y);
-                        most = fmaxf(fmaxf(most, fmaxf(fabsf(a.x), fabsf(a.y))), fmaxf(fabsf(b.x), fabsf(b.y)));
+            const uint32_t par = j & 1, cols = (uint32_t)c.n * P.group, first_col = c.tile * 256 + half * 128;
+            const bool item_ends = c.step + 1 == c.steps, active = first_col < cols;
+            if (active) {
+                if (fresh) {
+                    col = first_col + row;
+                    int skip;
+                    lo = 0;
+                    hi = 0x7FFFFFFF;
+                    if (col < cols) c.limits(P, (int)(col / P.group), lo, hi);
+                    c.limits(P, (int)((min(cols, first_col + 128) - 1) / P.group), lo_most, skip);
+                    c.limits(P, (int)(first_col / P.group), skip, hi_least);
+                    hi_least = min(hi_least, c.len);
+                    // the query over a power of two, in FP16; twice read, the second time out of the L1
+                    const uint8_t* q = P.q.d + (uint64_t)(c.row0 + col / P.group) * P.q.ld_row + (uint64_t)(c.head * P.group + col % P.group) * P.q.ld_head;
+                    float most = 0.0f;
+                    if (col < cols)
+                        for (uint32_t k = 0; k < S::kDim / 4; ++k) {
+                            const uint2 w = query_four(P, q + 8 * k);
+                            const float2 a = query_pair(P, w.x), b = query_pair(P, w.y);
+                            most = fmaxf(fmaxf(most, fmaxf(fabsf(a.x), fabsf(a.y))), fmaxf(fabsf(b.x), fabsf(b.y)));
+                        }
+                    const int up = query_lift(most);
+                    const float lift = copysignf(power_of_two(up), P.scale_log2);
+                    for (uint32_t k = 0; k < S::kDim / 8; ++k) {
+                        uint32_t h[4] = {};
+                        if (col < cols) {
+                            const uint2 w0 = query_four(P, q + 16 * k), w1 = query_four(P, q + 16 * k + 8);
+                            const float2 a = query_pair(P, w0.x), b = query_pair(P, w0.y), d = query_pair(P, w1.x), e = query_pair(P, w1.y);
+                            h[0] = pack_half(a.x * lift, a.y * lift);
+                            h[1] = pack_half(b.x * lift, b.y * lift);
+                            h[2] = pack_half(d.x * lift, d.y * lift);
+                            h[3] = pack_half(e.x * lift, e.y * lift);
+                        }
+                        sts128(q_tile + half * S::kTile + tile_at(row, k), h);
                     }
-                const int up = query_lift(most);
-                const float lift = copysignf(power_of_two(up), P.scale_log2);
-                for (uint32_t k = 0; k < S::kDim / 8; ++k) {
-                    uint32_t h[4] = {};
-                    if (col < cols) {
-                        const uint2 w0 = query_four(P, q + 16 * k), w1 = query_four(P, q + 16 * k + 8);
-                        const float2 a = query_pair(P, w0.x), b = query_pair(P, w0.y), d = query_pair(P, w1.x), e = query_pair(P, w1.y);
-                        h[0] = pack_half(a.x * lift, a.y * lift);
-                        h[1] = pack_half(b.x * lift, b.y * lift);
-                        h[2] = pack_half(d.x * lift, d.y * lift);
-                        h[3] = pack_half(e.x * lift, e.y * lift);
+                    factor = ldexpf(fabsf(P.scale_log2), -up);
+                    fence_async_shared();
+                    bar_arrive(q_full + 8 * half);
+                    top = -INFINITY;
+                    sum = 0.0f;
+                }
+                if (!wait.warp(my_s, turns & 1)) break;
+                tc_fence_after();
+                const int t0 = (int)((c.first_step + c.step) * 128);
+                const uint32_t k_ref = s_ref[par][0], new_ref = s_ref[par][1];
+                const bool plain = t0 >= lo_most && t0 + 128 <= hi_least && (s_gone[par][0] | s_gone[par][1] | s_gone[par][2] | s_gone[par][3]) == 0 &&
+                                   (s_poisoned[par][0] | s_poisoned[par][1] | s_poisoned[par][2] | s_poisoned[par][3]) == 0;
+                // above 0, that the largest product is the largest logit and -infinity stays
+                const float f = fmaxf(factor * ldexpf(1.0f, (int)k_ref - 127 - S::kLift), 1.17549435e-38f);
+                auto hide = [&](float* v, uint32_t chunk) {
+                    const uint32_t gone = s_gone[par][chunk], poisoned = s_poisoned[par][chunk];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        const int t = t0 + (int)chunk * 32 + k;
+                        if ((poisoned >> k) & 1) v[k] = __int_as_float(0x7FFFFFFF);
+                        if (t < lo || t >= hi || t >= c.len || ((gone >> k) & 1)) v[k] = -INFINITY;
                     }
-                    sts128(q_tile + tile_at(row, k), h);
-                }
-                factor = ldexpf(fabsf(P.scale_log2), -up);
-                fence_async_shared();
-                bar_arrive(q_full);
-                top = -INFINITY;
-                sum = 0.0f;
-            }
-            if (!wait.warp(s_full, par)) break;
-            tc_fence_after();
-            const int t0 = (int)((c.first_step + c.step) * 128);
-            const uint32_t k_ref = s_ref[par][0], new_ref = s_ref[par][1];
-            const bool plain = t0 >= lo_most && t0 + 128 <= hi_least && (s_gone[par][0] | s_gone[par][1] | s_gone[par][2] | s_gone[par][3]) == 0;
-            // above 0, that the largest product is the largest logit and -infinity stays
-            const float f = fmaxf(factor * ldexpf(1.0f, (int)k_ref - 127 - S::kLift), 1.17549435e-38f);
-            const uint32_t s_at = tmem + S::kS + lanes;
-            auto hide = [&](float* v, uint32_t chunk) {
-                const uint32_t gone = s_gone[par][chunk], poisoned = s_poisoned[par][chunk];
-#pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    const int t = t0 + (int)chunk * 32 + k;
-                    if ((poisoned >> k) & 1) v[k] = __int_as_float(0x7FFFFFFF);
-                    if (t < lo || t >= hi || t >= c.len || ((gone >> k) & 1)) v[k] = -INFINITY;
-                }
-            };
-            float best = -INFINITY;
-#pragma unroll
-            for (uint32_t k = 0; k < 4; ++k) {
-                float v[32];
-                tmem_ld32_async(s_at + 32 * k, v);
-                tmem_ld_wait();
-                if (!plain) hide(v, k);
-#pragma unroll
-                for (int i = 0; i < 32; i += 2) best = fmaxf(best, fmaxf(v[i], v[i + 1]));
-            }
-            best *= f;
-            // the sums in tensor memory are over 2^top of the weights and 2^v_ref of the values
-            float shrink = 1.0f;
-            if (best > top + 1.0f) {
-                shrink = exp2_fast(top - best);
-                top = best;
-            }
-            sum *= shrink;
-            if (!fresh && new_ref != v_ref) shrink *= ldexpf(1.0f, max((int)v_ref - (int)new_ref, -200));
-            if (!fresh && __any_sync(kAll, shrink != 1.0f)) {
+                };
+                float best = -INFINITY;
 #pragma unroll 1
-                for (uint32_t k = 0; k < S::kDim / 32; ++k) {
+                for (uint32_t k = 0; k < 4; ++k) {
                     float v[32];
-                    tmem_ld32_async(tmem + S::kO + lanes + 32 * k, v);
+                    tmem_ld32_async(at + 32 * k, v);
                     tmem_ld_wait();
+                    if (!plain) hide(v, k);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] *= shrink;
-                    tmem_st32(tmem + S::kO + lanes + 32 * k, v);
+                    for (int i = 0; i < 32; i += 2) best = fmaxf(best, fmaxf(v[i], v[i + 1]));
                 }
-            }
-            v_ref = new_ref;
-            fresh = false;
-            const float off = top == -INFINITY ? 14.0f : 14.0f - top;
+                best *= f;
+                // the sums in tensor memory are over 2^top of the weights and 2^v_ref of the values
+                float shrink = 1.0f;
+                if (best > top + 1.0f) {
+                    shrink = exp2_fast(top - best);
+                    top = best;
+                }
+                sum *= shrink;
+                if (!fresh && new_ref != v_ref) shrink *= ldexpf(1.0f, max((int)v_ref - (int)new_ref, -200));
+                if (!fresh && __any_sync(kAll, shrink != 1.0f)) {
+#pragma unroll 1
+                    for (uint32_t k = 0; k < S::kDim / 32; ++k) {
+                        float v[32];
+                        tmem_ld32_async(at + S::kO + 32 * k, v);
+                        tmem_ld_wait();
 #pragma unroll
-            for (uint32_t k = 0; k < 4; ++k) {
-                float v[32];
-                uint32_t h[16];
-                tmem_ld32_async(s_at + 32 * k, v);
-                tmem_ld_wait();
-                if (!plain) hide(v, k);
+                        for (int i = 0; i < 32; i += 2) mul_pair(v[i], v[i + 1], shrink);
+                        tmem_st32(at + S::kO + 32 * k, v);
+                    }
+                }
+                v_ref = new_ref;
+                const float off = top == -INFINITY ? 14.0f : 14.0f - top;
                 float more[2] = {0.0f, 0.0f};
+#pragma unroll 1
+                for (uint32_t k = 0; k < 4; ++k) {
+                    float v[32];
+                    uint32_t h[16];
+                    tmem_ld32_async(at + 32 * k, v);
+                    tmem_ld_wait();
+                    if (!plain) hide(v, k);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float a = exp2_fast(fmaf(v[2 * i], f, off)), b = exp2_fast(fmaf(v[2 * i + 1], f, off));
-                    more[0] += a;
-                    more[1] += b;
-                    h[i] = pack_half(a, b);
+                    for (int i = 0; i < 16; ++i) {
+                        fma_pair(v[2 * i], v[2 * i + 1], f, off);
+                        v[2 * i] = exp2_fast(v[2 * i]);
+                        v[2 * i + 1] = exp2_fast(v[2 * i + 1]);
+                        add_pair(more[0], more[1], v[2 * i], v[2 * i + 1]);
+                        h[i] = pack_half(v[2 * i], v[2 * i + 1]);
+                    }
+                    tmem_st16(at + 16 * k, h);
                 }
                 sum += more[0] + more[1];
-                tmem_st16(s_at + 16 * k, h);
-            }
-            tmem_st_wait();
-            tc_fence_before();
-            bar_arrive(p_full);
-
-            const bool item_ends = c.step + 1 == c.steps;
-            if (item_ends || j + 1 == count) {
-                if (!wait.warp(o_full, par)) break;
-                tc_fence_after();
-                const unsigned long long item_to = item_from + c.steps;
-                const bool begins = item_from >= from, whole = begins && item_to <= to;
-                const float weight = sum * (1.0f / 16384.0f);
-                const float unit = e8m0_value(v_ref), norm = whole ? (weight == 0.0f ? 0.0f : 1.0f / weight) : 1.0f;
-                constexpr float kDown = 1.0f / 16384.0f / (float)(1u << S::kLift);
-                const bool mine = col < (uint32_t)c.n * P.group;
-                const uint32_t head = c.head * P.group + col % P.group;
-                const uint64_t out_row = (uint64_t)c.row0 + col / P.group;
-                uint8_t* out = P.out.d + out_row * P.out.ld_row + head * P.out.ld_head;
-                float* part = partial_of<S>(P, gridDim.x, blockIdx.x, begins ? 1 : 0);
+                tmem_st_wait();
+                tc_fence_before();
+                bar_arrive(my_p);
+                if (item_ends || j + 1 == count) {
+                    if (!wait.warp(my_o, turns & 1)) break;
+                    tc_fence_after();
+                    const unsigned long long item_to = item_from + c.steps;
+                    const bool begins = item_from >= from, whole = begins && item_to <= to;
+                    const float weight = sum * (1.0f / 16384.0f);
+                    const float unit = e8m0_value(v_ref), norm = whole ? (weight == 0.0f ? 0.0f : 1.0f / weight) : 1.0f;
+                    constexpr float kDown = 1.0f / 16384.0f / (float)(1u << S::kLift);
+                    const bool mine = col < cols;
+                    const uint32_t head = c.head * P.group + col % P.group;
+                    const uint64_t out_row = (uint64_t)c.row0 + col / P.group;
+                    uint8_t* out = P.out.d + out_row * P.out.ld_row + head * P.out.ld_head;
+                    float* part = partial_of<S>(P, gridDim.x, blockIdx.x, begins ? 1 : 0);
 #pragma unroll 1
-                for (uint32_t k = 0; k < S::kDim / 32; ++k) {
-                    float v[32];
-                    tmem_ld32_async(tmem + S::kO + lanes + 32 * k, v);
-                    tmem_ld_wait();
+                    for (uint32_t k = 0; k < S::kDim / 32; ++k) {
+                        float v[32];
+                        tmem_ld32_async(at + S::kO + 32 * k, v);
+                        tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = v[i] * kDown * unit * norm;
-                    if (!mine) continue;
+                        for (int i = 0; i < 32; ++i) v[i] = v[i] * kDown * unit * norm;
+                        if (!mine) continue;
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        if (whole) store_out<4>(P, out, 32 * k + i, v + i);
-                        else *reinterpret_cast<float4*>(part + row * S::kDim + 32 * k + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                        for (int i = 0; i < 32; i += 4) {
+                            if (whole) store_out<4>(P, out, 32 * k + i, v + i);
+                            else *reinterpret_cast<float4*>(part + (half * 128 + row) * S::kDim + 32 * k + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                        }
                     }
-                }
-                if (mine && whole && P.lse) P.lse[out_row * P.q_heads + head] = lse_of(top, weight);
-                if (!whole) {
-                    part[S::kCols * S::kDim + row] = top;
-                    part[S::kCols * S::kDim + S::kCols + row] = weight;
-                    if (begins) {
-                        goes_on = true;
-                        if (row == 0) *ends = BlockEnd{item_to, total, c.columns(P), 1, {}};
+                    if (mine && whole && P.lse) P.lse[out_row * P.q_heads + head] = lse_of(top, weight);
+                    if (!whole) {
+                        part[S::kCols * S::kDim + half * 128 + row] = top;
+                        part[S::kCols * S::kDim + S::kCols + half * 128 + row] = weight;
+                        if (begins) {
+                            goes_on = true;
+                            if (threadIdx.x == 0) *ends = BlockEnd{item_to, total, c.columns(P), 1, {}};
+                        }
                     }
+                    tc_fence_before();                     // read before the next item's products
                 }
-                tc_fence_before();                         // read before the next item's products
-                item_from = item_to;
+                ++turns;
             }
-            if (++c.step == c.steps) {
+            fresh = item_ends;
+            if (item_ends) {
+                item_from += c.steps;
                 c.next_item(P);
-                fresh = true;
-            }
+            } else ++c.step;
         }
-        if (row == 0 && !goes_on) ends->there = 0;
+        if (threadIdx.x == 0 && !goes_on) ends->there = 0;
     }
     __syncthreads();
-    if (warp == 8) {
+    if (warp == 12) {
         // products under way end, or are waited for as long as anything else, before the block and its memories are given back
         if (s_failed) {
-            if (issued) settled(s_full, (issued - 1) & 1, P.spin_limit);
-            if (issued2) settled(o_full, (issued2 - 1) & 1, P.spin_limit);
+            for (uint32_t x = 0; x < 2; ++x) {
+                if (first_done[x]) settled(s_full + 8 * x, (first_done[x] - 1) & 1, P.spin_limit);
+                if (second_done[x]) settled(o_full + 8 * x, (second_done[x] - 1) & 1, P.spin_limit);
+            }
             if (lane == 0) {
                 atomicOr(P.B.marks, kKvGaveUp);
                 ends->there = 0;
