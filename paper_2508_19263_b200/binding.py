@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -770,31 +771,38 @@ class KvBatch:
         return made[0]
 
 
-def _kv_tensor(t: Optional[torch.Tensor], what: str, heads: int, dim: int) -> KvTensorDesc:
+# the C structures as packed bytes: made in one go, and nobody else's while a call is under way
+_pack_tensor = struct.Struct("<QQQ").pack                    # zc_kv_tensor
+_pack_attention = struct.Struct("<QQQQQQQIIfII4x").pack      # zc_kv_attention_args: q, out, lse, type, heads, scale, causal, window
+assert len(_pack_tensor(0, 0, 0)) == C.sizeof(KvTensorDesc) and len(_pack_attention(*[0] * 12)) == C.sizeof(KvAttentionArgs)
+
+
+def _kv_strides(t: torch.Tensor, what: str, heads: int, dim: int):
+    """(pitch of rows, of heads) of a tensor [rows, heads, dim]."""
     shape, stride = t.shape, t.stride()
     if len(shape) != 3 or shape[1] != heads or shape[2] != dim or stride[2] != 1:
         raise ValueError(f"{what}: [rows, {heads}, {dim}] with contiguous heads is wanted, got shape {tuple(shape)}, strides {stride}")
-    return KvTensorDesc(t.data_ptr(), stride[0], stride[1])
+    return stride[0], stride[1]
 
 
 def _kv_rows(call, where: str, cache: KvCache, batch: KvBatch, d_k: Optional[torch.Tensor], d_v: Optional[torch.Tensor], stream):
     one = d_k if d_k is not None else d_v
     if one is None:
         raise ValueError("neither keys nor values")
-    real = _REAL.get(one.dtype)
+    dtype, rows, dev = one.dtype, one.shape[0], one.get_device()
+    real = _REAL.get(dtype)
     if real is None:
-        raise TypeError(f"float32, bfloat16 or float16 is wanted, got {one.dtype}")
-    descs, devs = [], [cache._dev, batch._dev]
-    for t, what in ((d_k, "d_k"), (d_v, "d_v")):
-        if t is not None:
-            if t.dtype != one.dtype or t.shape[0] != one.shape[0]:
-                raise ValueError("d_k and d_v are of one type and have the same rows")
-            descs.append(_kv_tensor(t, what, cache.kv_heads, cache.head_dim))
-            devs.append(t.get_device())
-        else:
-            descs.append(None)
-    dev = _same_device(*devs)
-    status = call(cache._ref, batch._ref(one.shape[0]), real, *[C.addressof(d) if d is not None else None for d in descs], _stream_of(stream, dev))
+        raise TypeError(f"float32, bfloat16 or float16 is wanted, got {dtype}")
+    heads, dim = cache.kv_heads, cache.head_dim
+    k = v = None
+    if d_k is not None:
+        k = _pack_tensor(d_k.data_ptr(), *_kv_strides(d_k, "d_k", heads, dim))
+    if d_v is not None:
+        v = _pack_tensor(d_v.data_ptr(), *_kv_strides(d_v, "d_v", heads, dim))
+        if d_v is not one and (d_v.dtype != dtype or d_v.shape[0] != rows):
+            raise ValueError("d_k and d_v are of one type and have the same rows")
+    dev = _same_device(cache._dev, batch._dev, dev, d_v.get_device() if d_v is not None else dev)
+    status = call(cache._ref, batch._ref(rows), real, k, v, _stream_of(stream, dev))
     if status != OK:
         raise ZcError(status, where)
 
@@ -824,20 +832,21 @@ def kv_attention(cache: KvCache, batch: KvBatch, d_q: torch.Tensor, d_out: torch
     real = _REAL.get(d_q.dtype)
     if real is None or d_out.dtype != d_q.dtype:
         raise TypeError(f"d_q and d_out are bfloat16 or float16, got {d_q.dtype} and {d_out.dtype}")
-    rows, heads = d_q.shape[0], d_q.shape[1]
-    if d_out.shape != d_q.shape:
-        raise ValueError(f"d_q is {tuple(d_q.shape)}, d_out {tuple(d_out.shape)}")
-    args = KvAttentionArgs(_kv_tensor(d_q, "d_q", heads, cache.head_dim), _kv_tensor(d_out, "d_out", heads, cache.head_dim), None, real, heads,
-                           cache.head_dim ** -0.5 if scale is None else scale, causal, window)
-    devs = [cache._dev, batch._dev, d_q.get_device(), d_out.get_device(), d_workspace.get_device()]
+    shape, dim = d_q.shape, cache.head_dim
+    if d_out.shape != shape or len(shape) != 3:
+        raise ValueError(f"d_q is {tuple(shape)}, d_out {tuple(d_out.shape)}")
+    if not 0 <= window < 1 << 32:
+        raise ValueError("window is out of range")
+    rows, heads = shape[0], shape[1]
+    dev, lse = d_q.get_device(), 0
+    dev = _same_device(cache._dev, batch._dev, dev, d_out.get_device(), d_workspace.get_device(), d_lse.get_device() if d_lse is not None else dev)
     if d_lse is not None:
-        if d_lse.dtype != torch.float32 or tuple(d_lse.shape) != (rows, heads) or not d_lse.is_contiguous():
+        if d_lse.dtype != torch.float32 or d_lse.shape != (rows, heads) or not d_lse.is_contiguous():
             raise ValueError(f"d_lse is contiguous float32 of shape {(rows, heads)}")
-        args.d_lse = d_lse.data_ptr()
-        devs.append(d_lse.get_device())
-    dev = _same_device(*devs)
-    status = _lib.zc_kv_attention(cache._ref, batch._ref(rows), C.addressof(args), d_workspace.data_ptr(),
-                                  d_workspace.numel() * d_workspace.element_size(), _stream_of(stream, dev))
+        lse = d_lse.data_ptr()
+    args = _pack_attention(d_q.data_ptr(), *_kv_strides(d_q, "d_q", heads, dim), d_out.data_ptr(), *_kv_strides(d_out, "d_out", heads, dim), lse, real, heads,
+                           dim ** -0.5 if scale is None else scale, causal, window)
+    status = _lib.zc_kv_attention(cache._ref, batch._ref(rows), args, d_workspace.data_ptr(), d_workspace.nbytes, _stream_of(stream, dev))
     if status != OK:
         raise ZcError(status, "zc_kv_attention")
     return d_out

@@ -41,12 +41,12 @@ template <typename S>
 static size_t stream_workspace(uint32_t blocks) { return workspace_of<S>(blocks, blocks * S::kWarps * S::kPart); }
 
 template <typename S>
-static cudaError_t launch_join(const AttentionParams& P, uint32_t blocks, cudaLaunchConfig_t cfg)
+static cudaError_t launch_join(const AttentionParams& P, uint32_t blocks, uint32_t least, cudaLaunchConfig_t cfg)
 {
     cfg.gridDim = dim3(blocks, S::kCols / 8);
     cfg.blockDim = dim3(256);
     cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, kv_join_kernel<S>, P, blocks);
+    return cudaLaunchKernelEx(&cfg, kv_join_kernel<S>, P, blocks, least);
 }
 
 template <typename S>
@@ -63,7 +63,7 @@ static cudaError_t launch_stream(const AttentionParams& P, const CUtensorMap& ke
     cfg.attrs = at;
     cfg.numAttrs = 1;
     if (const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_stream_kernel<S>, P, keys, values)) return e;
-    return launch_join<S>(P, blocks, cfg);
+    return launch_join<S>(P, blocks, S::kWarps, cfg);
 }
 
 template <typename S>
@@ -81,7 +81,7 @@ static cudaError_t launch_prompt(const AttentionParams& P, uint32_t blocks, cuda
     cfg.attrs = at;
     cfg.numAttrs = 1;
     if (const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_prompt_kernel<S>, P)) return e;
-    return launch_join<S>(P, blocks, cfg);
+    return launch_join<S>(P, blocks, 1, cfg);
 }
 
 // Columns (rows times heads that share a head of the cache) up to which a sequence goes to the kernel of few rows.

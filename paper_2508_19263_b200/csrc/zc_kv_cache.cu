@@ -18,8 +18,17 @@ __global__ void kv_collect_kernel(unsigned int* marks, uint32_t at) { g_kv_answe
 
 unsigned int* kv_marks_word()
 {
+    // looked up on a device's first use
+    static std::atomic<unsigned int*> known[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
+    const bool keep = dev >= 0 && dev < 64;
+    if (keep)
+        if (unsigned int* p = known[dev].load(std::memory_order_relaxed)) return p;
     void* p = nullptr;
-    return cudaGetSymbolAddress(&p, g_kv_marks) == cudaSuccess ? (unsigned int*)p : nullptr;
+    if (cudaGetSymbolAddress(&p, g_kv_marks) != cudaSuccess) return nullptr;
+    if (keep) known[dev].store((unsigned int*)p, std::memory_order_relaxed);
+    return (unsigned int*)p;
 }
 
 struct CacheParams {

@@ -207,7 +207,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
     if (warp == 0) {
         unsigned long long total = 0;
         for (int pass = 0; pass < 2; ++pass) {
-            const unsigned long long from = pass ? share(total, blockIdx.x, gridDim.x) : 0;
+            const uint32_t blocks = working_blocks(total, 1, gridDim.x);
+            if (pass && blockIdx.x >= blocks) break;
+            const unsigned long long from = pass ? share(total, blockIdx.x, blocks) : 0;
             unsigned long long before = 0;
             bool found = false;
             PromptCursor many{};                          // a lane has one of 32 sequences
@@ -255,7 +257,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const unsigned long long total = s_total, from = share(total, blockIdx.x, gridDim.x), to = share(total, blockIdx.x + 1, gridDim.x);
+    const unsigned long long total = s_total;
+    const uint32_t blocks = working_blocks(total, 1, gridDim.x);
+    const unsigned long long from = blockIdx.x < blocks ? share(total, blockIdx.x, blocks) : 0, to = blockIdx.x < blocks ? share(total, blockIdx.x + 1, blocks) : 0;
     const uint32_t count = (uint32_t)(to - from), tmem = s_tmem;
     const Waiter wait{P.spin_limit, &s_failed};
     PromptCursor c;

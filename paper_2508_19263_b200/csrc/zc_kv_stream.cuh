@@ -58,6 +58,12 @@ __device__ __forceinline__ unsigned long long share(unsigned long long total, ui
     return all >> 32 ? all / runs : (uint32_t)all / runs;
 }
 
+// How many of `blocks` get steps where each takes `least` if it can.
+__device__ __forceinline__ uint32_t working_blocks(unsigned long long total, uint32_t least, uint32_t blocks)
+{
+    return total >= (unsigned long long)least * blocks ? blocks : total ? ((uint32_t)total + least - 1) / least : 1;
+}
+
 // A part of an item that a warp leaves to the block.
 struct StreamEntry {
     unsigned long long from, to;           // the item's steps among all
@@ -180,6 +186,18 @@ __device__ __forceinline__ void join_parts(uint32_t count, PART part, uint32_t s
     for (uint32_t k0 = 0; k0 < count; k0 += 32) {
         // a lane has a part
         const float* mine = k0 + lane < count ? part(k0 + lane) : nullptr;
+        const uint32_t some = min(32u, count - k0);
+        constexpr uint32_t kAtOnce = 16;                       // reads under way
+        float x[kAtOnce][N];
+        auto read = [&](uint32_t k1) {
+#pragma unroll
+            for (uint32_t k = 0; k < kAtOnce; ++k) {
+                const float* p = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(mine), min(k1 + k, some - 1))) + sums + lane * N;
+                if (N == 4) { const float4 y = *reinterpret_cast<const float4*>(p); x[k][0] = y.x; x[k][1] = y.y; x[k][N - 2] = y.z; x[k][N - 1] = y.w; }
+                else { const float2 y = *reinterpret_cast<const float2*>(p); x[k][0] = y.x; x[k][1] = y.y; }
+            }
+        };
+        read(0);
         const float t = mine ? mine[at] : -INFINITY, w = mine ? mine[weights] : 0.0f;
         float next = t;
         for (int d = 16; d; d >>= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, d));
@@ -191,16 +209,8 @@ __device__ __forceinline__ void join_parts(uint32_t count, PART part, uint32_t s
         weight = fmaf(weight, old, sum);
 #pragma unroll
         for (uint32_t n = 0; n < N; ++n) v[n] *= old;
-        const uint32_t some = min(32u, count - k0);
-        constexpr uint32_t kAtOnce = 16;                       // reads under way
         for (uint32_t k1 = 0; k1 < some; k1 += kAtOnce) {
-            float x[kAtOnce][N];
-#pragma unroll
-            for (uint32_t k = 0; k < kAtOnce; ++k) {
-                const float* p = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(mine), min(k1 + k, some - 1))) + sums + lane * N;
-                if (N == 4) { const float4 y = *reinterpret_cast<const float4*>(p); x[k][0] = y.x; x[k][1] = y.y; x[k][N - 2] = y.z; x[k][N - 1] = y.w; }
-                else { const float2 y = *reinterpret_cast<const float2*>(p); x[k][0] = y.x; x[k][1] = y.y; }
-            }
+            if (k1) read(k1);
 #pragma unroll
             for (uint32_t k = 0; k < kAtOnce; ++k) {
                 const float f = __shfl_sync(0xFFFFFFFFu, now, (k1 + k) & 31);
@@ -256,9 +266,11 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
         __syncthreads();
     }
     for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(kAll, total, d);
-    const uint32_t runs = gridDim.x * S::kWarps, run = blockIdx.x * S::kWarps + warp;
-    const unsigned long long from = share(total, run, runs), to = share(total, run + 1, runs);
-    const unsigned long long block_from = share(total, blockIdx.x, gridDim.x), block_to = share(total, blockIdx.x + 1, gridDim.x);
+    // with fewer steps than warps only so many blocks as have a step for each warp: parts of an item are joined in a block rather than between blocks
+    const uint32_t blocks = working_blocks(total, S::kWarps, gridDim.x), runs = blocks * S::kWarps, run = blockIdx.x * S::kWarps + warp;
+    const bool works = blockIdx.x < blocks;
+    const unsigned long long from = works ? share(total, run, runs) : 0, to = works ? share(total, run + 1, runs) : 0;
+    const unsigned long long block_from = works ? share(total, blockIdx.x, blocks) : 0, block_to = works ? share(total, blockIdx.x + 1, blocks) : 0;
 
     // ---- the place of step `from`: sequence, item of the sequence, step of the item ----
     uint32_t b = 0, item = 0, step = 0;
@@ -289,6 +301,14 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
     typename S::Place ahead;
     ahead.set(span, b, item, step);
     SeqSpan at_span = span;                              // `ahead` may come to the next 32 sequences before
+    // the first item's queries are on their way while its pages are looked up
+    if (from < to) {
+#pragma unroll
+        for (uint32_t t = 0; t < S::kNt; ++t) {
+            const uint32_t col = ahead.tile * S::kCols + 8 * t + g;
+            if (ahead.has(P, col)) asm volatile("prefetch.global.L1 [%0];" :: "l"(ahead.query(P, col) + i * (S::kDim / 2)));
+        }
+    }
     uint32_t place_base = 0xFFFFFFFFu, place_seq = 0xFFFFFFFFu;
     int pages = 0;
     uint32_t missing = 0;                                 // kGroups bits a stage: groups of 16 tokens that have no page
@@ -780,23 +800,18 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
 
 // The items that go on from one block to the next: a block for each eight columns of the item that begins and does not end in a block, a warp a column.
 template <typename S>
-__global__ void __launch_bounds__(256) kv_join_kernel(const AttentionParams P, uint32_t blocks)
+__global__ void __launch_bounds__(256) kv_join_kernel(const AttentionParams P, uint32_t grid, uint32_t least)
 {
     grid_wait();
     grid_launch_dependents();
     const BlockEnd end = reinterpret_cast<const BlockEnd*>(P.workspace)[blockIdx.x];
     const uint32_t lane = threadIdx.x & 31, in_tile = blockIdx.y * 8 + (threadIdx.x >> 5);
     if (!end.there || in_tile >= end.columns.count) return;
-    // up to the last block whose steps begin before the item's end; with fewer steps than blocks some have none, and no part
+    // up to the last block whose steps begin before the item's end
+    const uint32_t blocks = working_blocks(end.total, least, grid);
     const unsigned long long all = end.to * blocks - 1;
-    const uint32_t last = all >> 32 ? (uint32_t)(all / end.total) : (uint32_t)all / (uint32_t)end.total;
-    const bool gaps = end.total < blocks;
-    const uint32_t count = gaps ? (uint32_t)(end.to - share(end.total, blockIdx.x, blocks)) : last - blockIdx.x + 1;
-    auto part = [&](uint32_t k) -> const float* {
-        // with gaps a block has one step at most: the k-th next step's block is the last that begins at or before it
-        const uint32_t block = k == 0 ? blockIdx.x : gaps ? (uint32_t)(((share(end.total, blockIdx.x, blocks) + k + 1) * blocks - 1) / end.total) : blockIdx.x + k;
-        return partial_of<S>(P, blocks, block, k == 0 ? 1 : 0);
-    };
+    const uint32_t last = all >> 32 ? (uint32_t)(all / end.total) : (uint32_t)all / (uint32_t)end.total, count = last - blockIdx.x + 1;
+    auto part = [&](uint32_t k) -> const float* { return partial_of<S>(P, grid, blockIdx.x + k, k == 0 ? 1 : 0); };
     constexpr uint32_t N = S::kDim / 32;
     float v[N], best, weight;
     join_parts<S>(count, part, in_tile * S::kDim, S::kCols * S::kDim + in_tile, S::kCols * S::kDim + S::kCols + in_tile, v, best, weight);
