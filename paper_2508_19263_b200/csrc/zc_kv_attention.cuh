@@ -62,6 +62,38 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
+// Waits of these kernels: bounded, and over for every role when one has given up, which is looked for at every kPolls-th poll only: warps that poll take the
+// issue slots of those that work, so a poll is as few instructions as it can be (with a look at every poll, half of a many-row step's instructions were polls).
+constexpr uint32_t kPolls = 32;
+__device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity, uint32_t polls)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, %3;\n"
+                 "AGAIN_%=:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra OVER_%=;\n\t"
+                 "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra AGAIN_%=;\n"
+                 "OVER_%=:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity), "r"(polls) : "memory");
+    return ok != 0;
+}
+struct KvWaiter {
+    uint32_t limit, failed;                              // failed: shared address of the block's mark
+    __device__ __forceinline__ void give_up() const { asm volatile("st.volatile.shared.u32 [%0], 1;" :: "r"(failed) : "memory"); }
+    // all lanes of a converged warp
+    __device__ __forceinline__ bool warp(uint32_t bar, uint32_t parity) const
+    {
+        uint32_t left = limit;
+        while (true) {
+            const uint32_t some = min(left, kPolls - 1) + 1;
+            if (__all_sync(0xFFFFFFFFu, bar_poll(bar, parity, some))) return true;
+            uint32_t over;
+            asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(over) : "r"(failed) : "memory");
+            if (__any_sync(0xFFFFFFFFu, over != 0)) return false;
+            if (left < some) { give_up(); return false; }
+            left -= some;
+        }
+    }
+};
+
 // The rows of a sequence and the tokens that any of them sees.
 struct SeqRows {
     int n, row0, len, from, to;

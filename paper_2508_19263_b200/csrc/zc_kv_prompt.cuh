@@ -4,9 +4,9 @@
 // with a head is an item, a step is 128 tokens of an item.  As in the other kernel all steps in order are cut into equal runs, here one for each block
 // (a block an SM), and parts of items are joined by a second kernel.
 //
-// Roles: twice four warps have a row of a half of the tile a thread (maxima, exponentials, sums, the weights into tensor memory, results); four have a token a
-// thread and write keys and values as FP16 into shared memory, up to two steps ahead; one issues the matrix instructions.  The halves are half a step apart:
-// while one is at its softmax the other's products have the tensor cores, and both use what the four warps have made of the cache.
+// Roles: twice four warps have a row of a half of the tile a thread (maxima, exponentials, sums, the weights into tensor memory, results); twice four have a token's keys
+// or values a thread and write them as FP16 into shared memory, up to two steps ahead; one issues the matrix instructions.  The halves are half a step apart:
+// while one is at its softmax the other's products have the tensor cores, and both use what the eight warps have made of the cache.
 //   S = Q K^T: both operands in shared memory, 128-byte swizzle, the head's width fastest.  O += P V: P in tensor memory, in S's place; V as it is written,
 // the head's width fastest, which for this product is the outer axis.  S and O, FP32, of both halves are all of tensor memory's 512 columns (head_dim 128).
 //   Keys and values are element * 2^(s - R + kLift), R the largest scale byte that the item has met, for keys and for values: exact unless a scale is 2^-35 (E4M3:
@@ -26,7 +26,7 @@ struct PromptShape {
     static constexpr int kLift = kFp4 ? 12 : 6;                              // 6 * 2^12 and 448 * 2^6 are FP16 numbers
     static constexpr uint32_t kTile = 128 * kDim * 2;                        // 128 rows of FP16, pieces of 64 of the head's width one after the other
     static constexpr uint32_t kSmem = 6 * kTile + 1024;                      // queries of both halves; keys and values of two steps
-    static constexpr uint32_t kThreads = 13 * 32;
+    static constexpr uint32_t kThreads = 17 * 32;
     static constexpr uint32_t kHalf = 256, kO = 128, kTmem = 512;            // columns: of a half S, then O
 };
 
@@ -170,7 +170,7 @@ template <typename S>
 __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const AttentionParams P)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ __align__(8) uint64_t s_bars[15];
+    __shared__ __align__(8) uint64_t s_bars[16];
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_failed;
     __shared__ unsigned long long s_total, s_item_from;
@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
     const uint32_t lane = threadIdx.x & 31, warp = warp_index();
     const uint32_t base = (smem_u32(smem) + 1023) & ~1023u, q_tile = base, k_tile = base + 2 * S::kTile, v_tile = base + 4 * S::kTile;
     const uint32_t bars = smem_u32(s_bars);
-    // of each half: queries written; first product done; weights written; second product done.  Of each step parity: keys written; values written; both used; scales known
+    // of each half: queries written; first product done; weights written; second product done.  Of each step parity: keys written and values' scales known; values written; both used.  Of keys and values: scales known
     const uint32_t q_full = bars, s_full = bars + 16, p_full = bars + 32, o_full = bars + 48, k_full = bars + 64, v_full = bars + 80, kv_free = bars + 96, m_full = bars + 112;
     if (threadIdx.x == 0) {
         s_failed = 0;
@@ -192,14 +192,15 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
             bar_init(s_full + 8 * x, 1);
             bar_init(p_full + 8 * x, 128);
             bar_init(o_full + 8 * x, 1);
-            bar_init(k_full + 8 * x, 128);
+            bar_init(k_full + 8 * x, 256);
             bar_init(v_full + 8 * x, 128);
             bar_init(kv_free + 8 * x, 1);
         }
         bar_init(m_full, 4);
+        bar_init(m_full + 8, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) tmem_alloc<1>(smem_u32(&s_tmem), S::kTmem);
+    if (warp == 16) tmem_alloc<1>(smem_u32(&s_tmem), S::kTmem);
     grid_wait();
     grid_launch_dependents();
 
@@ -260,8 +261,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
     const unsigned long long total = s_total;
     const uint32_t blocks = working_blocks(total, 1, gridDim.x);
     const unsigned long long from = blockIdx.x < blocks ? share(total, blockIdx.x, blocks) : 0, to = blockIdx.x < blocks ? share(total, blockIdx.x + 1, blocks) : 0;
-    const uint32_t count = (uint32_t)(to - from), tmem = s_tmem;
-    const Waiter wait{P.spin_limit, &s_failed};
+    const uint32_t count = (uint32_t)(to - from), tmem = __shfl_sync(kAll, s_tmem, 0);
+    const KvWaiter wait{P.spin_limit, smem_u32(const_cast<uint32_t*>(&s_failed))};
     PromptCursor c;
     if (count) {
         c.sequence(P, s_start[0]);
@@ -273,22 +274,24 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
     BlockEnd* ends = reinterpret_cast<BlockEnd*>(P.workspace) + blockIdx.x;
     uint32_t first_done[2] = {}, second_done[2] = {};      // of the issuing warp: products issued, of each half
 
-    if (warp == 12) {
+    if (warp == 16) {
         // ---- matrix instructions ----
         const uint32_t qk = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);                               // FP16 operands, FP32 sums
         const uint32_t pv = (1u << 4) | (1u << 16) | ((S::kDim >> 3) << 17) | ((128u >> 4) << 24);               // the second operand by its outer axis
         uint32_t items[2] = {};
+        const uint64_t q_desc = operand_desc(q_tile), k_desc = operand_desc(k_tile), v_desc = outer_desc(v_tile);        // addresses in units of 16 bytes
         // a half's first product for step j; `fresh`: of a new item
         auto first = [&](uint32_t x, uint32_t j, bool fresh) -> bool {
             if (fresh && !wait.warp(q_full + 8 * x, items[x]++ & 1)) return false;
             if (!wait.warp(k_full + 8 * (j & 1), (j >> 1) & 1)) return false;
             tc_fence_after();
             if (P.skip_math) { wait.give_up(); return false; }
+            const uint64_t q = q_desc + x * (S::kTile >> 4), keys = k_desc + (j & 1) * (S::kTile >> 4);
             if (elect_one()) {
 #pragma unroll
                 for (uint32_t k = 0; k < S::kDim / 16; ++k) {
-                    const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
-                    mma_ss_f16(tmem + x * S::kHalf, operand_desc(q_tile + x * S::kTile + off), operand_desc(k_tile + (j & 1) * S::kTile + off), qk, k != 0);
+                    const uint32_t off = ((k >> 2) * 16384 + (k & 3) * 32) >> 4;
+                    mma_ss_f16(tmem + x * S::kHalf, q + off, keys + off, qk, k != 0);
                 }
                 mma_commit<1>(s_full + 8 * x);
             }
@@ -312,10 +315,11 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                 if (x < halves) {
                     if (!wait.warp(v_full + 8 * (j & 1), (j >> 1) & 1) || !wait.warp(p_full + 8 * x, second_done[x] & 1)) { ok = false; break; }
                     tc_fence_after();
+                    const uint64_t values = v_desc + (j & 1) * (S::kTile >> 4);
                     if (elect_one()) {
 #pragma unroll
                         for (uint32_t k = 0; k < 8; ++k)
-                            mma_ts_f16(tmem + x * S::kHalf + S::kO, tmem + x * S::kHalf + 8 * k, outer_desc(v_tile + (j & 1) * S::kTile + k * 2048), pv, !(fresh && k == 0));
+                            mma_ts_f16(tmem + x * S::kHalf + S::kO, tmem + x * S::kHalf + 8 * k, values + k * (2048 >> 4), pv, !(fresh && k == 0));
                         mma_commit<1>(o_full + 8 * x);
                         if (x + 1 == halves) mma_commit<1>(kv_free + 8 * (j & 1));
                     }
@@ -333,13 +337,13 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
             c = n;
         }
     } else if (warp >= 8) {
-        // ---- keys and values: a thread has a token ----
-        const uint32_t row = threadIdx.x - 256, group = row >> 5;
-        PromptCursor ahead = c;
+        // ---- keys (side 0) and values (side 1): a thread has a token ----
+        const uint32_t row = threadIdx.x & 127, group = row >> 5, side = (warp >> 2) & 1;
+        PromptCursor ahead = c;                            // the step whose elements are read, one ahead
         constexpr uint32_t kWords = S::kRow / 16;
-        uint4 kw[kWords], vw[kWords];
-        uint32_t ks = 0, vs = 0;
-        int page = -1, next_page = -1;
+        uint4 now[kWords], next[kWords];
+        uint32_t now_scales = 0, next_scales = 0;
+        int now_page = -2, next_page = -2, later_page = -2;
         auto find_page = [&](const PromptCursor& a) -> int {
             const uint32_t t = (a.first_step + a.step) * 128 + row;
             int lo, hi, skip;
@@ -347,91 +351,86 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
             a.limits(P, (int)((a.tile * 256 + a.columns_left(P) - 1) / P.group), skip, hi);
             return (int)t >= lo && (int)t < hi && t < (uint32_t)a.len ? kv_page(P.C, P.B, a.b, t >> P.C.page_shift) : -2;     // -2: nobody sees the token
         };
+        const uint8_t *elems = P.C.elems[side], *scales = P.C.scales[side];
         auto load = [&](const PromptCursor& a, int pg) {
             const uint32_t t = (a.first_step + a.step) * 128 + row;
             if (pg >= 0) {
                 const uint64_t at = (((uint64_t)pg * P.C.heads + a.head) << P.C.page_shift) + (t & ((1u << P.C.page_shift) - 1));
-                const uint4 *k = reinterpret_cast<const uint4*>(P.C.elems[0] + at * S::kRow), *v = reinterpret_cast<const uint4*>(P.C.elems[1] + at * S::kRow);
+                const uint4* w = reinterpret_cast<const uint4*>(elems + at * S::kRow);
 #pragma unroll
-                for (uint32_t i = 0; i < kWords; ++i) { kw[i] = k[i]; vw[i] = v[i]; }
-                if (S::kBlocks == 4) {
-                    ks = *reinterpret_cast<const uint32_t*>(P.C.scales[0] + at * 4);
-                    vs = *reinterpret_cast<const uint32_t*>(P.C.scales[1] + at * 4);
-                } else {
-                    ks = *reinterpret_cast<const uint16_t*>(P.C.scales[0] + at * 2);
-                    vs = *reinterpret_cast<const uint16_t*>(P.C.scales[1] + at * 2);
-                }
+                for (uint32_t i = 0; i < kWords; ++i) next[i] = w[i];
+                next_scales = S::kBlocks == 4 ? *reinterpret_cast<const uint32_t*>(scales + at * 4) : *reinterpret_cast<const uint16_t*>(scales + at * 2);
             }
         };
         auto advance = [&](PromptCursor& a) { if (++a.step == a.steps) a.next_item(P); };
-        uint32_t k_ref = 0, v_ref = 0;
+        uint32_t ref = 0;
+        const uint32_t tile = side ? v_tile : k_tile, full = side ? v_full : k_full, known = m_full + 8 * side;
         if (count) {
-            page = find_page(c);
-            load(c, page);
+            next_page = find_page(ahead);
+            load(ahead, next_page);
             advance(ahead);
-            if (count > 1) next_page = find_page(ahead);
+            if (count > 1) later_page = find_page(ahead);
         }
         for (uint32_t j = 0; j < count; ++j) {
             const uint32_t par = j & 1;
+            // the next step's elements are on their way while this one's are written, its pages a step earlier
+#pragma unroll
+            for (uint32_t i = 0; i < kWords; ++i) now[i] = next[i];
+            now_scales = next_scales;
+            now_page = next_page;
+            next_page = later_page;
+            if (j + 1 < count) {
+                load(ahead, next_page);
+                if (j + 2 < count) {
+                    advance(ahead);
+                    later_page = find_page(ahead);
+                }
+            }
             // the step before the last is over: its keys, values, and what is said of them
             if (j >= 2 && !wait.warp(kv_free + 8 * par, ((j >> 1) - 1) & 1)) break;
-            if (j && c.step == 0) k_ref = v_ref = 0;
-            const bool hidden = page < 0;
+            if (j && c.step == 0) ref = 0;
+            const bool hidden = now_page < 0;
             // the largest scales
-            uint32_t km = 0, vm = 0;
+            uint32_t most = 0;
             bool nan = false;
             if (!hidden) {
 #pragma unroll
                 for (uint32_t k = 0; k < S::kBlocks; ++k) {
-                    const uint32_t a = (ks >> (8 * k)) & 0xFF, b = (vs >> (8 * k)) & 0xFF;
-                    if (a != 255) km = max(km, a);
-                    if (b != 255) vm = max(vm, b);
-                    nan |= b == 255;
+                    const uint32_t a = (now_scales >> (8 * k)) & 0xFF;
+                    if (a != 255) most = max(most, a);
+                    nan |= a == 255;
                 }
-                if (!S::kFp4) {
+                if (!S::kFp4 && side) {
 #pragma unroll
-                    for (uint32_t i = 0; i < kWords; ++i) nan |= nan_bytes(vw[i].x) || nan_bytes(vw[i].y) || nan_bytes(vw[i].z) || nan_bytes(vw[i].w);
+                    for (uint32_t i = 0; i < kWords; ++i) nan |= nan_bytes(now[i].x) || nan_bytes(now[i].y) || nan_bytes(now[i].z) || nan_bytes(now[i].w);
                 }
             }
+            nan = nan && side;
             if (nan) {
-                // NaN that every row of the tile sees goes through the product, else the rows that see it are told
+                // NaN in values that every row of the tile sees goes through the product, else the rows that see it are told
                 const int t = (int)((c.first_step + c.step) * 128 + row);
                 int lo, hi, skip;
                 c.limits(P, (int)(c.tile * 256 / P.group), skip, hi);
                 c.limits(P, (int)((c.tile * 256 + c.columns_left(P) - 1) / P.group), lo, skip);
                 nan = t < lo || t >= hi;
             }
-            km = __reduce_max_sync(kAll, km);
-            vm = __reduce_max_sync(kAll, vm);
-            const uint32_t gone = __ballot_sync(kAll, page == -1), poisoned = __ballot_sync(kAll, nan);
+            most = __reduce_max_sync(kAll, most);
+            const uint32_t gone = __ballot_sync(kAll, now_page == -1), poisoned = __ballot_sync(kAll, nan);
             if (lane == 0) {
-                s_most[par][0][group] = km;
-                s_most[par][1][group] = vm;
-                s_gone[par][group] = gone;
-                s_poisoned[par][group] = poisoned;
-                bar_arrive(m_full);
+                s_most[par][side][group] = most;
+                if (side) s_poisoned[par][group] = poisoned;
+                else s_gone[par][group] = gone;
+                bar_arrive(known);
             }
-            if (!wait.warp(m_full, par)) break;
+            if (!wait.warp(known, par)) break;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                k_ref = max(k_ref, s_most[par][0][k]);
-                v_ref = max(v_ref, s_most[par][1][k]);
-            }
-            if (row == 0) { s_ref[par][0] = k_ref; s_ref[par][1] = v_ref; }
-            write_row<S>(k_tile + par * S::kTile, row, kw, ks, k_ref, hidden);
+            for (int k = 0; k < 4; ++k) ref = max(ref, s_most[par][side][k]);
+            if (row == 0) s_ref[par][side] = ref;
+            if (side) bar_arrive(k_full + 8 * par);        // what is said of the values comes with the keys
+            write_row<S>(tile + par * S::kTile, row, now, now_scales, ref, hidden || nan);
             fence_async_shared();
-            bar_arrive(k_full + 8 * par);
-            write_row<S>(v_tile + par * S::kTile, row, vw, vs, v_ref, hidden || nan);
-            fence_async_shared();
-            bar_arrive(v_full + 8 * par);
-            // the next step's elements are on their way while this one's are multiplied, its pages a step earlier
+            bar_arrive(full + 8 * par);
             advance(c);
-            page = next_page;
-            if (j + 1 < count) load(c, page);
-            if (j + 2 < count) {
-                advance(ahead);
-                next_page = find_page(ahead);
-            }
         }
     } else {
         // ---- rows of a half: a thread has one ----
@@ -491,26 +490,35 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                 const bool plain = t0 >= lo_most && t0 + 128 <= hi_least && (s_gone[par][0] | s_gone[par][1] | s_gone[par][2] | s_gone[par][3]) == 0 &&
                                    (s_poisoned[par][0] | s_poisoned[par][1] | s_poisoned[par][2] | s_poisoned[par][3]) == 0;
                 // above 0, that the largest product is the largest logit and -infinity stays
-                const float f = fmaxf(factor * ldexpf(1.0f, (int)k_ref - 127 - S::kLift), 1.17549435e-38f);
-                auto hide = [&](float* v, uint32_t chunk) {
-                    const uint32_t gone = s_gone[par][chunk], poisoned = s_poisoned[par][chunk];
+                const float f = fmaxf(factor * (e8m0_value(k_ref) * (1.0f / (float)(1u << S::kLift))), 1.17549435e-38f);
+                if (!plain) {
+                    // what the row does not see, in place
+#pragma unroll 1
+                    for (uint32_t k = 0; k < 4; ++k) {
+                        const uint32_t gone = s_gone[par][k], poisoned = s_poisoned[par][k];
+                        float v[32];
+                        tmem_ld32_async(at + 32 * k, v);
+                        tmem_ld_wait();
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        const int t = t0 + (int)chunk * 32 + k;
-                        if ((poisoned >> k) & 1) v[k] = __int_as_float(0x7FFFFFFF);
-                        if (t < lo || t >= hi || t >= c.len || ((gone >> k) & 1)) v[k] = -INFINITY;
+                        for (int i = 0; i < 32; ++i) {
+                            const int t = t0 + (int)(32 * k) + i;
+                            if ((poisoned >> i) & 1) v[i] = __int_as_float(0x7FFFFFFF);
+                            if (t < lo || t >= hi || t >= c.len || ((gone >> i) & 1)) v[i] = -INFINITY;
+                        }
+                        tmem_st32(at + 32 * k, v);
                     }
-                };
-                float best = -INFINITY;
+                    tmem_st_wait();
+                }
+                float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
                 for (uint32_t k = 0; k < 4; ++k) {
                     float v[32];
                     tmem_ld32_async(at + 32 * k, v);
                     tmem_ld_wait();
-                    if (!plain) hide(v, k);
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) best = fmaxf(best, fmaxf(v[i], v[i + 1]));
+                    for (int i = 0; i < 16; ++i) most[i & 3] = fmaxf(most[i & 3], fmaxf(v[2 * i], v[2 * i + 1]));
                 }
+                float best = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
                 best *= f;
                 // the sums in tensor memory are over 2^top of the weights and 2^v_ref of the values
                 float shrink = 1.0f;
@@ -540,7 +548,6 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                     uint32_t h[16];
                     tmem_ld32_async(at + 32 * k, v);
                     tmem_ld_wait();
-                    if (!plain) hide(v, k);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         fma_pair(v[2 * i], v[2 * i + 1], f, off);
@@ -604,7 +611,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
         if (threadIdx.x == 0 && !goes_on) ends->there = 0;
     }
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 16) {
         // products under way end, or are waited for as long as anything else, before the block and its memories are given back
         if (s_failed) {
             for (uint32_t x = 0; x < 2; ++x) {

@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
     }
 
     // ---- copies: one cursor runs ahead ----
-    const Waiter wait{P.spin_limit, &s_failed};
+    const KvWaiter wait{P.spin_limit, smem_u32(const_cast<uint32_t*>(&s_failed))};
     typename S::Place ahead;
     ahead.set(span, b, item, step);
     SeqSpan at_span = span;                              // `ahead` may come to the next 32 sequences before
