@@ -454,28 +454,37 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                     c.limits(P, (int)((min(cols, first_col + 128) - 1) / P.group), lo_most, skip);
                     c.limits(P, (int)(first_col / P.group), skip, hi_least);
                     hi_least = min(hi_least, c.len);
-                    // the query over a power of two, in FP16; twice read, the second time out of the L1
+                    // the query over a power of two, in FP16; twice read, the second time out of the L1; eight reads under way at a time
                     const uint8_t* q = P.q.d + (uint64_t)(c.row0 + col / P.group) * P.q.ld_row + (uint64_t)(c.head * P.group + col % P.group) * P.q.ld_head;
                     float most = 0.0f;
                     if (col < cols)
-                        for (uint32_t k = 0; k < S::kDim / 4; ++k) {
-                            const uint2 w = query_four(P, q + 8 * k);
-                            const float2 a = query_pair(P, w.x), b = query_pair(P, w.y);
-                            most = fmaxf(fmaxf(most, fmaxf(fabsf(a.x), fabsf(a.y))), fmaxf(fabsf(b.x), fabsf(b.y)));
+                        for (uint32_t k = 0; k < S::kDim / 4; k += 8) {
+                            uint2 w[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) w[i] = query_four(P, q + 8 * (k + i));
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float2 x = query_pair(P, w[i].x), y = query_pair(P, w[i].y);
+                                most = fmaxf(fmaxf(most, fmaxf(fabsf(x.x), fabsf(x.y))), fmaxf(fabsf(y.x), fabsf(y.y)));
+                            }
                         }
                     const int up = query_lift(most);
                     const float lift = copysignf(power_of_two(up), P.scale_log2);
-                    for (uint32_t k = 0; k < S::kDim / 8; ++k) {
-                        uint32_t h[4] = {};
-                        if (col < cols) {
-                            const uint2 w0 = query_four(P, q + 16 * k), w1 = query_four(P, q + 16 * k + 8);
-                            const float2 a = query_pair(P, w0.x), b = query_pair(P, w0.y), d = query_pair(P, w1.x), e = query_pair(P, w1.y);
-                            h[0] = pack_half(a.x * lift, a.y * lift);
-                            h[1] = pack_half(b.x * lift, b.y * lift);
-                            h[2] = pack_half(d.x * lift, d.y * lift);
-                            h[3] = pack_half(e.x * lift, e.y * lift);
+                    for (uint32_t k = 0; k < S::kDim / 8; k += 4) {
+                        uint2 w[8] = {};
+                        if (col < cols)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) w[i] = query_four(P, q + 16 * k + 8 * i);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t h[4];
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) {
+                                const float2 x = query_pair(P, n & 1 ? w[2 * i + n / 2].y : w[2 * i + n / 2].x);
+                                h[n] = pack_half(x.x * lift, x.y * lift);
+                            }
+                            sts128(q_tile + half * S::kTile + tile_at(row, k + i), h);
                         }
-                        sts128(q_tile + half * S::kTile + tile_at(row, k), h);
                     }
                     factor = ldexpf(fabsf(P.scale_log2), -up);
                     fence_async_shared();
