@@ -43,7 +43,7 @@ static size_t stream_workspace(uint32_t blocks) { return workspace_of<S>(blocks,
 template <typename S>
 static cudaError_t launch_join(const AttentionParams& P, uint32_t blocks, uint32_t least, cudaLaunchConfig_t cfg)
 {
-    cfg.gridDim = dim3(blocks, S::kCols / 8);
+    cfg.gridDim = dim3(blocks, S::kCols < 64 ? S::kCols / 8 : 8u);          // all of them are on the GPU at once
     cfg.blockDim = dim3(256);
     cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, kv_join_kernel<S>, P, blocks, least);

@@ -192,7 +192,8 @@ __device__ __forceinline__ void join_parts(uint32_t count, PART part, uint32_t s
         auto read = [&](uint32_t k1) {
 #pragma unroll
             for (uint32_t k = 0; k < kAtOnce; ++k) {
-                const float* p = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(mine), min(k1 + k, some - 1))) + sums + lane * N;
+                const float* p = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(mine), (k1 + k) & 31)) + sums + lane * N;
+                if (k1 + k >= some) continue;
                 if (N == 4) { const float4 y = *reinterpret_cast<const float4*>(p); x[k][0] = y.x; x[k][1] = y.y; x[k][N - 2] = y.z; x[k][N - 1] = y.w; }
                 else { const float2 y = *reinterpret_cast<const float2*>(p); x[k][0] = y.x; x[k][1] = y.y; }
             }
@@ -798,24 +799,26 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
     if (!goes_on && threadIdx.x == 0) ends->there = 0;
 }
 
-// The items that go on from one block to the next: a block for each eight columns of the item that begins and does not end in a block, a warp a column.
+// The items that go on from one block to the next: blocks for the item that begins and does not end in a block, a warp a column.
 template <typename S>
 __global__ void __launch_bounds__(256) kv_join_kernel(const AttentionParams P, uint32_t grid, uint32_t least)
 {
     grid_wait();
     grid_launch_dependents();
     const BlockEnd end = reinterpret_cast<const BlockEnd*>(P.workspace)[blockIdx.x];
-    const uint32_t lane = threadIdx.x & 31, in_tile = blockIdx.y * 8 + (threadIdx.x >> 5);
-    if (!end.there || in_tile >= end.columns.count) return;
+    const uint32_t lane = threadIdx.x & 31;
+    if (!end.there) return;
     // up to the last block whose steps begin before the item's end
     const uint32_t blocks = working_blocks(end.total, least, grid);
     const unsigned long long all = end.to * blocks - 1;
     const uint32_t last = all >> 32 ? (uint32_t)(all / end.total) : (uint32_t)all / (uint32_t)end.total, count = last - blockIdx.x + 1;
     auto part = [&](uint32_t k) -> const float* { return partial_of<S>(P, grid, blockIdx.x + k, k == 0 ? 1 : 0); };
     constexpr uint32_t N = S::kDim / 32;
-    float v[N], best, weight;
-    join_parts<S>(count, part, in_tile * S::kDim, S::kCols * S::kDim + in_tile, S::kCols * S::kDim + S::kCols + in_tile, v, best, weight);
-    finish_column<N>(P, end.columns, in_tile, lane * N, v, best, weight);
+    for (uint32_t in_tile = blockIdx.y * 8 + (threadIdx.x >> 5); in_tile < end.columns.count; in_tile += gridDim.y * 8) {
+        float v[N], best, weight;
+        join_parts<S>(count, part, in_tile * S::kDim, S::kCols * S::kDim + in_tile, S::kCols * S::kDim + S::kCols + in_tile, v, best, weight);
+        finish_column<N>(P, end.columns, in_tile, lane * N, v, best, weight);
+    }
 }
 
 }  // namespace zc
