@@ -146,13 +146,13 @@ def attention(case, q, scale, causal=True, window=0, left_out=()):
             size = torch.zeros_like(top)
         back = lambda z: z.transpose(1, 2).transpose(0, 1).reshape(n, q_heads, z.shape[-1]) if n else z.reshape(0, q_heads, z.shape[-1])  # noqa: E731
         out[r], lse[r] = back(o), back(top + torch.log(total))[..., 0]
-        bound[r] = back(terms * (2.0 ** -11 + size) + lost)
+        bound[r] = back(terms * (2.0 ** -12 + max(4096, length) * 2.0 ** -24 + size) + lost)
     return out, lse, bound
 
 
 def tolerance(want, bound, dtype):
     """How far a result may be off: half a step of its type, and `bound`.  With p the weights, each is off by 2^-12 where it is rounded to FP16, and their
-    sums over up to 4096 terms in FP32 by 2^-12.  Weights go into FP16 times 2^15 over the row's largest: what is below its least subnormal, 2^-24, is off by
+    sums over n terms in FP32 by n 2^-24 (n taken as 4096 at least: 2^-12).  Weights go into FP16 times 2^15 over the row's largest: what is below its least subnormal, 2^-24, is off by
     half of that, 2^-40 of the largest weight, for each value.  A logit of `dim` products summed in FP32 is off by (dim + 8) 2^-24 of its terms' magnitudes, which moves a weight, and the sum
     that it is divided by, by as much.  Keys and values go into FP16 over a power of two so that the largest of a head is at least 2^(15 - 9): E4M3 spans
     2^-9 .. 448 < 2^9 times its scale; below FP16's least subnormal they are off by half of it, 2^-25 / 2^6 = 2^-31 of the largest.
