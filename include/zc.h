@@ -548,8 +548,8 @@ typedef struct zc_kv_cache {
  * A row whose position is negative has no place in the cache: it is not stored, it is read as zeros, and a causal attention shows it
  * nothing.
  * What is wrong on the device is never followed: a length below 0 counts as 0, one above what the table's row has room for as that; a page
- * outside 0 .. n_pages - 1 is not touched, its tokens are not stored, are read as zeros and are left out of the attention.
- * zc_kv_status then says ZC_E_CORRUPT.  Table entries behind a sequence's last token are not read. */
+ * outside 0 .. n_pages - 1 is not touched, its tokens are not stored, are read as zeros and are left out of the attention; to the attention a
+ * sequence whose rows do not lie within n_rows has none.  zc_kv_status then says ZC_E_CORRUPT.  Table entries behind a sequence's last token are not read. */
 typedef struct zc_kv_batch {
     const int32_t* d_page_table;   /* [n_seqs] rows of max_pages pages, row pitch ld_page_table elements */
     const int32_t* d_lens;         /* [n_seqs] */
@@ -589,20 +589,23 @@ zc_status zc_kv_read(const zc_kv_cache* cache, const zc_kv_batch* batch, zc_real
  *   x_t = scale * sum_i q[r][h][i] * K_t[i],  out[r][h] = sum_t softmax(x)_t * V_t,  lse[r][h] = log sum_t exp(x_t)
  * over the tokens t of b that the row sees: all lens[b] of them, or where causal those up to its own position, and of these the last
  * `window` where window > 0.  A row that sees nothing gets zeros and lse = -infinity.  What is in the cache where no row looks (behind the last
- * token, outside the window) has no influence, whatever it is; NaN that a row sees makes NaN what depends on it. */
+ * token, outside the window) has no influence, whatever it is; NaN that a row sees makes NaN what depends on it, at most all of the row.
+ * Sums, maxima and the sum of weights are FP32.  Queries are used to 2^-31 of the row's largest element, exactly where they are above 2^-24 of it.  Weights are
+ * rounded to FP16 for the products with the values: off by 2^-12 of themselves, and by 2^-39 of the row's largest where they are far below it.  Sequences of many
+ * rows use keys and values to 2^-31 of the largest that the head has. */
 typedef struct zc_kv_attention_args {
     zc_kv_tensor q, out;           /* [n_rows][q_heads][head_dim] of `type`; must not overlap */
     float* d_lse;                  /* [n_rows][q_heads], no padding; null: not wanted */
     uint32_t type;                 /* ZC_REAL_BF16 or ZC_REAL_F16 */
     uint32_t q_heads;              /* a multiple of kv_heads */
-    float scale;                   /* finite */
+    float scale;                   /* magnitude at most 2e38 */
     uint32_t causal;               /* 0 or 1 */
     uint32_t window;               /* 0: none; only with causal */
 } zc_kv_attention_args;
 #define ZC_KV_MAX_GROUP 256u       /* query heads that share a head of the cache */
 
-/* Bytes of device scratch zc_kv_attention needs for up to q_heads query heads (it depends on neither lengths nor rows); 0 for arguments that it
- * would refuse. */
+/* Bytes of device scratch zc_kv_attention needs for up to q_heads query heads, for any lengths and rows of a batch with this max_new (more where rows times
+ * heads that share one are above 32); 0 for arguments that it would refuse. */
 size_t zc_kv_attention_workspace_bytes(const zc_kv_cache* cache, const zc_kv_batch* batch, uint32_t q_heads);
 /* d_workspace  workspace_bytes >= zc_kv_attention_workspace_bytes(), 256-byte aligned, contents need not be initialised; calls that
  *              overlap in time must not share it.  Asynchronous.  The result is the same every time.

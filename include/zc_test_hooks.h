@@ -27,9 +27,9 @@ zc_status zc_test_merge16(zc_format fmt, const uint8_t* h_e8, const uint8_t* h_s
  *   zc_test_stall_encoder   zc_compress hands out its batches from this number on, so batch 0 is
  *                           never packed and every look-back waits for a word nobody posts
  *   zc_test_stall_decoder   the decoder does not start the copies of the pieces it waits for, nor do
- *                           zc_fp8_matmul and zc_fp8_moe those of their operands
+ *                           zc_fp8_matmul and zc_fp8_moe those of their operands, nor zc_kv_attention of few rows those of the cache
  *   zc_test_stall_math      zc_fp8_matmul and zc_fp8_moe copy their operands but start no matrix
- *                           instruction, so that they give up with copies under way
+ *                           instruction, so that they give up with copies under way; zc_kv_attention of many rows starts none either
  *   zc_test_fp8_marks       what the last zc_fp8_status found: 1 a wait gave up, 2 a block that gave up waited until what
  *                           it had under way was done, 4 it waited for that in vain */
 /* Launch shapes (host arithmetic only, no GPU): worker warps per block the encoder would use for a plan with n_coded

@@ -754,27 +754,21 @@ class KvBatch:
             raise ValueError("max_new is out of range")
         self.page_table, self.lens, self.first, self.max_new, self.n_seqs = page_table, lens, first, max_new, seqs
         pitch = page_table.stride(0) if seqs > 1 else max(page_table.stride(0), pages)
-        self._desc = (page_table.data_ptr(), lens.data_ptr(), first.data_ptr(), pitch)
-        self._made = {}
+        self._front, self._back = (page_table.data_ptr(), lens.data_ptr(), first.data_ptr(), pitch), (pages, seqs, max_new)
         self._dev = lens.get_device()
         if any(t.get_device() != self._dev for t in (page_table, first)):
             raise ValueError("the batch's tensors are on several devices")
 
-    def _ref(self, n_rows: int):
+    def _ref(self, n_rows: int) -> bytes:
         """The descriptor for tensors of n_rows rows."""
-        made = self._made.get(n_rows)
-        if made is None:
-            if len(self._made) >= 8:
-                self._made.clear()
-            d = KvBatchDesc(*self._desc, n_rows, self.page_table.shape[1], self.n_seqs, self.max_new)
-            made = self._made[n_rows] = (C.addressof(d), d)
-        return made[0]
+        return _pack_batch(*self._front, n_rows, *self._back)
 
 
 # the C structures as packed bytes: made in one go, and nobody else's while a call is under way
 _pack_tensor = struct.Struct("<QQQ").pack                    # zc_kv_tensor
+_pack_batch = struct.Struct("<QQQQQIII4x").pack              # zc_kv_batch
 _pack_attention = struct.Struct("<QQQQQQQIIfII4x").pack      # zc_kv_attention_args: q, out, lse, type, heads, scale, causal, window
-assert len(_pack_tensor(0, 0, 0)) == C.sizeof(KvTensorDesc) and len(_pack_attention(*[0] * 12)) == C.sizeof(KvAttentionArgs)
+assert len(_pack_tensor(0, 0, 0)) == C.sizeof(KvTensorDesc) and len(_pack_batch(*[0] * 8)) == C.sizeof(KvBatchDesc) and len(_pack_attention(*[0] * 12)) == C.sizeof(KvAttentionArgs)
 
 
 def _kv_strides(t: torch.Tensor, what: str, heads: int, dim: int):

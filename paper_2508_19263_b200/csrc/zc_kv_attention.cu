@@ -84,7 +84,8 @@ static cudaError_t launch_prompt(const AttentionParams& P, uint32_t blocks, cuda
     return launch_join<S>(P, blocks, 1, cfg);
 }
 
-// Columns (rows times heads that share a head of the cache) up to which a sequence goes to the kernel of few rows.
+// Columns (rows times heads that share a head of the cache) up to which a sequence goes to the kernel of few rows.  It reads the cache once for each 16 of them, the
+// other works on 256 whatever there are: 16 sequences of up to 6000 tokens, 20 columns, E4M3: 66 us (two readings) and 132 us.
 constexpr uint32_t kFewColumns = 32;
 
 }  // namespace zc
@@ -112,7 +113,7 @@ zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, co
     if (args->type != ZC_REAL_BF16 && args->type != ZC_REAL_F16) return ZC_E_UNSUPPORTED;
     if (const zc_status s = check_cache(cache)) return s;
     if (const zc_status s = check_batch(cache, batch)) return s;
-    if (args->q_heads == 0 || args->q_heads % cache->kv_heads || args->causal > 1 || (args->window && !args->causal) || !(fabsf(args->scale) <= 3.402823466e38f)) return ZC_E_INVALID_ARG;
+    if (args->q_heads == 0 || args->q_heads % cache->kv_heads || args->causal > 1 || (args->window && !args->causal) || !(fabsf(args->scale) <= 2e38f)) return ZC_E_INVALID_ARG;
     if (args->q_heads / cache->kv_heads > ZC_KV_MAX_GROUP) return ZC_E_TOO_LARGE;
     if (batch->n_seqs == 0 || batch->n_rows == 0) return ZC_OK;
     for (const zc_kv_tensor* t : {&args->q, &args->out})

@@ -13,6 +13,9 @@
 // 2^-22) of the largest, off by at most 2^-25 / 2^kLift of 2^R then.  Queries as in the other kernel.
 //   Weights are 2^(x - m + 14) with m at most 1 below the row's largest so far: so the sums in tensor memory are only touched when it grows by more than
 // a factor of 2.  They are rounded to FP16: off by at most 2^-12 of it down to 2^-28 of the largest, by 2^-39 of the largest below; the sum of weights is FP32.
+//   Measured: 2048 rows, 32 heads, behind 32768 tokens in FP4: 1252 us, 906 TFLOP/s; of a step's 5100 cycles the tensor cores work 2050, a half's softmax takes 3000 (the
+// special function units 1024 of it).  Two blocks an SM with 128 rows each: 1634 us.  16 warps for the softmax, half a row a thread: 1379 us, the four that are
+// left for keys and values do not keep up.  A quarter of the exponentials by a polynomial on the FP32 units: 1 % less time.  (One B200, a graph of 20 calls.)
 #pragma once
 #include "zc_kv_stream.cuh"
 
@@ -238,7 +241,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                         const uint32_t steps = __shfl_sync(kAll, count, k);
                         const unsigned long long inside = from - before - (__shfl_sync(kAll, upto, k) - (unsigned long long)steps * P.C.heads);
                         if (lane == 0) {
-                            const uint32_t head = (uint32_t)inside / steps, step = (uint32_t)inside % steps;
+                            const uint32_t head = (uint32_t)(inside / steps), step = (uint32_t)(inside % steps);
                             s_start[0] = b;
                             s_start[1] = t0 + k;
                             s_start[2] = head;
