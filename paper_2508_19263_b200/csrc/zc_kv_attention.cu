@@ -131,7 +131,10 @@ zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, co
     P.lse = args->d_lse;
     P.q_heads = args->q_heads;
     P.group = args->q_heads / cache->kv_heads;
-    P.scale_log2 = args->scale * 1.44269504f;
+    P.scale_mantissa = 2.0f * (float)frexp((double)args->scale * 1.4426950408889634, &P.scale_exponent);
+    if (args->scale == 0.0f) { P.scale_mantissa = 1.0f; P.scale_exponent = -1000; }          // the least that logit_factor gives
+    else if (fabsf(P.scale_mantissa) == 2.0f) P.scale_mantissa *= 0.5f;
+    else --P.scale_exponent;
     P.causal = args->causal;
     P.window = args->window;
     P.workspace = (uint8_t*)d_workspace;

@@ -12,7 +12,8 @@ struct AttentionParams {
     float* lse;
     uint8_t* workspace;
     uint32_t q_heads, group;
-    float scale_log2;                   // scale * log2(e): exponentials are powers of two
+    float scale_mantissa;               // scale * log2(e), since exponentials are powers of two: +-1 .. 2, times 2^scale_exponent
+    int scale_exponent;
     uint32_t causal, window;
     uint32_t half_type;                 // queries and results in FP16, else BF16
     uint32_t q_wide, out_wide;          // four neighbours begin on 8 bytes
@@ -256,5 +257,11 @@ __device__ __forceinline__ int query_lift(float most)
     return e == 255 || most == 0.0f ? 0 : min(14 - ((int)e - 127), 126);
 }
 __device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }      // -126 .. 127
+// What makes a logit (times log2(e)) of a product that is over 2^-e, as far as FP32's normal numbers go.  Above 0, that the largest product is the largest logit
+// and -infinity stays: the scale's sign is with the queries.  One power of two for scale, queries and keys together: each for itself may be beyond FP32 where the logit is not.
+__device__ __forceinline__ float logit_factor(const AttentionParams& P, int e)
+{
+    return __uint_as_float((uint32_t)min(max(P.scale_exponent + e + 127, 1), 254) << 23 | (__float_as_uint(P.scale_mantissa) & 0x7FFFFFu));
+}
 
 }  // namespace zc

@@ -440,9 +440,10 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
         const uint32_t half = warp >> 2, row = threadIdx.x & 127, at = tmem + half * S::kHalf + (((warp & 3) * 32) << 16);
         const uint32_t my_s = s_full + 8 * half, my_p = p_full + 8 * half, my_o = o_full + 8 * half;
         unsigned long long item_from = s_item_from;
-        float factor = 0.0f, top = -INFINITY, sum = 0.0f;
+        float top = -INFINITY, sum = 0.0f;
         int lo = 0, hi = 0x7FFFFFFF, lo_most = 0, hi_least = 0;
         uint32_t col = 0, v_ref = 0, turns = 0;               // turns: steps in which the half had rows
+        int up = 0;                                           // the query is over 2^-up
         bool fresh = true, goes_on = false;
         for (uint32_t j = 0; j < count; ++j) {
             const uint32_t par = j & 1, cols = (uint32_t)c.n * P.group, first_col = c.tile * 256 + half * 128;
@@ -471,8 +472,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                                 most = fmaxf(fmaxf(most, fmaxf(fabsf(x.x), fabsf(x.y))), fmaxf(fabsf(y.x), fabsf(y.y)));
                             }
                         }
-                    const int up = query_lift(most);
-                    const float lift = copysignf(power_of_two(up), P.scale_log2);
+                    up = query_lift(most);
+                    const float lift = copysignf(power_of_two(up), P.scale_mantissa);
                     for (uint32_t k = 0; k < S::kDim / 8; k += 4) {
                         uint2 w[8] = {};
                         if (col < cols)
@@ -489,7 +490,6 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                             sts128(q_tile + half * S::kTile + tile_at(row, k + i), h);
                         }
                     }
-                    factor = ldexpf(fabsf(P.scale_log2), -up);
                     fence_async_shared();
                     bar_arrive(q_full + 8 * half);
                     top = -INFINITY;
@@ -501,8 +501,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                 const uint32_t k_ref = s_ref[par][0], new_ref = s_ref[par][1];
                 const bool plain = t0 >= lo_most && t0 + 128 <= hi_least && (s_gone[par][0] | s_gone[par][1] | s_gone[par][2] | s_gone[par][3]) == 0 &&
                                    (s_poisoned[par][0] | s_poisoned[par][1] | s_poisoned[par][2] | s_poisoned[par][3]) == 0;
-                // above 0, that the largest product is the largest logit and -infinity stays
-                const float f = fmaxf(factor * (e8m0_value(k_ref) * (1.0f / (float)(1u << S::kLift))), 1.17549435e-38f);
+                const float f = logit_factor(P, (int)k_ref - 127 - S::kLift - up);
                 if (!plain) {
                     // what the row does not see, in place
 #pragma unroll 1

@@ -11,7 +11,9 @@
 // as they are, by ldmatrix (transposed for V), and become FP16 in registers (one conversion for two elements, exact).  The order in which the
 // sum over a head's width goes is free, so Q is laid out in the order in which ldmatrix gives K's nibbles.
 //   Keys' scales multiply the FP32 sums of each 32 products, values' scales the weights: a block of 32 of the head's width has weights of its own,
-// 2^(s - R) times the softmax's, R the largest scale byte that the item's run has met.  So elements go into the products as they are.
+// 2^(s - R) times the softmax's, R the largest scale byte that the item's run has met.  So elements go into the products as they are.  Keys' scales are taken over 2^0, and
+// over the largest that the run has met from the first of 2^65 or more on, or where queries and scale are far from 1: products, or what makes logits of them, could be
+// beyond FP32 where the logits are not.
 //   Queries become FP16 over a power of two that brings the row's largest to 2^14 .. 2^15: BF16's eight bits are kept down to 2^-31 of it.
 //   Weights are 2^(x - max + 15), in FP32 for the sum, rounded to FP16 for the product with V: off by at most 2^-12 of it where it is above 2^-29 of the
 // largest (the scale's power of two counted in), by 2^-40 of the largest below.
@@ -125,6 +127,24 @@ __device__ __forceinline__ void mma_f16_first(float c[4], uint32_t a0, uint32_t 
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
                  : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(zero[0]), "f"(zero[1]), "f"(zero[2]), "f"(zero[3]));
 }
+// The largest of a lane's scale bytes, NaN (255) left out.  A word has four bytes, or two in its low half.
+template <bool FOUR, uint32_t N>
+__device__ __forceinline__ uint32_t largest_scale(const uint32_t (&w)[N])
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < N; ++j)
+#pragma unroll
+        for (uint32_t k = 0; k < (FOUR ? 4 : 2); ++k)
+            if (((w[j] >> (8 * k)) & 0xFF) != 255) most = max(most, (w[j] >> (8 * k)) & 0xFF);
+    return most;
+}
+// 2^(s - ref) in FP32, s <= ref; NaN for 255.
+__device__ __forceinline__ uint32_t key_factor(uint32_t s, uint32_t ref)
+{
+    const int e = (int)s - (int)ref + 127;
+    return s == 255 ? 0x7FFFFFFFu : e > 0 ? (uint32_t)e << 23 : 0x400000u >> min(-e, 31);
+}
 // 2^(s - ref) in FP16, s <= ref; NaN for 255.
 __device__ __forceinline__ uint32_t value_factor(uint32_t s, uint32_t ref)
 {
@@ -132,9 +152,9 @@ __device__ __forceinline__ uint32_t value_factor(uint32_t s, uint32_t ref)
     return s == 255 ? 0x7E00u : e > 0 ? (uint32_t)e << 10 : 0x400u >> min(1 - e, 31);
 }
 
-// Query of a column in the order of the keys' elements in a lane's registers, in FP16 times 2^k; factor: what makes a logit of a product.
+// Query of a column in the order of the keys' elements in a lane's registers, in FP16 times 2^lift, with the scale's sign.
 template <typename S>
-__device__ __forceinline__ void load_queries(const AttentionParams& P, const typename S::Place& c, uint32_t col, uint32_t i, uint32_t q[S::kDim / 8], float& factor)
+__device__ __forceinline__ void load_queries(const AttentionParams& P, const typename S::Place& c, uint32_t col, uint32_t i, uint32_t q[S::kDim / 8], int& lift)
 {
 #pragma unroll
     for (uint32_t k = 0; k < S::kDim / 8; ++k) q[k] = 0;
@@ -156,15 +176,13 @@ __device__ __forceinline__ void load_queries(const AttentionParams& P, const typ
     }
     most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
     most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-    const int k = query_lift(most);
-    const float lift = copysignf(power_of_two(k), P.scale_log2);
+    lift = query_lift(most);
+    const float up = copysignf(power_of_two(lift), P.scale_mantissa);
 #pragma unroll
     for (uint32_t j = 0; j < S::kDim / 8; ++j) {
         const float2 f = query_pair(P, q[j]);
-        q[j] = pack_half(f.x * lift, f.y * lift);
+        q[j] = pack_half(f.x * up, f.y * up);
     }
-    // above 0, that the largest product is the largest logit and -infinity stays: the scale's sign is with the queries
-    factor = fmaxf(ldexpf(fabsf(P.scale_log2), -k), 1.17549435e-38f);
 }
 template <typename S>
 __device__ __forceinline__ float* partial_of(const AttentionParams& P, uint32_t blocks, uint32_t block, uint32_t slot)
@@ -235,6 +253,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
     __shared__ unsigned long long s_cost[ZC_KV_MAX_SEQS / 32];
     __shared__ StreamEntry s_entry[S::kWarps * 2];
     __shared__ uint8_t s_order[S::kWarps][32];
+    __shared__ int8_t s_lift[S::kWarps][S::kCols];        // queries are over 2^-lift
     __shared__ volatile uint32_t s_failed;
     constexpr uint32_t kAll = 0xFFFFFFFFu;
     const uint32_t lane = threadIdx.x & 31, warp = warp_index(), g = lane >> 2, i = lane & 3;
@@ -372,22 +391,31 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
     float zero[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) asm volatile("mov.b32 %0, 0;" : "=f"(zero[k]));
-    uint32_t ref = 0;
-    bool fresh = true, ok = true;
+    uint32_t ref = 0, key_ref = 0;                       // scale bytes that values' and keys' scales are over
+    bool fresh = true, ok = true, careful = false;       // careful: key_ref is the largest so far, else 127
+    auto set_factors = [&]() {
+#pragma unroll
+        for (uint32_t t = 0; t < S::kNt; ++t) {
+            const float own = logit_factor(P, (int)key_ref - 127 - s_lift[warp][8 * t + g]);
+            factor[t][0] = __shfl_sync(kAll, own, 8 * i);
+            factor[t][1] = __shfl_sync(kAll, own, 8 * i + 4);
+        }
+    };
     uint32_t st = 0, parity = 0;
     for (uint32_t done = 0; done < count; ++done) {
         if (fresh) {
             // the item's columns: queries, limits
             fresh = false;
             ref = 0;
+            careful = false;
             lo_most = 0;
             hi_least = 0x7FFFFFFF;
 #pragma unroll
             for (uint32_t t = 0; t < S::kNt; ++t) {
-                float own;
-                load_queries<S>(P, at, at.tile * S::kCols + 8 * t + g, i, q[t], own);
-                factor[t][0] = __shfl_sync(kAll, own, 8 * i);
-                factor[t][1] = __shfl_sync(kAll, own, 8 * i + 4);
+                int lift;
+                load_queries<S>(P, at, at.tile * S::kCols + 8 * t + g, i, q[t], lift);
+                if (i == 0) s_lift[warp][8 * t + g] = (int8_t)lift;
+                careful |= abs(P.scale_exponent - lift) > 100;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const uint32_t col = at.tile * S::kCols + 8 * t + 2 * i + k;
@@ -402,6 +430,10 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
 #pragma unroll
                     for (int k = 0; k < 4; ++k) acc[t][m][k] = 0.0f;
             }
+            careful = __any_sync(kAll, careful);
+            __syncwarp();
+            key_ref = careful ? 0 : 127;
+            set_factors();
             lo_most = __reduce_max_sync(kAll, lo_most);
             hi_least = __reduce_min_sync(kAll, hi_least);
         }
@@ -439,7 +471,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                 hide |= nan;
                 if (hide) {
                     hidden |= 1u << j;
-                    vs[j] = 0;
+                    ks[j] = vs[j] = 0;
                     if (!S::kFp4) {
                         const uint32_t none[4] = {};
 #pragma unroll
@@ -449,16 +481,30 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                 }
             }
         }
-        // keys' scales, [token][block] in FP32
+        {
+            // keys' scales, [token][block] in FP32
+            uint32_t big = 0;                            // of 192 or more
 #pragma unroll
-        for (uint32_t j = 0; j < S::kOwn; ++j) {
-            uint32_t f[4];
+            for (uint32_t j = 0; j < S::kOwn; ++j) {
+                uint32_t f[4];
+                big |= ks[j] & (ks[j] << 1) & 0x80808080u;
 #pragma unroll
-            for (uint32_t k = 0; k < S::kBlocks; ++k) f[k] = __float_as_uint(e8m0_value((ks[j] >> (8 * k)) & 0xFF));
-            if (S::kBlocks == 4) sts128(factors + 16 * (32 * j + lane), f);
-            else sts64(factors + 8 * (32 * j + lane), f[0], f[1]);
+                for (uint32_t k = 0; k < S::kBlocks; ++k) f[k] = max((k < 3 ? ks[j] << (k < 3 ? 23 - 8 * k : 0) : ks[j] >> 1) & 0x7F800000u, 0x00400000u);
+                if (S::kBlocks == 4) sts128(factors + 16 * (32 * j + lane), f);
+                else sts64(factors + 8 * (32 * j + lane), f[0], f[1]);
+            }
+            careful = __any_sync(kAll, careful || big);
+            if (careful) {
+                key_ref = max(key_ref, __reduce_max_sync(kAll, largest_scale<S::kBlocks == 4>(ks)));
+                set_factors();
+#pragma unroll 1
+                for (uint32_t k = 0; k < S::kOwn * S::kBlocks; ++k) {
+                    const uint32_t j = k / S::kBlocks, b = k % S::kBlocks, w = j ? ks[S::kOwn - 1] : ks[0];
+                    sts_f1(factors + 4 * (S::kBlocks * (32 * j + lane) + b), __uint_as_float(key_factor((w >> (8 * b)) & 0xFF, key_ref)));
+                }
+            }
+            __syncwarp();
         }
-        __syncwarp();
 
         // logits, 16 tokens at a time: rows g and g + 8, columns 2i and 2i + 1.  They wait for the step's maximum where their keys were.
         float best[S::kNt][2];
@@ -584,12 +630,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
             }
             if (mine == 255) {
                 odd = true;
-                mine = 0;
-#pragma unroll
-                for (uint32_t j = 0; j < S::kOwn; ++j)
-#pragma unroll
-                    for (uint32_t k = 0; k < S::kBlocks; ++k)
-                        if (((vs[j] >> (8 * k)) & 0xFF) != 255) mine = max(mine, (vs[j] >> (8 * k)) & 0xFF);
+                mine = largest_scale<S::kBlocks == 4>(vs);
             }
             const uint32_t most = __reduce_max_sync(kAll, mine);
             if (most > ref) {
