@@ -225,14 +225,12 @@ __device__ __forceinline__ void store_out(const AttentionParams& P, uint8_t* out
         for (uint32_t k = 0; k < N; ++k) reinterpret_cast<uint16_t*>(out)[k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
     }
 }
+// What divides sums by their weights; 0 where nothing was seen.
+__device__ __forceinline__ float inverse_weight(float weight) { return weight == 0.0f ? 0.0f : 1.0f / weight; }
 // A joined column: a lane has N neighbours from d on.
 template <uint32_t N>
-__device__ __forceinline__ void finish_column(const AttentionParams& P, const ItemColumns& c, uint32_t in_tile, uint32_t d, const float* sums, float top, float weight)
+__device__ __forceinline__ void finish_column(const AttentionParams& P, const ItemColumns& c, uint32_t in_tile, uint32_t d, const float* v, float top, float weight)
 {
-    const float norm = weight == 0.0f ? 0.0f : 1.0f / weight;
-    float v[N];
-#pragma unroll
-    for (uint32_t k = 0; k < N; ++k) v[k] = sums[k] * norm;
     const uint32_t col = c.first + in_tile, head = c.head * P.group + col % P.group;
     const uint64_t row = (uint64_t)c.row0 + col / P.group;
     store_out<N>(P, P.out.d + row * P.out.ld_row + head * P.out.ld_head, d, v);

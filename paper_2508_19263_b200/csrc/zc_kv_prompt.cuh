@@ -579,8 +579,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                     const unsigned long long item_to = item_from + c.steps;
                     const bool begins = item_from >= from, whole = begins && item_to <= to;
                     const float weight = sum * (1.0f / 16384.0f);
-                    const float unit = e8m0_value(v_ref), norm = whole ? (weight == 0.0f ? 0.0f : 1.0f / weight) : 1.0f;
                     constexpr float kDown = 1.0f / 16384.0f / (float)(1u << S::kLift);
+                    const float unit = e8m0_value(v_ref), norm = kDown * inverse_weight(weight);        // before `unit`: the sum itself may be beyond FP32
                     const bool mine = col < cols;
                     const uint32_t head = c.head * P.group + col % P.group;
                     const uint64_t out_row = (uint64_t)c.row0 + col / P.group;
@@ -592,7 +592,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                         tmem_ld32_async(at + S::kO + 32 * k, v);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = v[i] * kDown * unit * norm;
+                        for (int i = 0; i < 32; ++i) v[i] = v[i] * norm * unit;
                         if (!mine) continue;
 #pragma unroll
                         for (int i = 0; i < 32; i += 4) {

@@ -42,7 +42,7 @@ struct StreamShape {
     // 12 warps of 168 registers where 8 columns are all, 8 of 255 for 16
     static constexpr uint32_t kWarps = NT_ == 1 ? 12 : 8, kStages = kRow == 32 ? 3 : 2;
     using Place = Cursor<kCols, kStep>;
-    // a part: sums [kCols][kDim + 4] (the padding spreads lanes over the banks), largest logits [kCols], sums of weights [kCols]
+    // a part: means of values [kCols][kDim + 4] (the padding spreads lanes over the banks), largest logits [kCols], sums of weights [kCols]
     static constexpr uint32_t kPartLd = kDim + 4, kPart = kCols * (kPartLd + 2);
     // shared memory of a warp
     static constexpr uint32_t kRing = kStages * kStage, kRingScales = kStages * 2 * kScales;
@@ -194,10 +194,11 @@ __device__ __forceinline__ float* part_in_workspace(const AttentionParams& P, ui
 {
     return partial_of<S>(P, gridDim.x, gridDim.x, 0) + (size_t)warp * S::kPart;
 }
-// The joined sums of a column whose parts begin at part(k), 0 <= k < count, all lanes together: a lane has kDim / 32 neighbours.
-// `at` and `weights` say where in a part the largest logit and the sum of weights of the column are, `sums` where its sums begin.
+// The joined means of a column whose parts begin at part(k), 0 <= k < count, all lanes together: a lane has kDim / 32 neighbours.  Parts hold means, not
+// sums, and are joined with shares that add up to 1: a sum may be beyond FP32 where the mean is not.
+// `at` and `weights` say where in a part the largest logit and the sum of weights of the column are, `means` where its means begin.
 template <typename S, typename PART>
-__device__ __forceinline__ void join_parts(uint32_t count, PART part, uint32_t sums, uint32_t at, uint32_t weights, float v[S::kDim / 32], float& best, float& weight)
+__device__ __forceinline__ void join_parts(uint32_t count, PART part, uint32_t means, uint32_t at, uint32_t weights, float v[S::kDim / 32], float& best, float& weight)
 {
     constexpr uint32_t N = S::kDim / 32;
     const uint32_t lane = threadIdx.x & 31;
@@ -214,7 +215,7 @@ __device__ __forceinline__ void join_parts(uint32_t count, PART part, uint32_t s
         auto read = [&](uint32_t k1) {
 #pragma unroll
             for (uint32_t k = 0; k < kAtOnce; ++k) {
-                const float* p = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(mine), (k1 + k) & 31)) + sums + lane * N;
+                const float* p = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(mine), (k1 + k) & 31)) + means + lane * N;
                 if (k1 + k >= some) continue;
                 if (N == 4) { const float4 y = *reinterpret_cast<const float4*>(p); x[k][0] = y.x; x[k][1] = y.y; x[k][N - 2] = y.z; x[k][N - 1] = y.w; }
                 else { const float2 y = *reinterpret_cast<const float2*>(p); x[k][0] = y.x; x[k][1] = y.y; }
@@ -225,18 +226,19 @@ __device__ __forceinline__ void join_parts(uint32_t count, PART part, uint32_t s
         float next = t;
         for (int d = 16; d; d >>= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, d));
         next = fmaxf(next, best);
-        const float off = next == -INFINITY ? 0.0f : next, old = exp2_fast(best - off), now = exp2_fast(t - off);
+        const float off = next == -INFINITY ? 0.0f : next, old = weight * exp2_fast(best - off), now = w * exp2_fast(t - off);
         best = next;
-        float sum = w * now;
+        float sum = now;
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-        weight = fmaf(weight, old, sum);
+        weight = old + sum;
+        const float norm = inverse_weight(weight), share = now * norm;
 #pragma unroll
-        for (uint32_t n = 0; n < N; ++n) v[n] *= old;
+        for (uint32_t n = 0; n < N; ++n) v[n] *= old * norm;
         for (uint32_t k1 = 0; k1 < some; k1 += kAtOnce) {
             if (k1) read(k1);
 #pragma unroll
             for (uint32_t k = 0; k < kAtOnce; ++k) {
-                const float f = __shfl_sync(0xFFFFFFFFu, now, (k1 + k) & 31);
+                const float f = __shfl_sync(0xFFFFFFFFu, share, (k1 + k) & 31);
                 if (k1 + k < some)
 #pragma unroll
                     for (uint32_t n = 0; n < N; ++n) v[n] = fmaf(x[k][n], f, v[n]);
@@ -734,7 +736,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                 for (int k = 0; k < 2; ++k) {
                     const uint32_t in_tile = 8 * t + 2 * i + k, col = at.tile * S::kCols + in_tile;
                     const float total_weight = sum[t][k] * (1.0f / 32768.0f);
-                    const float norm = whole ? (total_weight == 0.0f ? 0.0f : 1.0f / total_weight) : 1.0f;
+                    const float norm = kDown * inverse_weight(total_weight);         // before `unit`: the sum itself may be beyond FP32
                     uint8_t* out = nullptr;
                     if (whole && at.has(P, col)) {
                         out = at.out(P, col);
@@ -744,11 +746,11 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                     for (uint32_t m = 0; m < S::kTiles; m += S::kFp4 ? 2 : 1) {
                         constexpr uint32_t kSide = S::kFp4 ? 4 : 2;        // neighbours of the head's width
                         float v[4];
-                        v[0] = acc[t][m][k] * kDown * unit * norm;
-                        v[1] = acc[t][m][k + 2] * kDown * unit * norm;
+                        v[0] = acc[t][m][k] * norm * unit;
+                        v[1] = acc[t][m][k + 2] * norm * unit;
                         if (S::kFp4) {
-                            v[2] = acc[t][m + 1][k] * kDown * unit * norm;
-                            v[3] = acc[t][m + 1][k + 2] * kDown * unit * norm;
+                            v[2] = acc[t][m + 1][k] * norm * unit;
+                            v[3] = acc[t][m + 1][k + 2] * norm * unit;
                         }
                         const uint32_t d = 16 * m + kSide * g;
                         if (out) store_out<kSide>(P, out, d, v);

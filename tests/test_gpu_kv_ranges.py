@@ -33,3 +33,14 @@ def test_tiny_queries_are_not_rounded_up(new, fmt, shift):
     case.cache.k_scales.add_(shift)
     got = zc.kv_attention(case.cache, case.batch, q * 2.0 ** -shift, torch.empty_like(q), ws)
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("lens,new", [([333, 65], [1, 1]), ([333, 65], [70, 1]), ([20000], [1]), ([5000], [64])])
+@pytest.mark.parametrize("fmt,low,high", [(FP4, 60, 64), (FP4, 118, 124), (FP4, 123, 124), (E4M3, 110, 118), (E4M3, 117, 118)])
+def test_value_scales_over_all_of_their_range(lens, new, fmt, low, high):
+    # sums of values that are far beyond FP32, means that are not
+    case = ref.Case(zc, fmt, 128, 16, 2, lens, new, low=low, high=high)
+    case.cache.k_scales.random_(120, 124, generator=torch.Generator(device="cuda").manual_seed(1))
+    case.cache.v_elems.bitwise_and_(0x77 if fmt == FP4 else 0x7F)                    # of one sign
+    out, _ = check(case, queries(case, 4, BF16))
+    assert bool(torch.isfinite(out).all())
