@@ -39,7 +39,8 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float lse_of(float top, float weight) { return weight == 0.0f ? -INFINITY : (top + log2f(weight)) * 0.69314718f; }
+// of a sum of weights over 2^unit
+__device__ __forceinline__ float lse_of(float unit, float weight) { return weight == 0.0f ? -INFINITY : (unit + log2f(weight)) * 0.69314718f; }
 // whether one of four E4M3 bytes is NaN
 __device__ __forceinline__ bool nan_bytes(uint32_t w)
 {
@@ -257,9 +258,22 @@ __device__ __forceinline__ int query_lift(float most)
 __device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }      // -126 .. 127
 // What makes a logit (times log2(e)) of a product that is over 2^-e, as far as FP32's normal numbers go.  Above 0, that the largest product is the largest logit
 // and -infinity stays: the scale's sign is with the queries.  One power of two for scale, queries and keys together: each for itself may be beyond FP32 where the logit is not.
-__device__ __forceinline__ float logit_factor(const AttentionParams& P, int e)
+// Without the scale's mantissa (its bits are scale_mantissa_bits) for who has that with the keys' scales.
+__device__ __forceinline__ float logit_power(const AttentionParams& P, int e) { return __uint_as_float((uint32_t)min(max(P.scale_exponent + e + 127, 1), 254) << 23); }
+__device__ __forceinline__ uint32_t scale_mantissa_bits(const AttentionParams& P) { return __float_as_uint(P.scale_mantissa) & 0x7FFFFFu; }
+__device__ __forceinline__ float logit_factor(const AttentionParams& P, int e) { return __uint_as_float(__float_as_uint(logit_power(P, e)) | scale_mantissa_bits(P)); }
+
+// Weights are 2^(logit - unit).  A largest logit beyond what FP16 has for a weight moves the unit so that the largest weight is 2^14 .. 2^15, and gives what sums so far shrink by.
+//   The unit is a whole number, so that a weight's exponent, factor * product - unit, is what it should be: the rounding of a unit that is the largest logit itself
+// would be in it, which from 2^24 on puts the largest weight beyond FP16 or makes nothing of it.  From 2^23 on, where logits are whole numbers, it is the logit.
+//   The product is not rounded in that exponent, the largest logit is: from kFarLogit on, where that is 2^-5 and more, products have to be rounded as well, or exact.
+constexpr float kFarLogit = 524288.0f;
+__device__ __forceinline__ float move_unit(float& unit, float largest)
 {
-    return __uint_as_float((uint32_t)min(max(P.scale_exponent + e + 127, 1), 254) << 23 | (__float_as_uint(P.scale_mantissa) & 0x7FFFFFu));
+    if (!(largest - unit > 15.9f)) return 1.0f;            // also where both are -infinity
+    const float whole = ceilf(largest), to = fabsf(whole) < 8388608.0f ? whole - 15.0f : whole, shrink = exp2_fast(unit - to);
+    unit = to;
+    return shrink;
 }
 
 }  // namespace zc

@@ -11,8 +11,8 @@
 // the head's width fastest, which for this product is the outer axis.  S and O, FP32, of both halves are all of tensor memory's 512 columns (head_dim 128).
 //   Keys and values are element * 2^(s - R + kLift), R the largest scale byte that the item has met, for keys and for values: exact unless a scale is 2^-35 (E4M3:
 // 2^-22) of the largest, off by at most 2^-25 / 2^kLift of 2^R then.  Queries as in the other kernel.
-//   Weights are 2^(x - m + 14) with m at most 1 below the row's largest so far: so the sums in tensor memory are only touched when it grows by more than
-// a factor of 2.  They are rounded to FP16: off by at most 2^-12 of it down to 2^-28 of the largest, by 2^-39 of the largest below; the sum of weights is FP32.
+//   Weights are 2^(x - u) as in the other kernel: the sums in tensor memory are only touched when a row's largest weight grows by a factor of 1.8 or more.
+// They are rounded to FP16: off by at most 2^-12 of it down to 2^-28 of the largest, by 2^-39 of the largest below; the sum of weights is FP32.
 //   Measured: 2048 rows, 32 heads, behind 32768 tokens in FP4: 1252 us, 906 TFLOP/s; of a step's 5100 cycles the tensor cores work 2050, a half's softmax takes 3000 (the
 // special function units 1024 of it).  Two blocks an SM with 128 rows each: 1634 us.  16 warps for the softmax, half a row a thread: 1379 us, the four that are
 // left for keys and values do not keep up.  A quarter of the exponentials by a polynomial on the FP32 units: 1 % less time.  (One B200, a graph of 20 calls.)
@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                 const uint32_t k_ref = s_ref[par][0], new_ref = s_ref[par][1];
                 const bool plain = t0 >= lo_most && t0 + 128 <= hi_least && (s_gone[par][0] | s_gone[par][1] | s_gone[par][2] | s_gone[par][3]) == 0 &&
                                    (s_poisoned[par][0] | s_poisoned[par][1] | s_poisoned[par][2] | s_poisoned[par][3]) == 0;
-                const float f = logit_factor(P, (int)k_ref - 127 - S::kLift - up);
+                float f = logit_factor(P, (int)k_ref - 127 - S::kLift - up);
                 if (!plain) {
                     // what the row does not see, in place
 #pragma unroll 1
@@ -529,17 +529,13 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
 #pragma unroll
                     for (int i = 0; i < 16; ++i) most[i & 3] = fmaxf(most[i & 3], fmaxf(v[2 * i], v[2 * i + 1]));
                 }
-                float best = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-                best *= f;
+                const float best = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * f;
                 // the sums in tensor memory are over 2^top of the weights and 2^v_ref of the values
-                float shrink = 1.0f;
-                if (best > top + 1.0f) {
-                    shrink = exp2_fast(top - best);
-                    top = best;
-                }
+                float shrink = move_unit(top, best);
                 sum *= shrink;
                 if (!fresh && new_ref != v_ref) shrink *= ldexpf(1.0f, max((int)v_ref - (int)new_ref, -200));
-                if (!fresh && __any_sync(kAll, shrink != 1.0f)) {
+                if (__any_sync(kAll, shrink != 1.0f || fabsf(best) >= kFarLogit)) {
+                    if (!fresh)
 #pragma unroll 1
                     for (uint32_t k = 0; k < S::kDim / 32; ++k) {
                         float v[32];
@@ -549,9 +545,23 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                         for (int i = 0; i < 32; i += 2) mul_pair(v[i], v[i + 1], shrink);
                         tmem_st32(at + S::kO + 32 * k, v);
                     }
+                    if (__any_sync(kAll, fabsf(best) >= kFarLogit && best != -INFINITY)) {
+                        // logits as large as this are rounded before their differences are taken
+#pragma unroll 1
+                        for (uint32_t k = 0; k < 4; ++k) {
+                            float v[32];
+                            tmem_ld32_async(at + 32 * k, v);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) mul_pair(v[i], v[i + 1], f);
+                            tmem_st32(at + 32 * k, v);
+                        }
+                        tmem_st_wait();
+                        f = 1.0f;
+                    }
                 }
                 v_ref = new_ref;
-                const float off = top == -INFINITY ? 14.0f : 14.0f - top;
+                const float off = top == -INFINITY ? 0.0f : -top;
                 float more[2] = {0.0f, 0.0f};
 #pragma unroll 1
                 for (uint32_t k = 0; k < 4; ++k) {
@@ -578,8 +588,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                     tc_fence_after();
                     const unsigned long long item_to = item_from + c.steps;
                     const bool begins = item_from >= from, whole = begins && item_to <= to;
-                    const float weight = sum * (1.0f / 16384.0f);
-                    constexpr float kDown = 1.0f / 16384.0f / (float)(1u << S::kLift);
+                    const float weight = sum;
+                    constexpr float kDown = 1.0f / (float)(1u << S::kLift);
                     const float unit = e8m0_value(v_ref), norm = kDown * inverse_weight(weight);        // before `unit`: the sum itself may be beyond FP32
                     const bool mine = col < cols;
                     const uint32_t head = c.head * P.group + col % P.group;

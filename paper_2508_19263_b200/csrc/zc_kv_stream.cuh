@@ -15,8 +15,8 @@
 // over the largest that the run has met from the first of 2^65 or more on, or where queries and scale are far from 1: products, or what makes logits of them, could be
 // beyond FP32 where the logits are not.
 //   Queries become FP16 over a power of two that brings the row's largest to 2^14 .. 2^15: BF16's eight bits are kept down to 2^-31 of it.
-//   Weights are 2^(x - max + 15), in FP32 for the sum, rounded to FP16 for the product with V: off by at most 2^-12 of it where it is above 2^-29 of the
-// largest (the scale's power of two counted in), by 2^-40 of the largest below.
+//   Weights are 2^(x - u), u a whole number so that the largest is 2^14 .. 2^15.9, in FP32 for the sum, rounded to FP16 for the product with V: off by at most 2^-12 of it
+// where it is above 2^-28 of the largest (the scale's power of two counted in), by 2^-39 of the largest below.
 //   Measured: one token for 64 sequences of 2200 to 8200 tokens, 32 heads of queries over 8 in FP4: 108 us, 3.6 TB/s; the copies alone take 79 us, what is left are the
 // conversions' instructions: 600 for 32 tokens, of them 130 conversions and about 100 that bring a conversion its byte, at three warps a scheduler.  A call's
 // fixed part is 14 us (one sequence of 4096 tokens): a chain of reads (lengths, pages, elements), one step, joins in the block and between blocks.
@@ -42,7 +42,7 @@ struct StreamShape {
     // 12 warps of 168 registers where 8 columns are all, 8 of 255 for 16
     static constexpr uint32_t kWarps = NT_ == 1 ? 12 : 8, kStages = kRow == 32 ? 3 : 2;
     using Place = Cursor<kCols, kStep>;
-    // a part: means of values [kCols][kDim + 4] (the padding spreads lanes over the banks), largest logits [kCols], sums of weights [kCols]
+    // a part: means of values [kCols][kDim + 4] (the padding spreads lanes over the banks), what weights are over [kCols], sums of weights [kCols]
     static constexpr uint32_t kPartLd = kDim + 4, kPart = kCols * (kPartLd + 2);
     // shared memory of a warp
     static constexpr uint32_t kRing = kStages * kStage, kRingScales = kStages * 2 * kScales;
@@ -139,11 +139,11 @@ __device__ __forceinline__ uint32_t largest_scale(const uint32_t (&w)[N])
             if (((w[j] >> (8 * k)) & 0xFF) != 255) most = max(most, (w[j] >> (8 * k)) & 0xFF);
     return most;
 }
-// 2^(s - ref) in FP32, s <= ref; NaN for 255.
-__device__ __forceinline__ uint32_t key_factor(uint32_t s, uint32_t ref)
+// (1 + mantissa / 2^23) 2^(s - ref) in FP32, s <= ref; NaN for 255.
+__device__ __forceinline__ uint32_t key_factor(uint32_t s, uint32_t ref, uint32_t mantissa)
 {
     const int e = (int)s - (int)ref + 127;
-    return s == 255 ? 0x7FFFFFFFu : e > 0 ? (uint32_t)e << 23 : 0x400000u >> min(-e, 31);
+    return s == 255 ? 0x7FFFFFFFu : e > 0 ? (uint32_t)e << 23 | mantissa : (0x800000u | mantissa) >> min(1 - e, 31);
 }
 // 2^(s - ref) in FP16, s <= ref; NaN for 255.
 __device__ __forceinline__ uint32_t value_factor(uint32_t s, uint32_t ref)
@@ -196,7 +196,7 @@ __device__ __forceinline__ float* part_in_workspace(const AttentionParams& P, ui
 }
 // The joined means of a column whose parts begin at part(k), 0 <= k < count, all lanes together: a lane has kDim / 32 neighbours.  Parts hold means, not
 // sums, and are joined with shares that add up to 1: a sum may be beyond FP32 where the mean is not.
-// `at` and `weights` say where in a part the largest logit and the sum of weights of the column are, `means` where its means begin.
+// `at` and `weights` say where in a part that which weights are over and the sum of weights of the column are, `means` where its means begin.
 template <typename S, typename PART>
 __device__ __forceinline__ void join_parts(uint32_t count, PART part, uint32_t means, uint32_t at, uint32_t weights, float v[S::kDim / 32], float& best, float& weight)
 {
@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
     auto set_factors = [&]() {
 #pragma unroll
         for (uint32_t t = 0; t < S::kNt; ++t) {
-            const float own = logit_factor(P, (int)key_ref - 127 - s_lift[warp][8 * t + g]);
+            const float own = logit_power(P, (int)key_ref - 127 - s_lift[warp][8 * t + g]);
             factor[t][0] = __shfl_sync(kAll, own, 8 * i);
             factor[t][1] = __shfl_sync(kAll, own, 8 * i + 4);
         }
@@ -484,14 +484,15 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
             }
         }
         {
-            // keys' scales, [token][block] in FP32
+            // keys' scales times the mantissa of the call's, [token][block] in FP32: what is left of `factor` is a power of two
+            const uint32_t mantissa = scale_mantissa_bits(P);
             uint32_t big = 0;                            // of 192 or more
 #pragma unroll
             for (uint32_t j = 0; j < S::kOwn; ++j) {
                 uint32_t f[4];
                 big |= ks[j] & (ks[j] << 1) & 0x80808080u;
 #pragma unroll
-                for (uint32_t k = 0; k < S::kBlocks; ++k) f[k] = max((k < 3 ? ks[j] << (k < 3 ? 23 - 8 * k : 0) : ks[j] >> 1) & 0x7F800000u, 0x00400000u);
+                for (uint32_t k = 0; k < S::kBlocks; ++k) f[k] = max((k < 3 ? ks[j] << (k < 3 ? 23 - 8 * k : 0) : ks[j] >> 1) & 0x7F800000u | mantissa, 0x00400000u | mantissa >> 1);       // the latter for 2^-127
                 if (S::kBlocks == 4) sts128(factors + 16 * (32 * j + lane), f);
                 else sts64(factors + 8 * (32 * j + lane), f[0], f[1]);
             }
@@ -502,7 +503,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
 #pragma unroll 1
                 for (uint32_t k = 0; k < S::kOwn * S::kBlocks; ++k) {
                     const uint32_t j = k / S::kBlocks, b = k % S::kBlocks, w = j ? ks[S::kOwn - 1] : ks[0];
-                    sts_f1(factors + 4 * (S::kBlocks * (32 * j + lane) + b), __uint_as_float(key_factor((w >> (8 * b)) & 0xFF, key_ref)));
+                    sts_f1(factors + 4 * (S::kBlocks * (32 * j + lane) + b), __uint_as_float(key_factor((w >> (8 * b)) & 0xFF, key_ref, mantissa)));
                 }
             }
             __syncwarp();
@@ -590,8 +591,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
             }
         }
 
-        // the largest so far, a power of two over it
-        bool grew = false;
+        // what weights are over, after the largest so far
+        bool moved = false;
         float shrink[S::kNt][2], off[S::kNt][2];
 #pragma unroll
         for (uint32_t t = 0; t < S::kNt; ++t)
@@ -601,14 +602,12 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                 x = fmaxf(x, __shfl_xor_sync(kAll, x, 4));
                 x = fmaxf(x, __shfl_xor_sync(kAll, x, 8));
                 x = fmaxf(x, __shfl_xor_sync(kAll, x, 16)) * factor[t][k];
-                grew |= x > top[t][k];
-                x = fmaxf(x, top[t][k]);
-                shrink[t][k] = x == -INFINITY ? 1.0f : exp2_fast(top[t][k] - x);
-                top[t][k] = x;
-                off[t][k] = x == -INFINITY ? 15.0f : 15.0f - x;
+                shrink[t][k] = move_unit(top[t][k], x);
+                moved |= shrink[t][k] != 1.0f;
+                off[t][k] = top[t][k] == -INFINITY ? 0.0f : -top[t][k];
                 sum[t][k] *= shrink[t][k];
             }
-        if (__any_sync(kAll, grew)) {
+        if (__any_sync(kAll, moved)) {
 #pragma unroll
             for (uint32_t t = 0; t < S::kNt; ++t)
 #pragma unroll
@@ -727,7 +726,6 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                     for (int d = 4; d < 32; d <<= 1) sum[t][k] += __shfl_xor_sync(kAll, sum[t][k], d);
             const bool whole = item_from >= from && item_to <= to;
             const float unit = e8m0_value(ref);
-            constexpr float kDown = 1.0f / 32768.0f;       // the weights' 2^15 goes here, once
             const uint32_t slot = done + 1 == count ? 1u : 0u;           // the run's last part goes where its copies were, an earlier one (there is one at most) to the workspace
             float* early = part_in_workspace<S>(P, blockIdx.x * S::kWarps + warp);
 #pragma unroll
@@ -735,8 +733,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const uint32_t in_tile = 8 * t + 2 * i + k, col = at.tile * S::kCols + in_tile;
-                    const float total_weight = sum[t][k] * (1.0f / 32768.0f);
-                    const float norm = kDown * inverse_weight(total_weight);         // before `unit`: the sum itself may be beyond FP32
+                    const float total_weight = sum[t][k], norm = inverse_weight(total_weight);         // before `unit`: the sum itself may be beyond FP32
                     uint8_t* out = nullptr;
                     if (whole && at.has(P, col)) {
                         out = at.out(P, col);

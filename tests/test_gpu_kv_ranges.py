@@ -11,6 +11,54 @@ from test_gpu_kv_attention import BF16, E4M3, F16, FP4, check, clean, queries, w
 pytestmark = pytest.mark.gpu
 
 
+def big_logits(fmt, new, lens, group, least, loud, dtype=BF16, seed=3):
+    """A case whose keys are all the same but for one token of each sequence, `loud` times as large, and queries along the key, of both signs, twice as large with
+    every pair of heads: logits are exact in FP32 (whole multiples of a quarter below 2^24, over a power of two) up to the scale, from 2^least on, and far apart where they differ."""
+    case = ref.Case(zc, fmt, 128, 16, 2, lens, new, seed=seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    grid = torch.tensor(ref.MAGNITUDES, device="cuda")
+    key = grid[torch.randint(0, 8, (2, 128), generator=g, device="cuda")] * torch.randint(0, 2, (2, 128), generator=g, device="cuda").mul(2).sub(1)
+    every = zc.KvBatch(case.batch.page_table.clamp(min=0), case.batch.lens, torch.tensor([0] + list(torch.tensor(lens).cumsum(0)), dtype=torch.int32, device="cuda"), max(lens))
+    k = key.expand(sum(lens), 2, 128).clone()
+    at = 0
+    for n in lens:
+        if loud != 1 and n > 5:
+            k[at + 5] *= loud                                     # all rows see it
+        at += n
+    v = torch.randn(k.shape, generator=g, device="cuda") * 0.25 + 1.0
+    zc.kv_append(case.cache, every, k.to(BF16), v.to(BF16))
+    heads = 2 * group
+    power = torch.exp2(torch.arange(heads, device="cuda") // 2 % max(1, group // 2)).float()
+    sign = 1.0 - 2.0 * (torch.arange(heads, device="cuda") % 2)
+    q = (key.repeat_interleave(group, 0) * (power * sign)[:, None]).expand(case.rows, heads, 128).to(dtype).contiguous()
+    # the least of the logits is scale * |key|^2
+    scale = 1.1 * 2.0 ** least / (key * key).sum(-1).min().item()
+    return case, q, scale
+
+
+def check_exact_logits(case, q, scale):
+    """Weights are 0 or all the same: what is off is half a step of the result, FP32 sums over the tokens (n 2^-24, n taken as 4096 at least) and the weights' rounding."""
+    out, lse = torch.full_like(q, 7.0), torch.zeros(q.shape[:2], device="cuda")
+    zc.kv_attention(case.cache, case.batch, q, out, workspace(case, q.shape[1]), scale=scale, d_lse=lse)
+    scale = torch.tensor(scale, dtype=torch.float32).double().item()
+    want, want_lse, _ = ref.attention(case, q, scale)
+    top = torch.cat([case.tokens(b)[1].abs().amax(dim=(1, 2)).max().expand(n) for b, n in enumerate(case.new)])[:, None, None]
+    room = torch.finfo(q.dtype).eps / 2 * want.abs() * (1 + 2.0 ** -9) + top * (2.0 ** -12 + 2.0 ** -12)
+    off = (out.double() - want).abs() - room
+    assert bool((off <= 0).all()), f"{(~(off <= 0)).sum().item()} of {off.numel()} results are off, {torch.isnan(out).sum().item()} are NaN"
+    # scale in FP32 and times log2(e), the product, and back: six roundings of 2^-24 and log2(e) itself
+    assert bool(((lse.double() - want_lse).abs() <= 2.0 ** -21 * want_lse.abs() + 2.0 ** -19).all())
+
+
+@pytest.mark.parametrize("fmt", [FP4, E4M3])
+@pytest.mark.parametrize("new,lens", [([1, 1], [40, 700]), ([3, 1], [300, 20]), ([70, 33], [300, 129]), ([1], [9000])])
+@pytest.mark.parametrize("least,group", [(8, 4), (12, 16), (20, 16), (24, 2), (25, 16), (30, 8), (33, 16), (60, 32), (100, 16)])
+@pytest.mark.parametrize("loud", [1, 2])
+def test_large_logits(fmt, new, lens, least, group, loud):
+    case, q, scale = big_logits(fmt, new, lens, group, least, loud)
+    check_exact_logits(case, q, scale)
+
+
 @pytest.mark.parametrize("new", [1, 3, 70])
 @pytest.mark.parametrize("fmt,low,high", [(FP4, 60, 64), (FP4, 100, 105), (FP4, 110, 113), (FP4, 114, 118), (FP4, 116, 120), (FP4, 119, 124), (E4M3, 95, 100), (E4M3, 100, 105), (E4M3, 110, 115), (E4M3, 117, 119),
                                           (FP4, -115, -110), (FP4, -120, -114), (E4M3, -110, -100), (E4M3, -120, -112), (E4M3, 90, 112), (FP4, 80, 118), (FP4, -40, 100), (FP4, -126, 110)])
