@@ -443,6 +443,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
         float top = -INFINITY, sum = 0.0f;
         int lo = 0, hi = 0x7FFFFFFF, lo_most = 0, hi_least = 0;
         uint32_t col = 0, v_ref = 0, turns = 0;               // turns: steps in which the half had rows
+        uint32_t idle = 0;                                    // steps since then in which it had none
         int up = 0;                                           // the query is over 2^-up
         bool fresh = true, goes_on = false;
         for (uint32_t j = 0; j < count; ++j) {
@@ -495,7 +496,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                     top = -INFINITY;
                     sum = 0.0f;
                 }
-                if (!wait.warp(my_s, turns & 1)) break;
+                // the limit is a step's: a half that had no rows for some steps is that many ahead of the others
+                if (!KvWaiter{(uint32_t)min((unsigned long long)wait.limit * (idle + 1), 0xFFFFFFFEull), wait.failed}.warp(my_s, turns & 1)) break;
+                idle = 0;
                 tc_fence_after();
                 const int t0 = (int)((c.first_step + c.step) * 128);
                 const uint32_t k_ref = s_ref[par][0], new_ref = s_ref[par][1];
@@ -622,7 +625,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                     tc_fence_before();                     // read before the next item's products
                 }
                 ++turns;
-            }
+            } else ++idle;
             fresh = item_ends;
             if (item_ends) {
                 item_from += c.steps;

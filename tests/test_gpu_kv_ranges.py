@@ -92,3 +92,32 @@ def test_value_scales_over_all_of_their_range(lens, new, fmt, low, high):
     case.cache.v_elems.bitwise_and_(0x77 if fmt == FP4 else 0x7F)                    # of one sign
     out, _ = check(case, queries(case, 4, BF16))
     assert bool(torch.isfinite(out).all())
+
+
+def test_a_half_that_waits_for_its_rows_does_not_give_up():
+    # 40 columns a sequence leave the second half of a tile of 256 without rows, for all of a block's work but the last sequence's: hundreds of steps, with a limit that is
+    # many times a step's (16 polls do for the sequences of 40 alone)
+    seqs, tokens, page = 1500, 16384, 256
+    cache = zc.kv_empty(tokens // page, 1, page, 64, FP4)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for t in (cache.k_elems, cache.v_elems):
+        t.random_(0, 256, generator=g)
+    for t in (cache.k_scales, cache.v_scales):
+        t.fill_(125)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = torch.arange(tokens // page, dtype=torch.int32, device="cuda").expand(seqs, -1).contiguous()        # they share their pages
+    try:
+        for last in (40, 256):
+            first = [40 * b for b in range(seqs)] + [40 * (seqs - 1) + last]
+            batch = zc.KvBatch(table, i32([tokens] * seqs), i32(first), 256)
+            q = torch.randn((first[-1], 1, 64), generator=g, device="cuda").to(BF16)
+            ws = torch.empty(zc.kv_attention_workspace_bytes(cache, batch, 1), dtype=torch.uint8, device="cuda")
+            zc.test_set_wait_limit(0)
+            want = zc.kv_attention(cache, batch, q, torch.empty_like(q), ws)
+            assert zc.kv_status() == zc.OK
+            zc.test_set_wait_limit(64)
+            got = zc.kv_attention(cache, batch, q, torch.empty_like(q), ws)
+            assert zc.kv_status() == zc.OK
+            assert torch.equal(got, want)
+    finally:
+        zc.test_set_wait_limit(0)
