@@ -231,10 +231,12 @@ __global__ void __launch_bounds__(kCacheThreads) kv_append_kernel(const CachePar
     grid_launch_dependents();
     const int row0 = (int)(blockIdx.x * P.rows_per_block);
     const uint32_t pieces = kBlocks * P.rows_per_block * P.C.heads * 2;
+    const int first_row = P.B.first[0], end_row = min(P.B.first[P.B.n_seqs], (int)P.B.n_rows);        // the others are nobody's
     bool there = false;
     for (uint32_t i = threadIdx.x; i < pieces || !there; i += kCacheThreads) {
         const Piece c(P, kBlocks, i);
-        const bool mine = i < pieces && row0 + c.row < P.B.n_rows;
+        const int row = row0 + (int)c.row;
+        const bool mine = i < pieces && row >= first_row && row < end_row;
         float v[32];
         // the numbers do not wait for their place
         if (mine) load_block<T, WIDE>(P.t[c.side].d + (uint64_t)(row0 + c.row) * P.t[c.side].ld_row + c.head * P.t[c.side].ld_head + c.blk * kKvBlock * sizeof(T), v);

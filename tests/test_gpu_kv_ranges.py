@@ -121,3 +121,24 @@ def test_a_half_that_waits_for_its_rows_does_not_give_up():
             assert torch.equal(got, want)
     finally:
         zc.test_set_wait_limit(0)
+
+
+def test_rows_that_are_nobodys_are_not_read():
+    # a tensor with room for 262144 tokens: where the batch has one of them, writing takes a small part of the time that writing all of them takes (reading them alone would take most of it)
+    rows, heads, page = 1 << 18, 8, 256
+    cache = zc.kv_empty(rows // page, heads, page, 128, FP4)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = torch.arange(rows // page, dtype=torch.int32, device="cuda").reshape(1, -1)
+    k = torch.ones((rows, heads, 128), device="cuda")
+    times = []
+    for first in ([0, rows], [5, 6], [rows - 1, rows]):
+        batch = zc.KvBatch(table, i32([rows]), i32(first), 1)
+        zc.kv_append(cache, batch, k, k)
+        events = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        events[0].record()
+        for _ in range(10):
+            zc.kv_append(cache, batch, k, k)
+        events[1].record()
+        torch.cuda.synchronize()
+        times.append(events[0].elapsed_time(events[1]))
+    assert max(times[1:]) * 4 < times[0], times
