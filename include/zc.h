@@ -549,7 +549,8 @@ typedef struct zc_kv_cache {
  * nothing.
  * What is wrong on the device is never followed: a length below 0 counts as 0, one above what the table's row has room for as that; a page
  * outside 0 .. n_pages - 1 is not touched, its tokens are not stored, are read as zeros and are left out of the attention; to the attention a
- * sequence whose rows do not lie within n_rows has none.  zc_kv_status then says ZC_E_CORRUPT.  Table entries behind a sequence's last token are not read. */
+ * sequence whose rows do not lie within n_rows, or end before they begin, has none.  zc_kv_status then says ZC_E_CORRUPT.  (Rows that two sequences have since first falls
+ * get something of either.)  Table entries behind a sequence's last token are not read. */
 typedef struct zc_kv_batch {
     const int32_t* d_page_table;   /* [n_seqs] rows of max_pages pages, row pitch ld_page_table elements */
     const int32_t* d_lens;         /* [n_seqs] */
