@@ -831,6 +831,8 @@ def kv_attention(cache: KvCache, batch: KvBatch, d_q: torch.Tensor, d_out: torch
         raise ValueError(f"d_q is {tuple(shape)}, d_out {tuple(d_out.shape)}")
     if not 0 <= window < 1 << 32:
         raise ValueError("window is out of range")
+    if not d_workspace.is_contiguous():                         # its bytes are counted as if they followed one another
+        raise ValueError("d_workspace is contiguous")
     rows, heads = shape[0], shape[1]
     dev, lse = d_q.get_device(), 0
     dev = _same_device(cache._dev, batch._dev, dev, d_out.get_device(), d_workspace.get_device(), d_lse.get_device() if d_lse is not None else dev)
