@@ -142,3 +142,35 @@ def test_rows_that_are_nobodys_are_not_read():
         torch.cuda.synchronize()
         times.append(events[0].elapsed_time(events[1]))
     assert max(times[1:]) * 4 < times[0], times
+
+
+@pytest.mark.parametrize("dim,columns", [(128, 48), (128, 49), (64, 64), (64, 65)])
+def test_both_sides_of_the_choice_of_kernels(dim, columns):
+    # the most columns of the kernel of few rows, the least of that of many, alone and with sequences of the other kind beside them; the pages beyond 4 GB
+    pages, heads, page = (1 << 32) // (8 * 64 * dim // 2) + 40, 8, 64
+    cache = zc.KvCache(*[torch.zeros((pages, heads, page, w), dtype=torch.uint8, device="cuda") for w in (dim // 2, dim // 32, dim // 2, dim // 32)], FP4)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    lens = [300, 200, 77]
+    table = torch.full((3, 5), -1, dtype=torch.int32)
+    for b, n in enumerate(lens):
+        used = -(-n // page)
+        table[b, :used] = pages - 1 - 10 * b - torch.arange(used, dtype=torch.int32)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn((sum(lens), heads, dim), generator=g, device="cuda").to(BF16) for _ in range(2))
+    zc.kv_append(cache, zc.KvBatch(table.cuda(), i32(lens), i32([0, 300, 500, 577]), 300), k, v)
+    kv = [ref.values(*ref.quantize(t, FP4), FP4) for t in (k, v)]
+    for new in ([columns, columns, columns], [columns, 1, 70], [1, columns, 3]):
+        first = [0, new[0], new[0] + new[1], sum(new)]
+        batch = zc.KvBatch(table.cuda(), i32(lens), i32(first), columns)
+        q = torch.randn((sum(new), heads, dim), generator=g, device="cuda").to(BF16)
+        out = torch.empty_like(q)
+        zc.kv_attention(cache, batch, q, out, torch.empty(zc.kv_attention_workspace_bytes(cache, batch, heads), dtype=torch.uint8, device="cuda"))
+        at = 0
+        for b, n in enumerate(new):
+            kb, vb = (t[at: at + lens[b]] for t in kv)
+            at += lens[b]
+            x = torch.einsum("rhd,thd->hrt", q[first[b]: first[b + 1]].double(), kb) * dim ** -0.5
+            x = x.masked_fill(torch.arange(lens[b], device="cuda") > torch.arange(lens[b] - n, lens[b], device="cuda")[:, None], -math.inf)
+            want = torch.einsum("hrt,thd->rhd", torch.softmax(x, -1), vb)
+            # half a step of BF16; 2^-12 for the weights, as much for their sums, 2^-12 for logits of a few units in FP32
+            assert bool(((out[first[b]: first[b + 1]].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * vb.abs().amax(0)).all())
