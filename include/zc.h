@@ -616,7 +616,7 @@ zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, co
                           size_t workspace_bytes, void* cuda_stream);
 
 /* Waits for the stream, returns and clears what zc_kv_* calls on the current device have left since the last query, on whichever stream:
- * ZC_OK, ZC_E_DEVICE_TIMEOUT (a wait inside a kernel gave up; results are undefined) or ZC_E_CORRUPT (lengths or pages outside their ranges).
+ * ZC_OK, ZC_E_DEVICE_TIMEOUT (a wait inside a kernel gave up, or a call of several hours was not begun; results are undefined) or ZC_E_CORRUPT (lengths or pages outside their ranges).
  * Calls that are still running on other streams may report to a later query.  ZC_E_CUDA on a stream that is being captured; the capture goes on. */
 zc_status zc_kv_status(void* cuda_stream);
 

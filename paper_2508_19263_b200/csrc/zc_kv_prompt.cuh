@@ -264,8 +264,10 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
     const unsigned long long total = s_total;
     const uint32_t blocks = working_blocks(total, 1, gridDim.x);
     const unsigned long long from = blockIdx.x < blocks ? share(total, blockIdx.x, blocks) : 0, to = blockIdx.x < blocks ? share(total, blockIdx.x + 1, blocks) : 0;
-    const uint32_t count = (uint32_t)(to - from), tmem = __shfl_sync(kAll, s_tmem, 0);
+    const bool endless = (to - from) >> 32 != 0;          // three hours at 2.6 us a step: not begun
+    const uint32_t count = endless ? 0u : (uint32_t)(to - from), tmem = __shfl_sync(kAll, s_tmem, 0);
     const KvWaiter wait{P.spin_limit, smem_u32(const_cast<uint32_t*>(&s_failed))};
+    if (endless) wait.give_up();
     PromptCursor c;
     if (count) {
         c.sequence(P, s_start[0]);

@@ -338,7 +338,9 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
     uint32_t place_base = 0xFFFFFFFFu, place_seq = 0xFFFFFFFFu;
     int pages = 0;
     uint32_t missing = 0;                                 // kGroups bits a stage: groups of 16 tokens that have no page
-    const uint32_t count = (uint32_t)(to - from);        // 2^32 steps a warp would take days
+    const bool endless = (to - from) >> 32 != 0;          // five hours at 4 us a step: not begun
+    const uint32_t count = endless ? 0u : (uint32_t)(to - from);
+    if (endless) wait.give_up();
     uint32_t sent = 0;
     const uint32_t piece_tokens = min(1u << P.C.page_shift, S::kStep), pieces = S::kStep / piece_tokens;
     auto send = [&](uint32_t st) {
@@ -394,7 +396,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
 #pragma unroll
     for (int k = 0; k < 4; ++k) asm volatile("mov.b32 %0, 0;" : "=f"(zero[k]));
     uint32_t ref = 0, key_ref = 0;                       // scale bytes that values' and keys' scales are over
-    bool fresh = true, ok = true, careful = false;       // careful: key_ref is the largest so far, else 127
+    bool fresh = true, ok = !endless, careful = false;       // careful: key_ref is the largest so far, else 127
     auto set_factors = [&]() {
 #pragma unroll
         for (uint32_t t = 0; t < S::kNt; ++t) {

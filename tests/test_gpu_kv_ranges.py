@@ -174,3 +174,24 @@ def test_both_sides_of_the_choice_of_kernels(dim, columns):
             want = torch.einsum("hrt,thd->rhd", torch.softmax(x, -1), vb)
             # half a step of BF16; 2^-12 for the weights, as much for their sums, 2^-12 for logits of a few units in FP32
             assert bool(((out[first[b]: first[b + 1]].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * vb.abs().amax(0)).all())
+
+
+@pytest.mark.parametrize("columns,steps,width,max_new", [(8 * (1 << 18), 1776 << 14, 64, 1), (256 * (1 << 16), 148 << 16, 128, 1 << 24)])
+def test_calls_of_hours_are_not_begun(columns, steps, width, max_new):
+    # one page of zeros is all of a sequence of some 10^9 tokens: 2^32 steps for each warp of 148 blocks of 12 (few rows), for each of 148 blocks (many).  Counted in 32 bits that
+    # would be none at all, and for other numbers of blocks it could be hours, so it is for this one alone
+    if torch.cuda.get_device_properties(0).multi_processor_count != 148:
+        pytest.skip("the sizes are those of 148 multiprocessors")
+    cache = zc.kv_empty(1, 1, 256, 64, FP4)
+    for t in (cache.k_elems, cache.k_scales, cache.v_elems, cache.v_scales):
+        t.zero_()
+    table = torch.zeros((1, -(-steps * width // 256)), dtype=torch.int32, device="cuda")
+    batch = zc.KvBatch(table, torch.tensor([steps * width], dtype=torch.int32, device="cuda"), torch.tensor([0, columns], dtype=torch.int32, device="cuda"), max_new)
+    q = torch.zeros((columns, 1, 64), dtype=BF16, device="cuda")
+    out = torch.full_like(q, 7.0)
+    zc.kv_attention(cache, batch, q, out, torch.empty(zc.kv_attention_workspace_bytes(cache, batch, 1), dtype=torch.uint8, device="cuda"), causal=False)
+    assert zc.kv_status() == zc.E_DEVICE_TIMEOUT
+    # the next call is not disturbed
+    small = zc.KvBatch(table, torch.tensor([100], dtype=torch.int32, device="cuda"), torch.tensor([0, 3], dtype=torch.int32, device="cuda"), max_new)
+    zc.kv_attention(cache, small, q[:3], out[:3], torch.empty(zc.kv_attention_workspace_bytes(cache, small, 1), dtype=torch.uint8, device="cuda"))
+    assert zc.kv_status() == zc.OK and bool((out[:3] == 0).all())
