@@ -241,7 +241,10 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                         const uint32_t steps = __shfl_sync(kAll, count, k);
                         const unsigned long long inside = from - before - (__shfl_sync(kAll, upto, k) - (unsigned long long)steps * P.C.heads);
                         if (lane == 0) {
-                            const uint32_t head = (uint32_t)(inside / steps), step = (uint32_t)(inside % steps);
+                            uint32_t head = 0;               // below 2^10
+                            for (uint32_t bit = ZC_KV_MAX_HEADS / 2; bit; bit /= 2)
+                                if ((unsigned long long)(head + bit) * steps <= inside) head += bit;
+                            const uint32_t step = (uint32_t)(inside - (unsigned long long)head * steps);
                             s_start[0] = b;
                             s_start[1] = t0 + k;
                             s_start[2] = head;
