@@ -606,7 +606,7 @@ typedef struct zc_kv_attention_args {
 #define ZC_KV_MAX_GROUP 256u       /* query heads that share a head of the cache */
 
 /* Bytes of device scratch zc_kv_attention needs for up to q_heads query heads, for any lengths and rows of a batch with this max_new (more where rows times
- * heads that share one are above 48, 64 with a head_dim of 64); 0 for arguments that it would refuse. */
+ * heads that share one are above 32 to 64, depending on head_dim and format); 0 for arguments that it would refuse. */
 size_t zc_kv_attention_workspace_bytes(const zc_kv_cache* cache, const zc_kv_batch* batch, uint32_t q_heads);
 /* d_workspace  workspace_bytes >= zc_kv_attention_workspace_bytes(), 256-byte aligned, contents need not be initialised; calls that
  *              overlap in time must not share it.  Asynchronous.  The result is the same every time.

@@ -84,11 +84,14 @@ static cudaError_t launch_prompt(const AttentionParams& P, uint32_t blocks, cuda
     return launch_join<S>(P, blocks, 1, cfg);
 }
 
-// Columns (rows times heads that share a head of the cache) up to which a sequence goes to the kernel of few rows.  That reads the cache once for each 16 of them, the
-// other works on 256 whatever there are.  Us of few and of many rows, 8 heads: heads of 128, 16 sequences of 6000 tokens in E4M3: 40 columns 183 and 206, 48: 187 and 210, 56: 235 and
-// 208; in FP4: 48: 141 and 152, 56: 175 and 155; 64 sequences of 2000 in E4M3: 48: 262 and 305, 56: 325 and 310; one of 32768: 32: 57 and 68, 40: 77 and 69.
-// Heads of 64, 16 sequences in E4M3: 64: 128 and 136, 80: 154 and 137; 64 sequences in FP4: 64: 167 and 212, 80: 201 and 213; one in FP4: 56: 51 and 49.
-static uint32_t few_columns(uint32_t head_dim) { return head_dim == 128 ? 48 : 64; }
+// Columns (rows times heads that share a head of the cache) up to which a sequence goes to the kernel of few rows.  That reads and converts the cache once for each 16 of
+// them, the other works on 256 whatever there are.  Us of few rows and of many, 8 heads, by columns:
+//                                     16 sequences of 6000 tokens       64 of 2000                         one of 32768
+//   heads of 128, E4M3   32 and 40:   135, 154 and 179, 157             179, 252 and 248, 254              57, 62 and 76, 62
+//                 FP4    48 and 56:   139, 146 and 173, 148             196, 241 and 236, 244              59, 57 and 66, 58
+//   heads of 64,  E4M3   64 and 80:   126, 127 and 152, 129             174, 211 and 210, 214              51, 48 and 61, 52
+//                 FP4    64 and 80:   122, 120 and 147, 121             166, 204 and 200, 205              50, 47 and 60, 51
+static uint32_t few_columns(const zc_kv_cache* c) { return c->head_dim == 64 ? 64 : c->format == ZC_FMT_FP4_E2M1 ? 48 : 32; }
 
 }  // namespace zc
 
@@ -103,7 +106,7 @@ size_t zc_kv_attention_workspace_bytes(const zc_kv_cache* cache, const zc_kv_bat
     const bool wide = cache->head_dim == 128;
     size_t bytes = wide ? std::max(stream_workspace<StreamShape<true, 128, 1>>(n), stream_workspace<StreamShape<true, 128, 2>>(n))
                         : std::max(stream_workspace<StreamShape<true, 64, 1>>(n), stream_workspace<StreamShape<true, 64, 2>>(n));
-    if ((uint64_t)(q_heads / cache->kv_heads) * std::max(1u, batch->max_new) > few_columns(cache->head_dim))
+    if ((uint64_t)(q_heads / cache->kv_heads) * std::max(1u, batch->max_new) > few_columns(cache))
         bytes = std::max(bytes, wide ? workspace_of<PromptShape<true, 128>>(n, 0) : workspace_of<PromptShape<true, 64>>(n, 0));
     return bytes;
 }
@@ -161,7 +164,7 @@ zc_status zc_kv_attention(const zc_kv_cache* cache, const zc_kv_batch* batch, co
         cudaStream_t st = (cudaStream_t)cuda_stream;
         const uint64_t columns = (uint64_t)P.group * std::max(1u, batch->max_new);
         if (columns <= 8) return launch_stream<One>(P, maps[0], maps[1], blocks, st);
-        const uint32_t few = few_columns(cache->head_dim);
+        const uint32_t few = few_columns(cache);
         if (columns <= few) return launch_stream<Two>(P, maps[0], maps[1], blocks, st);
         // a sequence alone has the rows that are expected; of several some may have few
         if (batch->n_seqs > 1) P.most_rows = few / P.group;
