@@ -39,8 +39,8 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// of a sum of weights over 2^unit
-__device__ __forceinline__ float lse_of(float unit, float weight) { return weight == 0.0f ? -INFINITY : (unit + log2f(weight)) * 0.69314718f; }
+// Of a sum of weights, the largest of which is about 2^15, over 2^unit.
+__device__ __forceinline__ float lse_of(float unit, float weight) { return weight == 0.0f ? -INFINITY : (unit + 15.0f + log2f(weight * (1.0f / 32768.0f))) * 0.69314718f; }
 // whether one of four E4M3 bytes is NaN
 __device__ __forceinline__ bool nan_bytes(uint32_t w)
 {
@@ -226,8 +226,8 @@ __device__ __forceinline__ void store_out(const AttentionParams& P, uint8_t* out
         for (uint32_t k = 0; k < N; ++k) reinterpret_cast<uint16_t*>(out)[k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
     }
 }
-// What divides sums by their weights; 0 where nothing was seen.
-__device__ __forceinline__ float inverse_weight(float weight) { return weight == 0.0f ? 0.0f : 1.0f / weight; }
+// What divides sums by their weights; 0 where nothing was seen.  Off by 2^-22: results are rounded to 2^-9 or 2^-12.  (A correctly rounded one takes 0.5 us of a short call's 16.)
+__device__ __forceinline__ float inverse_weight(float weight) { return weight == 0.0f ? 0.0f : __fdividef(1.0f, weight); }
 // A joined column: a lane has N neighbours from d on.
 template <uint32_t N>
 __device__ __forceinline__ void finish_column(const AttentionParams& P, const ItemColumns& c, uint32_t in_tile, uint32_t d, const float* v, float top, float weight)
@@ -263,15 +263,18 @@ __device__ __forceinline__ float logit_power(const AttentionParams& P, int e) { 
 __device__ __forceinline__ uint32_t scale_mantissa_bits(const AttentionParams& P) { return __float_as_uint(P.scale_mantissa) & 0x7FFFFFu; }
 __device__ __forceinline__ float logit_factor(const AttentionParams& P, int e) { return __uint_as_float(__float_as_uint(logit_power(P, e)) | scale_mantissa_bits(P)); }
 
-// Weights are 2^(logit - unit).  A largest logit beyond what FP16 has for a weight moves the unit so that the largest weight is 2^14 .. 2^15, and gives what sums so far shrink by.
-//   The unit is a whole number, so that a weight's exponent, factor * product - unit, is what it should be: the rounding of a unit that is the largest logit itself
-// would be in it, which from 2^24 on puts the largest weight beyond FP16 or makes nothing of it.  From 2^23 on, where logits are whole numbers, it is the logit.
-//   The product is not rounded in that exponent, the largest logit is: from kFarLogit on, where that is 2^-5 and more, products have to be rounded as well, or exact.
+// Weights are 2^(logit - unit), the largest 2^15, which FP16 has exactly; where a row's logits are mostly below one of them that is the weight that counts (results in FP16 are off
+// by 2.3e-4 so, by 3.0e-4 with a whole number for the unit everywhere).  A largest logit that is more than `most` (15 or a little more) above the unit moves it, and gives what sums so far shrink by.
+//   The unit is what is subtracted, after its rounding, in weights and in sums alike.  From 2^12 on it is a whole number that makes the largest weight 2^14 .. 2^15: the rounding of
+// logit - 15 would move it further and further, from 2^24 on beyond FP16 or to nothing.  From 2^23 on, where logits are whole numbers, it is the logit.
+//   The product is not rounded in a weight's exponent, factor * product - unit, the largest logit is: from kFarLogit on, where that is 2^-5 and more, products have to be rounded as well, or exact.
 constexpr float kFarLogit = 524288.0f;
-__device__ __forceinline__ float move_unit(float& unit, float largest)
+__device__ __forceinline__ bool above_unit(float unit, float largest, float most) { return largest - unit > most; }           // not where both are -infinity
+__device__ __forceinline__ float move_unit(float& unit, float largest, float most)
 {
-    if (!(largest - unit > 15.9f)) return 1.0f;            // also where both are -infinity
-    const float whole = ceilf(largest), to = fabsf(whole) < 8388608.0f ? whole - 15.0f : whole, shrink = exp2_fast(unit - to);
+    if (!above_unit(unit, largest, most)) return 1.0f;
+    const float whole = ceilf(largest), to = fabsf(largest) < 4096.0f ? largest - 15.0f : fabsf(whole) < 8388608.0f ? whole - 15.0f : whole;
+    const float shrink = exp2_fast(unit - to);
     unit = to;
     return shrink;
 }

@@ -539,19 +539,20 @@ __global__ void __launch_bounds__(S::kThreads, 1) kv_prompt_kernel(const Attenti
                 }
                 const float best = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * f;
                 // the sums in tensor memory are over 2^top of the weights and 2^v_ref of the values
-                float shrink = move_unit(top, best);
+                float shrink = move_unit(top, best, 15.9f);
                 sum *= shrink;
                 if (!fresh && new_ref != v_ref) shrink *= ldexpf(1.0f, max((int)v_ref - (int)new_ref, -200));
                 if (__any_sync(kAll, shrink != 1.0f || fabsf(best) >= kFarLogit)) {
-                    if (!fresh)
+                    if (!fresh) {
 #pragma unroll 1
-                    for (uint32_t k = 0; k < S::kDim / 32; ++k) {
-                        float v[32];
-                        tmem_ld32_async(at + S::kO + 32 * k, v);
-                        tmem_ld_wait();
+                        for (uint32_t k = 0; k < S::kDim / 32; ++k) {
+                            float v[32];
+                            tmem_ld32_async(at + S::kO + 32 * k, v);
+                            tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 32; i += 2) mul_pair(v[i], v[i + 1], shrink);
-                        tmem_st32(at + S::kO + 32 * k, v);
+                            for (int i = 0; i < 32; i += 2) mul_pair(v[i], v[i + 1], shrink);
+                            tmem_st32(at + S::kO + 32 * k, v);
+                        }
                     }
                     if (__any_sync(kAll, fabsf(best) >= kFarLogit && best != -INFINITY)) {
                         // logits as large as this are rounded before their differences are taken

@@ -15,7 +15,7 @@
 // over the largest that the run has met from the first of 2^65 or more on, or where queries and scale are far from 1: products, or what makes logits of them, could be
 // beyond FP32 where the logits are not.
 //   Queries become FP16 over a power of two that brings the row's largest to 2^14 .. 2^15: BF16's eight bits are kept down to 2^-31 of it.
-//   Weights are 2^(x - u), u a whole number so that the largest is 2^14 .. 2^15.9, in FP32 for the sum, rounded to FP16 for the product with V: off by at most 2^-12 of it
+//   Weights are 2^(x - u), u so that the largest is 2^15, in FP32 for the sum, rounded to FP16 for the product with V: off by at most 2^-12 of it
 // where it is above 2^-28 of the largest (the scale's power of two counted in), by 2^-39 of the largest below.
 //   Measured: one token for 64 sequences of 2200 to 8200 tokens, 32 heads of queries over 8 in FP4: 108 us, 3.6 TB/s; the copies alone take 79 us, what is left are the
 // conversions' instructions: 600 for 32 tokens, of them 130 conversions and about 100 that bring a conversion its byte, at three warps a scheduler.  A call's
@@ -597,8 +597,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
         }
 
         // what weights are over, after the largest so far
-        bool moved = false;
-        float shrink[S::kNt][2], off[S::kNt][2];
+        bool above = false;
+        float off[S::kNt][2];
 #pragma unroll
         for (uint32_t t = 0; t < S::kNt; ++t)
 #pragma unroll
@@ -606,20 +606,27 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) kv_stream_kernel(const Atte
                 float x = best[t][k];
                 x = fmaxf(x, __shfl_xor_sync(kAll, x, 4));
                 x = fmaxf(x, __shfl_xor_sync(kAll, x, 8));
-                x = fmaxf(x, __shfl_xor_sync(kAll, x, 16)) * factor[t][k];
-                shrink[t][k] = move_unit(top[t][k], x);
-                moved |= shrink[t][k] != 1.0f;
-                off[t][k] = top[t][k] == -INFINITY ? 0.0f : -top[t][k];
-                sum[t][k] *= shrink[t][k];
+                best[t][k] = fmaxf(x, __shfl_xor_sync(kAll, x, 16)) * factor[t][k];
+                above |= above_unit(top[t][k], best[t][k], 15.0f);
             }
-        if (__any_sync(kAll, moved)) {
+        if (__any_sync(kAll, above)) {
 #pragma unroll
             for (uint32_t t = 0; t < S::kNt; ++t)
 #pragma unroll
-                for (uint32_t m = 0; m < S::kTiles; ++m)
+                for (int k = 0; k < 2; ++k) {
+                    const float shrink = move_unit(top[t][k], best[t][k], 15.0f);
+                    sum[t][k] *= shrink;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[t][m][k] *= shrink[t][k & 1];
+                    for (uint32_t m = 0; m < S::kTiles; ++m) {
+                        acc[t][m][k] *= shrink;
+                        acc[t][m][k + 2] *= shrink;
+                    }
+                }
         }
+#pragma unroll
+        for (uint32_t t = 0; t < S::kNt; ++t)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) off[t][k] = top[t][k] == -INFINITY ? 0.0f : -top[t][k];
 
         {
             // values' scales over the largest so far, [token][block] in FP16, twice in a word; every lane is done with the keys'

@@ -195,3 +195,15 @@ def test_calls_of_hours_are_not_begun(columns, steps, width, max_new):
     small = zc.KvBatch(table, torch.tensor([100], dtype=torch.int32, device="cuda"), torch.tensor([0, 3], dtype=torch.int32, device="cuda"), max_new)
     zc.kv_attention(cache, small, q[:3], out[:3], torch.empty(zc.kv_attention_workspace_bytes(cache, small, 1), dtype=torch.uint8, device="cuda"))
     assert zc.kv_status() == zc.OK and bool((out[:3] == 0).all())
+
+
+@pytest.mark.parametrize("fmt", [FP4, E4M3])
+@pytest.mark.parametrize("new,lens", [([1, 1], [40, 700]), ([3, 1], [300, 20]), ([70, 33], [300, 129]), ([1], [9000])])
+def test_a_weight_of_one_is_exact(fmt, new, lens):
+    # where one token has all of the weight the result is its value, to the bit: in FP16, which has the cache's elements exactly, half a step is 2^-12
+    case, q, scale = big_logits(fmt, new, lens, 4, 8, 2, F16)
+    out = zc.kv_attention(case.cache, case.batch, q, torch.empty_like(q), workspace(case, 8), scale=scale)
+    for b, n in enumerate(new):
+        v = case.tokens(b)[1][:, 5]                                # [heads of the cache][dim]; the queries of even heads point to it
+        rows = slice(case.first_list[b], case.first_list[b] + n)
+        assert torch.equal(out[rows, 0::2].double(), v.repeat_interleave(2, 0).expand(n, 4, 128))
