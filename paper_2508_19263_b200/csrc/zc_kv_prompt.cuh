@@ -11,11 +11,11 @@
 // the head's width fastest, which for this product is the outer axis.  S and O, FP32, of both halves are all of tensor memory's 512 columns (head_dim 128).
 //   Keys and values are element * 2^(s - R + kLift), R the largest scale byte that the item has met, for keys and for values: exact unless a scale is 2^-35 (E4M3:
 // 2^-22) of the largest, off by at most 2^-25 / 2^kLift of 2^R then.  Queries as in the other kernel.
-//   Weights are 2^(x - u) as in the other kernel: the sums in tensor memory are only touched when a row's largest weight grows by a factor of 1.8 or more.
-// They are rounded to FP16: off by at most 2^-12 of it down to 2^-28 of the largest, by 2^-39 of the largest below; the sum of weights is FP32.
-//   Measured: 2048 rows, 32 heads, behind 32768 tokens in FP4: 1252 us, 906 TFLOP/s; of a step's 5100 cycles the tensor cores work 2050, a half's softmax takes 3000 (the
+//   Weights are 2^(x - u) as in the other kernel, but u moves only where the largest is beyond 2^15.9, to 2^15 again: so the sums in tensor memory are touched only when a row's
+// largest weight grows by a factor of 1.8.  Rounded to FP16: off by at most 2^-12 of it down to 2^-29 of the largest, by 2^-40 of the largest below; the sum of weights is FP32.
+//   Measured: 2048 rows, 32 heads, behind 32768 tokens in FP4: 1293 us, 877 TFLOP/s; the tensor cores work 43 % of the time, a half's softmax takes some 3000 of a step's 5200 cycles (the
 // special function units 1024 of it).  Two blocks an SM with 128 rows each: 1634 us.  16 warps for the softmax, half a row a thread: 1379 us, the four that are
-// left for keys and values do not keep up.  A quarter of the exponentials by a polynomial on the FP32 units: 1 % less time.  (One B200, a graph of 20 calls.)
+// left for keys and values do not keep up.  A quarter of the exponentials by a polynomial on the FP32 units: 1 % less time.  (One B200.)  No registers are spilled.
 #pragma once
 #include "zc_kv_stream.cuh"
 

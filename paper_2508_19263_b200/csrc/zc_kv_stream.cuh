@@ -16,11 +16,12 @@
 // beyond FP32 where the logits are not.
 //   Queries become FP16 over a power of two that brings the row's largest to 2^14 .. 2^15: BF16's eight bits are kept down to 2^-31 of it.
 //   Weights are 2^(x - u), u so that the largest is 2^15, in FP32 for the sum, rounded to FP16 for the product with V: off by at most 2^-12 of it
-// where it is above 2^-28 of the largest (the scale's power of two counted in), by 2^-39 of the largest below.
-//   Measured: one token for 64 sequences of 2200 to 8200 tokens, 32 heads of queries over 8 in FP4: 108 us, 3.6 TB/s; the copies alone take 79 us, what is left are the
-// conversions' instructions: 600 for 32 tokens, of them 130 conversions and about 100 that bring a conversion its byte, at three warps a scheduler.  A call's
+// where it is above 2^-29 of the largest (the scale's power of two counted in), by 2^-40 of the largest below; where logits pass 2^12, 2^-28 and 2^-39.
+//   Measured: one token for 64 sequences of 2200 to 8200 tokens, 32 heads of queries over 8 in FP4: 109 us, 3.6 TB/s; the copies alone take 79 us, what is left are the
+// conversions' instructions: 630 for 32 tokens, of them 130 conversions and about 100 that bring a conversion its byte, at three warps a scheduler.  A call's
 // fixed part is 14 us (one sequence of 4096 tokens): a chain of reads (lengths, pages, elements), one step, joins in the block and between blocks.
-//   16 warps with 128 registers: 162 us (spills), 8 with 255: 121; elements scaled one by one instead of sums and weights: 119; 32 tokens a step: 119.
+//   16 warps with 128 registers: 162 us (spills), 8 with 255: 121; elements scaled one by one instead of sums and weights: 119; 32 tokens a step: 119.  In E4M3 with heads of
+// 128 the registers do not quite suffice: 8 bytes a thread are spilled by the 12 warps, 28 by the 8; nothing is in the other shapes.
 #pragma once
 #include <type_traits>
 
