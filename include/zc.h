@@ -593,9 +593,8 @@ zc_status zc_kv_read(const zc_kv_cache* cache, const zc_kv_batch* batch, zc_real
  * token, outside the window) has no influence, whatever it is; NaN that a row sees makes NaN what depends on it, at most all of the row.
  * Sums, maxima and the sum of weights are FP32.  Any scale byte goes with any query, whichever kernel has the call: scale, queries and keys may each be
  * beyond FP32 where their products are not; a row with a logit of 1e38 or more in magnitude is undefined.  Queries are used to 2^-31 of the row's largest element, exactly where
- * they are above 2^-24 of it.  Weights are rounded to FP16 for the products with the values: off by 2^-12 of themselves, the largest of a row by nothing where logits are below
- * 2^11, and by 2^-39 of the row's largest where they are far below it.  So values are used to 2^-39 of the largest that any row of the sequence sees in the head, where there are many
- * rows to 2^-31, and keys then too.  (Few and many: see max_new; the library chooses.) */
+ * they are above 2^-24 of it.  Weights are rounded to FP16 for the products with the values: off by 2^-12 of themselves, and by 2^-39 of the row's largest where they are far
+ * below it.  So values are used to 2^-39 of the largest that any row of the sequence sees in the head; in sequences of many rows (see max_new) values and keys to 2^-31 of it. */
 typedef struct zc_kv_attention_args {
     zc_kv_tensor q, out;           /* [n_rows][q_heads][head_dim] of `type`; must not overlap */
     float* d_lse;                  /* [n_rows][q_heads], no padding; null: not wanted */
